@@ -360,6 +360,99 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Serving operators over a paged 4-bit cache (Appendix C: keys are multiplied over the head dimension and quantized along it,
+ * values are multiplied over the tokens and quantized along them; the most recent, incomplete chunk of 32 tokens keeps its values
+ * in high precision and is quantized once, when it is whole).
+ *
+ * The cache: a pool of pages of `page_tokens` tokens (a multiple of 32, at most 2^20), each with all KV heads.  Per page, KV head and 32
+ * tokens it holds one cell of dfp4_paged_cell_bytes(head_dim) bytes (4.375 bits an element, some padding), whose layout is
+ * private to the library.  Values of a sequence's last length % 32 tokens are bf16 in the sequence's slot of `residual`.
+ *   pages     device, [n_pages, kv_heads, page_tokens / 32, cell], 256-byte aligned
+ *   residual  device, bf16 [n_slots, kv_heads, head_dim, 32], 16-byte aligned
+ *   head_dim  64, 96, 128, 192 or 256
+ * Neither need be cleared before use.
+ *
+ * A batch of sequences, for all three calls: sequence b brings the tokens cu_tokens[b] .. cu_tokens[b + 1] - 1 of the dense
+ * arrays, and they are the last ones of its lengths[b] tokens (the length after them).  Token t of the sequence lies in page
+ * table[b, t / page_tokens].  Tokens that would come before position 0 are in no page: they are not written, read as zeros, and
+ * attend to nothing.
+ *   cu_tokens int32 [batch + 1], ascending from 0 to `tokens`; lengths int32 [batch]; table int32 [batch, table_width];
+ *   slots int32 [batch], all device memory
+ *   max_new, max_length   the largest number of new tokens and the largest length of a sequence, as far as the caller knows (0: not
+ *             known).  They decide how work is split, not what is computed.
+ * Numbers in these arrays are used only as far as they lie in range: lengths are cut to the table's width, token ranges to
+ * `tokens`; tokens in pages outside the pool, and values in slots outside `residual`, count as absent (not written, read as zeros,
+ * not attended to).  Two sequences of one call must not share pages that are written, or slots.
+ */
+typedef struct dfp4_cache {
+    uint8_t* pages;
+    uint16_t* residual;
+    int64_t n_pages, page_tokens, n_slots, kv_heads, head_dim;
+} dfp4_cache;
+
+typedef struct dfp4_batch {
+    const int32_t* cu_tokens;
+    const int32_t* lengths;
+    const int32_t* table;
+    const int32_t* slots;
+    int64_t batch, table_width, tokens, max_new, max_length;
+} dfp4_batch;
+
+/* bytes of a cell, 0 for a head dimension that is not supported */
+size_t dfp4_paged_cell_bytes(int64_t head_dim);
+
+/*
+ * Quantizes the keys and values of new tokens into the cache, bit for bit as dfp4_quantize and dfp4_quantize_t do.
+ *   k, v     device, bf16 [tokens, kv_heads, head_dim]: token strides k_stride, v_stride and head strides k_head_stride,
+ *            v_head_stride in elements (multiples of 8), 16-byte aligned
+ * The values of a chunk that these tokens make whole are quantized together with those that the slot holds; values of a chunk that
+ * stays incomplete go to the slot.  So a sequence's tokens are written in order, and a length is taken back only within its
+ * incomplete chunk.
+ */
+int dfp4_paged_write(const void* k, int64_t k_stride, int64_t k_head_stride, const void* v, int64_t v_stride, int64_t v_head_stride,
+                     dfp4_cache cache, dfp4_batch batch, void* stream);
+
+/*
+ * Reads tokens back: the values that the cache stands for, of the batch's tokens (any last ones of a sequence, cu_tokens; lengths
+ * as they are now).  k, v: device, [tokens, kv_heads, head_dim] contiguous, 16-byte aligned; dtype DFP4_F32 or DFP4_BF16 (both exact).
+ */
+int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dtype, void* stream);
+
+/*
+ * Attention of the batch's new tokens over their sequences' cached tokens, these included (dfp4_paged_write comes first): the
+ * query at position p sees keys at t <= p, with a window > 0 those at t > p - window.
+ *   s = scale * q . k^ ;  softcap > 0: s = softcap * tanh(s / softcap) ;  slopes: s -= slopes[head] * (p - t)
+ *   out = sum over t of softmax(s)_t v^_t,  lse = log(sum over t of exp(s))     (no key: out = 0, lse = -infinity)
+ * with k^, v^ what the cache stands for.  Query head h reads KV head h / (heads / kv_heads).
+ *   q, out   device, bf16 [tokens, heads, head_dim], token and head strides in elements (multiples of 8), 16-byte aligned
+ *   slopes   device, f32 [heads], or NULL;  lse  device, f32 [tokens, heads], or NULL
+ *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads) bytes, 16-byte aligned (0 where no context
+ *            is split)
+ * Scores, softmax and sums are in fp32.  The matrix instructions take keys and values as they are, q as the sum of two FP8 numbers (its
+ * 8 bits) and a probability as the sum of two bf16 numbers.
+ */
+size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads);
+int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
+                         float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
+                         int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Norms of queries and keys per head and the rotation by position, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight     (weight NULL: y = x)
+ *   pair j of `rotary` / 2 turned by position * inv_freq[j]:  (a, b) -> (a cos - b sin, b cos + a sin);  the pair is elements
+ *   (j, j + rotary / 2), interleaved: (2j, 2j + 1); elements from `rotary` on stay.  One rounding, to bf16.
+ *   q, k     device, bf16 [tokens, heads, head_dim] / [tokens, kv_heads, head_dim], token and head strides in elements (multiples
+ *            of 8), 16-byte aligned; q_out, k_out contiguous, or (where q and k are) the inputs themselves.  kv_heads may be 0.
+ *   weights  device, f32 [head_dim] or NULL;  positions  int32 [tokens];  inv_freq  f32 [rotary / 2]
+ *   head_dim a multiple of 32 up to 256, rotary a multiple of 16 up to it (0: no rotation)
+ * Angles are taken in 64 bits, so that far positions turn as near ones do.
+ */
+int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, const void* k, int64_t k_stride,
+                   int64_t k_head_stride, int64_t kv_heads, int64_t tokens, int64_t head_dim, const float* q_weight,
+                   const float* k_weight, float eps, const int32_t* positions, const float* inv_freq, int64_t rotary,
+                   int interleaved, void* q_out, void* k_out, void* stream);
+
+/*
  * The formatbook in use (Section 3.1): out[d * 8 + i] = half-unit magnitude
  * (value = 0.5 * out[...]) of index i in dialect d, ascending.  `out` is a HOST
  * pointer to 128 bytes.

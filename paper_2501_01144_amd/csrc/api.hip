@@ -4,6 +4,7 @@
 
 #include "common.h"
 #include "formatbook.h"
+#include "paged.h"
 
 namespace dfp4 {
 
@@ -476,6 +477,94 @@ int dfp4_gemm_requant_batched(dfp4_tensor A, dfp4_tensor W, dfp4_tensor out, int
 size_t dfp4_gemm_requant_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 0 || K < 0) return 0;
     return gemm_requant_workspace_bytes(M, N, K);
+}
+
+// ---- serving operators over the paged cache -------------------------------------------------------------------------------
+
+static int check_paged(const dfp4_cache& c, const dfp4_batch& b) {
+    if (cell_bytes(c.head_dim) == 0 || c.page_tokens < 32 || c.page_tokens % 32 != 0 || c.n_pages < 0 || c.n_slots < 0 || c.kv_heads < 1)
+        return DFP4_ERR_SHAPE;
+    if (b.batch < 0 || b.table_width < 0 || b.tokens < 0 || b.max_new < 0 || b.max_length < 0) return DFP4_ERR_SHAPE;
+    const int64_t most = (int64_t)1 << 30;
+    if (c.page_tokens > (1 << 20) || c.n_pages > most || c.n_slots > most || c.kv_heads > (1 << 16) || b.batch > most || b.tokens > most ||
+        b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most)
+        return DFP4_ERR_SHAPE;
+    if (b.batch == 0 || b.tokens == 0) return DFP4_OK;
+    if ((c.n_pages > 0 && !c.pages) || (c.n_slots > 0 && !c.residual) || !b.cu_tokens || !b.lengths || !b.slots || (b.table_width > 0 && !b.table))
+        return DFP4_ERR_NULL;
+    if (!aligned(c.pages, 256) || !aligned(c.residual, 16) || !aligned(b.cu_tokens, 4) || !aligned(b.lengths, 4) || !aligned(b.table, 4) ||
+        !aligned(b.slots, 4))
+        return DFP4_ERR_ALIGN;
+    return DFP4_OK;
+}
+
+// a dense bf16 [tokens, heads, head_dim] with strides
+static int check_rows(const void* x, int64_t stride, int64_t head_stride) {
+    if (!x) return DFP4_ERR_NULL;
+    return aligned(x, 16) && stride % 8 == 0 && head_stride % 8 == 0 ? DFP4_OK : DFP4_ERR_ALIGN;
+}
+
+size_t dfp4_paged_cell_bytes(int64_t head_dim) { return cell_bytes(head_dim); }
+
+int dfp4_paged_write(const void* k, int64_t k_stride, int64_t k_head_stride, const void* v, int64_t v_stride, int64_t v_head_stride,
+                     dfp4_cache cache, dfp4_batch batch, void* stream) {
+    int rc = check_paged(cache, batch);
+    if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
+    if ((rc = check_rows(k, k_stride, k_head_stride)) != DFP4_OK || (rc = check_rows(v, v_stride, v_head_stride)) != DFP4_OK) return rc;
+    return launch_paged_write(k, k_stride, k_head_stride, v, v_stride, v_head_stride, cache, batch, static_cast<hipStream_t>(stream));
+}
+
+int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dtype, void* stream) {
+    int rc = check_paged(cache, batch);
+    if (rc == DFP4_OK && dtype != DFP4_F32 && dtype != DFP4_BF16) rc = DFP4_ERR_DTYPE;
+    if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
+    if ((rc = check_rows(k, 8, 8)) != DFP4_OK || (rc = check_rows(v, 8, 8)) != DFP4_OK) return rc;
+    return launch_paged_read(cache, batch, k, v, dtype, static_cast<hipStream_t>(stream));
+}
+
+static bool grouped(const dfp4_cache& cache, int64_t heads) { return heads > 0 && heads <= (1 << 16) && heads % cache.kv_heads == 0; }
+
+size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads) {
+    if (cell_bytes(cache.head_dim) == 0 || cache.kv_heads < 1 || cache.page_tokens < 32 || batch.batch < 1 || batch.tokens < 1 || batch.table_width < 0 ||
+        !grouped(cache, heads))
+        return 0;
+    return paged_attention_workspace_bytes(cache, batch, heads);
+}
+
+int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
+                         float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
+                         int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_paged(cache, batch);
+    if (rc == DFP4_OK && (!grouped(cache, heads) || batch.tokens * heads > (int64_t)1 << 30 || window < 0 || window > (int64_t)1 << 30 || !(softcap >= 0.0f)))
+        rc = DFP4_ERR_SHAPE;
+    if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
+    if ((rc = check_rows(q, q_stride, q_head_stride)) != DFP4_OK || (rc = check_rows(out, out_stride, out_head_stride)) != DFP4_OK) return rc;
+    if (!aligned(slopes, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return DFP4_ERR_ALIGN;
+    const size_t need = paged_attention_workspace_bytes(cache, batch, heads);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return DFP4_ERR_WORKSPACE;
+    const AttentionArgs a{paged_args(cache, batch), static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, slopes,
+                          static_cast<float*>(workspace), q_stride, q_head_stride, out_stride, out_head_stride, scale, softcap, (int)heads,
+                          (int)window, 1, 1};
+    return launch_paged_attention(a, cache, batch, static_cast<hipStream_t>(stream));
+}
+
+int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, const void* k, int64_t k_stride,
+                   int64_t k_head_stride, int64_t kv_heads, int64_t tokens, int64_t head_dim, const float* q_weight,
+                   const float* k_weight, float eps, const int32_t* positions, const float* inv_freq, int64_t rotary,
+                   int interleaved, void* q_out, void* k_out, void* stream) {
+    if (head_dim < 32 || head_dim > 256 || head_dim % 32 != 0 || rotary < 0 || rotary > head_dim || rotary % 16 != 0 || heads < 0 || kv_heads < 0 ||
+        heads > (1 << 16) || kv_heads > (1 << 16) || tokens < 0 || tokens > (int64_t)1 << 30)
+        return DFP4_ERR_SHAPE;
+    if (tokens == 0 || heads + kv_heads == 0) return DFP4_OK;
+    int rc = DFP4_OK;
+    if (heads > 0 && ((rc = check_rows(q, q_stride, q_head_stride)) != DFP4_OK || (rc = check_rows(q_out, 8, 8)) != DFP4_OK)) return rc;
+    if (kv_heads > 0 && ((rc = check_rows(k, k_stride, k_head_stride)) != DFP4_OK || (rc = check_rows(k_out, 8, 8)) != DFP4_OK)) return rc;
+    if (rotary > 0 && (!positions || !inv_freq)) return DFP4_ERR_NULL;
+    if (!aligned(q_weight, 4) || !aligned(k_weight, 4) || !aligned(positions, 4) || !aligned(inv_freq, 4)) return DFP4_ERR_ALIGN;
+    const NormRopeArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out),
+                         q_weight, k_weight, inv_freq, positions, q_stride, q_head_stride, k_stride, k_head_stride, (int)heads, (int)kv_heads,
+                         (int)tokens, (int)head_dim, (int)rotary, interleaved, eps};
+    return launch_norm_rope(a, static_cast<hipStream_t>(stream));
 }
 
 int dfp4_formatbook(uint8_t* out) {

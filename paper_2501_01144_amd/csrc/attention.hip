@@ -1,0 +1,548 @@
+// Attention of new tokens over the paged 4-bit cache (formulas and layouts: include/dfp4.h, paged.h).
+//
+// Rows of a (sequence, KV head) are its new tokens times the query heads of the group, so that they share keys and values.
+// With tokens as rows and query rows as columns, softmax statistics of a query are one number a lane:
+//   S^T = K Q^T, on the block-scaled instruction 16 x 16 x 128 in FP8.  Every DialectFP4 magnitude 0.5 u is an E4M3 number and a
+//     block's exponent byte is the instruction's scale, so a dword of codes costs eight vector instructions and no multiplication.
+//     A query goes in as the sum of two FP8 numbers (rounded to 4 bits, and what that left: the 8 bits of a bf16).
+//   O^T = V^T P^T, on 16 x 16 x 32 in bf16: the values' FP8 bytes become bf16 with their block's scale in one conversion for two (also
+//     exact), a probability is the sum of two bf16 numbers.  (As two FP8 numbers a probability has 8 bits down to 2^-19 of the largest and
+//     fewer below, which shows where the values at the largest are zero; a sixth fewer vector instructions for values.)
+// Both leave in lane (g, c) rows 4 g .. 4 g + 3 of column c, and O^T may take its 128 tokens in any order.  So row 4 g + i of tile t
+// (0 .. 7) of S^T is token 32 g + 4 t + i of a step of 128: a lane has the scores of the chunk of 32 whose values it expands and
+// whose probabilities it supplies, and nothing moves between lanes.
+//
+// Values of the sequence's last, incomplete chunk of 32 are bf16 and take the second instruction as they are, at the end.
+#include <type_traits>
+#include <utility>
+
+#include "paged.h"
+
+namespace dfp4 {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef short v2s __attribute__((ext_vector_type(2)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+// E4M3 bytes of the magnitudes 0.5 u of every dialect
+struct F8Rows { uint8_t b[kDialects][8]; };
+constexpr F8Rows make_f8_rows() {
+    F8Rows r{};
+    for (int d = 0; d < kDialects; ++d)
+        for (int j = 0; j < 8; ++j) {
+            const int u = kBook[d][j], top = u >= 8 ? 3 : u >= 4 ? 2 : u >= 2 ? 1 : 0;
+            r.b[d][j] = u == 0 ? 0 : (uint8_t)(((top - 1 + 7) << 3) | ((u << (3 - top)) & 7));
+        }
+    return r;
+}
+__device__ const F8Rows g_f8_rows = make_f8_rows();
+
+template <class F, int... I>
+__device__ __forceinline__ void each(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) { each(f, std::make_integer_sequence<int, N>{}); }
+
+// 16 codes (two dwords in the cell's order) to 16 FP8 bytes
+template <int AT>                                                    // into registers AT .. AT + 3
+__device__ __forceinline__ void expand16(uint2 c, uint2 row, v8i& a) {
+    a[AT] = (int)(__builtin_amdgcn_perm(row.y, row.x, c.x & 0x07070707u) | ((c.x << 4) & 0x80808080u));
+    a[AT + 1] = (int)(__builtin_amdgcn_perm(row.y, row.x, (c.x >> 4) & 0x07070707u) | (c.x & 0x80808080u));
+    a[AT + 2] = (int)(__builtin_amdgcn_perm(row.y, row.x, c.y & 0x07070707u) | ((c.y << 4) & 0x80808080u));
+    a[AT + 3] = (int)(__builtin_amdgcn_perm(row.y, row.x, (c.y >> 4) & 0x07070707u) | (c.y & 0x80808080u));
+}
+
+// four numbers (|x| <= 448) as FP8, and 2^5 times what that leaves as FP8: what rounding to 4 bits leaves is at most 2^-5 of the
+// largest, and so much further down reach the subnormal numbers
+constexpr int kLoShift = 5;
+__device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, int& hi, int& lo) {
+    int h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+    h = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, h, true);
+    const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+    constexpr float kBy = 1.0f / (1 << kLoShift);                   // the conversion divides by it
+    v2s l = {0, 0};
+    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x0 - a[0], x1 - a[1], kBy, false);
+    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x2 - b[0], x3 - b[1], kBy, true);
+    lo = __builtin_bit_cast(int, l);
+    hi = h;
+}
+
+// c += a (hi + 2^-5 lo), hi times 2^(sb - 127).  The compiler lets a result overlap an operand that it sees no further use of, which the instruction
+// overwrites before it has read it for the last time: operands are in use until the end here (the build checks).
+template <int OPSEL>
+__device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& lo, v4f& c, int sa, int sb, int sb_lo) {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, c, 0, 0, OPSEL, sa, 0, sb);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, c, 0, 0, OPSEL, sa, 0, sb_lo);
+    asm volatile("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
+}
+
+// 32 codes (in 16 bytes) of a scale and a dialect to bf16: fragments of four instructions, tokens 8 q .. 8 q + 7 in the q-th
+__device__ __forceinline__ void expand_bf16(uint4 c, uint2 row, uint32_t ebyte, v8b (&v)[4]) {
+    const float scale = as_f(ebyte << 23);                          // the conversion goes by the exponent bits (0: 2^-127)
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = __builtin_amdgcn_perm(row.y, row.x, w[q] & 0x07070707u) | ((w[q] << 4) & 0x80808080u);
+        const uint32_t hi = __builtin_amdgcn_perm(row.y, row.x, (w[q] >> 4) & 0x07070707u) | (w[q] & 0x80808080u);
+        const v2b x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+                          __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)};
+        v[q] = __builtin_bit_cast(v8b, x);
+    }
+}
+
+// eight probabilities as the sum of two bf16 each (the first cut off, the second rounded: 16 bits)
+__device__ __forceinline__ void split8(const float* x, v8b& hi, v8b& lo) {
+    uint32_t h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        h[j] = __builtin_amdgcn_perm(as_u(x[2 * j + 1]), as_u(x[2 * j]), 0x07060302u);
+        lo[2 * j] = (__bf16)(x[2 * j] - as_f(as_u(x[2 * j]) & 0xffff0000u));
+        lo[2 * j + 1] = (__bf16)(x[2 * j + 1] - as_f(as_u(x[2 * j + 1]) & 0xffff0000u));
+    }
+    hi = __builtin_bit_cast(v8b, make_uint4(h[0], h[1], h[2], h[3]));
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+// max over the four lanes of a column
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+constexpr float kNone = -__builtin_inff();
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Which keys a block of 16 query rows sees, and how they are split between workgroups: alike in the kernel that adds the parts up.
+struct Range {
+    int p_min, p_max;            // positions of the first and the last row
+    int first, end, whole;       // chunks of 32: [first, end), values quantized below `whole`
+    int steps, parts;            // of four chunks; workgroups that have some
+};
+__device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequence& s, int group, int row0) {
+    Range r;
+    const int rows = s.n * group, last_row = min(row0 + 15, rows - 1);
+    r.p_min = s.length - s.n + row0 / group;
+    r.p_max = s.length - s.n + last_row / group;
+    const int t_end = min(r.p_max + 1, s.length), t_begin = a.window > 0 ? max(0, r.p_min - a.window + 1) : 0;
+    r.first = t_begin / 32;
+    r.end = t_end > t_begin ? (t_end + 31) / 32 : r.first;
+    r.whole = min(r.end, s.length / 32);
+    r.steps = max(0, (r.whole - r.first + 3) / 4);
+    r.parts = min(a.splits, max(1, (r.steps + a.split_steps - 1) / a.split_steps));
+    return r;
+}
+
+// One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
+// add up in LDS.
+template <int D, bool EXTRA>
+__global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionArgs a) {
+    using C = Cell<D>;
+    constexpr int KT = C::KT, NJ = C::NJ;
+    constexpr uint32_t kPitch = D + 4;
+    __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
+    __shared__ __attribute__((aligned(16))) float s_o[kWaves * 16 * kPitch];
+    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const PagedArgs& p = a.paged;
+    const int b = (int)(blockIdx.x / (uint32_t)p.kv_heads), kv_head = (int)(blockIdx.x % (uint32_t)p.kv_heads), part = (int)blockIdx.y;
+    const int group = a.heads / p.kv_heads;
+    const Sequence s = sequence(p, b);
+    if (tid < kDialects * 8 / 4) reinterpret_cast<uint32_t*>(s_rows)[tid] = reinterpret_cast<const uint32_t*>(&g_f8_rows.b[0][0])[tid];
+    __syncthreads();
+    const uint2* const table = reinterpret_cast<const uint2*>(s_rows);
+    const float to_log2 = a.scale * kLog2e;
+
+    for (int row0 = (int)blockIdx.z * 16; row0 < s.n * group; row0 += (int)gridDim.z * 16) {
+        const Range r = key_range(a, s, group, row0);
+        if (part >= r.parts) continue;
+        const int step0 = part * a.split_steps, step1 = part == r.parts - 1 ? r.steps : min(r.steps, step0 + a.split_steps);
+        const int row = row0 + (int)c;
+        const bool row_ok = row < s.n * group;
+        const int head = kv_head * group + (row_ok ? row % group : 0);
+        const int64_t token = s.first + (row_ok ? row / group : 0);
+        const int pos = s.length - s.n + (row_ok ? row / group : 0);
+        const float slope = EXTRA && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+
+        // ---- queries: 16 rows, both parts, a scale per block of 32
+        v8i q_hi[KT], q_lo[KT];
+        int q_scale[KT];
+        each<KT>([&](auto kt_c) {
+            constexpr int kt = decltype(kt_c)::value;
+            const uint16_t* src = a.q + token * a.q_stride + (int64_t)head * a.q_head_stride + kt * 128;
+            // lane (g, c) supplies the scale of block g and halves g % 2 of blocks g / 2 and 2 + g / 2: the scales of those two come
+            // from the lanes that have them
+            auto scale_of = [&](uint32_t block) -> int {
+                if ((int)block >= C::blocks(kt) || !row_ok) return 127;
+                uint32_t top = 0;
+                const uint4* x = reinterpret_cast<const uint4*>(src + block * 32u);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 v = x[j];
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = max(top, max((w[k] >> 7) & 0xffu, (w[k] >> 23) & 0xffu));
+                }
+                return max((int)top - 7, kLoShift);                 // the largest magnitude becomes less than 2^8
+            };
+            q_scale[kt] = scale_of(g);
+            each<2>([&](auto h_c) {
+                constexpr int h = decltype(h_c)::value;
+                const uint32_t block = 2u * h + (g >> 1);
+                const int scale = __shfl(q_scale[kt], (int)(block * 16u + c));
+                const bool on = row_ok && (int)block < C::blocks(kt);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (on) v = *reinterpret_cast<const uint4*>(src + block * 32u + (g & 1u) * 16u + k * 8);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - scale);
+                    int hi, lo;
+                    split4(x[0], x[1], x[2], x[3], hi, lo);
+                    q_hi[kt][4 * h + 2 * k] = hi;
+                    q_lo[kt][4 * h + 2 * k] = lo;
+                    split4(x[4], x[5], x[6], x[7], hi, lo);
+                    q_hi[kt][4 * h + 2 * k + 1] = hi;
+                    q_lo[kt][4 * h + 2 * k + 1] = lo;
+                }
+            });
+        });
+
+        v4f o[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[j] = v4f{0, 0, 0, 0};
+        float m = kNone, l = 0.0f;
+
+        // a score to base 2: cap, bias and mask
+        auto finish = [&](float x, int t, bool there) {
+            x *= to_log2;
+            if constexpr (EXTRA) {
+                if (a.softcap > 0.0f) {
+                    // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
+                    const float cap = a.softcap * kLog2e, e = exp2_(x * (2.0f * kLog2e / cap));
+                    x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(e + 1.0f);
+                }
+                x -= slope * (float)(pos - t);
+            }
+            return there && t <= pos && (a.window <= 0 || t > pos - a.window) ? x : kNone;
+        };
+        // the running maximum takes in `top`; what was added up so far is scaled to it
+        auto raise = [&](float top) {
+            const float next = fmaxf(m, column_max(top)), base = next == kNone ? 0.0f : next;
+            const float by = exp2_(m - base);
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[j][i] *= by;
+            m = next;
+            return base;
+        };
+
+        // scores of a tile: the lane's token is at kc's place `token`
+        auto scores = [&](const uint8_t* kc, uint32_t token, auto t_c, const int (&scale)[KT], const uint32_t (&id)[KT]) {
+            constexpr int t = decltype(t_c)::value;                 // byte of `scale`
+            v4f acc = v4f{0, 0, 0, 0};
+            each<KT>([&](auto kt_c) {
+                constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
+                const uint8_t* row = kc + token * (D / 2) + kt * 64;
+                v8i k8;
+                if constexpr (nb == 4) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(row + g * 16u);
+                    expand16<0>(make_uint2(w.x, w.y), table[id[kt] & 15u], k8);
+                    expand16<4>(make_uint2(w.z, w.w), table[id[kt] >> 4], k8);
+                } else {
+                    expand16<0>(*reinterpret_cast<const uint2*>(row + g * 8u), table[id[kt] & 15u], k8);
+                    k8[4] = k8[5] = k8[6] = k8[7] = 0;
+                    // the queries are zero in lanes without a second half; what they read is their own first half
+                    if constexpr (nb == 3) expand16<4>(*reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u)), table[id[kt] >> 4], k8);
+                }
+                product<t>(k8, q_hi[kt], q_lo[kt], acc, scale[kt], q_scale[kt], q_scale[kt] - kLoShift);
+            });
+            return acc;
+        };
+        auto block_of = [&](int kt) { return kt * 4 + min(g, (uint32_t)(C::blocks(kt) - 1)); };
+
+        for (int step = step0 + wave; step < step1; step += kWaves) {
+            const int chunk0 = r.first + 4 * step;
+            // the step's cells; absent keys are masked, their codes are read anywhere and their values taken as zeros
+            const int64_t a0 = cell_offset<D>(p, b, kv_head, chunk0);
+            const int64_t a1 = chunk0 + 1 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 1) : -1;
+            const int64_t a2 = chunk0 + 2 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 2) : -1;
+            const int64_t a3 = chunk0 + 3 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 3) : -1;
+            if ((a0 & a1 & a2 & a3) < 0) continue;
+            auto pick = [&](uint32_t k) { return k == 0 ? a0 : k == 1 ? a1 : k == 2 ? a2 : a3; };
+            const int64_t ak = pick(c >> 2), av = pick(g);
+            const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
+
+            // ---- scores of 128 keys
+            float x[8][4];
+            {
+                uint2 scales[KT], ids[KT];
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    scales[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block_of(kt)) * 8u);
+                    ids[kt] = *reinterpret_cast<const uint2*>(kc + C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u);
+                }
+                each<8>([&](auto t_c) {
+                    constexpr int t = decltype(t_c)::value;
+                    int scale[KT];
+                    uint32_t id[KT];
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        scale[kt] = (int)(t < 4 ? scales[kt].x : scales[kt].y);
+                        id[kt] = ((t < 4 ? ids[kt].x : ids[kt].y) >> (8 * (t & 3))) & 0xffu;
+                    }
+                    const v4f acc = scores(kc, 4u * t + (c & 3u), std::integral_constant<int, t & 3>{}, scale, id);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][i] = acc[i];
+                });
+            }
+
+            // ---- softmax
+            float top = kNone;
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[t][i] = finish(x[t][i], 32 * (chunk0 + (int)g) + 4 * t + i, av >= 0);
+                    top = fmaxf(top, x[t][i]);
+                }
+            const float base = raise(top);
+            v8b p_hi[4], p_lo[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[2 * q + i / 4][i % 4] = exp2_(x[2 * q + i / 4][i % 4] - base);
+                    l += x[2 * q + i / 4][i % 4];
+                }
+                split8(x[2 * q], p_hi[q], p_lo[q]);
+            }
+
+            // ---- values
+            const uint32_t shift = 4u * (c & 1u);
+#pragma unroll
+            for (int w = 0; w < (NJ + 3) / 4; ++w) {
+                uint32_t scales = *reinterpret_cast<const uint32_t*>(vc + C::kVExps + c * C::VE + 4 * w);
+                const uint32_t ids = *reinterpret_cast<const uint32_t*>(vc + C::kVIds + (c >> 1) * C::VE + 4 * w) >> shift;
+                if (av < 0) scales = 0x7f7f7f7fu;                   // finite (the probabilities are zero)
+#pragma unroll
+                for (int jj = 0; jj < 4 && 4 * w + jj < NJ; ++jj) {
+                    const int j = 4 * w + jj;
+                    v8b v[4];
+                    expand_bf16(*reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u), table[(ids >> (8 * jj)) & 15u],
+                                (scales >> (8 * jj)) & 0xffu, v);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q], p_hi[q], o[j], 0, 0, 0);
+                        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q], p_lo[q], o[j], 0, 0, 0);
+                    }
+                }
+            }
+        }
+
+        // ---- the incomplete chunk: 32 keys, row 4 g + i of tile t (0, 1) is token 8 g + 4 t + i
+        const int left = r.end > r.whole ? s.length - 32 * r.whole : 0;
+        if (left > 0 && part == r.parts - 1 && wave == (step1 - step0) % kWaves && s.slot >= 0) {
+            const uint8_t* kc = cell<D>(p, b, kv_head, r.whole);
+            if (kc) {
+                float x[8];
+                each<2>([&](auto t_c) {
+                    constexpr int t = decltype(t_c)::value;
+                    const uint32_t token_in = 8u * (c >> 2) + 4u * t + (c & 3u);
+                    int scale[KT];
+                    uint32_t id[KT];
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        scale[kt] = kc[C::kKExps + ((c & 3u) * C::NB + block_of(kt)) * 8u + (token_in >> 2)];
+                        id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + (token_in >> 2)];
+                    }
+                    const v4f acc = scores(kc, token_in, std::integral_constant<int, 0>{}, scale, id);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[4 * t + i] = acc[i];
+                });
+                float top = kNone;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int in = 8 * (int)g + i;
+                    x[i] = finish(x[i], 32 * r.whole + in, in < left);
+                    top = fmaxf(top, x[i]);
+                }
+                const float base = raise(top);
+                v8b p_hi, p_lo;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = exp2_(x[i] - base);
+                    l += x[i];
+                }
+                split8(x, p_hi, p_lo);
+                const uint16_t* v = residual<D>(p, s.slot, kv_head);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(v + (16u * j + c) * 32u + 8u * g);
+                    uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {       // what the slot holds beyond the tokens there are is anything
+                        if (8 * (int)g + 2 * i >= left) u[i] = 0;
+                        else if (8 * (int)g + 2 * i + 1 >= left) u[i] &= 0xffffu;
+                    }
+                    const v8b vv = __builtin_bit_cast(v8b, make_uint4(u[0], u[1], u[2], u[3]));
+                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p_hi, o[j], 0, 0, 0);
+                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p_lo, o[j], 0, 0, 0);
+                }
+            }
+        }
+
+        // ---- the four waves together
+        l = column_sum(l);
+        if (lane < 16) {
+            s_m[wave][c] = m;
+            s_l[wave][c] = l;
+        }
+        __syncthreads();
+        const float all = fmaxf(fmaxf(s_m[0][c], s_m[1][c]), fmaxf(s_m[2][c], s_m[3][c]));
+        const float by = m == kNone ? 0.0f : exp2_(m - all);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            float4 v = make_float4(o[j][0] * by, o[j][1] * by, o[j][2] * by, o[j][3] * by);
+            *reinterpret_cast<float4*>(&s_o[(wave * 16 + c) * kPitch + 16 * j + 4 * g]) = v;
+        }
+        __syncthreads();
+        for (uint32_t i = tid; i < 16u * (D / 8); i += kThreads) {
+            const uint32_t rr = i / (D / 8), d = i % (D / 8) * 8u;
+            const int at_row = row0 + (int)rr;
+            if (at_row >= s.n * group) break;
+            const float top = fmaxf(fmaxf(s_m[0][rr], s_m[1][rr]), fmaxf(s_m[2][rr], s_m[3][rr]));
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += s_m[w][rr] == kNone ? 0.0f : s_l[w][rr] * exp2_(s_m[w][rr] - top);
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) v[j] += s_o[(w * 16 + rr) * kPitch + d + j];
+            }
+            const int64_t t = s.first + at_row / group;
+            const int h = kv_head * group + at_row % group;
+            if (r.parts == 1) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                v8b y;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = (__bf16)(v[j] * inv);
+                *reinterpret_cast<v8b*>(a.out + t * a.out_stride + (int64_t)h * a.out_head_stride + d) = y;
+                if (a.lse && d == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
+            } else {
+                const int64_t slot = (t * a.heads + h) * a.splits + part;
+                float4* dst = reinterpret_cast<float4*>(a.partial + slot * D + d);
+                dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+                dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+                if (d == 0) {
+                    float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
+                    ml[0] = top;
+                    ml[1] = sum;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Adds up the parts of a query row: one wave a row, D / 64 elements a lane.  Parts in their order: the same sum every time.
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(AttentionArgs a) {
+    const PagedArgs& p = a.paged;
+    const uint32_t lane = threadIdx.x & 63u;
+    const int b = (int)blockIdx.x, group = a.heads / p.kv_heads;
+    const Sequence s = sequence(p, b);
+    for (int64_t row = (int64_t)blockIdx.y * kWaves + (threadIdx.x >> 6); row < (int64_t)s.n * a.heads; row += (int64_t)gridDim.y * kWaves) {
+        const int64_t t = s.first + row / a.heads;
+        const int h = (int)(row % a.heads), in_group = (int)(row / a.heads) * group + h % group;
+        const int parts = key_range(a, s, group, in_group / 16 * 16).parts;
+        if (parts == 1) continue;                       // written by the only part
+        const int64_t slot = (t * a.heads + h) * a.splits;
+        const float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
+        float top = kNone, sum = 0.0f;
+        for (int k = 0; k < parts; ++k) top = fmaxf(top, ml[2 * k]);
+        float o[D / 64 + (D % 64 != 0)] = {};
+        for (int k = 0; k < parts; ++k) {
+            const float by = ml[2 * k] == kNone ? 0.0f : exp2_(ml[2 * k] - top);
+            sum += by * ml[2 * k + 1];
+#pragma unroll
+            for (int j = 0; 64 * j < D; ++j)
+                if (64 * j + (int)lane < D) o[j] += by * a.partial[(slot + k) * D + 64 * j + lane];
+        }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int j = 0; 64 * j < D; ++j)
+            if (64 * j + (int)lane < D)
+                reinterpret_cast<__bf16*>(a.out)[t * a.out_stride + (int64_t)h * a.out_head_stride + 64 * j + lane] = (__bf16)(o[j] * inv);
+        if (a.lse && lane == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
+    }
+}
+
+struct Split {
+    int splits, steps;           // workgroups along the keys, steps of 128 keys of each
+};
+int64_t row_blocks(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
+    const int64_t most = batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens;
+    const int64_t blocks = (most * (heads / cache.kv_heads) + 15) / 16;
+    return blocks < 65535 ? blocks : 65535;
+}
+Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
+    const int64_t table = batch.table_width * cache.page_tokens;
+    const int64_t most = batch.max_length > 0 && batch.max_length < table ? batch.max_length : table;
+    const int64_t rounds = (most + 128 * kWaves - 1) / (128 * kWaves);
+    const int64_t groups = batch.batch * cache.kv_heads * row_blocks(cache, batch, heads);
+    int64_t want = (4 * (int64_t)device_cu_count() + groups - 1) / groups;
+    if (want > rounds) want = rounds;
+    if (want < 1) want = 1;
+    if (want > 256) want = 256;
+    const int64_t per = (rounds + want - 1) / want;
+    return Split{(int)(rounds > 0 ? (rounds + per - 1) / per : 1), (int)(per > 0 ? per * kWaves : kWaves)};
+}
+
+}  // namespace
+
+size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
+    const Split sp = choose_split(cache, batch, heads);
+    return sp.splits > 1 ? (size_t)(batch.tokens * heads * sp.splits) * (size_t)(cache.head_dim + 2) * 4u : 0;
+}
+
+int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream) {
+    const Split sp = choose_split(cache, batch, a.heads);
+    a.splits = sp.splits;
+    a.split_steps = sp.steps;
+    const dim3 grid((uint32_t)(batch.batch * cache.kv_heads), (uint32_t)sp.splits, (uint32_t)row_blocks(cache, batch, a.heads));
+    const bool extra = a.softcap > 0.0f || a.slopes;
+    with_head_dim(cache.head_dim, [&](auto d) {
+        constexpr int kD = decltype(d)::value;
+        if (extra) hipLaunchKernelGGL((paged_attention_kernel<kD, true>), grid, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((paged_attention_kernel<kD, false>), grid, dim3(kThreads), 0, stream, a);
+        if (sp.splits > 1) {
+            const int64_t rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * a.heads;
+            const int64_t blocks = (rows + kWaves - 1) / kWaves;
+            hipLaunchKernelGGL((paged_attention_join_kernel<kD>), dim3((uint32_t)batch.batch, (uint32_t)(blocks < 65535 ? blocks : 65535)),
+                               dim3(kThreads), 0, stream, a);
+        }
+    });
+    return check_launch();
+}
+
+}  // namespace dfp4

@@ -1,0 +1,125 @@
+// The paged 4-bit cache: where a cell keeps what, and what a kernel knows of a batch.
+//
+// A cell holds 32 tokens of one KV head.  Its parts lie as the attention kernel's lanes read them (lane = 16 g + c).
+//   K codes  [token][unit of 16 elements, 8 bytes].  The block-scaled matrix instruction 16 x 16 x 128 on FP8 wants in lane (g, c) bytes
+//            16 g .. 16 g + 15 of both halves of the 128 it adds over, and the scale of the g-th 32 (checked on the hardware, random
+//            operands and scales): half g % 2 of blocks g / 2 and 2 + g / 2.  Where 128 elements are whole, both halves of a lane
+//            lie together (k_unit), so that it loads 16 bytes
+//   V codes  [d][dword of 8 tokens]: a lane takes the 32 tokens of a d
+//   K exps   [token % 4][block][token / 4]: a lane takes the 8 tokens 4 t + i of a block, t = 0 .. 7
+//   K ids    [token % 4][pair][token / 4]: dialects of blocks p and p + 2 of a 128 in one byte
+//   V exps   [d % 16][d / 16]       V ids  [d % 16 / 2][d / 16]: dialects of d (even) and d + 1
+// A code dword holds element j in the low nibble of byte j and element 4 + j in its high nibble, so that two table look-ups give
+// the bytes in order.
+#pragma once
+#include "common.h"
+#include "formatbook.h"
+
+namespace dfp4 {
+
+template <int D>
+struct Cell {
+    static constexpr int NB = D / 32;                    // blocks of a key
+    static constexpr int KT = (NB + 3) / 4;              // instructions that add over a key
+    static constexpr int NJ = D / 16;                    // 16-row tiles of V^T
+    static constexpr int VE = (NJ + 3) / 4 * 4;          // bytes of a row of V exps
+    static constexpr int NP = 2 * KT;                    // dialect bytes of a key
+    static constexpr uint32_t kVCodes = 16 * D, kKExps = 32 * D, kKIds = kKExps + 32 * NB, kVExps = kKIds + 32 * NP,
+                              kVIds = kVExps + 16 * VE, kEnd = kVIds + 8 * VE, kBytes = (kEnd + 63) / 64 * 64;
+    // blocks of instruction kt
+    static constexpr int blocks(int kt) { return NB - 4 * kt < 4 ? NB - 4 * kt : 4; }
+    // place (in units of 8 bytes) of elements 16 u .. 16 u + 15 of a key
+    static __host__ __device__ constexpr int k_unit(int u) {
+        return blocks(u / 8) == 4 ? u / 8 * 8 + u % 4 * 2 + u % 8 / 4 : u;
+    }
+};
+
+// the same for a head dimension known at run time; 0 if it is not supported
+inline uint32_t cell_bytes(int64_t D) {
+    return D == 64 ? Cell<64>::kBytes : D == 96 ? Cell<96>::kBytes : D == 128 ? Cell<128>::kBytes : D == 192 ? Cell<192>::kBytes
+         : D == 256 ? Cell<256>::kBytes : 0;
+}
+template <class F>
+inline void with_head_dim(int64_t D, F&& f) {
+    if (D == 64) f(std::integral_constant<int, 64>{});
+    else if (D == 96) f(std::integral_constant<int, 96>{});
+    else if (D == 128) f(std::integral_constant<int, 128>{});
+    else if (D == 192) f(std::integral_constant<int, 192>{});
+    else f(std::integral_constant<int, 256>{});
+}
+
+struct PagedArgs {
+    uint8_t* pages;
+    uint16_t* residual;
+    const int32_t *cu, *lengths, *table, *slots;
+    int n_pages, n_slots, page_chunks, kv_heads, batch, width, tokens;
+    uint64_t per_page;               // 2^40 / page_chunks, rounded up: chunk / page_chunks is chunk * per_page >> 40 (page_chunks <= 2^15,
+};                                   // chunk < 2^25)
+
+inline PagedArgs paged_args(const dfp4_cache& c, const dfp4_batch& b) {
+    return PagedArgs{c.pages, c.residual, b.cu_tokens, b.lengths, b.table, b.slots, (int)c.n_pages, (int)c.n_slots,
+                     (int)(c.page_tokens / 32), (int)c.kv_heads, (int)b.batch, (int)b.table_width, (int)b.tokens,
+                     (((uint64_t)1 << 40) + (uint64_t)(c.page_tokens / 32) - 1) / (uint64_t)(c.page_tokens / 32)};
+}
+
+// New tokens [first, first + n) of the dense arrays are positions [length - n, length) of the sequence.
+struct Sequence {
+    int first, n, length, slot;      // slot -1: none
+};
+
+__device__ __forceinline__ Sequence sequence(const PagedArgs& p, int b) {
+    const int t0 = min(max(p.cu[b], 0), p.tokens), t1 = min(max(p.cu[b + 1], t0), p.tokens);
+    const int64_t most = (int64_t)p.width * p.page_chunks * 32;
+    const int slot = p.slots[b];
+    return Sequence{t0, t1 - t0, (int)min((int64_t)max(p.lengths[b], 0), most), slot >= 0 && slot < p.n_slots ? slot : -1};
+}
+
+// Where the cell of a chunk of 32 tokens (which the length says is there) lies in the pool; -1 where its page is none of the pool's.
+template <int D>
+__device__ __forceinline__ int64_t cell_offset(const PagedArgs& p, int b, int head, int chunk) {
+    const int in_table = (int)((uint64_t)chunk * p.per_page >> 40), page = p.table[(int64_t)b * p.width + in_table];
+    if (page < 0 || page >= p.n_pages) return -1;
+    return (((int64_t)page * p.kv_heads + head) * p.page_chunks + (chunk - in_table * p.page_chunks)) * Cell<D>::kBytes;
+}
+template <int D>
+__device__ __forceinline__ uint8_t* cell(const PagedArgs& p, int b, int head, int chunk) {
+    const int64_t at = cell_offset<D>(p, b, head, chunk);
+    return at < 0 ? nullptr : p.pages + at;
+}
+
+// bf16 [head_dim, 32] of a slot
+template <int D>
+__device__ __forceinline__ uint16_t* residual(const PagedArgs& p, int slot, int head) {
+    return p.residual + ((int64_t)slot * p.kv_heads + head) * (D * 32);
+}
+
+int launch_paged_write(const void* k, int64_t ks, int64_t khs, const void* v, int64_t vs, int64_t vhs, const dfp4_cache& cache,
+                       const dfp4_batch& batch, hipStream_t stream);
+int launch_paged_read(const dfp4_cache& cache, const dfp4_batch& batch, void* k, void* v, int dtype, hipStream_t stream);
+
+struct AttentionArgs {
+    PagedArgs paged;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    const float* slopes;
+    float* partial;                  // [tokens, heads, splits, head_dim], then [tokens, heads, splits, 2]
+    int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+    float scale, softcap;
+    int heads, window, splits, split_steps;
+};
+size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads);
+int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream);
+
+struct NormRopeArgs {
+    const uint16_t *q, *k;
+    uint16_t *q_out, *k_out;
+    const float *q_weight, *k_weight, *inv_freq;
+    const int32_t* positions;
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride;
+    int heads, kv_heads, tokens, head_dim, rotary, interleaved;
+    float eps;
+};
+int launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);
+
+}  // namespace dfp4

@@ -27,6 +27,17 @@ class _CTensor(ctypes.Structure):
                 ("rows", ctypes.c_int64), ("K", ctypes.c_int64)]
 
 
+class _CCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64),
+                ("n_slots", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+
+
+class _CBatch(ctypes.Structure):
+    _fields_ = [("cu_tokens", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("batch", ctypes.c_int64), ("table_width", ctypes.c_int64), ("tokens", ctypes.c_int64), ("max_new", ctypes.c_int64),
+                ("max_length", ctypes.c_int64)]
+
+
 SYMBOLS = [
     "dfp4_quantize", "dfp4_quantize_b64", "dfp4_quantize_mse", "dfp4_quantize_t", "mxfp4_quantize_t", "dfp4_quantize_t_at", "dfp4_dequantize", "dfp4_gemm", "dfp4_gemm_batched", "dfp4_gemm_workspace_bytes", "dfp4_gemm_noalloc",
     "dfp4_quantize_block", "dfp4_dequantize_block", "dfp4_gemm_blocks",
@@ -37,6 +48,8 @@ SYMBOLS = [
     "dfp4_gemm_native_packed", "mxfp4_gemm_native_packed", "dfp4_gemm_native_splitk_bytes",
     "dfp4_gemm_requant", "mxfp4_gemm_requant", "dfp4_gemm_requant_workspace_bytes", "dfp4_gemm_requant_batched",
     "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_gemm", "dfp4_formatbook", "dfp4_strerror",
+    "dfp4_paged_cell_bytes", "dfp4_paged_write", "dfp4_paged_read", "dfp4_paged_attention_workspace_bytes", "dfp4_paged_attention",
+    "dfp4_norm_rope",
 ]
 
 
@@ -120,6 +133,19 @@ def load():
     lib.mxfp4_gemm_requant.restype = ci
     lib.dfp4_gemm_requant_workspace_bytes.argtypes = [i64, i64, i64]
     lib.dfp4_gemm_requant_workspace_bytes.restype = ctypes.c_size_t
+    cf = ctypes.c_float
+    lib.dfp4_paged_cell_bytes.argtypes = [i64]
+    lib.dfp4_paged_cell_bytes.restype = ctypes.c_size_t
+    lib.dfp4_paged_write.argtypes = [vp, i64, i64, vp, i64, i64, _CCache, _CBatch, vp]
+    lib.dfp4_paged_write.restype = ci
+    lib.dfp4_paged_read.argtypes = [_CCache, _CBatch, vp, vp, ci, vp]
+    lib.dfp4_paged_read.restype = ci
+    lib.dfp4_paged_attention_workspace_bytes.argtypes = [_CCache, _CBatch, i64]
+    lib.dfp4_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.dfp4_paged_attention.argtypes = [vp, i64, i64, i64, _CCache, _CBatch, cf, cf, i64, vp, vp, i64, i64, vp, vp, ctypes.c_size_t, vp]
+    lib.dfp4_paged_attention.restype = ci
+    lib.dfp4_norm_rope.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, i64, i64, vp, vp, cf, vp, vp, i64, ci, vp, vp, vp]
+    lib.dfp4_norm_rope.restype = ci
     lib.dfp4_formatbook.argtypes = [vp]
     lib.dfp4_strerror.argtypes = [ci]
     lib.dfp4_strerror.restype = ctypes.c_char_p
@@ -541,6 +567,83 @@ def gemm_batched(a, w, batch, M, N, dtype=torch.float32, out=None, workspace=Non
                                     batch, M, N, M * N, _ptr(workspace), nbytes, _stream()),
            "dfp4_gemm_batched")
     return out
+
+
+def _rows3(x, what):
+    assert x.dtype == torch.bfloat16 and x.dim() == 3 and x.is_cuda and (x.stride(2) == 1 or x.shape[2] == 1), \
+        f"{what}: bf16 [tokens, heads, head_dim] on the device, contiguous along head_dim"
+    return x
+
+
+def paged_write(k, v, cache, batch):
+    """dfp4_paged_write: quantize the keys and values of the batch's new tokens, bf16 [tokens, kv_heads, head_dim] each (token and
+    head strides allowed), into a kvcache.PagedCache; `batch` is a kvcache.PagedBatch."""
+    _rows3(k, "k"), _rows3(v, "v")
+    assert k.shape == v.shape and tuple(k.shape[1:]) == (cache.kv_heads, cache.head_dim)
+    _check(load().dfp4_paged_write(_ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), cache.c(), batch.c(k.shape[0]),
+                                   _stream()), "dfp4_paged_write")
+
+
+def paged_read(cache, batch, tokens=None, dtype=torch.bfloat16):
+    """dfp4_paged_read: the values that the cache stands for, k and v [tokens, kv_heads, head_dim], of the batch's tokens (`tokens`
+    of them, by default as many as batch.tokens says)."""
+    tokens = batch.tokens if tokens is None else tokens
+    shape = (tokens, cache.kv_heads, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=dtype, device=cache.pages.device) for _ in range(2))
+    _check(load().dfp4_paged_read(cache.c(), batch.c(tokens), _ptr(k), _ptr(v), BF16 if _is_bf16(dtype) else F32, _stream()), "dfp4_paged_read")
+    return k, v
+
+
+def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=None, return_lse=False, out=None, workspace=None):
+    """dfp4_paged_attention: attention of the batch's new tokens, q bf16 [tokens, heads, head_dim], over the cached tokens of
+    their sequences (these included: paged_write comes first).  scale: 1 / sqrt(head_dim) unless given; softcap, window: 0 is
+    none; slopes: f32 [heads].  Returns out, bf16 like q, or (out, lse), lse f32 [tokens, heads]."""
+    _rows3(q, "q")
+    tokens, heads, head_dim = q.shape
+    assert head_dim == cache.head_dim
+    if out is None:
+        out = torch.empty((tokens, heads, head_dim), dtype=torch.bfloat16, device=q.device)
+    _rows3(out, "out")
+    assert out.shape == q.shape
+    assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_cuda and slopes.is_contiguous() and slopes.numel() == heads)
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    c, b = cache.c(), batch.c(tokens)
+    need = int(load().dfp4_paged_attention_workspace_bytes(c, b, heads))
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, c, b, head_dim ** -0.5 if scale is None else scale, softcap, window,
+                                       _ptr(slopes), _ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(workspace),
+                                       workspace.numel() if workspace is not None else 0, _stream()), "dfp4_paged_attention")
+    return (out, lse) if return_lse else out
+
+
+def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
+    """dfp4_norm_rope: norms of queries and keys per head (where a weight, f32 [head_dim], is given) and their rotation by
+    position, in one pass.  q bf16 [tokens, heads, head_dim], k the same with its heads (or None); positions int32 [tokens];
+    inv_freq f32 [rotary / 2].  Returns q and k (out=(q, k): into these, which may be the inputs where those are contiguous)."""
+    _rows3(q, "q")
+    tokens, heads, head_dim = q.shape
+    if k is not None:
+        _rows3(k, "k")
+        assert k.shape[0] == tokens and k.shape[2] == head_dim
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.is_cuda and w.is_contiguous() and w.numel() == head_dim)
+    assert positions.dtype == torch.int32 and positions.is_cuda and positions.is_contiguous() and positions.numel() == tokens
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_cuda and inv_freq.is_contiguous()
+    if out is None:
+        out = tuple(None if x is None else torch.empty(x.shape, dtype=torch.bfloat16, device=q.device) for x in (q, k))
+    q_out, k_out = out
+    for x, y in ((q, q_out), (k, k_out)):
+        assert (x is None and y is None) or (y.dtype == torch.bfloat16 and y.is_cuda and y.is_contiguous() and y.shape == x.shape)
+    _check(load().dfp4_norm_rope(_ptr(q), q.stride(0), q.stride(1), heads, _ptr(k), k.stride(0) if k is not None else 0,
+                                 k.stride(1) if k is not None else 0, k.shape[1] if k is not None else 0, tokens, head_dim, _ptr(q_weight),
+                                 _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel(), 1 if interleaved else 0,
+                                 _ptr(q_out), _ptr(k_out), _stream()), "dfp4_norm_rope")
+    return q_out, k_out
+
+
+def paged_cell_bytes(head_dim):
+    return int(load().dfp4_paged_cell_bytes(head_dim))
 
 
 def formatbook():

@@ -12,6 +12,9 @@ Host-side bookkeeping only; the arithmetic is in the library's kernels
 (dfp4_quantize_t_at).  Unwritten blocks of the cache are zero (code 0, exponent
 byte 0), so a product over the whole capacity with zero-padded probabilities
 equals the product over the tokens present.
+
+PagedCache and PagedBatch are the same idea for many sequences, keys and values and all KV heads of a layer: the device memory of a
+paged cache and the arrays that describe a batch, for dfp4.paged_write, dfp4.paged_read and dfp4.paged_attention.
 """
 import torch
 
@@ -62,3 +65,49 @@ class ValueCache:
     def residual_values(self):
         """bf16 [n_residual, head_dim]: the tokens not yet quantized."""
         return self.residual[:self.n_residual]
+
+
+class PagedCache:
+    """Pages of `page_tokens` tokens (a multiple of 32) in 4 bits, and slots for the values of incomplete chunks of 32 tokens, which
+    are bf16 until the chunk is whole: one slot for a sequence as long as it lives."""
+
+    def __init__(self, n_pages, page_tokens, kv_heads, head_dim, n_slots, device):
+        cell = dfp4.paged_cell_bytes(head_dim)
+        assert cell > 0, "head_dim: 64, 96, 128, 192 or 256"
+        assert page_tokens > 0 and page_tokens % BLOCK == 0 and kv_heads > 0 and n_pages >= 0 and n_slots >= 0
+        self.n_pages, self.page_tokens, self.kv_heads, self.head_dim, self.n_slots = n_pages, page_tokens, kv_heads, head_dim, n_slots
+        self.pages = torch.zeros((n_pages, kv_heads, page_tokens // BLOCK, cell), dtype=torch.uint8, device=device)
+        self.residual = torch.zeros((n_slots, kv_heads, head_dim, BLOCK), dtype=torch.bfloat16, device=device)
+        self._c = None
+
+    def c(self):
+        if self._c is None:
+            self._c = dfp4._CCache(self.pages.data_ptr() if self.n_pages else 0, self.residual.data_ptr() if self.n_slots else 0, self.n_pages,
+                                   self.page_tokens, self.n_slots, self.kv_heads, self.head_dim)
+        return self._c
+
+
+class PagedBatch:
+    """What a call has to know of its sequences (include/dfp4.h, dfp4_batch): int32 tensors on the device.
+
+    cu_tokens [batch + 1]: sequence b brings rows cu_tokens[b] .. cu_tokens[b + 1] - 1; lengths [batch]: its tokens with these;
+    table [batch, width]: its pages; slots [batch]: its slot.  max_new, max_length: bounds that the host knows, 0: none (they decide
+    how work is split, not what is computed).  tokens: rows in all, where a call cannot take them from its arguments."""
+
+    def __init__(self, cu_tokens, lengths, table, slots, max_new=0, max_length=0, tokens=None):
+        n = lengths.numel()
+        assert cu_tokens.numel() == n + 1 and slots.numel() == n and table.dim() == 2 and table.shape[0] == n
+        for t in (cu_tokens, lengths, table, slots):
+            assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+        self.cu_tokens, self.lengths, self.table, self.slots = cu_tokens, lengths, table, slots
+        self.max_new, self.max_length, self._tokens = max_new, max_length, tokens
+
+    @property
+    def tokens(self):
+        if self._tokens is None:
+            self._tokens = int(self.cu_tokens[-1])           # waits for the device, once
+        return self._tokens
+
+    def c(self, tokens):
+        return dfp4._CBatch(self.cu_tokens.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr(), self.slots.data_ptr(), self.lengths.numel(),
+                            self.table.shape[1], tokens, self.max_new, self.max_length)

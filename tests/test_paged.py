@@ -1,0 +1,489 @@
+"""Serving operators over the paged 4-bit cache: norms and rotation, the cache written and read back, attention over it, each
+against a plain implementation in float64 (the quantizer: the oracle)."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import dfp4_oracle as O
+from paper_2501_01144_amd import dfp4, kvcache, synth
+
+DIMS = [64, 96, 128, 192, 256]
+HALF = torch.finfo(torch.bfloat16).eps / 2          # a rounding to bf16, relative to the value
+
+
+# ---- refusals: no device is touched ----------------------------------------------------------------------------------------
+
+def _cache(pages=256, residual=256, n_pages=4, page_tokens=32, n_slots=2, kv_heads=2, head_dim=64):
+    return dfp4._CCache(pages, residual, n_pages, page_tokens, n_slots, kv_heads, head_dim)
+
+
+def _batch(cu=256, lengths=256, table=256, slots=256, batch=2, table_width=2, tokens=4, max_new=0, max_length=0):
+    return dfp4._CBatch(cu, lengths, table, slots, batch, table_width, tokens, max_new, max_length)
+
+
+BAD = [
+    (dict(head_dim=80), {}, -2), (dict(head_dim=0), {}, -2), (dict(page_tokens=48), {}, -2), (dict(page_tokens=0), {}, -2), (dict(kv_heads=0), {}, -2),
+    (dict(n_pages=-1), {}, -2), (dict(n_slots=-1), {}, -2), (dict(n_pages=1 << 31), {}, -2), ({}, dict(batch=-1), -2), ({}, dict(tokens=-1), -2),
+    ({}, dict(table_width=1 << 26), -2), ({}, dict(max_new=-1), -2), ({}, dict(max_length=-5), -2), ({}, dict(batch=1 << 30), -2),
+    (dict(pages=0), {}, -1), (dict(residual=0), {}, -1), ({}, dict(cu=0), -1), ({}, dict(lengths=0), -1), ({}, dict(table=0), -1), ({}, dict(slots=0), -1),
+    (dict(pages=128), {}, -3), (dict(residual=8), {}, -3), ({}, dict(table=2), -3),
+]
+
+
+@pytest.mark.parametrize("cache,batch,rc", BAD)
+def test_calls_refuse_bad_caches_and_batches(cache, batch, rc):
+    lib, c, b, vp = dfp4.load(), _cache(**cache), _batch(**batch), ctypes.c_void_p
+    assert lib.dfp4_paged_write(vp(16), 128, 64, vp(16), 128, 64, c, b, vp(0)) == rc
+    assert lib.dfp4_paged_read(c, b, vp(16), vp(16), 1, vp(0)) == rc
+    assert lib.dfp4_paged_attention(vp(16), 256, 64, 4, c, b, 1.0, 0.0, 0, vp(0), vp(16), 256, 64, vp(0), vp(16), 1 << 30, vp(0)) == rc
+
+
+def test_calls_refuse_bad_arguments():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    c, b = _cache(), _batch()
+    write = lambda k=16, ks=128, kh=64, v=16, vs=128, vh=64: lib.dfp4_paged_write(vp(k), ks, kh, vp(v), vs, vh, c, b, vp(0))  # noqa: E731
+    assert (write(k=0), write(v=0), write(k=8), write(ks=4), write(kh=63), write(vs=132), write(vh=4)) == (-1, -1, -3, -3, -3, -3, -3)
+    read = lambda k=16, v=16, t=1: lib.dfp4_paged_read(c, b, vp(k), vp(v), t, vp(0))  # noqa: E731
+    assert (read(k=0), read(v=0), read(k=24), read(t=2)) == (-1, -1, -3, -4)
+
+    def attend(q=16, qs=256, qh=64, heads=4, softcap=0.0, window=0, slopes=0, out=16, os=256, oh=64, lse=0, ws=16, n=1 << 30, b=b):
+        return lib.dfp4_paged_attention(vp(q), qs, qh, heads, c, b, 1.0, softcap, window, vp(slopes), vp(out), os, oh, vp(lse), vp(ws), n, vp(0))
+    assert (attend(heads=3), attend(heads=0), attend(heads=-2), attend(window=-1), attend(softcap=-1.0), attend(softcap=float("nan"))) == (-2,) * 6
+    assert (attend(q=0), attend(out=0), attend(q=20), attend(qs=12), attend(oh=2), attend(slopes=2), attend(lse=1), attend(ws=8)) == (-1, -1) + (-3,) * 6
+    # a long context is split between workgroups, and that takes a workspace
+    long = _batch(table_width=1 << 12)
+    need = lib.dfp4_paged_attention_workspace_bytes(c, long, 4)
+    assert need > 0 and attend(b=long, ws=0, n=0) == -5 and attend(b=long, n=need - 1) == -5
+    assert lib.dfp4_paged_attention_workspace_bytes(c, _batch(table_width=4), 4) == 0
+    # nothing to do
+    assert attend(b=_batch(tokens=0)) == 0 and attend(b=_batch(batch=0)) == 0
+    assert lib.dfp4_paged_write(vp(0), 0, 0, vp(0), 0, 0, c, _batch(tokens=0), vp(0)) == 0
+
+    def rope(q=16, qs=256, qh=64, heads=2, k=16, ks=64, kh=64, kv=1, tokens=4, dim=64, pos=16, freq=16, rotary=64, qo=16, ko=16, w=0):
+        return lib.dfp4_norm_rope(vp(q), qs, qh, heads, vp(k), ks, kh, kv, tokens, dim, vp(w), vp(0), 1e-6, vp(pos), vp(freq), rotary, 0, vp(qo), vp(ko), vp(0))
+    assert (rope(dim=80), rope(dim=288), rope(dim=0), rope(rotary=8), rope(rotary=96), rope(rotary=-16), rope(tokens=-1), rope(heads=-1)) == (-2,) * 8
+    assert (rope(q=0), rope(k=0), rope(pos=0), rope(freq=0), rope(qo=0), rope(ko=0)) == (-1,) * 6
+    assert (rope(q=8), rope(qs=100), rope(kh=4), rope(qo=24), rope(w=2)) == (-3,) * 5
+    assert rope(tokens=0) == 0 and rope(heads=0, kv=0) == 0
+
+
+def test_cell_bytes():
+    # 4 bits an element, a scale and a dialect a block of 32, rounded up for the lanes that read them
+    for dim in DIMS:
+        assert 32 * dim <= dfp4.paged_cell_bytes(dim) - 3 * dim / 2 * 2 <= 32 * dim + 32 * 8
+    assert [dfp4.paged_cell_bytes(d) for d in (0, 32, 80, 160, 512, -64)] == [0] * 6
+    assert dfp4.paged_cell_bytes(128) == 4480
+
+
+# ---- plain implementations -------------------------------------------------------------------------------------------------
+
+def _quantized(x):
+    """x bf16 [rows, K]: the values of its 4-bit form, float64."""
+    return O.dfp4_dequantize(*O.dfp4_quantize(synth.to_f64(x))) if x.numel() else synth.to_f64(x)
+
+
+def _keys(k):
+    return _quantized(k.reshape(-1, k.shape[-1])).reshape(k.shape)
+
+
+def _values(v, length):
+    """v bf16 [length, heads, dim]: whole chunks of 32 tokens in 4 bits, the rest as it is."""
+    out = synth.to_f64(v).copy()
+    whole = length // 32 * 32
+    if whole:
+        t = v[:whole].permute(1, 2, 0).reshape(-1, whole)
+        out[:whole] = _quantized(t).reshape(v.shape[1], v.shape[2], whole).transpose(2, 0, 1)
+    return out
+
+
+class Sequences:
+    """Sequences of random keys and values in a cache of pages in random order, brought there in steps."""
+
+    def __init__(self, lengths, dim, kv_heads, page, seed=0, spare=3, poison=True, width=None, factor=6.0):
+        self.g = torch.Generator().manual_seed(seed)
+        self.lengths, self.dim, self.kv_heads, self.page = list(lengths), dim, kv_heads, page
+        n = len(lengths)
+        self.width = width or max(1, -(-max(lengths + [1]) // page))
+        n_pages = n * self.width + spare
+        self.cache = kvcache.PagedCache(n_pages, page, kv_heads, dim, n + 2, torch.device("cuda"))
+        if poison:                      # what nobody wrote may be anything
+            self.cache.pages.fill_(0xff)
+            self.cache.residual.fill_(float("nan"))
+        self.table = torch.randperm(n_pages, generator=self.g)[:n * self.width].view(n, self.width).int()
+        self.slots = torch.randperm(n + 2, generator=self.g)[:n].int()
+        self.k, self.v = [], []
+        for L in lengths:
+            k, v = torch.randn(L, kv_heads, dim, generator=self.g), torch.randn(L, kv_heads, dim, generator=self.g)
+            k[..., 3] *= factor
+            v[..., 5] *= factor
+            self.k.append(k.bfloat16())
+            self.v.append(v.bfloat16())
+
+    def batch(self, new, lengths=None, **hints):
+        cu = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32)
+        lengths = torch.tensor(self.lengths if lengths is None else lengths, dtype=torch.int32)
+        return kvcache.PagedBatch(cu.cuda(), lengths.cuda(), self.table.cuda(), self.slots.cuda(), tokens=int(sum(new)), **hints)
+
+    def write(self, new, after, **hints):
+        k, v = (torch.cat([x[b][after[b] - new[b]:after[b]] for b in range(len(new))]).cuda() for x in (self.k, self.v))
+        dfp4.paged_write(k, v, self.cache, self.batch(new, after, **hints))
+
+    def fill(self):
+        self.write(self.lengths, self.lengths, max_new=max(self.lengths))
+        return self
+
+    def stands_for(self):
+        return [_keys(k) for k in self.k], [_values(v, len(v)) for v in self.v]
+
+
+def _attention(s, q, new, scale, softcap=0.0, window=0, slopes=None):
+    """out, lse, and for the tolerance: sum p |v|, the largest sum |q| |k| of a row's keys, each [tokens, heads(, dim)]."""
+    ks, vs = s.stands_for()
+    q = synth.to_f64(q)
+    heads, group = q.shape[1], q.shape[1] // s.kv_heads
+    out, lse = np.zeros(q.shape), np.full(q.shape[:2], -np.inf)
+    size, dot = np.zeros(q.shape), np.zeros(q.shape[:2])
+    row = 0
+    for b, n in enumerate(new):
+        L = s.lengths[b]
+        for i in range(n):
+            p = L - n + i
+            lo = max(0, p - window + 1) if window else 0
+            for h in range(heads if p >= 0 else 0):
+                k, v = ks[b][lo:p + 1, h // group], vs[b][lo:p + 1, h // group]
+                z = scale * (k @ q[row, h])
+                if softcap:
+                    z = softcap * np.tanh(z / softcap)
+                if slopes is not None:
+                    z = z - float(slopes[h]) * (p - np.arange(lo, p + 1))
+                w = np.exp(z - z.max())
+                lse[row, h] = z.max() + math.log(w.sum())
+                w /= w.sum()
+                out[row, h], size[row, h], dot[row, h] = w @ v, w @ np.abs(v), (np.abs(k) @ np.abs(q[row, h])).max() * abs(scale)
+            row += 1
+    return out, lse, size, dot
+
+
+def _check_attention(got, lse, want):
+    """A probability is off by 2^-8 of itself at most (a bf16), the instruction's sums by 2^-12 of sum |a| |b|
+    (it aligns products to the largest), a score by that of its own sum; the result is rounded to bf16."""
+    out, wlse, size, dot = want
+    score = 2.0 ** -12 * dot
+    got, lse = got.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    tol = HALF * np.abs(out) + (2.0 ** -8 + 2.0 ** -12 + 2 * score[..., None]) * size + 1e-30
+    assert (np.abs(got - out) <= tol).all(), float((np.abs(got - out) / tol).max())
+    none = np.isneginf(wlse)
+    assert np.array_equal(np.isneginf(lse), none) and (got[none] == 0).all()
+    assert (np.abs(lse - wlse)[~none] <= (score + 2.0 ** -20 * (1 + np.abs(wlse)))[~none]).all()
+    norm = np.linalg.norm(out)
+    if norm:
+        assert np.linalg.norm(got - out) <= HALF * norm * 1.1
+
+
+def _attend(s, new, heads, seed=1, softcap=0.0, window=0, slopes=None, scale=None, **hints):
+    q = torch.randn(sum(new), heads, s.dim, generator=torch.Generator().manual_seed(seed))
+    q[..., 7] *= 3
+    q = q.bfloat16()
+    scale = s.dim ** -0.5 if scale is None else scale
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch(new, **hints), scale=scale, softcap=softcap, window=window,
+                                    slopes=None if slopes is None else slopes.cuda(), return_lse=True)
+    torch.cuda.synchronize()
+    _check_attention(got, lse, _attention(s, q, new, scale, softcap, window, slopes))
+    return q, got, lse
+
+
+# ---- the cache ---------------------------------------------------------------------------------------------------------------
+
+def _check_read(s, new, lengths, dtype, **hints):
+    k, v = dfp4.paged_read(s.cache, s.batch(new, lengths, **hints), dtype=dtype)
+    torch.cuda.synchronize()
+    row = 0
+    for b, n in enumerate(new):
+        if n:
+            L = lengths[b]
+            assert np.array_equal(k[row:row + n].double().cpu().numpy(), _keys(s.k[b][:L])[L - n:]), b
+            assert np.array_equal(v[row:row + n].double().cpu().numpy(), _values(s.v[b][:L], L)[L - n:]), b
+        row += n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("page,kv_heads,lengths", [(32, 1, [1, 31, 32, 33]), (64, 3, [200, 1, 64, 95]), (96, 2, [97, 300])])
+def test_cache_holds_what_the_quantizer_makes(dim, page, kv_heads, lengths):
+    s = Sequences(lengths, dim, kv_heads, page, seed=dim).fill()
+    _check_read(s, lengths, lengths, torch.bfloat16)
+    _check_read(s, [min(L, 5) for L in lengths], lengths, torch.float32, max_new=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps", [[1] * 70, [31, 1, 1, 31, 33, 5], [40, 64, 7, 20], [5, 100, 3, 3, 61]])
+def test_cache_grows_in_steps(steps):
+    """Steps that start and end anywhere in a chunk, begin and end in the same one, or span several."""
+    s = Sequences([sum(steps), sum(steps) - 9], 64, 2, 64, seed=len(steps))
+    at = [0, 0]
+    for n in steps:
+        new = [n, max(0, min(n, s.lengths[1] - at[1]))]
+        at = [at[0] + n, at[1] + new[1]]
+        s.write(new, at)
+        _check_read(s, at, at, torch.bfloat16)
+
+
+@pytest.mark.gpu
+def test_cache_from_strided_rows():
+    s = Sequences([77, 50], 128, 2, 64, seed=5)
+    joint = torch.randn(127, 3 + 2 + 2, 128, generator=s.g).bfloat16().cuda()         # queries, keys and values of a token in a row
+    k, v = joint[:, 3:5], joint[:, 5:]
+    s.k, s.v = ([x[:77].cpu().contiguous(), x[77:].cpu().contiguous()] for x in (k, v))
+    dfp4.paged_write(k, v, s.cache, s.batch([77, 50]))
+    _check_read(s, [77, 50], [77, 50], torch.bfloat16)
+    by_head = torch.empty(2, 127, 128, dtype=torch.bfloat16, device="cuda").copy_(k.transpose(0, 1))
+    s.cache.pages.fill_(0xff)
+    dfp4.paged_write(by_head.transpose(0, 1), v, s.cache, s.batch([77, 50], max_new=1))
+    _check_read(s, [77, 50], [77, 50], torch.float32, max_new=1)
+
+
+@pytest.mark.gpu
+def test_cache_beyond_four_gigabytes():
+    s = Sequences([70], 128, 1, 32, seed=3)
+    n_pages = (5 << 30) // dfp4.paged_cell_bytes(128)
+    s.cache = kvcache.PagedCache(n_pages, 32, 1, 128, 3, torch.device("cuda"))
+    s.table = torch.tensor([[n_pages - 1, n_pages - 5, n_pages // 2 + 1]], dtype=torch.int32)
+    s.fill()
+    _check_read(s, [70], [70], torch.bfloat16)
+    _attend(s, [3], 4)
+    assert int(s.cache.pages[:n_pages // 2].max()) == 0
+
+
+@pytest.mark.gpu
+def test_pages_and_slots_out_of_range_are_absent():
+    s = Sequences([100, 70, 40], 64, 2, 32, seed=8)
+    for bad in (-1, s.cache.n_pages, 2 ** 31 - 1, -2 ** 31):
+        s.table[0, 1] = bad                               # tokens 32 .. 63 of sequence 0
+        s.slots[1] = bad                                  # the incomplete chunk's values of sequence 1: tokens 64 .. 69
+        before = s.cache.pages.clone()
+        s.fill()
+        k, v = dfp4.paged_read(s.cache, s.batch(s.lengths))
+        out, lse = dfp4.paged_attention(torch.ones(3, 2, 64, dtype=torch.bfloat16, device="cuda"), s.cache, s.batch([1, 1, 1]), return_lse=True)
+        torch.cuda.synchronize()
+        used = set(int(x) for row, L in zip(s.table, s.lengths) for x in row[:-(-L // 32)] if 0 <= int(x) < s.cache.n_pages)
+        others = [x for x in range(s.cache.n_pages) if x not in used]
+        assert torch.equal(s.cache.pages[others], before[others])
+        k, v = k.double().cpu().numpy(), v.double().cpu().numpy()
+        want_k, want_v = s.stands_for()
+        want_k[0][32:64], want_v[0][32:64], want_v[1][64:] = 0, 0, 0
+        assert np.array_equal(k, np.concatenate(want_k)) and np.array_equal(v, np.concatenate(want_v))
+        seen = [np.r_[0:32, 64:100], np.r_[0:64], np.r_[0:40]]
+        for b in range(3):
+            z = want_k[b][seen[b]].sum(-1) / 8
+            w = np.exp(z - z.max(0))
+            w /= w.sum(0)
+            want = np.einsum("th,thd->hd", w, want_v[b][seen[b]])
+            assert np.abs(out[b].double().cpu().numpy() - want).max() <= 2.0 ** -6 * np.abs(want).max()
+            # a score: 64 products of at most 2^-12 of their sizes
+            assert np.abs(lse[b].double().cpu().numpy() - (z.max(0) + np.log(np.exp(z - z.max(0)).sum(0)))).max() <= 2.0 ** -12 * 64
+
+
+@pytest.mark.gpu
+def test_lengths_and_token_ranges_out_of_range():
+    """Lengths beyond the table, below zero, and shorter than their new tokens; ranges beyond the rows."""
+    s = Sequences([64, 64, 64], 64, 1, 32, seed=4, poison=False).fill()
+    b = s.batch([2, 2, 2], [10 ** 9, -7, 1])
+    q = torch.randn(6, 1, 64, generator=s.g).bfloat16().cuda()
+    out, lse = dfp4.paged_attention(q, s.cache, b, return_lse=True)
+    k, v = dfp4.paged_read(s.cache, b)
+    torch.cuda.synchronize()
+    assert (out[2:5] == 0).all() and torch.isneginf(lse[2:5]).all() and torch.isfinite(lse[[0, 1, 5]]).all()
+    assert (k[2:5] == 0).all() and (v[2:5] == 0).all()
+    assert np.array_equal(k[:2].double().cpu().numpy(), _keys(s.k[0])[62:])
+    for cu in ([-5, 3, 2, 10 ** 6], [0, 100, 100, 100], [4, 2, 0, -1]):
+        b.cu_tokens.copy_(torch.tensor(cu, dtype=torch.int32))
+        dfp4.paged_attention(q, s.cache, b)
+        dfp4.paged_read(s.cache, b)
+        torch.cuda.synchronize()
+
+
+# ---- attention -----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("page,kv_heads,heads,lengths,new", [
+    (32, 1, 1, [1], [1]),
+    (64, 2, 8, [1, 31, 32, 33, 128, 129, 700], [1] * 7),
+    (32, 2, 2, [5, 160, 161, 40], [5, 3, 2, 40]),
+    (96, 1, 5, [333, 200, 64], [7, 0, 33]),
+    (128, 3, 48, [257], [2]),
+])
+def test_attention(dim, page, kv_heads, heads, lengths, new):
+    s = Sequences(lengths, dim, kv_heads, page, seed=dim + heads).fill()
+    _attend(s, new, heads, max_new=max(new))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("options", [
+    dict(softcap=5.0), dict(window=1), dict(window=33), dict(window=64, softcap=20.0), dict(slopes=True), dict(slopes=True, window=100, softcap=30.0), dict(scale=0.5),
+    dict(scale=0.0), dict(scale=-0.3)])
+def test_attention_options(dim, options):
+    s = Sequences([300, 45, 129], dim, 2, 64, seed=dim).fill()
+    options = dict(options)
+    if options.get("slopes"):
+        options["slopes"] = torch.tensor([0.5, 0.25, 0.0, 0.03125, 0.1, 2.0])
+    _attend(s, [9, 45, 1], 6, **options)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_rows_without_keys(dim):
+    """More new tokens than the sequence is long: those before position 0 see nothing."""
+    s = Sequences([3, 0, 40, 1], dim, 2, 32, seed=dim)
+    s.lengths[1] = 0
+    new = [8, 4, 50, 1]
+    s.write([3, 0, 40, 1], s.lengths)
+    _attend(s, new, 4)
+    _attend(s, new, 4, window=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 192])
+@pytest.mark.parametrize("new", [1, 5, 70])
+def test_attention_of_long_contexts_is_split(dim, new):
+    s = Sequences([9000, 2049, 515], dim, 1, 64, seed=new).fill()
+    c, b = s.cache.c(), s.batch([new] * 3, max_new=new).c(3 * new)
+    assert dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4) > 0
+    q, got, lse = _attend(s, [new] * 3, 4, max_new=new)
+    # the same bits again, and with a workspace of the caller's that holds anything
+    ws = torch.full((dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4),), 0xff, dtype=torch.uint8, device="cuda")
+    again, lse2 = dfp4.paged_attention(q.cuda(), s.cache, s.batch([new] * 3, max_new=new), return_lse=True, workspace=ws)
+    assert torch.equal(again.view(torch.int16), got.view(torch.int16)) and torch.equal(lse2, lse)
+    with pytest.raises(dfp4.Dfp4Error, match="workspace"):
+        dfp4.paged_attention(q.cuda(), s.cache, s.batch([new] * 3, max_new=new), workspace=ws[:-16])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hints", [dict(), dict(max_new=1), dict(max_new=1000), dict(max_length=1), dict(max_length=10 ** 6), dict(max_new=2, max_length=400)])
+def test_attention_does_not_depend_on_the_hints(hints):
+    s = Sequences([1500, 300, 700], 128, 2, 32, seed=2).fill()
+    _attend(s, [40, 3, 17], 4, **hints)
+
+
+@pytest.mark.gpu
+def test_attention_of_extreme_values():
+    """Queries and keys from tiny to huge, scores that leave one key, values far above and below 1."""
+    for q_size, k_size, v_size, scale in [(1e-30, 1.0, 1.0, 1.0), (1e18, 1e18, 1.0, 1e-36), (1.0, 1e-25, 1e30, 1.0), (30.0, 30.0, 1e-30, 1.0), (1.0, 1.0, 1e-36, 1.0)]:
+        s = Sequences([150], 64, 1, 32, seed=9, factor=1.0)
+        s.k, s.v = [(s.k[0].double() * k_size).bfloat16()], [(s.v[0].double() * v_size).bfloat16()]
+        s.fill()
+        q = (torch.randn(2, 2, 64, generator=s.g).double() * q_size).bfloat16()
+        got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch([2]), scale=scale, return_lse=True)
+        want = _attention(s, q, [2], scale)
+        _check_attention(got, lse, (want[0], want[1], want[2] + 1e-38, want[3]))
+
+
+@pytest.mark.gpu
+def test_attention_into_strided_rows_on_another_stream():
+    s = Sequences([140, 35], 128, 2, 64, seed=6).fill()
+    joint = torch.randn(36, 4 + 2, 128, generator=s.g).bfloat16()
+    q = joint[:, :4].contiguous()
+    into = torch.full((36, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    dense = joint.cuda()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        got, lse = dfp4.paged_attention(dense[:, :4], s.cache, s.batch([1, 35]), out=into[:, 2:6], return_lse=True)
+    stream.synchronize()
+    _check_attention(got, lse, _attention(s, q, [1, 35], 128 ** -0.5))
+    assert (into[:, :2] == 7).all() and (into[:, 6:] == 7).all()
+
+
+@pytest.mark.gpu
+def test_a_step_in_a_graph():
+    """Norms, write and attention of one token a sequence, captured once; lengths and pages are device memory, so that every replay
+    is the next token."""
+    n, dim, kv, heads = 3, 128, 2, 8
+    s = Sequences([100, 62, 2100], dim, kv, 64, seed=11)
+    grown = [L - 8 for L in s.lengths]
+    s.write(grown, grown)
+    raw = torch.randn(8, n, heads + kv, dim, generator=s.g).bfloat16().cuda()
+    freq = (1.0 / 10000.0 ** (torch.arange(0, dim, 2).double() / dim)).float().cuda()
+    weight = torch.ones(dim, device="cuda")
+    x, v, pos = raw[0].clone(), s.v[0][:n].cuda().clone(), torch.zeros(n, dtype=torch.int32, device="cuda")
+    b = s.batch([1] * n, grown, max_new=1)
+
+    def step():
+        q, k = dfp4.norm_rope(x[:, :heads], x[:, heads:], pos, freq, weight, weight)
+        dfp4.paged_write(k, v, s.cache, b)
+        return k, dfp4.paged_attention(q, s.cache, b, return_lse=True)
+    # (captured without a run before it: what a run would write is written by the first replay)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        k, (out, lse) = step()
+    for i in range(8):
+        at = [L + i + 1 for L in grown]
+        new_v = torch.stack([s.v[j][at[j] - 1] for j in range(n)])
+        x.copy_(raw[i])
+        v.copy_(new_v.cuda())
+        b.lengths.copy_(torch.tensor(at, dtype=torch.int32))
+        pos.copy_(b.lengths - 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        for j in range(n):
+            s.k[j][at[j] - 1] = k[j].cpu()
+        q, _ = dfp4.norm_rope(x[:, :heads], x[:, heads:], pos, freq, weight, weight)
+        eager, eager_lse = dfp4.paged_attention(q, s.cache, s.batch([1] * n, at, max_new=1), return_lse=True)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), eager.view(torch.int16)) and torch.equal(got_lse, eager_lse), i
+    _check_attention(got, got_lse, _attention(s, q.cpu(), [1] * n, dim ** -0.5))
+
+
+# ---- norms and rotation ----------------------------------------------------------------------------------------------------------
+
+def _rope(x, w, pos, freq, interleaved, eps):
+    y = synth.to_f64(x)
+    if w is not None:
+        y = y / np.sqrt((y * y).mean(-1, keepdims=True) + eps) * w.double().numpy()
+    half = len(freq)
+    angle = pos.double().numpy()[:, None, None] * freq.double().numpy()
+    c, s = np.cos(angle), np.sin(angle)
+    out, size = y.copy(), np.abs(y)
+    i, j = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    out[..., i], out[..., j] = y[..., i] * c - y[..., j] * s, y[..., j] * c + y[..., i] * s
+    size[..., i] = size[..., j] = np.abs(y[..., i]) + np.abs(y[..., j])
+    return out, size
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,rotary", [(32, 32), (64, 64), (64, 32), (96, 96), (96, 16), (128, 128), (128, 0), (160, 80), (192, 192), (256, 256), (256, 64)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,kv_heads,norm", [(1, 32, 8, True), (37, 3, 1, True), (5, 17, 17, False), (3, 6, 0, True)])
+def test_norm_rope(dim, rotary, interleaved, tokens, heads, kv_heads, norm):
+    g = torch.Generator().manual_seed(dim + rotary)
+    x = (torch.randn(tokens, heads + kv_heads, dim, generator=g) * torch.exp(2 * torch.randn(tokens, 1, 1, generator=g))).bfloat16()
+    pos = torch.randint(0, 1 << 20, (tokens,), generator=g).int()
+    freq = (1.0 / 500000.0 ** (torch.arange(0, rotary, 2).double() / max(rotary, 1))).float()
+    wq, wk = ((1 + 0.3 * torch.randn(dim, generator=g)) if norm else None for _ in range(2))
+    d = x.cuda()
+    cuda = lambda t: None if t is None else t.cuda()  # noqa: E731
+    q, k = dfp4.norm_rope(d[:, :heads], d[:, heads:] if kv_heads else None, pos.cuda(), freq.cuda(), cuda(wq), cuda(wk), eps=1e-5, interleaved=interleaved)
+    torch.cuda.synchronize()
+    for got, part, w in ((q, x[:, :heads], wq), (k, x[:, heads:], wk)):
+        if got is None:
+            continue
+        want, size = _rope(part, w, pos, freq, interleaved, 1e-5)
+        # a rounding to bf16; before it some twenty roundings to fp32
+        assert (np.abs(got.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.gpu
+def test_norm_rope_in_place_and_zeros():
+    x, y = torch.randn(4, 6, 128).bfloat16().cuda(), torch.zeros(4, 2, 128, dtype=torch.bfloat16, device="cuda")
+    pos, freq, w = torch.arange(4, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda"), torch.ones(128, device="cuda")
+    q, k = dfp4.norm_rope(x, y, pos, freq, w, w)
+    q2, k2 = dfp4.norm_rope(x, y, pos, freq, w, w, out=(x, y))
+    torch.cuda.synchronize()
+    assert q2.data_ptr() == x.data_ptr() and torch.equal(q2.view(torch.int16), q.view(torch.int16)) and (k2 == 0).all()
