@@ -544,7 +544,7 @@ int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride,
     if (need > 0 && (!workspace || workspace_bytes < need)) return DFP4_ERR_WORKSPACE;
     const AttentionArgs a{paged_args(cache, batch), static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, slopes,
                           static_cast<float*>(workspace), q_stride, q_head_stride, out_stride, out_head_stride, scale, softcap, (int)heads,
-                          (int)window, 1, 1};
+                          (int)window, 1, 1, 16};
     return launch_paged_attention(a, cache, batch, static_cast<hipStream_t>(stream));
 }
 

@@ -82,7 +82,7 @@ template <int OPSEL>
 __device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& lo, v4f& c, int sa, int sb, int sb_lo) {
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, c, 0, 0, OPSEL, sa, 0, sb);
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, c, 0, 0, OPSEL, sa, 0, sb_lo);
-    asm volatile("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
+    asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
 }
 
 // 32 codes (in 16 bytes) of a scale and a dialect to bf16: fragments of four instructions, tokens 8 q .. 8 q + 7 in the q-th
@@ -112,38 +112,101 @@ __device__ __forceinline__ void split8(const float* x, v8b& hi, v8b& lo) {
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-// max over the four lanes of a column
+// over the four lanes of a column (16 and 32 apart)
 __device__ __forceinline__ float column_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+    v = fmaxf(as_f(r[0]), as_f(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(as_u(v), as_u(v), false, false);
+    return fmaxf(as_f(r[0]), as_f(r[1]));
 }
 __device__ __forceinline__ float column_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+    v = as_f(r[0]) + as_f(r[1]);
+    r = __builtin_amdgcn_permlane16_swap(as_u(v), as_u(v), false, false);
+    return as_f(r[0]) + as_f(r[1]);
 }
 
 constexpr float kNone = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// Which keys a block of 16 query rows sees, and how they are split between workgroups: alike in the kernel that adds the parts up.
+// Which keys a block of query rows sees, and how they are split between workgroups: alike in the kernel that adds the parts up.
 struct Range {
-    int p_min, p_max;            // positions of the first and the last row
     int first, end, whole;       // chunks of 32: [first, end), values quantized below `whole`
-    int steps, parts;            // of four chunks; workgroups that have some
+    int steps, parts;            // of four chunks (of one row tile: whole ones only); workgroups that have some
 };
 __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequence& s, int group, int row0) {
     Range r;
-    const int rows = s.n * group, last_row = min(row0 + 15, rows - 1);
-    r.p_min = s.length - s.n + row0 / group;
-    r.p_max = s.length - s.n + last_row / group;
-    const int t_end = min(r.p_max + 1, s.length), t_begin = a.window > 0 ? max(0, r.p_min - a.window + 1) : 0;
+    const int rows = s.n * group, last_row = min(row0 + a.rows, rows) - 1;
+    const int p_min = s.length - s.n + row0 / group, p_max = s.length - s.n + last_row / group;
+    const int t_end = min(p_max + 1, s.length), t_begin = a.window > 0 ? max(0, p_min - a.window + 1) : 0;
     r.first = t_begin / 32;
     r.end = t_end > t_begin ? (t_end + 31) / 32 : r.first;
     r.whole = min(r.end, s.length / 32);
-    r.steps = max(0, (r.whole - r.first + 3) / 4);
+    r.steps = max(0, ((a.rows == 16 ? r.whole : r.end) - r.first + 3) / 4);
     r.parts = min(a.splits, max(1, (r.steps + a.split_steps - 1) / a.split_steps));
     return r;
 }
+
+// A query row's 128 elements from kt * 128 on as this lane's share of an operand: both FP8 parts, and the scale of block g
+template <int D, int kt>
+__device__ __forceinline__ int load_query(const uint16_t* row, bool ok, uint32_t c, uint32_t g, v8i& hi, v8i& lo) {
+    const uint16_t* src = row + kt * 128;
+    uint32_t top = 0;
+    if (ok && (int)g < Cell<D>::blocks(kt)) {
+        const uint4* x = reinterpret_cast<const uint4*>(src + g * 32u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint4 v = x[j];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, max((w[k] >> 7) & 0xffu, (w[k] >> 23) & 0xffu));
+        }
+    }
+    const int scale = max((int)top - 7, kLoShift);                  // the largest magnitude becomes less than 2^8
+    each<2>([&](auto h_c) {
+        constexpr int h = decltype(h_c)::value;
+        const uint32_t block = 2u * h + (g >> 1);                   // half g % 2 of it; its scale is another lane's
+        const int by = __shfl(scale, (int)(block * 16u + c));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (ok && (int)block < Cell<D>::blocks(kt)) v = *reinterpret_cast<const uint4*>(src + block * 32u + (g & 1u) * 16u + k * 8);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - by);
+            int a, b;
+            split4(x[0], x[1], x[2], x[3], a, b);
+            hi[4 * h + 2 * k] = a;
+            lo[4 * h + 2 * k] = b;
+            split4(x[4], x[5], x[6], x[7], a, b);
+            hi[4 * h + 2 * k + 1] = a;
+            lo[4 * h + 2 * k + 1] = b;
+        }
+    });
+    return scale;
+}
+
+// What turns scores into exponents to base 2: cap, bias by distance and mask
+template <bool EXTRA>
+struct Scores {
+    float to_log2, cap, twice, slope;
+    int window;
+    __device__ __forceinline__ Scores(const AttentionArgs& a)
+        : Scores(a.scale, a.softcap, a.window) {}
+    __device__ __forceinline__ Scores(float scale, float softcap, int w)
+        : to_log2(scale * kLog2e), cap(softcap * kLog2e), twice(softcap > 0.0f ? 2.0f / softcap : 0.0f), slope(0.0f), window(w) {}
+    __device__ __forceinline__ float bend(float x, int behind) const {
+        x *= to_log2;
+        if constexpr (EXTRA) {
+            // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
+            if (cap > 0.0f) x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(exp2_(x * twice) + 1.0f);
+            x -= slope * (float)behind;
+        }
+        return x;
+    }
+    __device__ __forceinline__ bool seen(int behind) const { return behind >= 0 && (window <= 0 || behind < window); }
+};
 
 // One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
 // add up in LDS.
@@ -164,7 +227,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
     if (tid < kDialects * 8 / 4) reinterpret_cast<uint32_t*>(s_rows)[tid] = reinterpret_cast<const uint32_t*>(&g_f8_rows.b[0][0])[tid];
     __syncthreads();
     const uint2* const table = reinterpret_cast<const uint2*>(s_rows);
-    const float to_log2 = a.scale * kLog2e;
+    Scores<EXTRA> rule(a);
 
     for (int row0 = (int)blockIdx.z * 16; row0 < s.n * group; row0 += (int)gridDim.z * 16) {
         const Range r = key_range(a, s, group, row0);
@@ -175,52 +238,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         const int head = kv_head * group + (row_ok ? row % group : 0);
         const int64_t token = s.first + (row_ok ? row / group : 0);
         const int pos = s.length - s.n + (row_ok ? row / group : 0);
-        const float slope = EXTRA && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+        if (EXTRA && a.slopes) rule.slope = a.slopes[head] * kLog2e;
 
-        // ---- queries: 16 rows, both parts, a scale per block of 32
         v8i q_hi[KT], q_lo[KT];
         int q_scale[KT];
         each<KT>([&](auto kt_c) {
             constexpr int kt = decltype(kt_c)::value;
-            const uint16_t* src = a.q + token * a.q_stride + (int64_t)head * a.q_head_stride + kt * 128;
-            // lane (g, c) supplies the scale of block g and halves g % 2 of blocks g / 2 and 2 + g / 2: the scales of those two come
-            // from the lanes that have them
-            auto scale_of = [&](uint32_t block) -> int {
-                if ((int)block >= C::blocks(kt) || !row_ok) return 127;
-                uint32_t top = 0;
-                const uint4* x = reinterpret_cast<const uint4*>(src + block * 32u);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint4 v = x[j];
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top = max(top, max((w[k] >> 7) & 0xffu, (w[k] >> 23) & 0xffu));
-                }
-                return max((int)top - 7, kLoShift);                 // the largest magnitude becomes less than 2^8
-            };
-            q_scale[kt] = scale_of(g);
-            each<2>([&](auto h_c) {
-                constexpr int h = decltype(h_c)::value;
-                const uint32_t block = 2u * h + (g >> 1);
-                const int scale = __shfl(q_scale[kt], (int)(block * 16u + c));
-                const bool on = row_ok && (int)block < C::blocks(kt);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (on) v = *reinterpret_cast<const uint4*>(src + block * 32u + (g & 1u) * 16u + k * 8);
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - scale);
-                    int hi, lo;
-                    split4(x[0], x[1], x[2], x[3], hi, lo);
-                    q_hi[kt][4 * h + 2 * k] = hi;
-                    q_lo[kt][4 * h + 2 * k] = lo;
-                    split4(x[4], x[5], x[6], x[7], hi, lo);
-                    q_hi[kt][4 * h + 2 * k + 1] = hi;
-                    q_lo[kt][4 * h + 2 * k + 1] = lo;
-                }
-            });
+            q_scale[kt] = load_query<D, kt>(a.q + token * a.q_stride + (int64_t)head * a.q_head_stride, row_ok, c, g, q_hi[kt], q_lo[kt]);
         });
 
         v4f o[NJ];
@@ -228,18 +252,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         for (int j = 0; j < NJ; ++j) o[j] = v4f{0, 0, 0, 0};
         float m = kNone, l = 0.0f;
 
-        // a score to base 2: cap, bias and mask
         auto finish = [&](float x, int t, bool there) {
-            x *= to_log2;
-            if constexpr (EXTRA) {
-                if (a.softcap > 0.0f) {
-                    // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
-                    const float cap = a.softcap * kLog2e, e = exp2_(x * (2.0f * kLog2e / cap));
-                    x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(e + 1.0f);
-                }
-                x -= slope * (float)(pos - t);
-            }
-            return there && t <= pos && (a.window <= 0 || t > pos - a.window) ? x : kNone;
+            x = rule.bend(x, pos - t);
+            return there && rule.seen(pos - t) ? x : kNone;
         };
         // the running maximum takes in `top`; what was added up so far is scaled to it
         auto raise = [&](float top) {
@@ -464,6 +479,286 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Many query rows: a workgroup of eight waves takes 8 * 16 * RT of them, expands every step of 128 keys once into LDS, as the
+// operands that all waves read (keys in FP8, values in bf16), and each wave does both products for its RT tiles of 16 rows.
+// Wave w expands tile w of the keys and tiles w, w + 8 of the values; codes of the step after are loaded meanwhile, and where LDS has
+// room for two steps (D <= 128) one barrier a step is enough.  The incomplete chunk is part of the last step: its values are stored to
+// LDS as they are.  A probability is one bf16 number here.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <int D>
+struct Wide {
+    static constexpr int kWaves = 8, kThreads = 512, RT = D <= 128 ? 2 : 1, kRows = kWaves * 16 * RT, kBuffers = D <= 128 ? 2 : 1;
+    static constexpr uint32_t kK = 8 * Cell<D>::KT * 2048, kV = Cell<D>::NJ * 4096, kScales = Cell<D>::KT * 512, kStep = kK + kV + kScales;
+};
+
+template <int D, bool EXTRA>
+__global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionArgs a) {
+    using C = Cell<D>;
+    using W = Wide<D>;
+    constexpr int KT = C::KT, NJ = C::NJ, RT = W::RT, VT = (NJ + 7) / 8;
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[W::kBuffers * W::kStep];
+    __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const PagedArgs& p = a.paged;
+    const int b = (int)(blockIdx.x / (uint32_t)p.kv_heads), kv_head = (int)(blockIdx.x % (uint32_t)p.kv_heads), part = (int)blockIdx.y;
+    const int group = a.heads / p.kv_heads;
+    const Sequence s = sequence(p, b);
+    if (tid < kDialects * 8 / 4) reinterpret_cast<uint32_t*>(s_rows)[tid] = reinterpret_cast<const uint32_t*>(&g_f8_rows.b[0][0])[tid];
+    __syncthreads();
+    const uint2* const table = reinterpret_cast<const uint2*>(s_rows);
+
+    for (int row0 = (int)blockIdx.z * W::kRows; row0 < s.n * group; row0 += (int)gridDim.z * W::kRows) {
+        const Range r = key_range(a, s, group, row0);
+        if (part >= r.parts) continue;
+        const int step0 = part * a.split_steps, step1 = part == r.parts - 1 ? r.steps : min(r.steps, step0 + a.split_steps);
+        const int wave_row = row0 + wave * 16 * RT, rows = s.n * group;
+        // positions of the wave's rows (rows beyond the last have those of the last)
+        const int p_min = s.length - s.n + min(wave_row, rows - 1) / group, p_max = s.length - s.n + min(wave_row + 16 * RT, rows) / group
+                          - (min(wave_row + 16 * RT, rows) % group == 0 ? 1 : 0);
+        int pos[RT];
+        Scores<EXTRA> rule[2] = {Scores<EXTRA>(a), Scores<EXTRA>(a)};
+        v8i q_hi[RT][KT], q_lo[RT][KT];
+        int q_scale[RT][KT];
+        v4f o[RT][NJ];
+        float m[RT], l[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = wave_row + rt * 16 + (int)c, held = min(row, rows - 1);
+            const int head = kv_head * group + held % group;
+            pos[rt] = s.length - s.n + held / group;
+            if (EXTRA && a.slopes) rule[rt].slope = a.slopes[head] * kLog2e;
+            each<KT>([&](auto kt_c) {
+                constexpr int kt = decltype(kt_c)::value;
+                q_scale[rt][kt] = load_query<D, kt>(a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride, row < rows, c, g,
+                                                    q_hi[rt][kt], q_lo[rt][kt]);
+            });
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[rt][j] = v4f{0, 0, 0, 0};
+            m[rt] = kNone;
+            l[rt] = 0.0f;
+        }
+
+        // ---- what a thread expands of a step: its share of key tile `wave` and of value tiles `wave`, `wave` + 8
+        struct Raw {
+            uint4 k[KT], v[VT];
+            uint32_t k_id[KT], v_id[VT], v_scale[VT];
+            uint2 k_scale[KT];
+            bool k_there, v_there, all;
+            int tail;                                                // tokens of the lane's value chunk if it is the incomplete one, or 0
+        };
+        Raw raw;
+        auto load = [&](int step) {
+            const int chunk0 = r.first + 4 * step;
+            auto offset = [&](int k) -> int64_t { return chunk0 + k < r.end ? cell_offset<D>(p, b, kv_head, chunk0 + k) : -1; };
+            const int64_t a0 = offset(0), a1 = offset(1), a2 = offset(2), a3 = offset(3);
+            auto pick = [&](uint32_t k) { return k == 0 ? a0 : k == 1 ? a1 : k == 2 ? a2 : a3; };
+            const int64_t ak = pick(c >> 2), av = pick(g);
+            raw.tail = chunk0 + (int)g >= r.whole ? s.length - 32 * (chunk0 + (int)g) : 0;      // (the chunk at `whole`: fewer than 32)
+            raw.k_there = ak >= 0;
+            raw.v_there = av >= 0 && (raw.tail == 0 || s.slot >= 0);
+            raw.all = (a0 | a1 | a2 | a3) >= 0 && chunk0 + 4 <= r.whole;
+            const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
+            if (raw.k_there) {
+                each<KT>([&](auto kt_c) {
+                    constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
+                    const uint32_t block = kt * 4 + min(g, (uint32_t)(nb - 1));
+                    if (wave == kt) raw.k_scale[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block) * 8u);
+                    raw.k_id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + wave];
+                    const uint8_t* row = kc + (4u * wave + (c & 3u)) * (D / 2) + kt * 64;
+                    if constexpr (nb == 4) {
+                        raw.k[kt] = *reinterpret_cast<const uint4*>(row + g * 16u);
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(row + g * 8u);
+                        uint2 y = x;
+                        if constexpr (nb == 3) y = *reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u));
+                        raw.k[kt] = make_uint4(x.x, x.y, y.x, y.y);
+                    }
+                });
+            }
+            if (raw.v_there && raw.tail == 0) {
+#pragma unroll
+                for (int i = 0; i < VT; ++i) {
+                    const int j = wave + 8 * i;
+                    if (j < NJ) {
+                        raw.v[i] = *reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u);
+                        raw.v_scale[i] = vc[C::kVExps + c * C::VE + j];
+                        raw.v_id[i] = vc[C::kVIds + (c >> 1) * C::VE + j];
+                    }
+                }
+            }
+        };
+        auto store = [&](uint8_t* to) {
+            each<KT>([&](auto kt_c) {
+                constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
+                v8i k8 = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (raw.k_there) {
+                    expand16<0>(make_uint2(raw.k[kt].x, raw.k[kt].y), table[raw.k_id[kt] & 15u], k8);
+                    if constexpr (nb > 2) expand16<4>(make_uint2(raw.k[kt].z, raw.k[kt].w), table[raw.k_id[kt] >> 4], k8);
+                }
+                uint8_t* at = to + (wave * KT + kt) * 2048 + lane * 16u;
+                *reinterpret_cast<int4*>(at) = make_int4(k8[0], k8[1], k8[2], k8[3]);
+                *reinterpret_cast<int4*>(at + 1024) = make_int4(k8[4], k8[5], k8[6], k8[7]);
+                if (wave == kt) *reinterpret_cast<uint2*>(to + W::kK + W::kV + kt * 512 + lane * 8u) = raw.k_there ? raw.k_scale[kt] : make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+            });
+#pragma unroll
+            for (int i = 0; i < VT; ++i) {
+                const int j = wave + 8 * i;
+                if (j >= NJ) break;
+                v8b v[4] = {};
+                if (raw.v_there && raw.tail == 0) {
+                    expand_bf16(raw.v[i], table[(raw.v_id[i] >> (4u * (c & 1u))) & 15u], raw.v_scale[i], v);
+                } else if (raw.v_there) {
+                    const uint16_t* from = residual<D>(p, s.slot, kv_head) + (16u * j + c) * 32u;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + 8 * q);
+                        uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {                // what the slot holds beyond the tokens there are is anything
+                            if (8 * q + 2 * k >= raw.tail) u[k] = 0;
+                            else if (8 * q + 2 * k + 1 >= raw.tail) u[k] &= 0xffffu;
+                        }
+                        v[q] = __builtin_bit_cast(v8b, make_uint4(u[0], u[1], u[2], u[3]));
+                    }
+                }
+                uint8_t* at = to + W::kK + j * 4096 + lane * 16u;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *reinterpret_cast<v8b*>(at + q * 1024) = v[q];
+            }
+        };
+        auto work = [&](const uint8_t* from, int step, bool there, bool all) {
+            const int chunk0 = r.first + 4 * step;
+            if (32 * chunk0 > p_max) return;                         // later than all of the wave's rows
+            const bool inside = all && 32 * chunk0 + 127 <= p_min && (a.window <= 0 || 32 * chunk0 > p_max - a.window);
+            float x[RT][8][4];
+            uint2 scales[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) scales[kt] = *reinterpret_cast<const uint2*>(from + W::kK + W::kV + kt * 512 + lane * 8u);
+            each<8>([&](auto t_c) {
+                constexpr int t = decltype(t_c)::value;
+                v4f acc[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[rt] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const int4 lo = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + lane * 16u);
+                    const int4 hi = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + 1024 + lane * 16u);
+                    const v8i k8 = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    const int scale = (int)(t < 4 ? scales[kt].x : scales[kt].y);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+                        product<(t & 3)>(k8, q_hi[rt][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt], q_scale[rt][kt] - kLoShift);
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[rt][t][i] = acc[rt][i];
+            });
+            v8b pr[RT][4];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float top = kNone;
+                const int behind = pos[rt] - 32 * (chunk0 + (int)g);
+                if (inside) {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            x[rt][t][i] = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
+                            top = fmaxf(top, x[rt][t][i]);
+                        }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float y = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
+                            x[rt][t][i] = there && rule[rt].seen(behind - 4 * t - i) ? y : kNone;
+                            top = fmaxf(top, x[rt][t][i]);
+                        }
+                }
+                const float next = fmaxf(m[rt], column_max(top)), base = next == kNone ? 0.0f : next;
+                if (__any(next > m[rt])) {
+                    const float by = exp2_(m[rt] - base);
+                    l[rt] *= by;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][j][i] *= by;
+                    m[rt] = next;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float e = exp2_(x[rt][2 * q + i / 4][i % 4] - base);
+                        l[rt] += e;
+                        pr[rt][q][i] = (__bf16)e;
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v8b v = *reinterpret_cast<const v8b*>(from + W::kK + j * 4096 + q * 1024 + lane * 16u);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) o[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[rt][q], o[rt][j], 0, 0, 0);
+                }
+        };
+
+        __syncthreads();                                             // of the row block before
+        if (step0 < step1) {
+            load(step0);
+            store(s_x);
+            bool there = raw.v_there, all = raw.all;
+            for (int step = step0; step < step1; ++step) {
+                const uint8_t* from = s_x + (W::kBuffers == 2 ? ((step - step0) & 1) * W::kStep : 0u);
+                __syncthreads();
+                if (step + 1 < step1) load(step + 1);
+                work(from, step, there, all);
+                if (W::kBuffers == 1) __syncthreads();
+                there = raw.v_there;
+                all = raw.all;
+                if (step + 1 < step1) store(s_x + (W::kBuffers == 2 ? ((step + 1 - step0) & 1) * W::kStep : 0u));
+            }
+        }
+
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = wave_row + rt * 16 + (int)c;
+            const float sum = column_sum(l[rt]);
+            if (row >= rows) continue;
+            const int64_t t = s.first + row / group;
+            const int h = kv_head * group + row % group;
+            if (r.parts == 1) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                uint16_t* dst = a.out + t * a.out_stride + (int64_t)h * a.out_head_stride + 4u * g;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+                    v4b y;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[rt][j][i] * inv);
+                    *reinterpret_cast<v4b*>(dst + 16 * j) = y;
+                }
+                if (a.lse && g == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (m[rt] + log2f(sum)) / kLog2e : kNone;
+            } else {
+                const int64_t slot = (t * a.heads + h) * a.splits + part;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    *reinterpret_cast<v4f*>(a.partial + slot * D + 16 * j + 4u * g) = o[rt][j];
+                if (g == 0) {
+                    float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
+                    ml[0] = m[rt];
+                    ml[1] = sum;
+                }
+            }
+        }
+    }
+}
+
 // Adds up the parts of a query row: one wave a row, D / 64 elements a lane.  Parts in their order: the same sum every time.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(AttentionArgs a) {
@@ -474,7 +769,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
     for (int64_t row = (int64_t)blockIdx.y * kWaves + (threadIdx.x >> 6); row < (int64_t)s.n * a.heads; row += (int64_t)gridDim.y * kWaves) {
         const int64_t t = s.first + row / a.heads;
         const int h = (int)(row % a.heads), in_group = (int)(row / a.heads) * group + h % group;
-        const int parts = key_range(a, s, group, in_group / 16 * 16).parts;
+        const int parts = key_range(a, s, group, in_group / a.rows * a.rows).parts;
         if (parts == 1) continue;                       // written by the only part
         const int64_t slot = (t * a.heads + h) * a.splits;
         const float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
@@ -498,24 +793,25 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
 }
 
 struct Split {
+    int rows, blocks;            // query rows of a workgroup, workgroups along them
     int splits, steps;           // workgroups along the keys, steps of 128 keys of each
 };
-int64_t row_blocks(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
-    const int64_t most = batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens;
-    const int64_t blocks = (most * (heads / cache.kv_heads) + 15) / 16;
-    return blocks < 65535 ? blocks : 65535;
-}
 Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
     const int64_t table = batch.table_width * cache.page_tokens;
     const int64_t most = batch.max_length > 0 && batch.max_length < table ? batch.max_length : table;
-    const int64_t rounds = (most + 128 * kWaves - 1) / (128 * kWaves);
-    const int64_t groups = batch.batch * cache.kv_heads * row_blocks(cache, batch, heads);
-    int64_t want = (4 * (int64_t)device_cu_count() + groups - 1) / groups;
+    const int64_t new_rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * (heads / cache.kv_heads);
+    const bool wide = new_rows > 16;
+    const int64_t rows = !wide ? 16 : cache.head_dim <= 128 ? 256 : 128;
+    int64_t blocks = (new_rows + rows - 1) / rows;
+    if (blocks > 65535) blocks = 65535;
+    const int64_t unit = wide ? 4 : kWaves, steps = (most + 127) / 128;              // steps that a workgroup has at least
+    const int64_t rounds = (steps + unit - 1) / unit, groups = batch.batch * cache.kv_heads * blocks;
+    int64_t want = ((wide ? 1 : 4) * (int64_t)device_cu_count() + (wide ? 0 : groups - 1)) / groups;
     if (want > rounds) want = rounds;
-    if (want < 1) want = 1;
     if (want > 256) want = 256;
-    const int64_t per = (rounds + want - 1) / want;
-    return Split{(int)(rounds > 0 ? (rounds + per - 1) / per : 1), (int)(per > 0 ? per * kWaves : kWaves)};
+    if (want < 1) want = 1;
+    const int64_t per = rounds > 0 ? (rounds + want - 1) / want : 1;
+    return Split{(int)rows, (int)blocks, (int)(rounds > 0 ? (rounds + per - 1) / per : 1), (int)(per * unit)};
 }
 
 }  // namespace
@@ -529,12 +825,18 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
     const Split sp = choose_split(cache, batch, a.heads);
     a.splits = sp.splits;
     a.split_steps = sp.steps;
-    const dim3 grid((uint32_t)(batch.batch * cache.kv_heads), (uint32_t)sp.splits, (uint32_t)row_blocks(cache, batch, a.heads));
+    a.rows = sp.rows;
+    const dim3 grid((uint32_t)(batch.batch * cache.kv_heads), (uint32_t)sp.splits, (uint32_t)sp.blocks);
     const bool extra = a.softcap > 0.0f || a.slopes;
     with_head_dim(cache.head_dim, [&](auto d) {
         constexpr int kD = decltype(d)::value;
-        if (extra) hipLaunchKernelGGL((paged_attention_kernel<kD, true>), grid, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((paged_attention_kernel<kD, false>), grid, dim3(kThreads), 0, stream, a);
+        if (sp.rows > 16) {
+            if (extra) hipLaunchKernelGGL((paged_attention_wide_kernel<kD, true>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
+            else hipLaunchKernelGGL((paged_attention_wide_kernel<kD, false>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
+        } else {
+            if (extra) hipLaunchKernelGGL((paged_attention_kernel<kD, true>), grid, dim3(kThreads), 0, stream, a);
+            else hipLaunchKernelGGL((paged_attention_kernel<kD, false>), grid, dim3(kThreads), 0, stream, a);
+        }
         if (sp.splits > 1) {
             const int64_t rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * a.heads;
             const int64_t blocks = (rows + kWaves - 1) / kWaves;

@@ -107,6 +107,7 @@ struct AttentionArgs {
     int64_t q_stride, q_head_stride, out_stride, out_head_stride;
     float scale, softcap;
     int heads, window, splits, split_steps;
+    int rows;                        // query rows of a workgroup
 };
 size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads);
 int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream);
