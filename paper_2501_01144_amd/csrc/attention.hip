@@ -147,9 +147,10 @@ __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequenc
     return r;
 }
 
-// A query row's 128 elements from kt * 128 on as this lane's share of an operand: both FP8 parts, and the scale of block g
+// A query row's 128 elements from kt * 128 on as this lane's share of an operand (`negative`: their negatives): both FP8 parts, and
+// the scale of block g
 template <int D, int kt>
-__device__ __forceinline__ int load_query(const uint16_t* row, bool ok, uint32_t c, uint32_t g, v8i& hi, v8i& lo) {
+__device__ __forceinline__ int load_query(const uint16_t* row, bool ok, bool negative, uint32_t c, uint32_t g, v8i& hi, v8i& lo) {
     const uint16_t* src = row + kt * 128;
     uint32_t top = 0;
     if (ok && (int)g < Cell<D>::blocks(kt)) {
@@ -171,7 +172,8 @@ __device__ __forceinline__ int load_query(const uint16_t* row, bool ok, uint32_t
         for (int k = 0; k < 2; ++k) {
             uint4 v = make_uint4(0, 0, 0, 0);
             if (ok && (int)block < Cell<D>::blocks(kt)) v = *reinterpret_cast<const uint4*>(src + block * 32u + (g & 1u) * 16u + k * 8);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t flip = negative ? 0x80008000u : 0u;
+            const uint32_t w[4] = {v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - by);
@@ -187,26 +189,30 @@ __device__ __forceinline__ int load_query(const uint16_t* row, bool ok, uint32_t
     return scale;
 }
 
-// What turns scores into exponents to base 2: cap, bias by distance and mask
+// What turns scores into exponents to base 2.  Where there is neither cap nor bias (nor a scale of zero) a score stays as it is,
+// masked or not, until the largest is taken from it (the factor is positive: its sign goes into the query).
 template <bool EXTRA>
 struct Scores {
-    float to_log2, cap, twice, slope;
-    int window;
+    float factor, cap, twice, slope;
+    uint32_t reach;              // a key so many positions behind the query, or less, is seen
     __device__ __forceinline__ Scores(const AttentionArgs& a)
-        : Scores(a.scale, a.softcap, a.window) {}
-    __device__ __forceinline__ Scores(float scale, float softcap, int w)
-        : to_log2(scale * kLog2e), cap(softcap * kLog2e), twice(softcap > 0.0f ? 2.0f / softcap : 0.0f), slope(0.0f), window(w) {}
+        : factor(fabsf(a.scale) * kLog2e), cap(a.softcap * kLog2e), twice(a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f), slope(0.0f),
+          reach(a.window > 0 ? (uint32_t)a.window - 1u : 0x7fffffffu) {}
     __device__ __forceinline__ float bend(float x, int behind) const {
-        x *= to_log2;
         if constexpr (EXTRA) {
+            x *= factor;
             // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
             if (cap > 0.0f) x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(exp2_(x * twice) + 1.0f);
             x -= slope * (float)behind;
         }
         return x;
     }
-    __device__ __forceinline__ bool seen(int behind) const { return behind >= 0 && (window <= 0 || behind < window); }
+    // keys after the query are a large number of positions behind it
+    __device__ __forceinline__ float mask(float x, int behind) const { return (uint32_t)behind <= reach ? x : kNone; }
+    __device__ __forceinline__ float log2_of(float x) const { return EXTRA ? x : x * factor; }      // of the largest score
+    __device__ __forceinline__ float above(float x, float base) const { return EXTRA ? x - base : fmaf(x, factor, -base); }
 };
+constexpr int kNever = -0x40000000;      // positions behind: a key that is not there
 
 // One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
 // add up in LDS.
@@ -244,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         int q_scale[KT];
         each<KT>([&](auto kt_c) {
             constexpr int kt = decltype(kt_c)::value;
-            q_scale[kt] = load_query<D, kt>(a.q + token * a.q_stride + (int64_t)head * a.q_head_stride, row_ok, c, g, q_hi[kt], q_lo[kt]);
+            q_scale[kt] = load_query<D, kt>(a.q + token * a.q_stride + (int64_t)head * a.q_head_stride, row_ok, a.scale < 0.0f, c, g, q_hi[kt], q_lo[kt]);
         });
 
         v4f o[NJ];
@@ -252,20 +258,18 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         for (int j = 0; j < NJ; ++j) o[j] = v4f{0, 0, 0, 0};
         float m = kNone, l = 0.0f;
 
-        auto finish = [&](float x, int t, bool there) {
-            x = rule.bend(x, pos - t);
-            return there && rule.seen(pos - t) ? x : kNone;
-        };
         // the running maximum takes in `top`; what was added up so far is scaled to it
         auto raise = [&](float top) {
-            const float next = fmaxf(m, column_max(top)), base = next == kNone ? 0.0f : next;
-            const float by = exp2_(m - base);
-            l *= by;
+            const float next = fmaxf(m, rule.log2_of(column_max(top))), base = next == kNone ? 0.0f : next;
+            if (__any(next > m)) {
+                const float by = exp2_(m - base);
+                l *= by;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[j][i] *= by;
-            m = next;
+                    for (int i = 0; i < 4; ++i) o[j][i] *= by;
+                m = next;
+            }
             return base;
         };
 
@@ -293,16 +297,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         };
         auto block_of = [&](int kt) { return kt * 4 + min(g, (uint32_t)(C::blocks(kt) - 1)); };
 
+        int pages = step0 + wave < step1 ? four_pages(p, b, r.first + 4 * (step0 + wave), r.whole) : 0;
         for (int step = step0 + wave; step < step1; step += kWaves) {
             const int chunk0 = r.first + 4 * step;
             // the step's cells; absent keys are masked, their codes are read anywhere and their values taken as zeros
-            const int64_t a0 = cell_offset<D>(p, b, kv_head, chunk0);
-            const int64_t a1 = chunk0 + 1 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 1) : -1;
-            const int64_t a2 = chunk0 + 2 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 2) : -1;
-            const int64_t a3 = chunk0 + 3 < r.whole ? cell_offset<D>(p, b, kv_head, chunk0 + 3) : -1;
-            if ((a0 & a1 & a2 & a3) < 0) continue;
-            auto pick = [&](uint32_t k) { return k == 0 ? a0 : k == 1 ? a1 : k == 2 ? a2 : a3; };
-            const int64_t ak = pick(c >> 2), av = pick(g);
+            const Four at = four_cells<D>(p, kv_head, chunk0, r.whole, pages);
+            pages = four_pages(p, b, chunk0 + 4 * kWaves, r.whole);
+            if (at.none()) continue;
+            const int64_t ak = at.pick(c >> 2), av = at.pick(g);
             const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
 
             // ---- scores of 128 keys
@@ -331,11 +333,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 
             // ---- softmax
             float top = kNone;
+            const int behind = av >= 0 ? pos - 32 * (chunk0 + (int)g) : kNever;
 #pragma unroll
             for (int t = 0; t < 8; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[t][i] = finish(x[t][i], 32 * (chunk0 + (int)g) + 4 * t + i, av >= 0);
+                    x[t][i] = rule.mask(rule.bend(x[t][i], behind - 4 * t - i), behind - 4 * t - i);
                     top = fmaxf(top, x[t][i]);
                 }
             const float base = raise(top);
@@ -344,7 +347,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             for (int q = 0; q < 4; ++q) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[2 * q + i / 4][i % 4] = exp2_(x[2 * q + i / 4][i % 4] - base);
+                    x[2 * q + i / 4][i % 4] = exp2_(rule.above(x[2 * q + i / 4][i % 4], base));
                     l += x[2 * q + i / 4][i % 4];
                 }
                 split8(x[2 * q], p_hi[q], p_lo[q]);
@@ -395,15 +398,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                 float top = kNone;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int in = 8 * (int)g + i;
-                    x[i] = finish(x[i], 32 * r.whole + in, in < left);
+                    const int in = 8 * (int)g + i, behind = in < left ? pos - 32 * r.whole - in : kNever;
+                    x[i] = rule.mask(rule.bend(x[i], behind), behind);
                     top = fmaxf(top, x[i]);
                 }
                 const float base = raise(top);
                 v8b p_hi, p_lo;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[i] = exp2_(x[i] - base);
+                    x[i] = exp2_(rule.above(x[i], base));
                     l += x[i];
                 }
                 split8(x, p_hi, p_lo);
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             if (EXTRA && a.slopes) rule[rt].slope = a.slopes[head] * kLog2e;
             each<KT>([&](auto kt_c) {
                 constexpr int kt = decltype(kt_c)::value;
-                q_scale[rt][kt] = load_query<D, kt>(a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride, row < rows, c, g,
+                q_scale[rt][kt] = load_query<D, kt>(a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride, row < rows, a.scale < 0.0f, c, g,
                                                     q_hi[rt][kt], q_lo[rt][kt]);
             });
 #pragma unroll
@@ -549,16 +552,16 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             int tail;                                                // tokens of the lane's value chunk if it is the incomplete one, or 0
         };
         Raw raw;
+        int pages = step0 < step1 ? four_pages(p, b, r.first + 4 * step0, r.end) : 0;
         auto load = [&](int step) {
             const int chunk0 = r.first + 4 * step;
-            auto offset = [&](int k) -> int64_t { return chunk0 + k < r.end ? cell_offset<D>(p, b, kv_head, chunk0 + k) : -1; };
-            const int64_t a0 = offset(0), a1 = offset(1), a2 = offset(2), a3 = offset(3);
-            auto pick = [&](uint32_t k) { return k == 0 ? a0 : k == 1 ? a1 : k == 2 ? a2 : a3; };
-            const int64_t ak = pick(c >> 2), av = pick(g);
+            const Four at = four_cells<D>(p, kv_head, chunk0, r.end, pages);
+            pages = four_pages(p, b, chunk0 + 4, r.end);
+            const int64_t ak = at.pick(c >> 2), av = at.pick(g);
             raw.tail = chunk0 + (int)g >= r.whole ? s.length - 32 * (chunk0 + (int)g) : 0;      // (the chunk at `whole`: fewer than 32)
             raw.k_there = ak >= 0;
             raw.v_there = av >= 0 && (raw.tail == 0 || s.slot >= 0);
-            raw.all = (a0 | a1 | a2 | a3) >= 0 && chunk0 + 4 <= r.whole;
+            raw.all = at.all() && chunk0 + 4 <= r.whole;
             const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
             if (raw.k_there) {
                 each<KT>([&](auto kt_c) {
@@ -636,20 +639,29 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             uint2 scales[KT];
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) scales[kt] = *reinterpret_cast<const uint2*>(from + W::kK + W::kV + kt * 512 + lane * 8u);
+            // operands are read a tile ahead
+            auto keys = [&](int t, v8i (&k8)[KT]) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const int4 lo = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + lane * 16u);
+                    const int4 hi = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + 1024 + lane * 16u);
+                    k8[kt] = v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                }
+            };
+            v8i k8[2][KT];
+            keys(0, k8[0]);
             each<8>([&](auto t_c) {
                 constexpr int t = decltype(t_c)::value;
+                if constexpr (t < 7) keys(t + 1, k8[(t + 1) & 1]);
                 v4f acc[RT];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) acc[rt] = v4f{0, 0, 0, 0};
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const int4 lo = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + lane * 16u);
-                    const int4 hi = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + 1024 + lane * 16u);
-                    const v8i k8 = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                     const int scale = (int)(t < 4 ? scales[kt].x : scales[kt].y);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
-                        product<(t & 3)>(k8, q_hi[rt][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt], q_scale[rt][kt] - kLoShift);
+                        product<(t & 3)>(k8[t & 1][kt], q_hi[rt][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt], q_scale[rt][kt] - kLoShift);
                 }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
@@ -660,7 +672,7 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 float top = kNone;
-                const int behind = pos[rt] - 32 * (chunk0 + (int)g);
+                const int behind = inside || there ? pos[rt] - 32 * (chunk0 + (int)g) : kNever;
                 if (inside) {
 #pragma unroll
                     for (int t = 0; t < 8; ++t)
@@ -674,12 +686,11 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
                     for (int t = 0; t < 8; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float y = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
-                            x[rt][t][i] = there && rule[rt].seen(behind - 4 * t - i) ? y : kNone;
+                            x[rt][t][i] = rule[rt].mask(rule[rt].bend(x[rt][t][i], behind - 4 * t - i), behind - 4 * t - i);
                             top = fmaxf(top, x[rt][t][i]);
                         }
                 }
-                const float next = fmaxf(m[rt], column_max(top)), base = next == kNone ? 0.0f : next;
+                const float next = fmaxf(m[rt], rule[rt].log2_of(column_max(top))), base = next == kNone ? 0.0f : next;
                 if (__any(next > m[rt])) {
                     const float by = exp2_(m[rt] - base);
                     l[rt] *= by;
@@ -693,19 +704,25 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float e = exp2_(x[rt][2 * q + i / 4][i % 4] - base);
+                        const float e = exp2_(rule[rt].above(x[rt][2 * q + i / 4][i % 4], base));
                         l[rt] += e;
                         pr[rt][q][i] = (__bf16)e;
                     }
             }
+            auto values = [&](int j, v8b (&v)[4]) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const v8b*>(from + W::kK + j * 4096 + q * 1024 + lane * 16u);
+            };
+            v8b v[2][4];
+            values(0, v[0]);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const v8b v = *reinterpret_cast<const v8b*>(from + W::kK + j * 4096 + q * 1024 + lane * 16u);
+            for (int j = 0; j < NJ; ++j) {
+                if (j + 1 < NJ) values(j + 1, v[(j + 1) & 1]);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) o[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[rt][q], o[rt][j], 0, 0, 0);
-                }
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) o[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j & 1][q], pr[rt][q], o[rt][j], 0, 0, 0);
+            }
         };
 
         __syncthreads();                                             // of the row block before
@@ -827,7 +844,7 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
     a.split_steps = sp.steps;
     a.rows = sp.rows;
     const dim3 grid((uint32_t)(batch.batch * cache.kv_heads), (uint32_t)sp.splits, (uint32_t)sp.blocks);
-    const bool extra = a.softcap > 0.0f || a.slopes;
+    const bool extra = a.softcap > 0.0f || a.slopes || a.scale == 0.0f;
     with_head_dim(cache.head_dim, [&](auto d) {
         constexpr int kD = decltype(d)::value;
         if (sp.rows > 16) {

@@ -74,17 +74,45 @@ __device__ __forceinline__ Sequence sequence(const PagedArgs& p, int b) {
     return Sequence{t0, t1 - t0, (int)min((int64_t)max(p.lengths[b], 0), most), slot >= 0 && slot < p.n_slots ? slot : -1};
 }
 
-// Where the cell of a chunk of 32 tokens (which the length says is there) lies in the pool; -1 where its page is none of the pool's.
+// Where the cell of a chunk of 32 tokens lies in the pool, given its page's number in the table; -1 where that is none of the pool's.
 template <int D>
-__device__ __forceinline__ int64_t cell_offset(const PagedArgs& p, int b, int head, int chunk) {
-    const int in_table = (int)((uint64_t)chunk * p.per_page >> 40), page = p.table[(int64_t)b * p.width + in_table];
+__device__ __forceinline__ int64_t cell_offset(const PagedArgs& p, int head, int chunk, int in_table, int page) {
     if (page < 0 || page >= p.n_pages) return -1;
     return (((int64_t)page * p.kv_heads + head) * p.page_chunks + (chunk - in_table * p.page_chunks)) * Cell<D>::kBytes;
 }
+__device__ __forceinline__ int place_in_table(const PagedArgs& p, int chunk) { return (int)((uint64_t)chunk * p.per_page >> 40); }
+
+// the cell of a chunk that the length says is there
 template <int D>
 __device__ __forceinline__ uint8_t* cell(const PagedArgs& p, int b, int head, int chunk) {
-    const int64_t at = cell_offset<D>(p, b, head, chunk);
+    const int in_table = place_in_table(p, chunk);
+    const int64_t at = cell_offset<D>(p, head, chunk, in_table, p.table[(int64_t)b * p.width + in_table]);
     return at < 0 ? nullptr : p.pages + at;
+}
+
+// The cells of four consecutive chunks, of those below `limit` (which the length says are there).  The numbers of their pages are
+// loaded by lanes 0 .. 3 a step ahead (`pages`), so that the addresses need not wait for the table.
+__device__ __forceinline__ int four_pages(const PagedArgs& p, int b, int chunk0, int limit) {
+    const int chunk = min(chunk0 + (int)(threadIdx.x & 3u), limit - 1);
+    return p.table[(int64_t)b * p.width + place_in_table(p, max(chunk, 0))];
+}
+struct Four {
+    int64_t c0, c1, c2, c3;
+    __device__ __forceinline__ int64_t pick(uint32_t k) const {
+        const int64_t lo = k & 1u ? c1 : c0, hi = k & 1u ? c3 : c2;
+        return k & 2u ? hi : lo;
+    }
+    __device__ __forceinline__ bool none() const { return (c0 & c1 & c2 & c3) < 0; }
+    __device__ __forceinline__ bool all() const { return (c0 | c1 | c2 | c3) >= 0; }
+};
+template <int D>
+__device__ __forceinline__ Four four_cells(const PagedArgs& p, int head, int chunk0, int limit, int pages) {
+    auto one = [&](int k) {
+        const int chunk = chunk0 + k;
+        const int64_t to = cell_offset<D>(p, head, chunk, place_in_table(p, chunk), __builtin_amdgcn_readlane(pages, k));
+        return chunk < limit ? to : (int64_t)-1;
+    };
+    return Four{one(0), one(1), one(2), one(3)};
 }
 
 // bf16 [head_dim, 32] of a slot
