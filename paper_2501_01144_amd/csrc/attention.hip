@@ -79,10 +79,15 @@ __device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, i
 // c += a (hi + 2^-5 lo), hi times 2^(sb - 127).  The compiler lets a result overlap an operand that it sees no further use of, which the instruction
 // overwrites before it has read it for the last time: operands are in use until the end here (the build checks).
 template <int OPSEL>
+__device__ __forceinline__ void times(const v8i& a, const v8i& b, v4f& c, int sa, int sb) {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, OPSEL, sa, 0, sb);
+}
+__device__ __forceinline__ void keep(v4f& c, const v8i& a, const v8i& hi, const v8i& lo) { asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo)); }
+template <int OPSEL>
 __device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& lo, v4f& c, int sa, int sb, int sb_lo) {
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, c, 0, 0, OPSEL, sa, 0, sb);
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, c, 0, 0, OPSEL, sa, 0, sb_lo);
-    asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
+    times<OPSEL>(a, hi, c, sa, sb);
+    times<OPSEL>(a, lo, c, sa, sb_lo);
+    keep(c, a, hi, lo);
 }
 
 // 32 codes (in 16 bytes) of a scale and a dialect to bf16: fragments of four instructions, tokens 8 q .. 8 q + 7 in the q-th
@@ -140,7 +145,7 @@ __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequenc
     const int p_min = s.length - s.n + row0 / group, p_max = s.length - s.n + last_row / group;
     const int t_end = min(p_max + 1, s.length), t_begin = a.window > 0 ? max(0, p_min - a.window + 1) : 0;
     r.first = t_begin / 32;
-    r.end = t_end > t_begin ? (t_end + 31) / 32 : r.first;
+    r.end = t_end > t_begin && a.paged.n_pages > 0 ? (t_end + 31) / 32 : r.first;
     r.whole = min(r.end, s.length / 32);
     r.steps = max(0, ((a.rows == 16 ? r.whole : r.end) - r.first + 3) / 4);
     r.parts = min(a.splits, max(1, (r.steps + a.split_steps - 1) / a.split_steps));
@@ -548,7 +553,7 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             uint4 k[KT], v[VT];
             uint32_t k_id[KT], v_id[VT], v_scale[VT];
             uint2 k_scale[KT];
-            bool k_there, v_there, all;
+            bool v_there, all;
             int tail;                                                // tokens of the lane's value chunk if it is the incomplete one, or 0
         };
         Raw raw;
@@ -559,60 +564,52 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             pages = four_pages(p, b, chunk0 + 4, r.end);
             const int64_t ak = at.pick(c >> 2), av = at.pick(g);
             raw.tail = chunk0 + (int)g >= r.whole ? s.length - 32 * (chunk0 + (int)g) : 0;      // (the chunk at `whole`: fewer than 32)
-            raw.k_there = ak >= 0;
             raw.v_there = av >= 0 && (raw.tail == 0 || s.slot >= 0);
             raw.all = at.all() && chunk0 + 4 <= r.whole;
             const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
-            if (raw.k_there) {
-                each<KT>([&](auto kt_c) {
-                    constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
-                    const uint32_t block = kt * 4 + min(g, (uint32_t)(nb - 1));
-                    if (wave == kt) raw.k_scale[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block) * 8u);
-                    raw.k_id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + wave];
-                    const uint8_t* row = kc + (4u * wave + (c & 3u)) * (D / 2) + kt * 64;
-                    if constexpr (nb == 4) {
-                        raw.k[kt] = *reinterpret_cast<const uint4*>(row + g * 16u);
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(row + g * 8u);
-                        uint2 y = x;
-                        if constexpr (nb == 3) y = *reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u));
-                        raw.k[kt] = make_uint4(x.x, x.y, y.x, y.y);
-                    }
-                });
-            }
-            if (raw.v_there && raw.tail == 0) {
-#pragma unroll
-                for (int i = 0; i < VT; ++i) {
-                    const int j = wave + 8 * i;
-                    if (j < NJ) {
-                        raw.v[i] = *reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u);
-                        raw.v_scale[i] = vc[C::kVExps + c * C::VE + j];
-                        raw.v_id[i] = vc[C::kVIds + (c >> 1) * C::VE + j];
-                    }
+            // (whatever lies there where the chunk is absent)
+            each<KT>([&](auto kt_c) {
+                constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
+                const uint32_t block = kt * 4 + min(g, (uint32_t)(nb - 1));
+                raw.k_scale[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block) * 8u);
+                raw.k_id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + wave];
+                const uint8_t* row = kc + (4u * wave + (c & 3u)) * (D / 2) + kt * 64;
+                if constexpr (nb == 4) {
+                    raw.k[kt] = *reinterpret_cast<const uint4*>(row + g * 16u);
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(row + g * 8u);
+                    uint2 y = x;
+                    if constexpr (nb == 3) y = *reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u));
+                    raw.k[kt] = make_uint4(x.x, x.y, y.x, y.y);
                 }
+            });
+#pragma unroll
+            for (int i = 0; i < VT; ++i) {
+                const int j = min(wave + 8 * i, NJ - 1);
+                raw.v[i] = *reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u);
+                raw.v_scale[i] = vc[C::kVExps + c * C::VE + j];
+                raw.v_id[i] = vc[C::kVIds + (c >> 1) * C::VE + j];
             }
         };
         auto store = [&](uint8_t* to) {
             each<KT>([&](auto kt_c) {
                 constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
                 v8i k8 = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (raw.k_there) {
-                    expand16<0>(make_uint2(raw.k[kt].x, raw.k[kt].y), table[raw.k_id[kt] & 15u], k8);
-                    if constexpr (nb > 2) expand16<4>(make_uint2(raw.k[kt].z, raw.k[kt].w), table[raw.k_id[kt] >> 4], k8);
-                }
+                expand16<0>(make_uint2(raw.k[kt].x, raw.k[kt].y), table[raw.k_id[kt] & 15u], k8);
+                if constexpr (nb > 2) expand16<4>(make_uint2(raw.k[kt].z, raw.k[kt].w), table[raw.k_id[kt] >> 4], k8);
                 uint8_t* at = to + (wave * KT + kt) * 2048 + lane * 16u;
                 *reinterpret_cast<int4*>(at) = make_int4(k8[0], k8[1], k8[2], k8[3]);
                 *reinterpret_cast<int4*>(at + 1024) = make_int4(k8[4], k8[5], k8[6], k8[7]);
-                if (wave == kt) *reinterpret_cast<uint2*>(to + W::kK + W::kV + kt * 512 + lane * 8u) = raw.k_there ? raw.k_scale[kt] : make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+                if (wave == kt) *reinterpret_cast<uint2*>(to + W::kK + W::kV + kt * 512 + lane * 8u) = raw.k_scale[kt];
             });
 #pragma unroll
             for (int i = 0; i < VT; ++i) {
                 const int j = wave + 8 * i;
                 if (j >= NJ) break;
-                v8b v[4] = {};
-                if (raw.v_there && raw.tail == 0) {
-                    expand_bf16(raw.v[i], table[(raw.v_id[i] >> (4u * (c & 1u))) & 15u], raw.v_scale[i], v);
-                } else if (raw.v_there) {
+                v8b v[4];
+                // an absent chunk: anything finite (its probabilities are zero)
+                expand_bf16(raw.v[i], table[(raw.v_id[i] >> (4u * (c & 1u))) & 15u], raw.v_there ? raw.v_scale[i] : 127u, v);
+                if (raw.v_there && raw.tail > 0) {
                     const uint16_t* from = residual<D>(p, s.slot, kv_head) + (16u * j + c) * 32u;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -660,8 +657,11 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
                 for (int kt = 0; kt < KT; ++kt) {
                     const int scale = (int)(t < 4 ? scales[kt].x : scales[kt].y);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-                        product<(t & 3)>(k8[t & 1][kt], q_hi[rt][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt], q_scale[rt][kt] - kLoShift);
+                    for (int rt = 0; rt < RT; ++rt) times<(t & 3)>(k8[t & 1][kt], q_hi[rt][kt], acc[rt], scale, q_scale[rt][kt]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) times<(t & 3)>(k8[t & 1][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt] - kLoShift);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) keep(acc[rt], k8[t & 1][kt], q_hi[rt][kt], q_lo[rt][kt]);
                 }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
@@ -673,23 +673,23 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             for (int rt = 0; rt < RT; ++rt) {
                 float top = kNone;
                 const int behind = inside || there ? pos[rt] - 32 * (chunk0 + (int)g) : kNever;
-                if (inside) {
+                if constexpr (EXTRA) {
 #pragma unroll
                     for (int t = 0; t < 8; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            x[rt][t][i] = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
-                            top = fmaxf(top, x[rt][t][i]);
-                        }
-                } else {
-#pragma unroll
-                    for (int t = 0; t < 8; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            x[rt][t][i] = rule[rt].mask(rule[rt].bend(x[rt][t][i], behind - 4 * t - i), behind - 4 * t - i);
-                            top = fmaxf(top, x[rt][t][i]);
-                        }
+                        for (int i = 0; i < 4; ++i) x[rt][t][i] = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
                 }
+                if (!inside) {
+                    asm volatile("");                                // a branch, not 64 selections at every step
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[rt][t][i] = rule[rt].mask(x[rt][t][i], behind - 4 * t - i);
+                }
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][t][i]);
                 const float next = fmaxf(m[rt], rule[rt].log2_of(column_max(top))), base = next == kNone ? 0.0f : next;
                 if (__any(next > m[rt])) {
                     const float by = exp2_(m[rt] - base);
@@ -733,12 +733,12 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
             for (int step = step0; step < step1; ++step) {
                 const uint8_t* from = s_x + (W::kBuffers == 2 ? ((step - step0) & 1) * W::kStep : 0u);
                 __syncthreads();
-                if (step + 1 < step1) load(step + 1);
+                load(step + 1);                                      // (beyond the last: anything)
                 work(from, step, there, all);
                 if (W::kBuffers == 1) __syncthreads();
                 there = raw.v_there;
                 all = raw.all;
-                if (step + 1 < step1) store(s_x + (W::kBuffers == 2 ? ((step + 1 - step0) & 1) * W::kStep : 0u));
+                store(s_x + (W::kBuffers == 2 ? ((step + 1 - step0) & 1) * W::kStep : 0u));
             }
         }
 
