@@ -26,6 +26,7 @@ constexpr int kThreads = 256, kWaves = 4;
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef short v2s __attribute__((ext_vector_type(2)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
@@ -90,12 +91,12 @@ __device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& 
     keep(c, a, hi, lo);
 }
 
-// 32 codes (in 16 bytes) of a scale and a dialect to bf16: fragments of four instructions, tokens 8 q .. 8 q + 7 in the q-th
-__device__ __forceinline__ void expand_bf16(uint4 c, uint2 row, uint32_t ebyte, v8b (&v)[4]) {
+// N dwords of codes of a scale and a dialect to bf16: fragments of N instructions, tokens 8 q .. 8 q + 7 in the q-th
+template <int N>
+__device__ __forceinline__ void expand_bf16(const uint32_t* w, uint2 row, uint32_t ebyte, v8b (&v)[N]) {
     const float scale = as_f(ebyte << 23);                          // the conversion goes by the exponent bits (0: 2^-127)
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < N; ++q) {
         const uint32_t lo = __builtin_amdgcn_perm(row.y, row.x, w[q] & 0x07070707u) | ((w[q] << 4) & 0x80808080u);
         const uint32_t hi = __builtin_amdgcn_perm(row.y, row.x, (w[q] >> 4) & 0x07070707u) | (w[q] & 0x80808080u);
         const v2b x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
@@ -131,13 +132,23 @@ __device__ __forceinline__ float column_sum(float v) {
     return as_f(r[0]) + as_f(r[1]);
 }
 
+// over the two lanes of a column of 32 x 32
+__device__ __forceinline__ float pair_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+    return fmaxf(as_f(r[0]), as_f(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+    return as_f(r[0]) + as_f(r[1]);
+}
+
 constexpr float kNone = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Which keys a block of query rows sees, and how they are split between workgroups: alike in the kernel that adds the parts up.
 struct Range {
     int first, end, whole;       // chunks of 32: [first, end), values quantized below `whole`
-    int steps, parts;            // of four chunks (of one row tile: whole ones only); workgroups that have some
+    int steps, parts;            // of four chunks (16 rows: of whole ones) or two (128 rows); workgroups that have some
 };
 __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequence& s, int group, int row0) {
     Range r;
@@ -147,7 +158,7 @@ __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequenc
     r.first = t_begin / 32;
     r.end = t_end > t_begin && a.paged.n_pages > 0 ? (t_end + 31) / 32 : r.first;
     r.whole = min(r.end, s.length / 32);
-    r.steps = max(0, ((a.rows == 16 ? r.whole : r.end) - r.first + 3) / 4);
+    r.steps = a.rows == 16 ? max(0, (r.whole - r.first + 3) / 4) : a.rows == 128 ? (r.end - r.first + 1) / 2 : (r.end - r.first + 3) / 4;
     r.parts = min(a.splits, max(1, (r.steps + a.split_steps - 1) / a.split_steps));
     return r;
 }
@@ -369,7 +380,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                 for (int jj = 0; jj < 4 && 4 * w + jj < NJ; ++jj) {
                     const int j = 4 * w + jj;
                     v8b v[4];
-                    expand_bf16(*reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u), table[(ids >> (8 * jj)) & 15u],
+                    const uint4 w4 = *reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u);
+                    expand_bf16<4>(&w4.x, table[(ids >> (8 * jj)) & 15u],
                                 (scales >> (8 * jj)) & 0xffu, v);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -488,26 +500,31 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Many query rows: a workgroup of eight waves takes 8 * 16 * RT of them, expands every step of 128 keys once into LDS, as the
-// operands that all waves read (keys in FP8, values in bf16), and each wave does both products for its RT tiles of 16 rows.
-// Wave w expands tile w of the keys and tiles w, w + 8 of the values; codes of the step after are loaded meanwhile, and where LDS has
-// room for two steps (D <= 128) one barrier a step is enough.  The incomplete chunk is part of the last step: its values are stored to
-// LDS as they are.  A probability is one bf16 number here.
+// Many query rows: a workgroup expands every step of 32 NC keys once into LDS, as the operands that all its waves read (keys in FP8,
+// values in bf16), and each wave does both products for 32 rows, on 32 x 32 x 64 and 32 x 32 x 16: a query is a column again,
+// now of two lanes (h, c).  They hold rows 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
+// 16 h + 4 a + i of a chunk, so that a lane supplies the probabilities of the 16 tokens whose scores it has, eight to an instruction.
+// A chunk is a tile: its cell, and whether it is there, are the same for all lanes.
+// Codes of the next step are loaded while this one is multiplied, and expanded into the other half of LDS: one barrier a step.
+// The incomplete chunk is part of the last step: its values are stored to LDS as they are.  A probability is one bf16 number here.
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 struct Wide {
-    static constexpr int kWaves = 8, kThreads = 512, RT = D <= 128 ? 2 : 1, kRows = kWaves * 16 * RT, kBuffers = D <= 128 ? 2 : 1;
-    static constexpr uint32_t kK = 8 * Cell<D>::KT * 2048, kV = Cell<D>::NJ * 4096, kScales = Cell<D>::KT * 512, kStep = kK + kV + kScales;
+    static constexpr int kWaves = D <= 128 ? 8 : 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;      // (D > 128: 512 registers a lane)
+    static constexpr int NC = D <= 128 ? 4 : 2;                      // chunks of a step
+    static constexpr int KS = (D + 63) / 64, DT = D / 32;            // instructions that add over a key, tiles of V^T
+    static constexpr int KP = (NC * KS + kWaves - 1) / kWaves, VP = (NC * DT + kWaves - 1) / kWaves;      // pieces that a wave expands
+    static constexpr uint32_t kK = NC * KS * 2048, kV = NC * DT * 2048, kScales = KS * 256, kStep = kK + kV + kScales;
 };
 
 template <int D, bool EXTRA>
-__global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_attention_wide_kernel(AttentionArgs a) {
     using C = Cell<D>;
     using W = Wide<D>;
-    constexpr int KT = C::KT, NJ = C::NJ, RT = W::RT, VT = (NJ + 7) / 8;
-    __shared__ __attribute__((aligned(16))) uint8_t s_x[W::kBuffers * W::kStep];
+    constexpr int KS = W::KS, DT = W::DT, NC = W::NC, KP = W::KP, VP = W::VP;
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[2 * W::kStep];
     __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 31u, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
     const PagedArgs& p = a.paged;
     const int b = (int)(blockIdx.x / (uint32_t)p.kv_heads), kv_head = (int)(blockIdx.x % (uint32_t)p.kv_heads), part = (int)blockIdx.y;
@@ -516,259 +533,277 @@ __global__ __launch_bounds__(512, 2) void paged_attention_wide_kernel(AttentionA
     if (tid < kDialects * 8 / 4) reinterpret_cast<uint32_t*>(s_rows)[tid] = reinterpret_cast<const uint32_t*>(&g_f8_rows.b[0][0])[tid];
     __syncthreads();
     const uint2* const table = reinterpret_cast<const uint2*>(s_rows);
+    const uint32_t key = 16u * ((c >> 2) & 1u) + 4u * (c >> 3) + (c & 3u);      // token of row c of a tile of scores
 
     for (int row0 = (int)blockIdx.z * W::kRows; row0 < s.n * group; row0 += (int)gridDim.z * W::kRows) {
         const Range r = key_range(a, s, group, row0);
         if (part >= r.parts) continue;
         const int step0 = part * a.split_steps, step1 = part == r.parts - 1 ? r.steps : min(r.steps, step0 + a.split_steps);
-        const int wave_row = row0 + wave * 16 * RT, rows = s.n * group;
+        const int wave_row = row0 + wave * 32, rows = s.n * group;
         // positions of the wave's rows (rows beyond the last have those of the last)
-        const int p_min = s.length - s.n + min(wave_row, rows - 1) / group, p_max = s.length - s.n + min(wave_row + 16 * RT, rows) / group
-                          - (min(wave_row + 16 * RT, rows) % group == 0 ? 1 : 0);
-        int pos[RT];
-        Scores<EXTRA> rule[2] = {Scores<EXTRA>(a), Scores<EXTRA>(a)};
-        v8i q_hi[RT][KT], q_lo[RT][KT];
-        int q_scale[RT][KT];
-        v4f o[RT][NJ];
-        float m[RT], l[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int row = wave_row + rt * 16 + (int)c, held = min(row, rows - 1);
-            const int head = kv_head * group + held % group;
-            pos[rt] = s.length - s.n + held / group;
-            if (EXTRA && a.slopes) rule[rt].slope = a.slopes[head] * kLog2e;
-            each<KT>([&](auto kt_c) {
-                constexpr int kt = decltype(kt_c)::value;
-                q_scale[rt][kt] = load_query<D, kt>(a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride, row < rows, a.scale < 0.0f, c, g,
-                                                    q_hi[rt][kt], q_lo[rt][kt]);
-            });
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) o[rt][j] = v4f{0, 0, 0, 0};
-            m[rt] = kNone;
-            l[rt] = 0.0f;
-        }
+        const int p_min = s.length - s.n + min(wave_row, rows - 1) / group, p_max = s.length - s.n + (min(wave_row + 32, rows) - 1) / group;
+        const int row = wave_row + (int)c, held = min(row, rows - 1);
+        const int head = kv_head * group + held % group, pos = s.length - s.n + held / group;
+        Scores<EXTRA> rule(a);
+        if (EXTRA && a.slopes) rule.slope = a.slopes[head] * kLog2e;
 
-        // ---- what a thread expands of a step: its share of key tile `wave` and of value tiles `wave`, `wave` + 8
-        struct Raw {
-            uint4 k[KT], v[VT];
-            uint32_t k_id[KT], v_id[VT], v_scale[VT];
-            uint2 k_scale[KT];
-            bool v_there, all;
-            int tail;                                                // tokens of the lane's value chunk if it is the incomplete one, or 0
-        };
-        Raw raw;
-        int pages = step0 < step1 ? four_pages(p, b, r.first + 4 * step0, r.end) : 0;
-        auto load = [&](int step) {
-            const int chunk0 = r.first + 4 * step;
-            const Four at = four_cells<D>(p, kv_head, chunk0, r.end, pages);
-            pages = four_pages(p, b, chunk0 + 4, r.end);
-            const int64_t ak = at.pick(c >> 2), av = at.pick(g);
-            raw.tail = chunk0 + (int)g >= r.whole ? s.length - 32 * (chunk0 + (int)g) : 0;      // (the chunk at `whole`: fewer than 32)
-            raw.v_there = av >= 0 && (raw.tail == 0 || s.slot >= 0);
-            raw.all = at.all() && chunk0 + 4 <= r.whole;
-            const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
-            // (whatever lies there where the chunk is absent)
-            each<KT>([&](auto kt_c) {
-                constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
-                const uint32_t block = kt * 4 + min(g, (uint32_t)(nb - 1));
-                raw.k_scale[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block) * 8u);
-                raw.k_id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + wave];
-                const uint8_t* row = kc + (4u * wave + (c & 3u)) * (D / 2) + kt * 64;
-                if constexpr (nb == 4) {
-                    raw.k[kt] = *reinterpret_cast<const uint4*>(row + g * 16u);
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(row + g * 8u);
-                    uint2 y = x;
-                    if constexpr (nb == 3) y = *reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u));
-                    raw.k[kt] = make_uint4(x.x, x.y, y.x, y.y);
-                }
-            });
+        // ---- queries: halves h of blocks 2 ks and 2 ks + 1, the scale of block 2 ks + h
+        v8i q_hi[KS], q_lo[KS];
+        int q_scale[KS];
+        {
+            const uint16_t* src = a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride;
+            const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+            each<KS>([&](auto ks_c) {
+                constexpr int ks = decltype(ks_c)::value;
+                uint4 v[2][2];
+                uint32_t top[2] = {0, 0};
 #pragma unroll
-            for (int i = 0; i < VT; ++i) {
-                const int j = min(wave + 8 * i, NJ - 1);
-                raw.v[i] = *reinterpret_cast<const uint4*>(vc + C::kVCodes + (16u * j + c) * 16u);
-                raw.v_scale[i] = vc[C::kVExps + c * C::VE + j];
-                raw.v_id[i] = vc[C::kVIds + (c >> 1) * C::VE + j];
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        v[y][k] = make_uint4(0, 0, 0, 0);
+                        if (row < rows && 2 * ks + y < C::NB) v[y][k] = *reinterpret_cast<const uint4*>(src + (2 * ks + y) * 32 + h * 16u + k * 8);
+                        const uint32_t w[4] = {v[y][k].x, v[y][k].y, v[y][k].z, v[y][k].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) top[y] = max(top[y], max((w[j] >> 7) & 0xffu, (w[j] >> 23) & 0xffu));
+                    }
+                    top[y] = max(top[y], (uint32_t)__shfl_xor((int)top[y], 32));
+                    top[y] = (uint32_t)max((int)top[y] - 7, kLoShift);          // the largest magnitude becomes less than 2^8
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t w[4] = {v[y][k].x ^ flip, v[y][k].y ^ flip, v[y][k].z ^ flip, v[y][k].w ^ flip};
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - (int)top[y]);
+                        int hi, lo;
+                        split4(x[0], x[1], x[2], x[3], hi, lo);
+                        q_hi[ks][4 * y + 2 * k] = hi;
+                        q_lo[ks][4 * y + 2 * k] = lo;
+                        split4(x[4], x[5], x[6], x[7], hi, lo);
+                        q_hi[ks][4 * y + 2 * k + 1] = hi;
+                        q_lo[ks][4 * y + 2 * k + 1] = lo;
+                    }
+                }
+                q_scale[ks] = (int)(h ? top[1] : top[0]);
+            });
+        }
+        v16f o[DT];
+#pragma unroll
+        for (int j = 0; j < DT; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
+        float m = kNone, l = 0.0f;
+
+        // ---- what a wave expands of a step: pieces wave, wave + kWaves, .. of the keys (chunk, ks) and of the values (chunk, tile)
+        uint2 k_code[KP][2], v_code[VP];
+        uint32_t k_id[KP], k_scale[KP], v_id[VP], v_scale[VP];
+        uint32_t there = 0;                                          // of the step loaded: bit k: chunk k
+        int pages = step0 < step1 ? four_pages(p, b, r.first + NC * step0, r.end) : 0;
+        auto load = [&](int step) {
+            const int chunk0 = r.first + NC * step;
+            auto place = [&](int k) {                                // wave-uniform; 0 for a chunk that is not there
+                const int64_t at = cell_offset<D>(p, kv_head, chunk0 + k, place_in_table(p, chunk0 + k), __builtin_amdgcn_readlane(pages, k));
+                return p.pages + (at < 0 || chunk0 + k >= r.end ? (int64_t)0 : at);
+            };
+            const bool mine = chunk0 + (int)(lane & 3u) < r.end && pages >= 0 && pages < p.n_pages && (chunk0 + (int)(lane & 3u) < r.whole || s.slot >= 0);
+            there = (uint32_t)__ballot(mine) & ((1u << NC) - 1u);
+#pragma unroll
+            for (int n = 0; n < KP; ++n) {
+                const int piece = min(wave + n * W::kWaves, NC * KS - 1), ks = piece % KS, block = min(2 * ks + (int)h, C::NB - 1);
+                const uint8_t* kc = place(piece / KS);
+                const uint8_t* at = kc + key * (D / 2);
+                // (of a last block alone: the other half's queries are zero, and what is read there is the first's)
+                const int u0 = 4 * ks + (int)h, u1 = 2 * ks + 1 < C::NB ? u0 + 2 : u0;
+                k_code[n][0] = *reinterpret_cast<const uint2*>(at + C::k_unit(u0) * 8);
+                k_code[n][1] = *reinterpret_cast<const uint2*>(at + C::k_unit(u1) * 8);
+                k_scale[n] = kc[C::kKExps + ((key & 3u) * C::NB + block) * 8u + (key >> 2)];
+                // dialects of blocks 2 ks and 2 ks + 1: the same half of two bytes (pairs are two blocks apart)
+                const uint8_t* ids = kc + C::kKIds + ((key & 3u) * C::NP + ks / 2 * 2) * 8u + (key >> 2);
+                k_id[n] = ((uint32_t)ids[0] | (uint32_t)ids[8] << 8) >> (ks & 1 ? 4 : 0);
             }
+#pragma unroll
+            for (int n = 0; n < VP; ++n) {
+                const int piece = min(wave + n * W::kWaves, NC * DT - 1), tile = piece % DT;
+                const uint8_t* vc = place(piece / DT);
+                const uint32_t d = 32u * tile + c;
+                v_code[n] = *reinterpret_cast<const uint2*>(vc + C::kVCodes + d * 16u + h * 8u);
+                v_scale[n] = vc[C::kVExps + (d & 15u) * C::VE + (d >> 4)];
+                v_id[n] = vc[C::kVIds + ((d & 15u) >> 1) * C::VE + (d >> 4)];
+            }
+            pages = four_pages(p, b, chunk0 + NC, r.end);
         };
-        auto store = [&](uint8_t* to) {
-            each<KT>([&](auto kt_c) {
-                constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
-                v8i k8 = {0, 0, 0, 0, 0, 0, 0, 0};
-                expand16<0>(make_uint2(raw.k[kt].x, raw.k[kt].y), table[raw.k_id[kt] & 15u], k8);
-                if constexpr (nb > 2) expand16<4>(make_uint2(raw.k[kt].z, raw.k[kt].w), table[raw.k_id[kt] >> 4], k8);
-                uint8_t* at = to + (wave * KT + kt) * 2048 + lane * 16u;
+        auto store = [&](uint8_t* to, int step) {
+            const int chunk0 = r.first + NC * step;
+#pragma unroll
+            for (int n = 0; n < KP; ++n) {
+                const int piece = wave + n * W::kWaves;
+                if (NC * KS % W::kWaves != 0 && piece >= NC * KS) break;
+                v8i k8;
+                expand16<0>(k_code[n][0], table[k_id[n] & 15u], k8);
+                expand16<4>(k_code[n][1], table[(k_id[n] >> 8) & 15u], k8);
+                uint8_t* at = to + piece * 2048 + lane * 16u;
                 *reinterpret_cast<int4*>(at) = make_int4(k8[0], k8[1], k8[2], k8[3]);
                 *reinterpret_cast<int4*>(at + 1024) = make_int4(k8[4], k8[5], k8[6], k8[7]);
-                if (wave == kt) *reinterpret_cast<uint2*>(to + W::kK + W::kV + kt * 512 + lane * 8u) = raw.k_scale[kt];
-            });
+                to[W::kK + W::kV + (piece % KS) * 256 + lane * 4u + piece / KS] = (uint8_t)k_scale[n];
+            }
 #pragma unroll
-            for (int i = 0; i < VT; ++i) {
-                const int j = wave + 8 * i;
-                if (j >= NJ) break;
-                v8b v[4];
+            for (int n = 0; n < VP; ++n) {
+                const int piece = wave + n * W::kWaves, chunk = chunk0 + piece / DT;
+                if (NC * DT % W::kWaves != 0 && piece >= NC * DT) break;
+                const uint32_t d = 32u * (piece % DT) + c;
+                v8b v[2];
                 // an absent chunk: anything finite (its probabilities are zero)
-                expand_bf16(raw.v[i], table[(raw.v_id[i] >> (4u * (c & 1u))) & 15u], raw.v_there ? raw.v_scale[i] : 127u, v);
-                if (raw.v_there && raw.tail > 0) {
-                    const uint16_t* from = residual<D>(p, s.slot, kv_head) + (16u * j + c) * 32u;
+                const bool here = (there >> (piece / DT)) & 1u;
+                expand_bf16<2>(&v_code[n].x, table[(v_id[n] >> (4u * (d & 1u))) & 15u], here ? v_scale[n] : 127u, v);
+                if (here && chunk >= r.whole) {
+                    const uint16_t* from = residual<D>(p, s.slot, kv_head) + d * 32u + h * 16u;
+                    const int left = s.length - 32 * chunk - 16 * (int)h;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < 2; ++q) {
                         const uint4 w = *reinterpret_cast<const uint4*>(from + 8 * q);
                         uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {                // what the slot holds beyond the tokens there are is anything
-                            if (8 * q + 2 * k >= raw.tail) u[k] = 0;
-                            else if (8 * q + 2 * k + 1 >= raw.tail) u[k] &= 0xffffu;
+                            if (8 * q + 2 * k >= left) u[k] = 0;
+                            else if (8 * q + 2 * k + 1 >= left) u[k] &= 0xffffu;
                         }
                         v[q] = __builtin_bit_cast(v8b, make_uint4(u[0], u[1], u[2], u[3]));
                     }
                 }
-                uint8_t* at = to + W::kK + j * 4096 + lane * 16u;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) *reinterpret_cast<v8b*>(at + q * 1024) = v[q];
+                uint8_t* at = to + W::kK + piece * 2048 + lane * 16u;
+                *reinterpret_cast<v8b*>(at) = v[0];
+                *reinterpret_cast<v8b*>(at + 1024) = v[1];
             }
         };
-        auto work = [&](const uint8_t* from, int step, bool there, bool all) {
-            const int chunk0 = r.first + 4 * step;
+        auto work = [&](const uint8_t* from, int step, uint32_t present) {
+            const int chunk0 = r.first + NC * step;
             if (32 * chunk0 > p_max) return;                         // later than all of the wave's rows
-            const bool inside = all && 32 * chunk0 + 127 <= p_min && (a.window <= 0 || 32 * chunk0 > p_max - a.window);
-            float x[RT][8][4];
-            uint2 scales[KT];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) scales[kt] = *reinterpret_cast<const uint2*>(from + W::kK + W::kV + kt * 512 + lane * 8u);
-            // operands are read a tile ahead
-            auto keys = [&](int t, v8i (&k8)[KT]) {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const int4 lo = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + lane * 16u);
-                    const int4 hi = *reinterpret_cast<const int4*>(from + (t * KT + kt) * 2048 + 1024 + lane * 16u);
-                    k8[kt] = v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                }
+            const bool inside = present == (1u << NC) - 1u && 32 * (chunk0 + NC) - 1 <= p_min && chunk0 + NC <= r.whole &&
+                                (a.window <= 0 || 32 * chunk0 > p_max - a.window);
+            // operands are read an instruction pair ahead
+            auto key_tile = [&](int n) {
+                const uint8_t* at = from + n * 2048 + lane * 16u;
+                const int4 lo = *reinterpret_cast<const int4*>(at), hi = *reinterpret_cast<const int4*>(at + 1024);
+                return v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             };
-            v8i k8[2][KT];
-            keys(0, k8[0]);
-            each<8>([&](auto t_c) {
+            auto value_tile = [&](int n) { return *reinterpret_cast<const v8b*>(from + W::kK + n * 1024 + lane * 16u); };
+            int scale[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) scale[ks] = *reinterpret_cast<const int*>(from + W::kK + W::kV + ks * 256 + lane * 4u);
+            v16f x[NC];
+            v8i k8[2];
+            k8[0] = key_tile(0);
+            each<NC>([&](auto t_c) {
                 constexpr int t = decltype(t_c)::value;
-                if constexpr (t < 7) keys(t + 1, k8[(t + 1) & 1]);
-                v4f acc[RT];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) acc[rt] = v4f{0, 0, 0, 0};
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const int scale = (int)(t < 4 ? scales[kt].x : scales[kt].y);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) times<(t & 3)>(k8[t & 1][kt], q_hi[rt][kt], acc[rt], scale, q_scale[rt][kt]);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) times<(t & 3)>(k8[t & 1][kt], q_lo[rt][kt], acc[rt], scale, q_scale[rt][kt] - kLoShift);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) keep(acc[rt], k8[t & 1][kt], q_hi[rt][kt], q_lo[rt][kt]);
-                }
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[rt][t][i] = acc[rt][i];
+                for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
+                each<KS>([&](auto ks_c) {
+                    constexpr int ks = decltype(ks_c)::value, n = t * KS + ks;
+                    if constexpr (n + 1 < NC * KS) k8[(n + 1) & 1] = key_tile(n + 1);
+                    x[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8[n & 1], q_hi[ks], x[t], 0, 0, t, scale[ks], 0, q_scale[ks]);
+                    x[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8[n & 1], q_lo[ks], x[t], 0, 0, t, scale[ks], 0, q_scale[ks] - kLoShift);
+                    asm("" : "+v"(x[t]) : "v"(k8[n & 1]), "v"(q_hi[ks]), "v"(q_lo[ks]));
+                });
             });
-            v8b pr[RT][4];
+            v8b v[2][DT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float top = kNone;
-                const int behind = inside || there ? pos[rt] - 32 * (chunk0 + (int)g) : kNever;
-                if constexpr (EXTRA) {
+            for (int j = 0; j < DT; ++j) v[0][j] = value_tile(2 * j);
+            const int behind = pos - 32 * chunk0 - 16 * (int)h;      // positions that token 16 h of the first chunk is behind the query
+            if constexpr (EXTRA) {
 #pragma unroll
-                    for (int t = 0; t < 8; ++t)
+                for (int t = 0; t < NC; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[rt][t][i] = rule[rt].bend(x[rt][t][i], behind - 4 * t - i);
+                    for (int i = 0; i < 16; ++i) x[t][i] = rule.bend(x[t][i], behind - 32 * t - i);
+            }
+            if (!inside) {
+                asm volatile("");                                    // a branch, not 64 selections at every step
+#pragma unroll
+                for (int t = 0; t < NC; ++t) {
+                    const int from_t = (present >> t) & 1u ? behind - 32 * t : kNever;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = rule.mask(x[t][i], from_t - i);
                 }
-                if (!inside) {
-                    asm volatile("");                                // a branch, not 64 selections at every step
+            }
+            float top = kNone;
 #pragma unroll
-                    for (int t = 0; t < 8; ++t)
+            for (int t = 0; t < NC; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[rt][t][i] = rule[rt].mask(x[rt][t][i], behind - 4 * t - i);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+            const float next = fmaxf(m, rule.log2_of(pair_max(top))), base = next == kNone ? 0.0f : next;
+            if (__any(next > m)) {
+                const float by = exp2_(m - base);
+                l *= by;
+#pragma unroll
+                for (int j = 0; j < DT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[j][i] *= by;
+                m = next;
+            }
+            each<NC>([&](auto t_c) {
+                constexpr int t = decltype(t_c)::value;
+                v8b pr[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float e = exp2_(rule.above(x[t][i], base));
+                    l += e;
+                    pr[i / 8][i % 8] = (__bf16)e;
                 }
 #pragma unroll
-                for (int t = 0; t < 8; ++t)
+                for (int q = 0; q < 2; ++q) {
+                    if (2 * t + q + 1 < 2 * NC) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][t][i]);
-                const float next = fmaxf(m[rt], rule[rt].log2_of(column_max(top))), base = next == kNone ? 0.0f : next;
-                if (__any(next > m[rt])) {
-                    const float by = exp2_(m[rt] - base);
-                    l[rt] *= by;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][j][i] *= by;
-                    m[rt] = next;
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float e = exp2_(rule[rt].above(x[rt][2 * q + i / 4][i % 4], base));
-                        l[rt] += e;
-                        pr[rt][q][i] = (__bf16)e;
+                        for (int j = 0; j < DT; ++j) v[1 - q][j] = value_tile(((t + q) * DT + j) * 2 + 1 - q);
                     }
-            }
-            auto values = [&](int j, v8b (&v)[4]) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const v8b*>(from + W::kK + j * 4096 + q * 1024 + lane * 16u);
-            };
-            v8b v[2][4];
-            values(0, v[0]);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                if (j + 1 < NJ) values(j + 1, v[(j + 1) & 1]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) o[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j & 1][q], pr[rt][q], o[rt][j], 0, 0, 0);
-            }
+                    for (int j = 0; j < DT; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[q][j], pr[q], o[j], 0, 0, 0);
+                }
+            });
         };
 
         __syncthreads();                                             // of the row block before
         if (step0 < step1) {
             load(step0);
-            store(s_x);
-            bool there = raw.v_there, all = raw.all;
+            store(s_x, step0);
+            uint32_t present = there;
             for (int step = step0; step < step1; ++step) {
-                const uint8_t* from = s_x + (W::kBuffers == 2 ? ((step - step0) & 1) * W::kStep : 0u);
+                const uint8_t* from = s_x + ((step - step0) & 1) * W::kStep;
                 __syncthreads();
                 load(step + 1);                                      // (beyond the last: anything)
-                work(from, step, there, all);
-                if (W::kBuffers == 1) __syncthreads();
-                there = raw.v_there;
-                all = raw.all;
-                store(s_x + (W::kBuffers == 2 ? ((step + 1 - step0) & 1) * W::kStep : 0u));
+                work(from, step, present);
+                present = there;
+                store(s_x + ((step + 1 - step0) & 1) * W::kStep, step + 1);
             }
         }
 
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int row = wave_row + rt * 16 + (int)c;
-            const float sum = column_sum(l[rt]);
-            if (row >= rows) continue;
+        const float sum = pair_sum(l);
+        if (row < rows) {
             const int64_t t = s.first + row / group;
-            const int h = kv_head * group + row % group;
+            // rows 8 a + 4 h + i of a tile: elements of head_dim
             if (r.parts == 1) {
                 const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-                uint16_t* dst = a.out + t * a.out_stride + (int64_t)h * a.out_head_stride + 4u * g;
+                uint16_t* dst = a.out + t * a.out_stride + (int64_t)head * a.out_head_stride + 4u * h;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    typedef __bf16 v4b __attribute__((ext_vector_type(4)));
-                    v4b y;
+                for (int j = 0; j < DT; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[rt][j][i] * inv);
-                    *reinterpret_cast<v4b*>(dst + 16 * j) = y;
-                }
-                if (a.lse && g == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (m[rt] + log2f(sum)) / kLog2e : kNone;
+                    for (int k = 0; k < 4; ++k) {
+                        typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+                        v4b y;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[j][4 * k + i] * inv);
+                        *reinterpret_cast<v4b*>(dst + 32 * j + 8 * k) = y;
+                    }
+                if (a.lse && h == 0) a.lse[t * a.heads + head] = sum > 0.0f ? (m + log2f(sum)) / kLog2e : kNone;
             } else {
-                const int64_t slot = (t * a.heads + h) * a.splits + part;
+                const int64_t slot = (t * a.heads + head) * a.splits + part;
+                float* dst = a.partial + slot * D + 4u * h;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    *reinterpret_cast<v4f*>(a.partial + slot * D + 16 * j + 4u * g) = o[rt][j];
-                if (g == 0) {
+                for (int j = 0; j < DT; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<v4f*>(dst + 32 * j + 8 * k) = v4f{o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
+                if (h == 0) {
                     float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
-                    ml[0] = m[rt];
+                    ml[0] = m;
                     ml[1] = sum;
                 }
             }
@@ -811,7 +846,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
 
 struct Split {
     int rows, blocks;            // query rows of a workgroup, workgroups along them
-    int splits, steps;           // workgroups along the keys, steps of 128 keys of each
+    int splits, steps;           // workgroups along the keys, steps (of 128 keys; with 128 rows, of 64) of each
 };
 Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
     const int64_t table = batch.table_width * cache.page_tokens;
@@ -821,7 +856,7 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     const int64_t rows = !wide ? 16 : cache.head_dim <= 128 ? 256 : 128;
     int64_t blocks = (new_rows + rows - 1) / rows;
     if (blocks > 65535) blocks = 65535;
-    const int64_t unit = wide ? 4 : kWaves, steps = (most + 127) / 128;              // steps that a workgroup has at least
+    const int64_t unit = rows == 128 ? 8 : 4, steps = rows == 128 ? (most + 63) / 64 : (most + 127) / 128;      // (a workgroup has 512 keys at least)
     const int64_t rounds = (steps + unit - 1) / unit, groups = batch.batch * cache.kv_heads * blocks;
     int64_t want = ((wide ? 1 : 4) * (int64_t)device_cu_count() + (wide ? 0 : groups - 1)) / groups;
     if (want > rounds) want = rounds;
