@@ -214,15 +214,16 @@ struct Scores {
     __device__ __forceinline__ Scores(const AttentionArgs& a)
         : factor(fabsf(a.scale) * kLog2e), cap(a.softcap * kLog2e), twice(a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f), slope(0.0f),
           reach(a.window > 0 ? (uint32_t)a.window - 1u : 0x7fffffffu) {}
-    __device__ __forceinline__ float bend(float x, int behind) const {
+    // `lean`: the bias of a key from which this one is `on` positions on
+    __device__ __forceinline__ float bend(float x, float lean, int on) const {
         if constexpr (EXTRA) {
-            x *= factor;
             // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
-            if (cap > 0.0f) x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(exp2_(x * twice) + 1.0f);
-            x -= slope * (float)behind;
+            if (cap > 0.0f) x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(exp2_(x * factor * twice) + 1.0f) + fmaf(slope, (float)on, lean);
+            else x = fmaf(x, factor, fmaf(slope, (float)on, lean));
         }
         return x;
     }
+    __device__ __forceinline__ float lean(int behind) const { return EXTRA ? -slope * (float)behind : 0.0f; }
     // keys after the query are a large number of positions behind it
     __device__ __forceinline__ float mask(float x, int behind) const { return (uint32_t)behind <= reach ? x : kNone; }
     __device__ __forceinline__ float log2_of(float x) const { return EXTRA ? x : x * factor; }      // of the largest score
@@ -350,11 +351,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             // ---- softmax
             float top = kNone;
             const int behind = av >= 0 ? pos - 32 * (chunk0 + (int)g) : kNever;
+            const float lean = rule.lean(behind);
 #pragma unroll
             for (int t = 0; t < 8; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[t][i] = rule.mask(rule.bend(x[t][i], behind - 4 * t - i), behind - 4 * t - i);
+                    x[t][i] = rule.mask(rule.bend(x[t][i], lean, 4 * t + i), behind - 4 * t - i);
                     top = fmaxf(top, x[t][i]);
                 }
             const float base = raise(top);
@@ -416,7 +418,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int in = 8 * (int)g + i, behind = in < left ? pos - 32 * r.whole - in : kNever;
-                    x[i] = rule.mask(rule.bend(x[i], behind), behind);
+                    x[i] = rule.mask(rule.bend(x[i], rule.lean(behind), 0), behind);
                     top = fmaxf(top, x[i]);
                 }
                 const float base = raise(top);
@@ -710,10 +712,11 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
             for (int j = 0; j < DT; ++j) v[0][j] = value_tile(2 * j);
             const int behind = pos - 32 * chunk0 - 16 * (int)h;      // positions that token 16 h of the first chunk is behind the query
             if constexpr (EXTRA) {
+                const float lean = rule.lean(behind);
 #pragma unroll
                 for (int t = 0; t < NC; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[t][i] = rule.bend(x[t][i], behind - 32 * t - i);
+                    for (int i = 0; i < 16; ++i) x[t][i] = rule.bend(x[t][i], lean, 32 * t + i);
             }
             if (!inside) {
                 asm volatile("");                                    // a branch, not 64 selections at every step
@@ -858,7 +861,8 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     if (blocks > 65535) blocks = 65535;
     const int64_t unit = rows == 128 ? 8 : 4, steps = rows == 128 ? (most + 63) / 64 : (most + 127) / 128;      // (a workgroup has 512 keys at least)
     const int64_t rounds = (steps + unit - 1) / unit, groups = batch.batch * cache.kv_heads * blocks;
-    int64_t want = ((wide ? 1 : 4) * (int64_t)device_cu_count() + (wide ? 0 : groups - 1)) / groups;
+    const int64_t cus = device_cu_count();
+    int64_t want = wide ? (4 * groups < 3 * cus ? (3 * cus / 2 + groups - 1) / groups : 1) : (4 * cus + groups - 1) / groups;
     if (want > rounds) want = rounds;
     if (want > 256) want = 256;
     if (want < 1) want = 1;
