@@ -231,15 +231,39 @@ struct Scores {
 };
 constexpr int kNever = -0x40000000;      // positions behind: a key that is not there
 
+// BYTES from `from` (wave-uniform) to LDS at `to`, lane by lane 16 bytes, by loads that no register receives (loads_of(BYTES) of
+// them: what waits for them counts them).  An instruction's offset counts for both addresses.
+constexpr int loads_of(uint32_t bytes) { return (int)((bytes + 1023) / 1024); }
+template <uint32_t BYTES>
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, uint32_t to, uint32_t lane) {
+    each<loads_of(BYTES)>([&](auto n_c) {
+        constexpr uint32_t at = decltype(n_c)::value * 1024u, whole = at / 4096u * 4096u;
+        const uint32_t offset = lane * 16u + whole, lds = to + whole;
+        const uint8_t* const base = from;
+        if (at + 1024u <= BYTES || lane * 16u < BYTES - at)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(lds), "v"(offset), "s"(base), "n"(at - whole) : "m0", "memory");
+    });
+}
+// until at most N vector memory operations are under way (those begin and end in order)
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// until LDS has answered: what it was read for may be overwritten
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
-// add up in LDS.
+// add up in LDS.  A step's cells come to LDS whole, by loads that bypass the registers: the next step's keys are asked for as soon as
+// this one's are multiplied, its values as soon as these are, so that a wave has 9 KiB (head_dim 128) or more under way all the time.
 template <int D, bool EXTRA>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionArgs a) {
     using C = Cell<D>;
     constexpr int KT = C::KT, NJ = C::NJ;
     constexpr uint32_t kPitch = D + 4;
     __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
-    __shared__ __attribute__((aligned(16))) float s_o[kWaves * 16 * kPitch];
+    // a wave's step as it lies in memory: keys of four chunks, then their values; at the end the waves' sums
+    constexpr uint32_t kStage = 4 * (C::kKeys + C::kValues), kSums = 16 * kPitch * 4;
+    static_assert(kStage >= kSums, "");
+    __shared__ __attribute__((aligned(16))) uint8_t s_stage[kWaves * kStage];
+    float* const s_o = reinterpret_cast<float*>(s_stage);
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
@@ -314,15 +338,34 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         };
         auto block_of = [&](int kt) { return kt * 4 + min(g, (uint32_t)(C::blocks(kt) - 1)); };
 
-        int pages = step0 + wave < step1 ? four_pages(p, b, r.first + 4 * (step0 + wave), r.whole) : 0;
+        constexpr int kKeyLoads = 4 * loads_of(C::kKeys), kValueLoads = 4 * loads_of(C::kValues);
+        uint8_t* const stage = s_stage + wave * kStage;
+        const uint32_t stage_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)stage;
+        auto ask = [&](const Four& at, auto values_c) {
+            constexpr bool kVal = decltype(values_c)::value;
+            constexpr uint32_t kBytes = kVal ? C::kValues : C::kKeys;
+            auto one = [&](int64_t cell_at, uint32_t k) {             // (absent ones: the pool's first, so that every step has as many loads)
+                load_to_lds<kBytes>(p.pages + (cell_at < 0 ? (int64_t)0 : cell_at) + (kVal ? C::kKeys : 0u), stage_at + (kVal ? 4 * C::kKeys : 0u) + k * kBytes, lane);
+            };
+            one(at.c0, 0), one(at.c1, 1), one(at.c2, 2), one(at.c3, 3);
+        };
+        Four next = {-1, -1, -1, -1};
+        FourPages pages = {};
+        if (step0 + wave < step1) {
+            const int chunk0 = r.first + 4 * (step0 + wave);
+            next = four_cells<D>(p, kv_head, chunk0, r.whole, four_pages_uniform(p, b, chunk0, r.whole));
+            pages = four_pages_uniform(p, b, chunk0 + 4 * kWaves, r.whole);
+            ask(next, std::false_type{});
+            ask(next, std::true_type{});
+        }
         for (int step = step0 + wave; step < step1; step += kWaves) {
             const int chunk0 = r.first + 4 * step;
-            // the step's cells; absent keys are masked, their codes are read anywhere and their values taken as zeros
-            const Four at = four_cells<D>(p, kv_head, chunk0, r.whole, pages);
-            pages = four_pages(p, b, chunk0 + 4 * kWaves, r.whole);
-            if (at.none()) continue;
-            const int64_t ak = at.pick(c >> 2), av = at.pick(g);
-            const uint8_t *kc = p.pages + max(ak, (int64_t)0), *vc = p.pages + max(av, (int64_t)0);
+            const bool more = step + kWaves < step1;
+            // absent keys are masked, their values finite
+            const Four at = next;
+            const bool here = at.there(g);
+            const uint8_t *kc = stage + (c >> 2) * C::kKeys, *vc = stage + 4 * C::kKeys + g * C::kValues - C::kVCodes;
+            wait_loads<kValueLoads>();                               // the keys are there
 
             // ---- scores of 128 keys
             float x[8][4];
@@ -348,9 +391,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                 });
             }
 
+            wait_reads();
+            if (more) {
+                next = four_cells<D>(p, kv_head, chunk0 + 4 * kWaves, r.whole, pages);
+                pages = four_pages_uniform(p, b, chunk0 + 8 * kWaves, r.whole);
+                ask(next, std::false_type{});
+            }
+
             // ---- softmax
             float top = kNone;
-            const int behind = av >= 0 ? pos - 32 * (chunk0 + (int)g) : kNever;
+            const int behind = here ? pos - 32 * (chunk0 + (int)g) : kNever;
             const float lean = rule.lean(behind);
 #pragma unroll
             for (int t = 0; t < 8; ++t)
@@ -372,12 +422,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             }
 
             // ---- values
+            if (more) wait_loads<kKeyLoads>();
+            else wait_loads<0>();
             const uint32_t shift = 4u * (c & 1u);
 #pragma unroll
             for (int w = 0; w < (NJ + 3) / 4; ++w) {
                 uint32_t scales = *reinterpret_cast<const uint32_t*>(vc + C::kVExps + c * C::VE + 4 * w);
                 const uint32_t ids = *reinterpret_cast<const uint32_t*>(vc + C::kVIds + (c >> 1) * C::VE + 4 * w) >> shift;
-                if (av < 0) scales = 0x7f7f7f7fu;                   // finite (the probabilities are zero)
+                if (!here) scales = 0x7f7f7f7fu;                    // finite (the probabilities are zero)
 #pragma unroll
                 for (int jj = 0; jj < 4 && 4 * w + jj < NJ; ++jj) {
                     const int j = 4 * w + jj;
@@ -392,6 +444,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                     }
                 }
             }
+            wait_reads();
+            if (more) ask(next, std::true_type{});
         }
 
         // ---- the incomplete chunk: 32 keys, row 4 g + i of tile t (0, 1) is token 8 g + 4 t + i
@@ -448,6 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 
         // ---- the four waves together
         l = column_sum(l);
+        __syncthreads();                                             // the stages are read
         if (lane < 16) {
             s_m[wave][c] = m;
             s_l[wave][c] = l;

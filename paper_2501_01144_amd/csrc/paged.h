@@ -24,8 +24,9 @@ struct Cell {
     static constexpr int NJ = D / 16;                    // 16-row tiles of V^T
     static constexpr int VE = (NJ + 3) / 4 * 4;          // bytes of a row of V exps
     static constexpr int NP = 2 * KT;                    // dialect bytes of a key
-    static constexpr uint32_t kVCodes = 16 * D, kKExps = 32 * D, kKIds = kKExps + 32 * NB, kVExps = kKIds + 32 * NP,
-                              kVIds = kVExps + 16 * VE, kEnd = kVIds + 8 * VE, kBytes = (kEnd + 63) / 64 * 64;
+    // all of a cell's keys, then all of its values: each is loaded to LDS as it lies
+    static constexpr uint32_t kKExps = 16 * D, kKIds = kKExps + 32 * NB, kKeys = kKIds + 32 * NP, kVCodes = kKeys, kVExps = kVCodes + 16 * D,
+                              kVIds = kVExps + 16 * VE, kValues = kVIds + 8 * VE - kVCodes, kBytes = (kKeys + kValues + 63) / 64 * 64;
     // blocks of instruction kt
     static constexpr int blocks(int kt) { return NB - 4 * kt < 4 ? NB - 4 * kt : 4; }
     // place (in units of 8 bytes) of elements 16 u .. 16 u + 15 of a key
@@ -91,28 +92,32 @@ __device__ __forceinline__ uint8_t* cell(const PagedArgs& p, int b, int head, in
 }
 
 // The cells of four consecutive chunks, of those below `limit` (which the length says are there).  The numbers of their pages are
-// loaded by lanes 0 .. 3 a step ahead (`pages`), so that the addresses need not wait for the table.
+// loaded a step ahead, so that the addresses need not wait for the table: by lanes 0 .. 3, or as scalars.
 __device__ __forceinline__ int four_pages(const PagedArgs& p, int b, int chunk0, int limit) {
     const int chunk = min(chunk0 + (int)(threadIdx.x & 3u), limit - 1);
     return p.table[(int64_t)b * p.width + place_in_table(p, max(chunk, 0))];
 }
 struct Four {
     int64_t c0, c1, c2, c3;
-    __device__ __forceinline__ int64_t pick(uint32_t k) const {
-        const int64_t lo = k & 1u ? c1 : c0, hi = k & 1u ? c3 : c2;
-        return k & 2u ? hi : lo;
-    }
-    __device__ __forceinline__ bool none() const { return (c0 & c1 & c2 & c3) < 0; }
-    __device__ __forceinline__ bool all() const { return (c0 | c1 | c2 | c3) >= 0; }
+    __device__ __forceinline__ bool there(uint32_t k) const { return (k & 2u ? (k & 1u ? c3 : c2) : (k & 1u ? c1 : c0)) >= 0; }
 };
+// The same with the pages' numbers in scalar registers, for addresses that are wave-uniform.
+struct FourPages { int n0, n1, n2, n3; };
+__device__ __forceinline__ FourPages four_pages_uniform(const PagedArgs& p, int b, int chunk0, int limit) {
+    // (constant memory for the time of the kernel: scalar loads, which wait for nothing that goes to vector registers or LDS)
+    typedef const __attribute__((address_space(4))) int32_t* Table;
+    const Table row = (Table)(uintptr_t)(p.table + (int64_t)b * p.width);
+    auto one = [&](int k) { return row[place_in_table(p, max(min(chunk0 + k, limit - 1), 0))]; };
+    return FourPages{one(0), one(1), one(2), one(3)};
+}
 template <int D>
-__device__ __forceinline__ Four four_cells(const PagedArgs& p, int head, int chunk0, int limit, int pages) {
-    auto one = [&](int k) {
+__device__ __forceinline__ Four four_cells(const PagedArgs& p, int head, int chunk0, int limit, const FourPages& pages) {
+    auto one = [&](int k, int page) {
         const int chunk = chunk0 + k;
-        const int64_t to = cell_offset<D>(p, head, chunk, place_in_table(p, chunk), __builtin_amdgcn_readlane(pages, k));
+        const int64_t to = cell_offset<D>(p, head, chunk, place_in_table(p, chunk), page);
         return chunk < limit ? to : (int64_t)-1;
     };
-    return Four{one(0), one(1), one(2), one(3)};
+    return Four{one(0, pages.n0), one(1, pages.n1), one(2, pages.n2), one(3, pages.n3)};
 }
 
 // bf16 [head_dim, 32] of a slot
