@@ -426,12 +426,12 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  * with k^, v^ what the cache stands for.  Query head h reads KV head h / (heads / kv_heads).
  *   q, out   device, bf16 [tokens, heads, head_dim], token and head strides in elements (multiples of 8), 16-byte aligned
  *   slopes   device, f32 [heads], or NULL;  lse  device, f32 [tokens, heads], or NULL
- *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads) bytes, 16-byte aligned (0 where no context
+ *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads, window) bytes, 16-byte aligned (0 where no context
  *            is split)
  * Scores, softmax and sums are in fp32.  The matrix instructions take keys and values as they are, q as the sum of two FP8 numbers (its
  * 8 bits) and a probability as the sum of two bf16 numbers.
  */
-size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads);
+size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
 int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
                          float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -524,11 +524,11 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
 
 static bool grouped(const dfp4_cache& cache, int64_t heads) { return heads > 0 && heads <= (1 << 16) && heads % cache.kv_heads == 0; }
 
-size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads) {
-    if (cell_bytes(cache.head_dim) == 0 || cache.kv_heads < 1 || cache.page_tokens < 32 || batch.batch < 1 || batch.tokens < 1 || batch.table_width < 0 ||
+size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window) {
+    if (cell_bytes(cache.head_dim) == 0 || cache.kv_heads < 1 || cache.page_tokens < 32 || batch.batch < 1 || batch.tokens < 1 || batch.table_width < 0 || window < 0 ||
         !grouped(cache, heads))
         return 0;
-    return paged_attention_workspace_bytes(cache, batch, heads);
+    return paged_attention_workspace_bytes(cache, batch, heads, window);
 }
 
 int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
@@ -540,7 +540,7 @@ int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride,
     if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
     if ((rc = check_rows(q, q_stride, q_head_stride)) != DFP4_OK || (rc = check_rows(out, out_stride, out_head_stride)) != DFP4_OK) return rc;
     if (!aligned(slopes, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return DFP4_ERR_ALIGN;
-    const size_t need = paged_attention_workspace_bytes(cache, batch, heads);
+    const size_t need = paged_attention_workspace_bytes(cache, batch, heads, window);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DFP4_ERR_WORKSPACE;
     const AttentionArgs a{paged_args(cache, batch), static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, slopes,
                           static_cast<float*>(workspace), q_stride, q_head_stride, out_stride, out_head_stride, scale, softcap, (int)heads,

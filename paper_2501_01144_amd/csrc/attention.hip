@@ -229,6 +229,7 @@ struct Scores {
     __device__ __forceinline__ float log2_of(float x) const { return EXTRA ? x : x * factor; }      // of the largest score
     __device__ __forceinline__ float above(float x, float base) const { return EXTRA ? x - base : fmaf(x, factor, -base); }
 };
+constexpr int kMaxParts = 256;       // the joining kernel has a thread for each
 constexpr int kNever = -0x40000000;      // positions behind: a key that is not there
 
 // BYTES from `from` (wave-uniform) to LDS at `to`, lane by lane 16 bytes, by loads that no register receives (loads_of(BYTES) of
@@ -259,8 +260,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
     constexpr int KT = C::KT, NJ = C::NJ;
     constexpr uint32_t kPitch = D + 4;
     __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
-    // a wave's step as it lies in memory: keys of four chunks, then their values; at the end the waves' sums
-    constexpr uint32_t kStage = 4 * (C::kKeys + C::kValues), kSums = 16 * kPitch * 4;
+    // a wave's step as it lies in memory: keys of four chunks, then their values; at the end the waves' sums.  Wide heads have one
+    // place for both in turn, so that two workgroups fit on a compute unit: one's loads run beside the other's arithmetic.
+    constexpr bool kShared = D > 128;
+    constexpr uint32_t kValuesAt = kShared ? 0u : 4 * C::kKeys, kStage = 4 * (kShared ? (C::kKeys > C::kValues ? C::kKeys : C::kValues) : C::kKeys + C::kValues),
+                       kSums = 16 * kPitch * 4;
     static_assert(kStage >= kSums, "");
     __shared__ __attribute__((aligned(16))) uint8_t s_stage[kWaves * kStage];
     float* const s_o = reinterpret_cast<float*>(s_stage);
@@ -345,7 +349,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             constexpr bool kVal = decltype(values_c)::value;
             constexpr uint32_t kBytes = kVal ? C::kValues : C::kKeys;
             auto one = [&](int64_t cell_at, uint32_t k) {             // (absent ones: the pool's first, so that every step has as many loads)
-                load_to_lds<kBytes>(p.pages + (cell_at < 0 ? (int64_t)0 : cell_at) + (kVal ? C::kKeys : 0u), stage_at + (kVal ? 4 * C::kKeys : 0u) + k * kBytes, lane);
+                load_to_lds<kBytes>(p.pages + (cell_at < 0 ? (int64_t)0 : cell_at) + (kVal ? C::kKeys : 0u), stage_at + (kVal ? kValuesAt : 0u) + k * kBytes, lane);
             };
             one(at.c0, 0), one(at.c1, 1), one(at.c2, 2), one(at.c3, 3);
         };
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             next = four_cells<D>(p, kv_head, chunk0, r.whole, four_pages_uniform(p, b, chunk0, r.whole));
             pages = four_pages_uniform(p, b, chunk0 + 4 * kWaves, r.whole);
             ask(next, std::false_type{});
-            ask(next, std::true_type{});
+            if (!kShared) ask(next, std::true_type{});
         }
         for (int step = step0 + wave; step < step1; step += kWaves) {
             const int chunk0 = r.first + 4 * step;
@@ -364,8 +368,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             // absent keys are masked, their values finite
             const Four at = next;
             const bool here = at.there(g);
-            const uint8_t *kc = stage + (c >> 2) * C::kKeys, *vc = stage + 4 * C::kKeys + g * C::kValues - C::kVCodes;
-            wait_loads<kValueLoads>();                               // the keys are there
+            const uint8_t *kc = stage + (c >> 2) * C::kKeys, *vc = stage + kValuesAt + g * C::kValues - C::kVCodes;
+            wait_loads<kShared ? 0 : kValueLoads>();                               // the keys are there
 
             // ---- scores of 128 keys
             float x[8][4];
@@ -392,10 +396,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             }
 
             wait_reads();
+            if (kShared) ask(at, std::true_type{});
             if (more) {
                 next = four_cells<D>(p, kv_head, chunk0 + 4 * kWaves, r.whole, pages);
                 pages = four_pages_uniform(p, b, chunk0 + 8 * kWaves, r.whole);
-                ask(next, std::false_type{});
+                if (!kShared) ask(next, std::false_type{});
             }
 
             // ---- softmax
@@ -422,7 +427,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             }
 
             // ---- values
-            if (more) wait_loads<kKeyLoads>();
+            if (more && !kShared) wait_loads<kKeyLoads>();
             else wait_loads<0>();
             const uint32_t shift = 4u * (c & 1u);
 #pragma unroll
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                 }
             }
             wait_reads();
-            if (more) ask(next, std::true_type{});
+            if (more) ask(next, std::integral_constant<bool, !kShared>{});
         }
 
         // ---- the incomplete chunk: 32 keys, row 4 g + i of tile t (0, 1) is token 8 g + 4 t + i
@@ -869,9 +874,10 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
     }
 }
 
-// Adds up the parts of a query row: one wave a row, D / 64 elements a lane.  Parts in their order: the same sum every time.
+// Adds up the parts of a query row.  Parts in their order: the same sum every time.  Few parts: one wave a row, D / 64 elements a lane.
+constexpr int kFewParts = 8;
 template <int D>
-__global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(kThreads) void paged_attention_join_few_kernel(AttentionArgs a) {
     const PagedArgs& p = a.paged;
     const uint32_t lane = threadIdx.x & 63u;
     const int b = (int)blockIdx.x, group = a.heads / p.kv_heads;
@@ -886,6 +892,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
         float top = kNone, sum = 0.0f;
         for (int k = 0; k < parts; ++k) top = fmaxf(top, ml[2 * k]);
         float o[D / 64 + (D % 64 != 0)] = {};
+#pragma unroll 2
         for (int k = 0; k < parts; ++k) {
             const float by = ml[2 * k] == kNone ? 0.0f : exp2_(ml[2 * k] - top);
             sum += by * ml[2 * k + 1];
@@ -901,39 +908,111 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
         if (a.lse && lane == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
     }
 }
+// Many parts: one workgroup a row.  D / 4 threads take all of its elements of every (256 * 4 / D)-th part, so that
+// 256 parts are read in a few round trips (one wave, part after part: 60 us of 97 for one token over 131072).  The order in which
+// parts are added depends on their number alone: the same sum every time.
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(AttentionArgs a) {
+    constexpr uint32_t kLanes = D / 4, kGroups = kThreads / kLanes;
+    __shared__ float s_w[kMaxParts], s_red[kWaves], s_l[kWaves];
+    __shared__ __attribute__((aligned(16))) float s_o[kGroups * D];
+    const PagedArgs& p = a.paged;
+    const uint32_t tid = threadIdx.x;
+    const int b = (int)blockIdx.x, group = a.heads / p.kv_heads;
+    const Sequence s = sequence(p, b);
+    for (int64_t row = blockIdx.y; row < (int64_t)s.n * a.heads; row += gridDim.y) {
+        const int64_t t = s.first + row / a.heads;
+        const int h = (int)(row % a.heads), in_group = (int)(row / a.heads) * group + h % group;
+        const int parts = key_range(a, s, group, in_group / a.rows * a.rows).parts;
+        if (parts == 1) continue;                       // written by the only part
+        const int64_t slot = (t * a.heads + h) * a.splits;
+        const float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
+        // weights of the parts (at most one a thread)
+        float mine = kNone, size = 0.0f;
+        if ((int)tid < parts) {
+            mine = ml[2 * tid];
+            size = ml[2 * tid + 1];
+        }
+        float top = mine;
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+        if ((tid & 63u) == 0) s_red[tid >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+        const float by = mine == kNone ? 0.0f : exp2_(mine - top);
+        s_w[tid] = by;
+        float sum = by * size;
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+        if ((tid & 63u) == 0) s_l[tid >> 6] = sum;
+        __syncthreads();
+        sum = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+        const uint32_t d = tid % kLanes, first = tid / kLanes;
+        float4 o = make_float4(0, 0, 0, 0);
+        if (first < kGroups) {
+#pragma unroll 4
+            for (int k = (int)first; k < parts; k += (int)kGroups) {
+                const float4 v = *reinterpret_cast<const float4*>(a.partial + (slot + k) * D + 4u * d);
+                const float w = s_w[k];
+                o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
+            }
+            *reinterpret_cast<float4*>(&s_o[first * D + 4u * d]) = o;
+        }
+        __syncthreads();
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        if (tid < (uint32_t)D) {
+            float v = 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < kGroups; ++k) v += s_o[k * D + tid];
+            reinterpret_cast<__bf16*>(a.out)[t * a.out_stride + (int64_t)h * a.out_head_stride + tid] = (__bf16)(v * inv);
+        }
+        if (a.lse && tid == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
+        __syncthreads();
+    }
+}
 
 struct Split {
     int rows, blocks;            // query rows of a workgroup, workgroups along them
     int splits, steps;           // workgroups along the keys, steps (of 128 keys; with 128 rows, of 64) of each
 };
-Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
-    const int64_t table = batch.table_width * cache.page_tokens;
-    const int64_t most = batch.max_length > 0 && batch.max_length < table ? batch.max_length : table;
-    const int64_t new_rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * (heads / cache.kv_heads);
+// How many parts the keys are split in, from what the host knows.  A workgroup costs what a round of 512 keys costs, or two, before its
+// first; `at_once` of them run at a time.  Of the numbers of parts that fill the chip once, twice, three or four times the one whose
+// (times) x (rounds + that) is least.
+Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
+    const int64_t new_tokens = batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens;
+    int64_t most = batch.table_width * cache.page_tokens;
+    if (batch.max_length > 0 && batch.max_length < most) most = batch.max_length;
+    const int64_t new_rows = new_tokens * (heads / cache.kv_heads);
     const bool wide = new_rows > 16;
     const int64_t rows = !wide ? 16 : cache.head_dim <= 128 ? 256 : 128;
     int64_t blocks = (new_rows + rows - 1) / rows;
     if (blocks > 65535) blocks = 65535;
-    const int64_t unit = rows == 128 ? 8 : 4, steps = rows == 128 ? (most + 63) / 64 : (most + 127) / 128;      // (a workgroup has 512 keys at least)
-    const int64_t rounds = (steps + unit - 1) / unit, groups = batch.batch * cache.kv_heads * blocks;
-    const int64_t cus = device_cu_count();
-    int64_t want = wide ? (4 * groups < 3 * cus ? (3 * cus / 2 + groups - 1) / groups : 1) : (4 * cus + groups - 1) / groups;
-    if (want > rounds) want = rounds;
-    if (want > 256) want = 256;
-    if (want < 1) want = 1;
-    const int64_t per = rounds > 0 ? (rounds + want - 1) / want : 1;
-    return Split{(int)rows, (int)blocks, (int)(rounds > 0 ? (rounds + per - 1) / per : 1), (int)(per * unit)};
+    const int64_t seen = (rows + heads / cache.kv_heads - 1) / (heads / cache.kv_heads) + window + 31;      // by a block of rows, with a window
+    if (window > 0 && seen < most) most = seen;
+    const int64_t rounds = most > 0 ? (most + 511) / 512 : 1, unit = rows == 128 ? 8 : 4, groups = batch.batch * cache.kv_heads * blocks;
+    const int64_t at_once = (int64_t)device_cu_count() * (wide ? 1 : 2), before = wide ? 1 : 2;
+    int64_t best = 1, cost = ((groups + at_once - 1) / at_once) * (before + rounds);
+    for (int64_t times = 1; times <= 4; ++times) {
+        int64_t want = times * at_once / groups;
+        if (want > rounds) want = rounds;
+        if (want > kMaxParts) want = kMaxParts;
+        if (want < 2) continue;
+        const int64_t c = ((groups * want + at_once - 1) / at_once) * (before + (rounds + want - 1) / want);
+        if (c < cost) best = want, cost = c;
+    }
+    const int64_t per = (rounds + best - 1) / best;
+    return Split{(int)rows, (int)blocks, (int)((rounds + per - 1) / per), (int)(per * unit)};
 }
 
 }  // namespace
 
-size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads) {
-    const Split sp = choose_split(cache, batch, heads);
+size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
+    const Split sp = choose_split(cache, batch, heads, window);
     return sp.splits > 1 ? (size_t)(batch.tokens * heads * sp.splits) * (size_t)(cache.head_dim + 2) * 4u : 0;
 }
 
 int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream) {
-    const Split sp = choose_split(cache, batch, a.heads);
+    const Split sp = choose_split(cache, batch, a.heads, a.window);
     a.splits = sp.splits;
     a.split_steps = sp.steps;
     a.rows = sp.rows;
@@ -950,9 +1029,10 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
         }
         if (sp.splits > 1) {
             const int64_t rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * a.heads;
-            const int64_t blocks = (rows + kWaves - 1) / kWaves;
-            hipLaunchKernelGGL((paged_attention_join_kernel<kD>), dim3((uint32_t)batch.batch, (uint32_t)(blocks < 65535 ? blocks : 65535)),
-                               dim3(kThreads), 0, stream, a);
+            const int64_t blocks = sp.splits <= kFewParts ? (rows + kWaves - 1) / kWaves : rows;
+            const dim3 join((uint32_t)batch.batch, (uint32_t)(blocks < 65535 ? blocks : 65535));
+            if (sp.splits <= kFewParts) hipLaunchKernelGGL((paged_attention_join_few_kernel<kD>), join, dim3(kThreads), 0, stream, a);
+            else hipLaunchKernelGGL((paged_attention_join_kernel<kD>), join, dim3(kThreads), 0, stream, a);
         }
     });
     return check_launch();

@@ -142,7 +142,7 @@ struct AttentionArgs {
     int heads, window, splits, split_steps;
     int rows;                        // query rows of a workgroup
 };
-size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads);
+size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window);
 int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream);
 
 struct NormRopeArgs {

@@ -140,7 +140,7 @@ def load():
     lib.dfp4_paged_write.restype = ci
     lib.dfp4_paged_read.argtypes = [_CCache, _CBatch, vp, vp, ci, vp]
     lib.dfp4_paged_read.restype = ci
-    lib.dfp4_paged_attention_workspace_bytes.argtypes = [_CCache, _CBatch, i64]
+    lib.dfp4_paged_attention_workspace_bytes.argtypes = [_CCache, _CBatch, i64, i64]
     lib.dfp4_paged_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.dfp4_paged_attention.argtypes = [vp, i64, i64, i64, _CCache, _CBatch, cf, cf, i64, vp, vp, i64, i64, vp, vp, ctypes.c_size_t, vp]
     lib.dfp4_paged_attention.restype = ci
@@ -608,7 +608,7 @@ def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=N
     assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_cuda and slopes.is_contiguous() and slopes.numel() == heads)
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
     c, b = cache.c(), batch.c(tokens)
-    need = int(load().dfp4_paged_attention_workspace_bytes(c, b, heads))
+    need = int(load().dfp4_paged_attention_workspace_bytes(c, b, heads, window))
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, c, b, head_dim ** -0.5 if scale is None else scale, softcap, window,

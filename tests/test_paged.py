@@ -55,9 +55,9 @@ def test_calls_refuse_bad_arguments():
     assert (attend(q=0), attend(out=0), attend(q=20), attend(qs=12), attend(oh=2), attend(slopes=2), attend(lse=1), attend(ws=8)) == (-1, -1) + (-3,) * 6
     # a long context is split between workgroups, and that takes a workspace
     long = _batch(table_width=1 << 12)
-    need = lib.dfp4_paged_attention_workspace_bytes(c, long, 4)
+    need = lib.dfp4_paged_attention_workspace_bytes(c, long, 4, 0)
     assert need > 0 and attend(b=long, ws=0, n=0) == -5 and attend(b=long, n=need - 1) == -5
-    assert lib.dfp4_paged_attention_workspace_bytes(c, _batch(table_width=4), 4) == 0
+    assert lib.dfp4_paged_attention_workspace_bytes(c, _batch(table_width=4), 4, 0) == 0
     # nothing to do
     assert attend(b=_batch(tokens=0)) == 0 and attend(b=_batch(batch=0)) == 0
     assert lib.dfp4_paged_write(vp(0), 0, 0, vp(0), 0, 0, c, _batch(tokens=0), vp(0)) == 0
@@ -353,10 +353,10 @@ def test_attention_rows_without_keys(dim):
 def test_attention_of_long_contexts_is_split(dim, new):
     s = Sequences([9000, 2049, 515], dim, 1, 64, seed=new).fill()
     c, b = s.cache.c(), s.batch([new] * 3, max_new=new).c(3 * new)
-    assert dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4) > 0
+    assert dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4, 0) > 0
     q, got, lse = _attend(s, [new] * 3, 4, max_new=new)
     # the same bits again, and with a workspace of the caller's that holds anything
-    ws = torch.full((dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4),), 0xff, dtype=torch.uint8, device="cuda")
+    ws = torch.full((dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4, 0),), 0xff, dtype=torch.uint8, device="cuda")
     again, lse2 = dfp4.paged_attention(q.cuda(), s.cache, s.batch([new] * 3, max_new=new), return_lse=True, workspace=ws)
     assert torch.equal(again.view(torch.int16), got.view(torch.int16)) and torch.equal(lse2, lse)
     with pytest.raises(dfp4.Dfp4Error, match="workspace"):
