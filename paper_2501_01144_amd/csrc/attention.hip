@@ -367,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             const bool more = step + kWaves < step1;
             // absent keys are masked, their values finite
             const Four at = next;
-            const bool here = at.there(g);
+            const bool here = (at.there() >> g) & 1u;
             const uint8_t *kc = stage + (c >> 2) * C::kKeys, *vc = stage + kValuesAt + g * C::kValues - C::kVCodes;
             wait_loads<kShared ? 0 : kValueLoads>();                               // the keys are there
 

@@ -99,7 +99,9 @@ __device__ __forceinline__ int four_pages(const PagedArgs& p, int b, int chunk0,
 }
 struct Four {
     int64_t c0, c1, c2, c3;
-    __device__ __forceinline__ bool there(uint32_t k) const { return (k & 2u ? (k & 1u ? c3 : c2) : (k & 1u ? c1 : c0)) >= 0; }
+    __device__ __forceinline__ uint32_t there() const {             // bit k: chunk k
+        return (c0 >= 0 ? 1u : 0u) | (c1 >= 0 ? 2u : 0u) | (c2 >= 0 ? 4u : 0u) | (c3 >= 0 ? 8u : 0u);
+    }
 };
 // The same with the pages' numbers in scalar registers, for addresses that are wave-uniform.
 struct FourPages { int n0, n1, n2, n3; };
