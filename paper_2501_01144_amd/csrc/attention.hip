@@ -286,6 +286,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         const int step0 = part * a.split_steps, step1 = part == r.parts - 1 ? r.steps : min(r.steps, step0 + a.split_steps);
         const int row = row0 + (int)c;
         const bool row_ok = row < s.n * group;
+        // positions of the first and the last row
+        const int p_min = s.length - s.n + row0 / group, p_max = s.length - s.n + (min(row0 + 16, s.n * group) - 1) / group;
         const int head = kv_head * group + (row_ok ? row % group : 0);
         const int64_t token = s.first + (row_ok ? row / group : 0);
         const int pos = s.length - s.n + (row_ok ? row / group : 0);
@@ -404,16 +406,26 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             }
 
             // ---- softmax
-            float top = kNone;
             const int behind = here ? pos - 32 * (chunk0 + (int)g) : kNever;
-            const float lean = rule.lean(behind);
+            if constexpr (EXTRA) {
+                const float lean = rule.lean(behind);
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][i] = rule.bend(x[t][i], lean, 4 * t + i);
+            }
+            if (!(at.there() == 15u && 32 * chunk0 + 127 <= p_min && p_max - 32 * chunk0 <= (int)rule.reach)) {
+                asm volatile("");                                    // a branch, not 32 selections at every step
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][i] = rule.mask(x[t][i], behind - 4 * t - i);
+            }
+            float top = kNone;
 #pragma unroll
             for (int t = 0; t < 8; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[t][i] = rule.mask(rule.bend(x[t][i], lean, 4 * t + i), behind - 4 * t - i);
-                    top = fmaxf(top, x[t][i]);
-                }
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, x[t][i]);
             const float base = raise(top);
             v8b p_hi[4], p_lo[4];
 #pragma unroll

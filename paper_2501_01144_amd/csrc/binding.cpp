@@ -21,7 +21,8 @@ PyObject* g_error = nullptr;          // Dfp4Error
     F(dfp4_gemm) F(mxfp4_gemm) F(dfp4_gemm_batched) F(dfp4_gemm_workspace_bytes) F(dfp4_gemm_prepared_bytes)                \
     F(dfp4_gemm_prepare) F(mxfp4_gemm_prepare) F(dfp4_gemm_prepared_workspace_bytes) F(dfp4_gemm_prepared)                  \
     F(mxfp4_gemm_prepared) F(dfp4_native_packed_bytes) F(dfp4_native_pack) F(mxfp4_native_pack)                             \
-    F(dfp4_gemm_native_packed) F(mxfp4_gemm_native_packed) F(dfp4_gemm_native_splitk_bytes) F(dfp4_strerror)
+    F(dfp4_gemm_native_packed) F(mxfp4_gemm_native_packed) F(dfp4_gemm_native_splitk_bytes) F(dfp4_strerror)         \
+    F(dfp4_paged_write) F(dfp4_paged_read) F(dfp4_paged_attention_workspace_bytes) F(dfp4_paged_attention) F(dfp4_norm_rope)
 #define DFP4_DECLARE(NAME) decltype(&::NAME) p_##NAME = nullptr;
 DFP4_FUNCTIONS(DFP4_DECLARE)
 #undef DFP4_DECLARE
@@ -231,6 +232,112 @@ PyObject* gemm_native_packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- serving operators.  Caches and batches come as the addresses of their C structures (kvcache.PagedCache, kvcache.PagedBatch keep
+// them as long as they live); the rows of this call go into the copy.
+
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Failure{};
+    return v;
+}
+template <class T>
+T structure(PyObject* o) {
+    const void* at = PyLong_AsVoidPtr(o);
+    if (!at) {
+        if (PyErr_Occurred()) throw Failure{};
+        fail(PyExc_ValueError, "a cache and a batch are expected");
+    }
+    return *static_cast<const T*>(at);
+}
+const at::Tensor& rows3(PyObject* o) {
+    const at::Tensor& x = tensor(o);
+    if (x.scalar_type() != at::kBFloat16 || x.dim() != 3 || !x.is_cuda() || (x.stride(2) != 1 && x.size(2) != 1))
+        fail(PyExc_AssertionError, "bf16 [tokens, heads, head_dim] on the device, contiguous along head_dim, is expected");
+    return x;
+}
+// a contiguous tensor of `n` numbers on the device, or None
+template <class T>
+const T* numbers(PyObject* o, at::ScalarType type, int64_t n, const char* what) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& x = tensor(o);
+    if (x.scalar_type() != type || !x.is_cuda() || !x.is_contiguous() || (n >= 0 && x.numel() != n)) fail(PyExc_AssertionError, what);
+    return reinterpret_cast<const T*>(data(x));
+}
+
+// paged_write(k, v, cache, batch)
+PyObject* paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 4, [&]() -> PyObject* {
+        const at::Tensor &k = rows3(a[0]), &v = rows3(a[1]);
+        const dfp4_cache cache = structure<dfp4_cache>(a[2]);
+        dfp4_batch batch = structure<dfp4_batch>(a[3]);
+        batch.tokens = k.size(0);
+        if (k.sizes() != v.sizes() || k.size(1) != cache.kv_heads || k.size(2) != cache.head_dim)
+            fail(PyExc_AssertionError, "k and v: [tokens, kv_heads, head_dim] of the cache");
+        enqueue("dfp4_paged_write", p_dfp4_paged_write, data(k), k.stride(0), k.stride(1), data(v), v.stride(0), v.stride(1), cache, batch, stream());
+        Py_RETURN_NONE;
+    });
+}
+
+// paged_read(cache, batch, tokens, bf16, a tensor on the cache's device) -> k, v
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 5, [&]() -> PyObject* {
+        const dfp4_cache cache = structure<dfp4_cache>(a[0]);
+        dfp4_batch batch = structure<dfp4_batch>(a[1]);
+        batch.tokens = number(a[2]);
+        const bool bf16 = a[3] == Py_True;
+        const at::Device dev = tensor(a[4]).device();
+        at::Tensor k = result({batch.tokens, cache.kv_heads, cache.head_dim}, bf16, dev), v = result({batch.tokens, cache.kv_heads, cache.head_dim}, bf16, dev);
+        enqueue("dfp4_paged_read", p_dfp4_paged_read, cache, batch, data(k), data(v), dtype(bf16), stream());
+        return Py_BuildValue("NN", THPVariable_Wrap(std::move(k)), THPVariable_Wrap(std::move(v)));
+    });
+}
+
+// paged_attention(q, cache, batch, scale, softcap, window, slopes or None, return_lse) -> out or (out, lse)
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 8, [&]() -> PyObject* {
+        const at::Tensor& q = rows3(a[0]);
+        const dfp4_cache cache = structure<dfp4_cache>(a[1]);
+        dfp4_batch batch = structure<dfp4_batch>(a[2]);
+        batch.tokens = q.size(0);
+        const int64_t heads = q.size(1), window = number(a[5]);
+        if (q.size(2) != cache.head_dim) fail(PyExc_AssertionError, "q: head_dim of the cache");
+        const float* slopes = numbers<float>(a[6], at::kFloat, heads, "slopes: contiguous f32 [heads] on the device");
+        const bool with_lse = a[7] == Py_True;
+        const at::Device dev = q.device();
+        at::Tensor out = result({batch.tokens, heads, cache.head_dim}, true, dev), lse, ws;
+        if (with_lse) lse = result({batch.tokens, heads}, false, dev);
+        const size_t need = p_dfp4_paged_attention_workspace_bytes(cache, batch, heads, window);
+        if (need > 0) ws = bytes((int64_t)need, dev);
+        enqueue("dfp4_paged_attention", p_dfp4_paged_attention, data(q), q.stride(0), q.stride(1), heads, cache, batch, (float)real(a[3]), (float)real(a[4]),
+                window, slopes, data(out), out.stride(0), out.stride(1), with_lse ? reinterpret_cast<float*>(data(lse)) : nullptr,
+                need > 0 ? data(ws) : nullptr, need, stream());
+        if (!with_lse) return THPVariable_Wrap(std::move(out));
+        return Py_BuildValue("NN", THPVariable_Wrap(std::move(out)), THPVariable_Wrap(std::move(lse)));
+    });
+}
+
+// norm_rope(q, k or None, positions, inv_freq, q_weight or None, k_weight or None, eps, interleaved) -> q, k
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 8, [&]() -> PyObject* {
+        const at::Tensor& q = rows3(a[0]);
+        const bool both = a[1] != Py_None;
+        const at::Tensor& k = both ? rows3(a[1]) : q;
+        const int64_t tokens = q.size(0), dim = q.size(2);
+        if (k.size(0) != tokens || k.size(2) != dim) fail(PyExc_AssertionError, "q and k: the same tokens and head_dim");
+        const int32_t* positions = numbers<int32_t>(a[2], at::kInt, tokens, "positions: contiguous int32 [tokens] on the device");
+        const float* freq = numbers<float>(a[3], at::kFloat, -1, "inv_freq: contiguous f32 [rotary / 2] on the device");
+        const float *qw = numbers<float>(a[4], at::kFloat, dim, "q_weight: contiguous f32 [head_dim] on the device"),
+                    *kw = numbers<float>(a[5], at::kFloat, dim, "k_weight: contiguous f32 [head_dim] on the device");
+        at::Tensor q_out = result(q.sizes(), true, q.device()), k_out;
+        if (both) k_out = result(k.sizes(), true, q.device());
+        enqueue("dfp4_norm_rope", p_dfp4_norm_rope, data(q), q.stride(0), q.stride(1), q.size(1), both ? data(k) : nullptr, k.stride(0), k.stride(1),
+                both ? k.size(1) : 0, tokens, dim, qw, kw, (float)real(a[6]), positions, freq, a[3] == Py_None ? 0 : 2 * tensor(a[3]).numel(),
+                a[7] == Py_True ? 1 : 0, data(q_out), both ? data(k_out) : nullptr, stream());
+        PyObject* second = both ? THPVariable_Wrap(std::move(k_out)) : Py_NewRef(Py_None);
+        return Py_BuildValue("NN", THPVariable_Wrap(std::move(q_out)), second);
+    });
+}
+
 // bind(path of libdfp4.so, exception class)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 2, [&]() -> PyObject* {
@@ -251,7 +358,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define DFP4_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DFP4_METHOD(bind), DFP4_METHOD(quantize), DFP4_METHOD(dequantize), DFP4_METHOD(gemm), DFP4_METHOD(gemm_batched),
                          DFP4_METHOD(gemm_prepare), DFP4_METHOD(gemm_prepared), DFP4_METHOD(quantize_native), DFP4_METHOD(native_pack),
-                         DFP4_METHOD(gemm_native_packed), {nullptr, nullptr, 0, nullptr}};
+                         DFP4_METHOD(gemm_native_packed), DFP4_METHOD(paged_write), DFP4_METHOD(paged_read), DFP4_METHOD(paged_attention),
+                         DFP4_METHOD(norm_rope), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -569,51 +569,40 @@ def gemm_batched(a, w, batch, M, N, dtype=torch.float32, out=None, workspace=Non
     return out
 
 
-def _rows3(x, what):
-    assert x.dtype == torch.bfloat16 and x.dim() == 3 and x.is_cuda and (x.stride(2) == 1 or x.shape[2] == 1), \
-        f"{what}: bf16 [tokens, heads, head_dim] on the device, contiguous along head_dim"
-    return x
-
-
 def paged_write(k, v, cache, batch):
     """dfp4_paged_write: quantize the keys and values of the batch's new tokens, bf16 [tokens, kv_heads, head_dim] each (token and
     head strides allowed), into a kvcache.PagedCache; `batch` is a kvcache.PagedBatch."""
-    _rows3(k, "k"), _rows3(v, "v")
-    assert k.shape == v.shape and tuple(k.shape[1:]) == (cache.kv_heads, cache.head_dim)
-    _check(load().dfp4_paged_write(_ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), cache.c(), batch.c(k.shape[0]),
-                                   _stream()), "dfp4_paged_write")
+    _calls().paged_write(k, v, cache.at, batch.at)
 
 
 def paged_read(cache, batch, tokens=None, dtype=torch.bfloat16):
     """dfp4_paged_read: the values that the cache stands for, k and v [tokens, kv_heads, head_dim], of the batch's tokens (`tokens`
     of them, by default as many as batch.tokens says)."""
-    tokens = batch.tokens if tokens is None else tokens
-    shape = (tokens, cache.kv_heads, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.pages.device) for _ in range(2))
-    _check(load().dfp4_paged_read(cache.c(), batch.c(tokens), _ptr(k), _ptr(v), BF16 if _is_bf16(dtype) else F32, _stream()), "dfp4_paged_read")
-    return k, v
+    return _calls().paged_read(cache.at, batch.at, batch.tokens if tokens is None else tokens, _is_bf16(dtype), cache.pages)
 
 
 def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=None, return_lse=False, out=None, workspace=None):
     """dfp4_paged_attention: attention of the batch's new tokens, q bf16 [tokens, heads, head_dim], over the cached tokens of
     their sequences (these included: paged_write comes first).  scale: 1 / sqrt(head_dim) unless given; softcap, window: 0 is
     none; slopes: f32 [heads].  Returns out, bf16 like q, or (out, lse), lse f32 [tokens, heads]."""
-    _rows3(q, "q")
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    if out is None and workspace is None:
+        return _calls().paged_attention(q, cache.at, batch.at, scale, softcap, window, slopes, bool(return_lse))
     tokens, heads, head_dim = q.shape
-    assert head_dim == cache.head_dim
     if out is None:
         out = torch.empty((tokens, heads, head_dim), dtype=torch.bfloat16, device=q.device)
-    _rows3(out, "out")
-    assert out.shape == q.shape
+    for x in (q, out):
+        assert x.dtype == torch.bfloat16 and x.is_cuda and x.stride(2) == 1 and x.shape == q.shape and head_dim == cache.head_dim
     assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_cuda and slopes.is_contiguous() and slopes.numel() == heads)
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
-    c, b = cache.c(), batch.c(tokens)
-    need = int(load().dfp4_paged_attention_workspace_bytes(c, b, heads, window))
+    b = batch.c(tokens)
+    need = int(load().dfp4_paged_attention_workspace_bytes(cache.c, b, heads, window))
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, c, b, head_dim ** -0.5 if scale is None else scale, softcap, window,
-                                       _ptr(slopes), _ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(workspace),
-                                       workspace.numel() if workspace is not None else 0, _stream()), "dfp4_paged_attention")
+    _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, cache.c, b, scale, softcap, window, _ptr(slopes), _ptr(out), out.stride(0),
+                                       out.stride(1), _ptr(lse), _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream()),
+           "dfp4_paged_attention")
     return (out, lse) if return_lse else out
 
 
@@ -621,20 +610,17 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6,
     """dfp4_norm_rope: norms of queries and keys per head (where a weight, f32 [head_dim], is given) and their rotation by
     position, in one pass.  q bf16 [tokens, heads, head_dim], k the same with its heads (or None); positions int32 [tokens];
     inv_freq f32 [rotary / 2].  Returns q and k (out=(q, k): into these, which may be the inputs where those are contiguous)."""
-    _rows3(q, "q")
+    if out is None:
+        return _calls().norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, bool(interleaved))
     tokens, heads, head_dim = q.shape
-    if k is not None:
-        _rows3(k, "k")
-        assert k.shape[0] == tokens and k.shape[2] == head_dim
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_cuda and w.is_contiguous() and w.numel() == head_dim)
     assert positions.dtype == torch.int32 and positions.is_cuda and positions.is_contiguous() and positions.numel() == tokens
     assert inv_freq.dtype == torch.float32 and inv_freq.is_cuda and inv_freq.is_contiguous()
-    if out is None:
-        out = tuple(None if x is None else torch.empty(x.shape, dtype=torch.bfloat16, device=q.device) for x in (q, k))
     q_out, k_out = out
     for x, y in ((q, q_out), (k, k_out)):
-        assert (x is None and y is None) or (y.dtype == torch.bfloat16 and y.is_cuda and y.is_contiguous() and y.shape == x.shape)
+        assert (x is None and y is None) or (x.dtype == y.dtype == torch.bfloat16 and x.is_cuda and y.is_cuda and x.stride(2) == 1 and y.is_contiguous() and
+                                             y.shape == x.shape and (x.shape[0], x.shape[2]) == (tokens, head_dim))
     _check(load().dfp4_norm_rope(_ptr(q), q.stride(0), q.stride(1), heads, _ptr(k), k.stride(0) if k is not None else 0,
                                  k.stride(1) if k is not None else 0, k.shape[1] if k is not None else 0, tokens, head_dim, _ptr(q_weight),
                                  _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel(), 1 if interleaved else 0,

@@ -16,6 +16,8 @@ equals the product over the tokens present.
 PagedCache and PagedBatch are the same idea for many sequences, keys and values and all KV heads of a layer: the device memory of a
 paged cache and the arrays that describe a batch, for dfp4.paged_write, dfp4.paged_read and dfp4.paged_attention.
 """
+import ctypes
+
 import torch
 
 from . import dfp4
@@ -78,13 +80,9 @@ class PagedCache:
         self.n_pages, self.page_tokens, self.kv_heads, self.head_dim, self.n_slots = n_pages, page_tokens, kv_heads, head_dim, n_slots
         self.pages = torch.zeros((n_pages, kv_heads, page_tokens // BLOCK, cell), dtype=torch.uint8, device=device)
         self.residual = torch.zeros((n_slots, kv_heads, head_dim, BLOCK), dtype=torch.bfloat16, device=device)
-        self._c = None
-
-    def c(self):
-        if self._c is None:
-            self._c = dfp4._CCache(self.pages.data_ptr() if self.n_pages else 0, self.residual.data_ptr() if self.n_slots else 0, self.n_pages,
-                                   self.page_tokens, self.n_slots, self.kv_heads, self.head_dim)
-        return self._c
+        self.c = dfp4._CCache(self.pages.data_ptr() if n_pages else 0, self.residual.data_ptr() if n_slots else 0, n_pages, page_tokens,
+                              n_slots, kv_heads, head_dim)
+        self.at = ctypes.addressof(self.c)       # for the native module
 
 
 class PagedBatch:
@@ -99,8 +97,10 @@ class PagedBatch:
         assert cu_tokens.numel() == n + 1 and slots.numel() == n and table.dim() == 2 and table.shape[0] == n
         for t in (cu_tokens, lengths, table, slots):
             assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
-        self.cu_tokens, self.lengths, self.table, self.slots = cu_tokens, lengths, table, slots
+        self.cu_tokens, self.lengths, self.table, self.slots = cu_tokens, lengths, table, slots     # (their contents may change, they not)
         self.max_new, self.max_length, self._tokens = max_new, max_length, tokens
+        self._c = dfp4._CBatch(cu_tokens.data_ptr(), lengths.data_ptr(), table.data_ptr(), slots.data_ptr(), n, table.shape[1], 0, max_new, max_length)
+        self.at = ctypes.addressof(self._c)      # for the native module, which fills in the rows
 
     @property
     def tokens(self):
@@ -109,5 +109,6 @@ class PagedBatch:
         return self._tokens
 
     def c(self, tokens):
-        return dfp4._CBatch(self.cu_tokens.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr(), self.slots.data_ptr(), self.lengths.numel(),
-                            self.table.shape[1], tokens, self.max_new, self.max_length)
+        b = dfp4._CBatch.from_buffer_copy(self._c)
+        b.tokens = tokens
+        return b

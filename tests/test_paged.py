@@ -352,7 +352,7 @@ def test_attention_rows_without_keys(dim):
 @pytest.mark.parametrize("new", [1, 5, 70])
 def test_attention_of_long_contexts_is_split(dim, new):
     s = Sequences([9000, 2049, 515], dim, 1, 64, seed=new).fill()
-    c, b = s.cache.c(), s.batch([new] * 3, max_new=new).c(3 * new)
+    c, b = s.cache.c, s.batch([new] * 3, max_new=new).c(3 * new)
     assert dfp4.load().dfp4_paged_attention_workspace_bytes(c, b, 4, 0) > 0
     q, got, lse = _attend(s, [new] * 3, 4, max_new=new)
     # the same bits again, and with a workspace of the caller's that holds anything
