@@ -214,16 +214,26 @@ struct Scores {
     __device__ __forceinline__ Scores(const AttentionArgs& a)
         : factor(fabsf(a.scale) * kLog2e), cap(a.softcap * kLog2e), twice(a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f), slope(0.0f),
           reach(a.window > 0 ? (uint32_t)a.window - 1u : 0x7fffffffu) {}
-    // `lean`: the bias of a key from which this one is `on` positions on
-    __device__ __forceinline__ float bend(float x, float lean, int on) const {
+    // N scores whose keys are 0, 1, .. positions on from one `behind` behind the query
+    template <int N>
+    __device__ __forceinline__ void bend(float* x, int behind) const {
         if constexpr (EXTRA) {
-            // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
-            if (cap > 0.0f) x = cap - 2.0f * cap * __builtin_amdgcn_rcpf(exp2_(x * factor * twice) + 1.0f) + fmaf(slope, (float)on, lean);
-            else x = fmaf(x, factor, fmaf(slope, (float)on, lean));
+            if (cap > 0.0f) {
+                asm volatile("");                                   // one branch
+                // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(exp2_(x[i] * (factor * twice)) + 1.0f), cap);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] *= factor;
+            }
+            if (slope != 0.0f) {
+                const float lean = -slope * (float)behind;
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] += fmaf(slope, (float)i, lean);
+            }
         }
-        return x;
     }
-    __device__ __forceinline__ float lean(int behind) const { return EXTRA ? -slope * (float)behind : 0.0f; }
     // keys after the query are a large number of positions behind it
     __device__ __forceinline__ float mask(float x, int behind) const { return (uint32_t)behind <= reach ? x : kNone; }
     __device__ __forceinline__ float log2_of(float x) const { return EXTRA ? x : x * factor; }      // of the largest score
@@ -407,13 +417,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 
             // ---- softmax
             const int behind = here ? pos - 32 * (chunk0 + (int)g) : kNever;
-            if constexpr (EXTRA) {
-                const float lean = rule.lean(behind);
-#pragma unroll
-                for (int t = 0; t < 8; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[t][i] = rule.bend(x[t][i], lean, 4 * t + i);
-            }
+            rule.template bend<32>(&x[0][0], behind);
             if (!(at.there() == 15u && 32 * chunk0 + 127 <= p_min && p_max - 32 * chunk0 <= (int)rule.reach)) {
                 asm volatile("");                                    // a branch, not 32 selections at every step
 #pragma unroll
@@ -489,7 +493,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int in = 8 * (int)g + i, behind = in < left ? pos - 32 * r.whole - in : kNever;
-                    x[i] = rule.mask(rule.bend(x[i], rule.lean(behind), 0), behind);
+                    rule.template bend<1>(&x[i], behind);
+                    x[i] = rule.mask(x[i], behind);
                     top = fmaxf(top, x[i]);
                 }
                 const float base = raise(top);
@@ -784,11 +789,15 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
             for (int j = 0; j < DT; ++j) v[0][j] = value_tile(2 * j);
             const int behind = pos - 32 * chunk0 - 16 * (int)h;      // positions that token 16 h of the first chunk is behind the query
             if constexpr (EXTRA) {
-                const float lean = rule.lean(behind);
 #pragma unroll
-                for (int t = 0; t < NC; ++t)
+                for (int t = 0; t < NC; ++t) {
+                    float y[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[t][i] = rule.bend(x[t][i], lean, 32 * t + i);
+                    for (int i = 0; i < 16; ++i) y[i] = x[t][i];
+                    rule.template bend<16>(y, behind - 32 * t);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = y[i];
+                }
             }
             if (!inside) {
                 asm volatile("");                                    // a branch, not 64 selections at every step
