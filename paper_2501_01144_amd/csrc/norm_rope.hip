@@ -1,7 +1,12 @@
 // Norms of queries and keys per head and their rotation by position, in one pass (formulas in include/dfp4.h).
 //
-// A head is head_dim / 8 lanes of 8 elements (16 bytes), rounded up to a power of two for the sum of squares.  A workgroup takes
-// one token; its cosines and sines, alike for all heads, are computed once and kept in LDS.  Bound by memory: 4 bytes an element.
+// Bound by memory: 4 bytes an element.  A head is head_dim / 8 lanes of eight elements, rounded up to a power of two for the sum of
+// squares (within a row of 16 lanes by DPP).  A lane has both elements of its pairs: with pairs rotary / 2 apart 4 + 4 elements (8 bytes
+// a load, so that nothing moves between lanes), else eight in a row.  Its place in a head, and so its cosines and weights, are the same
+// for all heads: they are in registers.  A workgroup takes as many tokens as it has threads for their cosines and sines, which it
+// computes at once and hands over in LDS, and a share of their heads: all where there are many tokens, 16 where there are few.
+// 8192 tokens, 32 + 8 heads of 128 (168 MB): a first version (one token a workgroup, pairs exchanged by shuffles, cosines read
+// for every head) 96 us.
 #include "paged.h"
 
 namespace dfp4 {
@@ -10,76 +15,118 @@ namespace {
 
 constexpr int kThreads = 256;
 
+typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
-__device__ __forceinline__ uint32_t bf16_bits(float x) {             // round to nearest even; the inputs are finite
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+
+template <int CTRL>
+__device__ __forceinline__ float across(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// sum over LANES neighbouring lanes: neighbours 1 and 2 apart, then mirrored in 8 and in 16 lanes, then 16 apart
+template <uint32_t LANES>
+__device__ __forceinline__ float head_sum(float v) {
+    v += across<0xB1>(v);
+    v += across<0x4E>(v);
+    if constexpr (LANES >= 8) v += across<0x141>(v);
+    if constexpr (LANES >= 16) v += across<0x140>(v);
+    if constexpr (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        v = as_f(r[0]) + as_f(r[1]);
+    }
+    return v;
 }
 
+struct Launch {
+    NormRopeArgs a;
+    int tokens, passes;          // tokens of a workgroup; heads of a token: passes * kThreads / LANES
+};
+
 template <uint32_t LANES>                                            // of a head
-__global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRopeArgs a) {
-    __shared__ float s_cos[128], s_sin[128];
+__global__ __launch_bounds__(kThreads) void norm_rope_kernel(Launch p) {
+    const NormRopeArgs& a = p.a;
+    __shared__ __attribute__((aligned(16))) float s_cos[kThreads], s_sin[kThreads];      // [token][pair]
+    constexpr int kHeads = kThreads / (int)LANES;                    // at a time
     const uint32_t tid = threadIdx.x, sub = tid % LANES, half = (uint32_t)a.rotary / 2u;
-    const int t = (int)blockIdx.x;
-    for (uint32_t j = tid; j < half; j += kThreads) {
+    const int t0 = (int)blockIdx.x * p.tokens, tokens = min(p.tokens, a.tokens - t0);
+    if (tid < (uint32_t)tokens * half) {
         // the angle in turns, in 64 bits: a position of 2^20 and a frequency of 1 leave 32 of their bits to the fraction
-        const double turns = (double)a.positions[t] * (double)a.inv_freq[j] * 0.15915494309189533577;
-        const float frac = (float)(turns - rint(turns));
-        sincospif(2.0f * frac, &s_sin[j], &s_cos[j]);
+        const double turns = (double)a.positions[t0 + (int)(tid / half)] * (double)a.inv_freq[tid % half] * 0.15915494309189533577;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s_sin[tid], &s_cos[tid]);
+    }
+    // the lane's elements: d0 .. d0 + 3 and d1 .. d1 + 3
+    const bool in = sub * 8u < (uint32_t)a.head_dim, turn = a.interleaved ? sub * 8u < (uint32_t)a.rotary : sub * 4u < half;
+    const uint32_t d0 = !in ? 0u : !a.interleaved && turn ? sub * 4u : sub * 8u, d1 = !in ? 4u : !a.interleaved && turn ? d0 + half : d0 + 4u;
+    float wq[8], wk[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t d = (j < 4 ? d0 : d1 - 4u) + j;
+        wq[j] = a.q_weight ? a.q_weight[d] : 1.0f;
+        wk[j] = a.k_weight ? a.k_weight[d] : 1.0f;
     }
     __syncthreads();
-    const uint32_t d0 = sub * 8u;
-    const bool in = d0 < (uint32_t)a.head_dim;
-    const int heads = a.heads + a.kv_heads;
-    for (int h = (int)(tid / LANES); h < (heads + (int)(kThreads / LANES) - 1) / (int)(kThreads / LANES) * (int)(kThreads / LANES); h += (int)(kThreads / LANES)) {
-        const bool is_q = h < a.heads, on = in && h < heads;
-        const uint16_t* src = is_q ? a.q + (int64_t)t * a.q_stride + (int64_t)h * a.q_head_stride
-                                   : a.k + (int64_t)t * a.k_stride + (int64_t)(h - a.heads) * a.k_head_stride;
-        const float* w = is_q ? a.q_weight : a.k_weight;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (on) raw = *reinterpret_cast<const uint4*>(src + d0);
-        const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
-        float x[8];
+    const int heads = a.heads + a.kv_heads, first = (int)blockIdx.y * p.passes * kHeads + (int)(tid / LANES), end = min(heads, first + p.passes * kHeads);
+    const float per = 1.0f / (float)a.head_dim;
+    for (int n = 0; n < tokens; ++n) {
+        const int64_t t = t0 + n;
+        float c[4] = {1, 1, 1, 1}, s[4] = {0, 0, 0, 0};              // pair by pair (interleaved: elements 2 j, 2 j + 1)
+        if (turn) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = as_f((j & 1) ? u[j / 2] & 0xffff0000u : u[j / 2] << 16);
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
-#pragma unroll
-        for (uint32_t m = 1; m < LANES; m *= 2) sum += __shfl_xor(sum, (int)m);
-        if (w) {
-            const float r = 1.0f / sqrtf(sum / (float)a.head_dim + a.eps);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= r * (in ? w[d0 + j] : 0.0f);
-        }
-        float y[8];
-        if (a.interleaved) {
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const uint32_t p = (d0 + j) / 2u;
-                const bool turn = d0 + j < (uint32_t)a.rotary;
-                const float c = turn ? s_cos[p] : 1.0f, s = turn ? s_sin[p] : 0.0f;
-                y[j] = x[j] * c - x[j + 1] * s;
-                y[j + 1] = x[j + 1] * c + x[j] * s;
-            }
-        } else {
-            // the other element of a pair lies half / 8 lanes on or back (rotary is a multiple of 16)
-            const bool turn = d0 < (uint32_t)a.rotary, upper = d0 >= half;
-            const uint32_t lane = tid & 63u, other = turn ? (upper ? lane - half / 8u : lane + half / 8u) : lane;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float o = __shfl(x[j], (int)other);
-                const uint32_t p = turn ? d0 + j - (upper ? half : 0u) : 0u;
-                const float c = turn ? s_cos[p] : 1.0f, s = turn ? s_sin[p] : 0.0f;
-                y[j] = x[j] * c + (upper ? o * s : -o * s);
+            for (int j = 0; j < 4; ++j) {
+                c[j] = s_cos[n * half + sub * 4u + j];
+                s[j] = s_sin[n * half + sub * 4u + j];
             }
         }
-        if (on) {
-            uint32_t o[4];
+        auto source = [&](int h) {
+            return h < a.heads ? a.q + t * a.q_stride + (int64_t)h * a.q_head_stride : a.k + t * a.k_stride + (int64_t)(h - a.heads) * a.k_head_stride;
+        };
+        uint2 next[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+        auto load = [&](int h) {
+            if (in && h < end) {
+                next[0] = *reinterpret_cast<const uint2*>(source(h) + d0);
+                next[1] = *reinterpret_cast<const uint2*>(source(h) + d1);
+            }
+        };
+        load(first);
+        for (int i = 0; i < p.passes; ++i) {
+            const int h = first + i * kHeads;
+            const uint32_t u[4] = {next[0].x, next[0].y, next[1].x, next[1].y};
+            if (i + 1 < p.passes) load(h + kHeads);
+            float x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = bf16_bits(y[2 * j]) | (bf16_bits(y[2 * j + 1]) << 16);
-            uint16_t* dst = is_q ? a.q_out + ((int64_t)t * a.heads + h) * a.head_dim : a.k_out + ((int64_t)t * a.kv_heads + (h - a.heads)) * a.head_dim;
-            *reinterpret_cast<uint4*>(dst + d0) = make_uint4(o[0], o[1], o[2], o[3]);
+            for (int j = 0; j < 8; ++j) x[j] = as_f((j & 1) ? u[j / 2] & 0xffff0000u : u[j / 2] << 16);
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+            const bool is_q = h < a.heads;
+            if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
+                // (lanes of a head that are beyond head_dim hold zeros)
+                const float r = 1.0f / sqrtf(head_sum<LANES>(sum) * per + a.eps);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= r * (is_q ? wq[j] : wk[j]);
+            }
+            float y[8];
+            if (a.interleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    y[2 * j] = x[2 * j] * c[j] - x[2 * j + 1] * s[j];
+                    y[2 * j + 1] = x[2 * j + 1] * c[j] + x[2 * j] * s[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    y[j] = x[j] * c[j] - x[4 + j] * s[j];
+                    y[4 + j] = x[4 + j] * c[j] + x[j] * s[j];
+                }
+            }
+            if (in && h < end) {
+                uint16_t* dst = is_q ? a.q_out + (t * a.heads + h) * a.head_dim : a.k_out + (t * a.kv_heads + (h - a.heads)) * a.head_dim;
+                v4b o[2];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j / 4][j % 4] = (__bf16)y[j];
+                *reinterpret_cast<v4b*>(dst + d0) = o[0];
+                *reinterpret_cast<v4b*>(dst + d1) = o[1];
+            }
         }
     }
 }
@@ -87,11 +134,20 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRopeArgs a) {
 }  // namespace
 
 int launch_norm_rope(const NormRopeArgs& a, hipStream_t stream) {
-    const dim3 grid((uint32_t)a.tokens), block(kThreads);
-    if (a.head_dim <= 32) hipLaunchKernelGGL((norm_rope_kernel<4>), grid, block, 0, stream, a);
-    else if (a.head_dim <= 64) hipLaunchKernelGGL((norm_rope_kernel<8>), grid, block, 0, stream, a);
-    else if (a.head_dim <= 128) hipLaunchKernelGGL((norm_rope_kernel<16>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((norm_rope_kernel<32>), grid, block, 0, stream, a);
+    const int lanes = a.head_dim <= 32 ? 4 : a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : 32, at_once = kThreads / lanes;
+    const int rounds = (a.heads + a.kv_heads + at_once - 1) / at_once, fit = a.rotary > 0 ? kThreads / (a.rotary / 2) : 4;
+    const int cus = device_cu_count();
+    // as many tokens a workgroup as leave a few workgroups to a compute unit, then the heads split until there are enough
+    int tokens = a.tokens / (4 * cus);
+    tokens = tokens < 1 ? 1 : tokens < fit ? tokens : fit;
+    const int64_t groups = ((int64_t)a.tokens + tokens - 1) / tokens;
+    const int passes = groups >= 4 * cus ? rounds : 1;
+    const Launch p{a, tokens, passes};
+    const dim3 grid((uint32_t)groups, (uint32_t)((rounds + passes - 1) / passes)), block(kThreads);
+    if (lanes == 4) hipLaunchKernelGGL((norm_rope_kernel<4>), grid, block, 0, stream, p);
+    else if (lanes == 8) hipLaunchKernelGGL((norm_rope_kernel<8>), grid, block, 0, stream, p);
+    else if (lanes == 16) hipLaunchKernelGGL((norm_rope_kernel<16>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((norm_rope_kernel<32>), grid, block, 0, stream, p);
     return check_launch();
 }
 

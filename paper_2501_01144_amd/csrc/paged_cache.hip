@@ -72,9 +72,14 @@ __global__ __launch_bounds__(kThreads) void paged_write_kernel(WriteArgs a) {
             }
             if (old > 0) {
                 const uint16_t* r = s.slot >= 0 ? residual<D>(a.paged, s.slot, head) : nullptr;
-                for (uint32_t i = tid; i < (uint32_t)old * D; i += kThreads) {
-                    const uint32_t d = i / (uint32_t)old, t = i % (uint32_t)old;
-                    s_v[t * kPitch + d] = r ? r[d * 32u + t] : (uint16_t)0;
+                for (uint32_t i = tid; i < D * 4u; i += kThreads) {  // eight tokens of a d
+                    const uint32_t d = i >> 2, t = (i & 3u) * 8u;
+                    if ((int)t >= old) continue;
+                    const uint4 x = r ? *reinterpret_cast<const uint4*>(r + d * 32u + t) : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if ((int)t + j < old) s_v[(t + j) * kPitch + d] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
                 }
             }
         }
