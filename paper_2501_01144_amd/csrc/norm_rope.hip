@@ -67,6 +67,22 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Launch p) {
     __syncthreads();
     const int heads = a.heads + a.kv_heads, first = (int)blockIdx.y * p.passes * kHeads + (int)(tid / LANES), end = min(heads, first + p.passes * kHeads);
     const float per = 1.0f / (float)a.head_dim;
+    // two heads ahead, over all heads of all tokens
+    uint2 next[2][2] = {};
+    int load_n = 0, load_h = first;
+    auto load = [&](uint2 (&to)[2]) {
+        if (in && load_n < tokens && load_h < end) {
+            const int64_t t = t0 + load_n;
+            const uint16_t* from = load_h < a.heads ? a.q + t * a.q_stride + (int64_t)load_h * a.q_head_stride
+                                                    : a.k + t * a.k_stride + (int64_t)(load_h - a.heads) * a.k_head_stride;
+            to[0] = *reinterpret_cast<const uint2*>(from + d0);
+            to[1] = *reinterpret_cast<const uint2*>(from + d1);
+        }
+        load_h += kHeads;
+        if (load_h - first == p.passes * kHeads) load_h = first, ++load_n;
+    };
+    load(next[0]);
+    load(next[1]);
     for (int n = 0; n < tokens; ++n) {
         const int64_t t = t0 + n;
         float c[4] = {1, 1, 1, 1}, s[4] = {0, 0, 0, 0};              // pair by pair (interleaved: elements 2 j, 2 j + 1)
@@ -77,21 +93,12 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Launch p) {
                 s[j] = s_sin[n * half + sub * 4u + j];
             }
         }
-        auto source = [&](int h) {
-            return h < a.heads ? a.q + t * a.q_stride + (int64_t)h * a.q_head_stride : a.k + t * a.k_stride + (int64_t)(h - a.heads) * a.k_head_stride;
-        };
-        uint2 next[2] = {make_uint2(0, 0), make_uint2(0, 0)};
-        auto load = [&](int h) {
-            if (in && h < end) {
-                next[0] = *reinterpret_cast<const uint2*>(source(h) + d0);
-                next[1] = *reinterpret_cast<const uint2*>(source(h) + d1);
-            }
-        };
-        load(first);
         for (int i = 0; i < p.passes; ++i) {
             const int h = first + i * kHeads;
-            const uint32_t u[4] = {next[0].x, next[0].y, next[1].x, next[1].y};
-            if (i + 1 < p.passes) load(h + kHeads);
+            const uint32_t u[4] = {next[0][0].x, next[0][0].y, next[0][1].x, next[0][1].y};
+            next[0][0] = next[1][0];
+            next[0][1] = next[1][1];
+            load(next[1]);
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = as_f((j & 1) ? u[j / 2] & 0xffff0000u : u[j / 2] << 16);
@@ -101,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Launch p) {
             const bool is_q = h < a.heads;
             if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
                 // (lanes of a head that are beyond head_dim hold zeros)
-                const float r = 1.0f / sqrtf(head_sum<LANES>(sum) * per + a.eps);
+                const float r = __builtin_amdgcn_rsqf(head_sum<LANES>(sum) * per + a.eps);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= r * (is_q ? wq[j] : wk[j]);
             }
