@@ -487,7 +487,8 @@ static int check_paged(const dfp4_cache& c, const dfp4_batch& b) {
     if (b.batch < 0 || b.table_width < 0 || b.tokens < 0 || b.max_new < 0 || b.max_length < 0) return DFP4_ERR_SHAPE;
     const int64_t most = (int64_t)1 << 30;
     if (c.page_tokens > (1 << 20) || c.n_pages > most || c.n_slots > most || c.kv_heads > (1 << 16) || b.batch > most || b.tokens > most ||
-        b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most)
+        b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most ||
+        c.n_pages * c.kv_heads > ((int64_t)1 << 31) / (c.page_tokens / 32))
         return DFP4_ERR_SHAPE;
     if (b.batch == 0 || b.tokens == 0) return DFP4_OK;
     if ((c.n_pages > 0 && !c.pages) || (c.n_slots > 0 && !c.residual) || !b.cu_tokens || !b.lengths || !b.slots || (b.table_width > 0 && !b.table))

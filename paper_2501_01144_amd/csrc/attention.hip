@@ -680,12 +680,12 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
         int pages = step0 < step1 ? four_pages(p, b, r.first + NC * step0, r.end) : 0;
         auto load = [&](int step) {
             const int chunk0 = r.first + NC * step;
-            auto place = [&](int k) {                                // wave-uniform; 0 for a chunk that is not there
-                const int64_t at = cell_offset<D>(p, kv_head, chunk0 + k, place_in_table(p, chunk0 + k), __builtin_amdgcn_readlane(pages, k));
-                return p.pages + (at < 0 || chunk0 + k >= r.end ? (int64_t)0 : at);
-            };
-            const bool mine = chunk0 + (int)(lane & 3u) < r.end && pages >= 0 && pages < p.n_pages && (chunk0 + (int)(lane & 3u) < r.whole || s.slot >= 0);
-            there = (uint32_t)__ballot(mine) & ((1u << NC) - 1u);
+            // lanes 0 .. 3: whether the chunk is there, and its cell (the pool's first page for one that is not)
+            const int chunk = chunk0 + (int)(lane & 3u);
+            const bool held_page = (uint32_t)pages < (uint32_t)p.n_pages;
+            there = (uint32_t)__ballot(chunk < r.end && held_page && (chunk < r.whole || s.slot >= 0)) & ((1u << NC) - 1u);
+            const int number = (int)cell_number(p, kv_head, chunk, place_in_table(p, chunk), held_page ? pages : 0);
+            auto place = [&](int k) { return p.pages + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(number, k) * C::kBytes; };
 #pragma unroll
             for (int n = 0; n < KP; ++n) {
                 const int piece = min(wave + n * W::kWaves, NC * KS - 1), ks = piece % KS, block = min(2 * ks + (int)h, C::NB - 1);

@@ -76,10 +76,15 @@ __device__ __forceinline__ Sequence sequence(const PagedArgs& p, int b) {
 }
 
 // Where the cell of a chunk of 32 tokens lies in the pool, given its page's number in the table; -1 where that is none of the pool's.
+// (The pool has fewer than 2^31 cells.)
+__device__ __forceinline__ uint32_t cell_number(const PagedArgs& p, int head, int chunk, int in_table, int page) {
+    return ((uint32_t)page * (uint32_t)p.kv_heads + (uint32_t)head) * (uint32_t)p.page_chunks + (uint32_t)(chunk - in_table * p.page_chunks);
+}
 template <int D>
 __device__ __forceinline__ int64_t cell_offset(const PagedArgs& p, int head, int chunk, int in_table, int page) {
-    if (page < 0 || page >= p.n_pages) return -1;
-    return (((int64_t)page * p.kv_heads + head) * p.page_chunks + (chunk - in_table * p.page_chunks)) * Cell<D>::kBytes;
+    const bool there = (uint32_t)page < (uint32_t)p.n_pages;
+    const int64_t at = (int64_t)((uint64_t)cell_number(p, head, chunk, in_table, there ? page : 0) * Cell<D>::kBytes);
+    return there ? at : (int64_t)-1;
 }
 __device__ __forceinline__ int place_in_table(const PagedArgs& p, int chunk) { return (int)((uint64_t)chunk * p.per_page >> 40); }
 
