@@ -487,3 +487,15 @@ def test_norm_rope_in_place_and_zeros():
     q2, k2 = dfp4.norm_rope(x, y, pos, freq, w, w, out=(x, y))
     torch.cuda.synchronize()
     assert q2.data_ptr() == x.data_ptr() and torch.equal(q2.view(torch.int16), q.view(torch.int16)) and (k2 == 0).all()
+
+
+@pytest.mark.gpu
+def test_the_layer_of_the_example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    off, _ = example.run(prompts=(40, 31, 1), tokens=5)
+    assert off <= HALF
