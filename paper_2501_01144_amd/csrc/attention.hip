@@ -1010,7 +1010,10 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     if (blocks > 65535) blocks = 65535;
     const int64_t seen = (rows + heads / cache.kv_heads - 1) / (heads / cache.kv_heads) + window + 31;      // by a block of rows, with a window
     if (window > 0 && seen < most) most = seen;
-    const int64_t rounds = most > 0 ? (most + 511) / 512 : 1, unit = rows == 128 ? 8 : 4, groups = batch.batch * cache.kv_heads * blocks;
+    const int64_t rounds = most > 0 ? (most + 511) / 512 : 1, unit = rows == 128 ? 8 : 4;
+    // (sequences have fewer new tokens than the one with most: the rows of all of them, and a block begun for each, bound the blocks too)
+    const int64_t all = (batch.tokens * (heads / cache.kv_heads) + rows - 1) / rows + batch.batch;
+    const int64_t groups = cache.kv_heads * (all < batch.batch * blocks ? all : batch.batch * blocks);
     const int64_t at_once = (int64_t)device_cu_count() * (wide ? 1 : 2), before = wide ? 1 : 2;
     int64_t best = 1, cost = ((groups + at_once - 1) / at_once) * (before + rounds);
     for (int64_t times = 1; times <= 4; ++times) {
