@@ -895,38 +895,47 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
     }
 }
 
-// Adds up the parts of a query row.  Parts in their order: the same sum every time.  Few parts: one wave a row, D / 64 elements a lane.
+// Adds up the parts of a query row.  Parts in their order: the same sum every time.  Few parts: D / 4 threads a row, all of whose
+// parts are loaded at once (28000 rows of 64: a wave a row, part after part, 15 us, so 8).
 constexpr int kFewParts = 8;
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_attention_join_few_kernel(AttentionArgs a) {
+    constexpr uint32_t kLanes = D / 4, kRows = kThreads / kLanes;
     const PagedArgs& p = a.paged;
-    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t sub = threadIdx.x % kLanes;
     const int b = (int)blockIdx.x, group = a.heads / p.kv_heads;
     const Sequence s = sequence(p, b);
-    for (int64_t row = (int64_t)blockIdx.y * kWaves + (threadIdx.x >> 6); row < (int64_t)s.n * a.heads; row += (int64_t)gridDim.y * kWaves) {
+    if (threadIdx.x >= kLanes * kRows) return;
+    for (int row = (int)(blockIdx.y * kRows + threadIdx.x / kLanes); row < s.n * a.heads; row += (int)(gridDim.y * kRows)) {
         const int64_t t = s.first + row / a.heads;
-        const int h = (int)(row % a.heads), in_group = (int)(row / a.heads) * group + h % group;
+        const int h = row % a.heads, in_group = row / a.heads * group + h % group;
         const int parts = key_range(a, s, group, in_group / a.rows * a.rows).parts;
         if (parts == 1) continue;                       // written by the only part
         const int64_t slot = (t * a.heads + h) * a.splits;
         const float* ml = a.partial + (int64_t)p.tokens * a.heads * a.splits * D + slot * 2;
-        float top = kNone, sum = 0.0f;
-        for (int k = 0; k < parts; ++k) top = fmaxf(top, ml[2 * k]);
-        float o[D / 64 + (D % 64 != 0)] = {};
-#pragma unroll 2
-        for (int k = 0; k < parts; ++k) {
-            const float by = ml[2 * k] == kNone ? 0.0f : exp2_(ml[2 * k] - top);
-            sum += by * ml[2 * k + 1];
+        float2 w[kFewParts];
+        float4 v[kFewParts];
 #pragma unroll
-            for (int j = 0; 64 * j < D; ++j)
-                if (64 * j + (int)lane < D) o[j] += by * a.partial[(slot + k) * D + 64 * j + lane];
+        for (int k = 0; k < kFewParts; ++k) {
+            const int at = k < parts ? k : 0;
+            w[k] = *reinterpret_cast<const float2*>(ml + 2 * at);
+            v[k] = *reinterpret_cast<const float4*>(a.partial + (slot + at) * D + 4u * sub);
+        }
+        float top = kNone, sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kFewParts; ++k) top = fmaxf(top, w[k].x);
+        float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < kFewParts; ++k) {
+            const float by = k < parts && w[k].x != kNone ? exp2_(w[k].x - top) : 0.0f;
+            sum += by * w[k].y;
+            o.x += by * v[k].x; o.y += by * v[k].y; o.z += by * v[k].z; o.w += by * v[k].w;
         }
         const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-        for (int j = 0; 64 * j < D; ++j)
-            if (64 * j + (int)lane < D)
-                reinterpret_cast<__bf16*>(a.out)[t * a.out_stride + (int64_t)h * a.out_head_stride + 64 * j + lane] = (__bf16)(o[j] * inv);
-        if (a.lse && lane == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
+        typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+        const v4b y = {(__bf16)(o.x * inv), (__bf16)(o.y * inv), (__bf16)(o.z * inv), (__bf16)(o.w * inv)};
+        *reinterpret_cast<v4b*>(a.out + t * a.out_stride + (int64_t)h * a.out_head_stride + 4u * sub) = y;
+        if (a.lse && sub == 0) a.lse[t * a.heads + h] = sum > 0.0f ? (top + log2f(sum)) / kLog2e : kNone;
     }
 }
 // Many parts: one workgroup a row.  D / 4 threads take all of its elements of every (256 * 4 / D)-th part, so that
@@ -1053,7 +1062,7 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
         }
         if (sp.splits > 1) {
             const int64_t rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * a.heads;
-            const int64_t blocks = sp.splits <= kFewParts ? (rows + kWaves - 1) / kWaves : rows;
+            const int64_t blocks = sp.splits <= kFewParts ? (rows + 1024 / kD - 1) / (1024 / kD) : rows;
             const dim3 join((uint32_t)batch.batch, (uint32_t)(blocks < 65535 ? blocks : 65535));
             if (sp.splits <= kFewParts) hipLaunchKernelGGL((paged_attention_join_few_kernel<kD>), join, dim3(kThreads), 0, stream, a);
             else hipLaunchKernelGGL((paged_attention_join_kernel<kD>), join, dim3(kThreads), 0, stream, a);
