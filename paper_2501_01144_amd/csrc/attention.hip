@@ -148,7 +148,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // Which keys a block of query rows sees, and how they are split between workgroups: alike in the kernel that adds the parts up.
 struct Range {
     int first, end, whole;       // chunks of 32: [first, end), values quantized below `whole`
-    int steps, parts;            // of four chunks (16 rows: of whole ones) or two (128 rows); workgroups that have some
+    int steps, parts;            // of four chunks (16 rows: of whole ones); workgroups that have some
 };
 __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequence& s, int group, int row0) {
     Range r;
@@ -158,7 +158,7 @@ __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequenc
     r.first = t_begin / 32;
     r.end = t_end > t_begin && a.paged.n_pages > 0 ? (t_end + 31) / 32 : r.first;
     r.whole = min(r.end, s.length / 32);
-    r.steps = a.rows == 16 ? max(0, (r.whole - r.first + 3) / 4) : a.rows == 128 ? (r.end - r.first + 1) / 2 : (r.end - r.first + 3) / 4;
+    r.steps = (max(a.rows == 16 ? r.whole : r.end, r.first) - r.first + 3) / 4;
     r.parts = min(a.splits, max(1, (r.steps + a.split_steps - 1) / a.split_steps));
     return r;
 }
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Many query rows: a workgroup expands every step of 32 NC keys once into LDS, as the operands that all its waves read (keys in FP8,
+// Many query rows (head_dim up to 128): a workgroup expands every step of 128 keys once into LDS, as the operands that all its waves read (keys in FP8,
 // values in bf16), and each wave does both products for 32 rows, on 32 x 32 x 64 and 32 x 32 x 16: a query is a column again,
 // now of two lanes (h, c).  They hold rows 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
 // 16 h + 4 a + i of a chunk, so that a lane supplies the probabilities of the 16 tokens whose scores it has, eight to an instruction.
@@ -589,15 +589,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 struct Wide {
-    static constexpr int kWaves = D <= 128 ? 8 : 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;      // (D > 128: 512 registers a lane)
-    static constexpr int NC = D <= 128 ? 4 : 2;                      // chunks of a step
+    static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32 * kWaves;
+    static constexpr int NC = 4;                                     // chunks of a step
     static constexpr int KS = (D + 63) / 64, DT = D / 32;            // instructions that add over a key, tiles of V^T
     static constexpr int KP = (NC * KS + kWaves - 1) / kWaves, VP = (NC * DT + kWaves - 1) / kWaves;      // pieces that a wave expands
     static constexpr uint32_t kK = NC * KS * 2048, kV = NC * DT * 2048, kScales = KS * 256, kStep = kK + kV + kScales;
 };
 
 template <int D, bool EXTRA>
-__global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_attention_wide_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_kernel(AttentionArgs a) {
     using C = Cell<D>;
     using W = Wide<D>;
     constexpr int KS = W::KS, DT = W::DT, NC = W::NC, KP = W::KP, VP = W::VP;
@@ -756,7 +756,7 @@ __global__ __launch_bounds__(Wide<D>::kThreads, D <= 128 ? 2 : 1) void paged_att
         };
         auto work = [&](const uint8_t* from, int step, uint32_t present) {
             const int chunk0 = r.first + NC * step;
-            if (32 * chunk0 > p_max) return;                         // later than all of the wave's rows
+            if (wave_row >= rows || 32 * chunk0 > p_max) return;     // no rows, or all of them earlier
             const bool inside = present == (1u << NC) - 1u && 32 * (chunk0 + NC) - 1 <= p_min && chunk0 + NC <= r.whole &&
                                 (a.window <= 0 || 32 * chunk0 > p_max - a.window);
             // operands are read an instruction pair ahead
@@ -1003,7 +1003,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
 
 struct Split {
     int rows, blocks;            // query rows of a workgroup, workgroups along them
-    int splits, steps;           // workgroups along the keys, steps (of 128 keys; with 128 rows, of 64) of each
+    int splits, steps;           // workgroups along the keys, steps of 128 keys of each
 };
 // How many parts the keys are split in, from what the host knows.  A workgroup costs what a round of 512 keys costs, or two, before its
 // first; `at_once` of them run at a time.  Of the numbers of parts that fill the chip once, twice, three or four times the one whose
@@ -1013,13 +1013,19 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     int64_t most = batch.table_width * cache.page_tokens;
     if (batch.max_length > 0 && batch.max_length < most) most = batch.max_length;
     const int64_t new_rows = new_tokens * (heads / cache.kv_heads);
-    const bool wide = new_rows > 16;
-    const int64_t rows = !wide ? 16 : cache.head_dim <= 128 ? 256 : 128;
+    // In rounds of 512 keys of 16 rows.  The wide kernel expands keys once for 256 rows but wants a compute unit for itself: heads of
+    // 128 on 8 KV heads, us wide / 16 rows a workgroup: 64 rows of 16 sequences of 4000 tokens 56 / 53, 96 rows 60 / 93; 96 rows of
+    // 4 sequences (1536 rounds) 31 / 35; 512 rows of one sequence of 2000 (1024 rounds) 33 / 28, 2048 rows 43 / 56.  Heads above 128 leave
+    // it no registers (a version with half the waves took 729 us for 2048 rows of 4 sequences, heads of 256; 609 so).
+    const int64_t keys = window > 0 && window + new_tokens < most ? window + new_tokens : most;
+    const bool wide = cache.head_dim <= 128 && new_rows > 64 &&
+                      batch.batch * cache.kv_heads * ((new_rows + 15) / 16) * ((keys + 511) / 512) > 5 * (int64_t)device_cu_count();
+    const int64_t rows = wide ? 256 : 16;
     int64_t blocks = (new_rows + rows - 1) / rows;
     if (blocks > 65535) blocks = 65535;
     const int64_t seen = (rows + heads / cache.kv_heads - 1) / (heads / cache.kv_heads) + window + 31;      // by a block of rows, with a window
     if (window > 0 && seen < most) most = seen;
-    const int64_t rounds = most > 0 ? (most + 511) / 512 : 1, unit = rows == 128 ? 8 : 4;
+    const int64_t rounds = most > 0 ? (most + 511) / 512 : 1;
     // (sequences have fewer new tokens than the one with most: the rows of all of them, and a block begun for each, bound the blocks too)
     const int64_t all = (batch.tokens * (heads / cache.kv_heads) + rows - 1) / rows + batch.batch;
     const int64_t groups = cache.kv_heads * (all < batch.batch * blocks ? all : batch.batch * blocks);
@@ -1034,7 +1040,7 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
         if (c < cost) best = want, cost = c;
     }
     const int64_t per = (rounds + best - 1) / best;
-    return Split{(int)rows, (int)blocks, (int)((rounds + per - 1) / per), (int)(per * unit)};
+    return Split{(int)rows, (int)blocks, (int)((rounds + per - 1) / per), (int)(per * 4)};
 }
 
 }  // namespace
@@ -1053,10 +1059,13 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
     const bool extra = a.softcap > 0.0f || a.slopes || a.scale == 0.0f;
     with_head_dim(cache.head_dim, [&](auto d) {
         constexpr int kD = decltype(d)::value;
-        if (sp.rows > 16) {
-            if (extra) hipLaunchKernelGGL((paged_attention_wide_kernel<kD, true>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
-            else hipLaunchKernelGGL((paged_attention_wide_kernel<kD, false>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
-        } else {
+        if constexpr (kD <= 128) {
+            if (sp.rows > 16) {
+                if (extra) hipLaunchKernelGGL((paged_attention_wide_kernel<kD, true>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
+                else hipLaunchKernelGGL((paged_attention_wide_kernel<kD, false>), grid, dim3(Wide<kD>::kThreads), 0, stream, a);
+            }
+        }
+        if (sp.rows == 16) {
             if (extra) hipLaunchKernelGGL((paged_attention_kernel<kD, true>), grid, dim3(kThreads), 0, stream, a);
             else hipLaunchKernelGGL((paged_attention_kernel<kD, false>), grid, dim3(kThreads), 0, stream, a);
         }

@@ -364,6 +364,37 @@ def test_attention_of_long_contexts_is_split(dim, new):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 96, 128])
+@pytest.mark.parametrize("options", [dict(), dict(window=100), dict(softcap=5.0, slopes=True), dict(scale=-0.2), dict(scale=0.0, window=33)])
+def test_attention_of_many_rows(dim, options):
+    """Enough rows for the kernel that expands keys once for 256 of them (2400 rows of each KV head, a table wide enough)."""
+    s = Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40).fill()
+    options = dict(options)
+    if options.get("slopes"):
+        options["slopes"] = torch.tensor([0.5, 0.25, 0.0, 0.03125, 0.1, 2.0, 1.0, 0.01])
+    _attend(s, [90, 33, 3, 0, 64], 8, max_new=600, **options)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_attention_of_many_rows_split_and_without_keys(dim):
+    """The same where the keys are split, rows come before position 0, and pages or slots are missing: against 16 rows a workgroup."""
+    s = Sequences([3000, 40, 0, 777], dim, 1, 32, seed=dim, width=1024).fill()
+    new = [70, 90, 5, 64]
+    q, got, lse = _attend(s, new, 8, max_new=90)
+    assert dfp4.load().dfp4_paged_attention_workspace_bytes(s.cache.c, s.batch(new, max_new=90).c(sum(new)), 8, 0) > 0
+    s.table[0, 5], s.table[0, 90], s.table[3, 0], s.slots[3] = -1, 10 ** 6, s.cache.n_pages, -1
+    many, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch(new, max_new=90), return_lse=True)
+    few, lse2 = dfp4.paged_attention(q.cuda(), s.cache, s.batch(new, max_new=1), return_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isfinite(many).all() and torch.equal(torch.isneginf(lse), torch.isneginf(lse2))
+    # both are within 2^-8 sum p |v| (and a rounding) of the same values
+    assert float((many.float() - few.float()).norm() / few.float().norm()) <= 2 * HALF
+    assert float((lse - lse2)[~torch.isneginf(lse)].abs().max()) <= 2.0 ** -10
+    assert (many[70:70 + 50] == 0).all() and not torch.equal(many[:70], got[:70])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hints", [dict(), dict(max_new=1), dict(max_new=1000), dict(max_length=1), dict(max_length=10 ** 6), dict(max_new=2, max_length=400)])
 def test_attention_does_not_depend_on_the_hints(hints):
     s = Sequences([1500, 300, 700], 128, 2, 32, seed=2).fill()
