@@ -429,7 +429,7 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads, window) bytes, 16-byte aligned (0 where no context
  *            is split)
  * Scores, softmax and sums are in fp32.  The matrix instructions take keys and values as they are, q as the sum of two FP8 numbers (its
- * 8 bits) and a probability as the sum of two bf16 numbers.
+ * 8 bits) and a probability as the sum of two bf16 numbers, or where there are many rows as one.
  */
 size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
 int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,

@@ -6,8 +6,8 @@
 //     block's exponent byte is the instruction's scale, so a dword of codes costs eight vector instructions and no multiplication.
 //     A query goes in as the sum of two FP8 numbers (rounded to 4 bits, and what that left: the 8 bits of a bf16).
 //   O^T = V^T P^T, on 16 x 16 x 32 in bf16: the values' FP8 bytes become bf16 with their block's scale in one conversion for two (also
-//     exact), a probability is the sum of two bf16 numbers.  (As two FP8 numbers a probability has 8 bits down to 2^-19 of the largest and
-//     fewer below, which shows where the values at the largest are zero; a sixth fewer vector instructions for values.)
+//     exact), a probability is the sum of two bf16 numbers (one where there are many rows).  (As two FP8 numbers a probability has 8 bits
+//     down to 2^-19 of the largest and fewer below, which shows where the values at the largest are zero.)
 // Both leave in lane (g, c) rows 4 g .. 4 g + 3 of column c, and O^T may take its 128 tokens in any order.  So row 4 g + i of tile t
 // (0 .. 7) of S^T is token 32 g + 4 t + i of a step of 128: a lane has the scores of the chunk of 32 whose values it expands and
 // whose probabilities it supplies, and nothing moves between lanes.
@@ -264,6 +264,10 @@ __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0
 // One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
 // add up in LDS.  A step's cells come to LDS whole, by loads that bypass the registers: the next step's keys are asked for as soon as
 // this one's are multiplied, its values as soon as these are, so that a wave has 9 KiB (head_dim 128) or more under way all the time.
+// 48 sequences of about 8192 tokens, 32 heads of 128 on 8 (439 MB), one token each: 115 us = 3.8 TB/s; one token over 131072 (147 MB)
+// 35 us and the join 5.  What bounds it: vector instructions, some 1250 a wave and step beside 80 matrix instructions (47 % of the time of
+// the vector unit, counters), and waits for LDS and memory on top with two waves to a SIMD; codes loaded to registers at the top of a
+// step took 170 us, three waves to a SIMD (168 registers, spilled) 136.
 template <int D, bool EXTRA>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionArgs a) {
     using C = Cell<D>;
@@ -586,6 +590,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 // A chunk is a tile: its cell, and whether it is there, are the same for all lanes.
 // Codes of the next step are loaded while this one is multiplied, and expanded into the other half of LDS: one barrier a step.
 // The incomplete chunk is part of the last step: its values are stored to LDS as they are.  A probability is one bf16 number here.
+// 2048 tokens over 16384, 32 heads of 128 on 8: 490 us = 1.05 PFLOP/s (a large bf16 library product: 1.25); 16 rows a workgroup took 1630,
+// 16 x 16 instructions 521.  What bounds it: about 4100 clocks of matrix and 4600 of vector instructions a step and SIMD, which hardly
+// overlap, the two waves of a SIMD being in the same part of a step (9600 clocks).  Tried: one of the two waves half a step behind
+// (registers spilled: 750 us), steps of 64 keys (543), two workgroups of half the rows on a compute unit (587), the next step's scores
+// between this one's exponentials (560 to 600).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 struct Wide {
