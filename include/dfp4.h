@@ -421,7 +421,7 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
 /*
  * Attention of the batch's new tokens over their sequences' cached tokens, these included (dfp4_paged_write comes first): the
  * query at position p sees keys at t <= p, with a window > 0 those at t > p - window.
- *   s = scale * q . k^ ;  softcap > 0: s = softcap * tanh(s / softcap) ;  slopes: s -= slopes[head] * (p - t)
+ *   s = scale * q . k^ ;  softcap > 0 (at most 1e30): s = softcap * tanh(s / softcap) ;  slopes: s -= slopes[head] * (p - t)
  *   out = sum over t of softmax(s)_t v^_t,  lse = log(sum over t of exp(s))     (no key: out = 0, lse = -infinity)
  * with k^, v^ what the cache stands for.  Query head h reads KV head h / (heads / kv_heads).
  *   q, out   device, bf16 [tokens, heads, head_dim], token and head strides in elements (multiples of 8), 16-byte aligned

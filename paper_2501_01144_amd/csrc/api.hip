@@ -536,7 +536,7 @@ int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride,
                          float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     int rc = check_paged(cache, batch);
-    if (rc == DFP4_OK && (!grouped(cache, heads) || batch.tokens * heads > (int64_t)1 << 30 || window < 0 || window > (int64_t)1 << 30 || !(softcap >= 0.0f)))
+    if (rc == DFP4_OK && (!grouped(cache, heads) || batch.tokens * heads > (int64_t)1 << 30 || window < 0 || window > (int64_t)1 << 30 || !(softcap >= 0.0f && softcap <= 1e30f)))
         rc = DFP4_ERR_SHAPE;
     if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
     if ((rc = check_rows(q, q_stride, q_head_stride)) != DFP4_OK || (rc = check_rows(out, out_stride, out_head_stride)) != DFP4_OK) return rc;

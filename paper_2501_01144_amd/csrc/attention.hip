@@ -77,18 +77,13 @@ __device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, i
     hi = h;
 }
 
-// c += a (hi + 2^-5 lo), hi times 2^(sb - 127).  The compiler lets a result overlap an operand that it sees no further use of, which the instruction
-// overwrites before it has read it for the last time: operands are in use until the end here (the build checks).
-template <int OPSEL>
-__device__ __forceinline__ void times(const v8i& a, const v8i& b, v4f& c, int sa, int sb) {
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, OPSEL, sa, 0, sb);
-}
-__device__ __forceinline__ void keep(v4f& c, const v8i& a, const v8i& hi, const v8i& lo) { asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo)); }
+// c += a (hi + 2^-5 lo), hi times 2^(sb - 127).  The compiler lets a result overlap an operand that it sees no further use of, which the
+// instruction overwrites before it has read it for the last time: operands are in use until the end here (the build checks).
 template <int OPSEL>
 __device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& lo, v4f& c, int sa, int sb, int sb_lo) {
-    times<OPSEL>(a, hi, c, sa, sb);
-    times<OPSEL>(a, lo, c, sa, sb_lo);
-    keep(c, a, hi, lo);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, c, 0, 0, OPSEL, sa, 0, sb);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, c, 0, 0, OPSEL, sa, 0, sb_lo);
+    asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
 }
 
 // N dwords of codes of a scale and a dialect to bf16: fragments of N instructions, tokens 8 q .. 8 q + 7 in the q-th

@@ -51,7 +51,7 @@ def test_calls_refuse_bad_arguments():
 
     def attend(q=16, qs=256, qh=64, heads=4, softcap=0.0, window=0, slopes=0, out=16, os=256, oh=64, lse=0, ws=16, n=1 << 30, b=b):
         return lib.dfp4_paged_attention(vp(q), qs, qh, heads, c, b, 1.0, softcap, window, vp(slopes), vp(out), os, oh, vp(lse), vp(ws), n, vp(0))
-    assert (attend(heads=3), attend(heads=0), attend(heads=-2), attend(window=-1), attend(softcap=-1.0), attend(softcap=float("nan"))) == (-2,) * 6
+    assert (attend(heads=3), attend(heads=0), attend(heads=-2), attend(window=-1), attend(softcap=-1.0), attend(softcap=float("nan")), attend(softcap=float("inf"))) == (-2,) * 7
     assert (attend(q=0), attend(out=0), attend(q=20), attend(qs=12), attend(oh=2), attend(slopes=2), attend(lse=1), attend(ws=8)) == (-1, -1) + (-3,) * 6
     # a long context is split between workgroups, and that takes a workspace
     long = _batch(table_width=1 << 12)
