@@ -202,12 +202,16 @@ __device__ __forceinline__ int load_query(const uint16_t* row, bool ok, bool neg
 
 // What turns scores into exponents to base 2.  Where there is neither cap nor bias (nor a scale of zero) a score stays as it is,
 // masked or not, until the largest is taken from it (the factor is positive: its sign goes into the query).
+// cap tanh(y) = cap - 2 cap / (exp(2 y) + 1), for a score z = cap y.  That is a difference of numbers of size cap, off by about 2^-22 cap.  Up to
+// a cap of 128 that is 2^-15 of a probability, which a bf16 result does not show.  Above, a score below |y| = 1/8 is the series
+// z (1 - y^2 / 3 + 2 y^4 / 15) instead, off by 17/315 y^6 < 2^-22 of itself, so that it is off by 2^-19 of itself at most whatever the cap is, and
+// a cap that no score comes near leaves it alone.  (2048 tokens over 16384, 32 heads of 128: 765 us, with the series 910.)
 template <bool EXTRA>
 struct Scores {
     float factor, cap, twice, slope;
     uint32_t reach;              // a key so many positions behind the query, or less, is seen
     __device__ __forceinline__ Scores(const AttentionArgs& a)
-        : factor(fabsf(a.scale) * kLog2e), cap(a.softcap * kLog2e), twice(a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f), slope(0.0f),
+        : factor(fabsf(a.scale) * kLog2e), cap(a.softcap * kLog2e), twice(a.softcap > 0.0f ? fminf(2.0f / a.softcap, 3e38f) : 0.0f), slope(0.0f),
           reach(a.window > 0 ? (uint32_t)a.window - 1u : 0x7fffffffu) {}
     // N scores whose keys are 0, 1, .. positions on from one `behind` behind the query
     template <int N>
@@ -215,9 +219,20 @@ struct Scores {
         if constexpr (EXTRA) {
             if (cap > 0.0f) {
                 asm volatile("");                                   // one branch
-                // cap tanh(y) = cap - 2 cap / (exp(2 y) + 1)
+                auto far = [&](float t) { return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(exp2_(t) + 1.0f), cap); };
+                if (cap <= 128.0f * kLog2e) {
+                    const float by = fminf(factor * twice, 3e38f);  // (finite: a score may be zero)
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(exp2_(x[i] * (factor * twice)) + 1.0f), cap);
+                    for (int i = 0; i < N; ++i) x[i] = far(x[i] * by);
+                } else {
+                    constexpr float k = 0.5f / kLog2e;              // y = k t
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const float z = x[i] * factor, t = z * twice, t2 = t * t;
+                        const float near = fmaf(z, t2 * fmaf(t2, 2.0f / 15.0f * k * k * k * k, -k * k / 3.0f), z);
+                        x[i] = fabsf(t) < 0.125f / k ? near : far(t);
+                    }
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) x[i] *= factor;

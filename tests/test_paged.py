@@ -530,3 +530,40 @@ def test_the_layer_of_the_example():
     spec.loader.exec_module(example)
     off, _ = example.run(prompts=(40, 31, 1), tokens=5)
     assert off <= HALF
+
+
+# ---- scores with caps of any size -----------------------------------------------------------------------------------------------
+
+def _few_or_many_rows(dim, many):
+    """Sequences, new tokens, heads and hints of a call with few rows, or with enough for the kernel that takes 256 rows a workgroup."""
+    if many:
+        return Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40).fill(), [90, 33, 3, 0, 64], 8, dict(max_new=90)
+    return Sequences([300, 45, 129], dim, 2, 64, seed=dim).fill(), [9, 45, 1], 6, dict(max_new=45)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,many", [(64, False), (128, False), (256, False), (64, True), (96, True), (128, True)])
+def test_caps_far_above_the_scores_leave_them_alone(dim, many):
+    s, new, heads, hints = _few_or_many_rows(dim, many)
+    scale = dim ** -0.5
+    q, _, plain = _attend(s, new, heads, **hints)
+    want = _attention(s, q, new, scale)
+    seen = ~np.isneginf(want[1])
+    for cap in (1e3, 1e6, 1e10, 1e30):
+        _, _, lse = _attend(s, new, heads, softcap=cap, **hints)
+        shift = (lse - plain).double().cpu().numpy()[seen]
+        want_shift = (_attention(s, q, new, scale, softcap=cap)[1] - want[1])[seen]
+        # both calls have the same scores: a cap changes one by what it should and 2^-18 of it (at most `dot`); two results of 2^-20
+        tol = 2.0 ** -18 * want[3][seen] + 2 * 2.0 ** -20 * (1 + np.abs(want[1][seen]))
+        assert (np.abs(shift - want_shift) <= tol).all(), (cap, float((np.abs(shift - want_shift) / tol).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,many", [(128, False), (128, True)])
+@pytest.mark.parametrize("cap", [1e-39, 1e-30, 0.01, 1.0, 300.0])
+def test_caps_near_and_below_the_scores(dim, many, cap):
+    s, new, heads, hints = _few_or_many_rows(dim, many)
+    _attend(s, new, heads, softcap=cap, **hints)
+    s.k[0][:] = 0                                    # scores of zero
+    s.fill()
+    _attend(s, new, heads, softcap=cap, scale=4.0, **hints)
