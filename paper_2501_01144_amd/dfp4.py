@@ -577,7 +577,7 @@ def paged_write(k, v, cache, batch):
 
 def paged_read(cache, batch, tokens=None, dtype=torch.bfloat16):
     """dfp4_paged_read: the values that the cache stands for, k and v [tokens, kv_heads, head_dim], of the batch's tokens (`tokens`
-    of them, by default as many as batch.tokens says)."""
+    of them, by default batch.tokens, which waits for the device unless the batch was given the number)."""
     return _calls().paged_read(cache.at, batch.at, batch.tokens if tokens is None else tokens, _is_bf16(dtype), cache.pages)
 
 

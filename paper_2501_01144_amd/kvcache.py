@@ -90,7 +90,8 @@ class PagedBatch:
 
     cu_tokens [batch + 1]: sequence b brings rows cu_tokens[b] .. cu_tokens[b + 1] - 1; lengths [batch]: its tokens with these;
     table [batch, width]: its pages; slots [batch]: its slot.  max_new, max_length: bounds that the host knows, 0: none (they decide
-    how work is split, not what is computed).  tokens: rows in all, where a call cannot take them from its arguments."""
+    how work is split, not what is computed).  tokens: rows in all, where a call cannot take them from its arguments (paged_read);
+    where it is not given it is read from cu_tokens whenever it is asked for, which waits for the device."""
 
     def __init__(self, cu_tokens, lengths, table, slots, max_new=0, max_length=0, tokens=None):
         n = lengths.numel()
@@ -104,9 +105,8 @@ class PagedBatch:
 
     @property
     def tokens(self):
-        if self._tokens is None:
-            self._tokens = int(self.cu_tokens[-1])           # waits for the device, once
-        return self._tokens
+        # (the contents of cu_tokens may change: nothing is kept)
+        return int(self.cu_tokens[-1]) if self._tokens is None else self._tokens
 
     def c(self, tokens):
         b = dfp4._CBatch.from_buffer_copy(self._c)

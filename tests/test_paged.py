@@ -567,3 +567,18 @@ def test_caps_near_and_below_the_scores(dim, many, cap):
     s.k[0][:] = 0                                    # scores of zero
     s.fill()
     _attend(s, new, heads, softcap=cap, scale=4.0, **hints)
+
+
+# ---- batches whose tensors change -----------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_read_takes_the_tokens_that_a_batch_has_now():
+    s = Sequences([70, 40], 64, 2, 32, seed=21).fill()
+    b = s.batch([3, 2])
+    b = kvcache.PagedBatch(b.cu_tokens, b.lengths, b.table, b.slots)
+    for new in ([3, 2], [70, 40], [1, 0], [0, 0], [5, 33]):
+        b.cu_tokens.copy_(torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32))
+        k, v = dfp4.paged_read(s.cache, b)
+        assert b.tokens == len(k) == len(v) == sum(new)
+        want_k, want_v = ([x[i][len(x[i]) - n:] for i, n in enumerate(new)] for x in s.stands_for())
+        assert np.array_equal(k.double().cpu().numpy(), np.concatenate(want_k)) and np.array_equal(v.double().cpu().numpy(), np.concatenate(want_v))
