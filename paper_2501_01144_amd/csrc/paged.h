@@ -14,6 +14,7 @@
 #pragma once
 #include "common.h"
 #include "formatbook.h"
+#include "page_of.h"
 
 namespace dfp4 {
 
@@ -54,13 +55,13 @@ struct PagedArgs {
     uint16_t* residual;
     const int32_t *cu, *lengths, *table, *slots;
     int n_pages, n_slots, page_chunks, kv_heads, batch, width, tokens;
-    uint64_t per_page;               // 2^40 / page_chunks, rounded up: chunk / page_chunks is chunk * per_page >> 40 (page_chunks <= 2^15,
-};                                   // chunk < 2^25)
+    PageDivision pages_of;           // by page_chunks
+};
 
 inline PagedArgs paged_args(const dfp4_cache& c, const dfp4_batch& b) {
     return PagedArgs{c.pages, c.residual, b.cu_tokens, b.lengths, b.table, b.slots, (int)c.n_pages, (int)c.n_slots,
                      (int)(c.page_tokens / 32), (int)c.kv_heads, (int)b.batch, (int)b.table_width, (int)b.tokens,
-                     (((uint64_t)1 << 40) + (uint64_t)(c.page_tokens / 32) - 1) / (uint64_t)(c.page_tokens / 32)};
+                     page_division((uint32_t)(c.page_tokens / 32))};
 }
 
 // New tokens [first, first + n) of the dense arrays are positions [length - n, length) of the sequence.
@@ -86,7 +87,7 @@ __device__ __forceinline__ int64_t cell_offset(const PagedArgs& p, int head, int
     const int64_t at = (int64_t)((uint64_t)cell_number(p, head, chunk, in_table, there ? page : 0) * Cell<D>::kBytes);
     return there ? at : (int64_t)-1;
 }
-__device__ __forceinline__ int place_in_table(const PagedArgs& p, int chunk) { return (int)((uint64_t)chunk * p.per_page >> 40); }
+__device__ __forceinline__ int place_in_table(const PagedArgs& p, int chunk) { return page_of(p.pages_of, chunk); }
 
 // the cell of a chunk that the length says is there
 template <int D>

@@ -582,3 +582,52 @@ def test_read_takes_the_tokens_that_a_batch_has_now():
         assert b.tokens == len(k) == len(v) == sum(new)
         want_k, want_v = ([x[i][len(x[i]) - n:] for i, n in enumerate(new)] for x in s.stands_for())
         assert np.array_equal(k.double().cpu().numpy(), np.concatenate(want_k)) and np.array_equal(v.double().cpu().numpy(), np.concatenate(want_v))
+
+
+# ---- positions far beyond any cache that fits ------------------------------------------------------------------------------------
+
+def test_the_page_of_a_chunk(tmp_path):
+    """chunk / chunks of a page for every size of a page, around every power of two and every border of a page near it."""
+    import os
+    import subprocess
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2501_01144_amd", "csrc")
+    (tmp_path / "t.cpp").write_text(r"""
+#include <cstdio>
+#include <initializer_list>
+#include "page_of.h"
+int main() {
+    for (uint32_t n = 1; n <= 1u << 15; ++n) {
+        const dfp4::PageDivision by = dfp4::page_division(n);
+        for (int bit = 0; bit < 31; ++bit)
+            for (int64_t near : {(int64_t)1 << bit, ((int64_t)1 << bit) / n * n, ((((int64_t)1 << bit) / n) + 1) * n})
+                for (int64_t chunk = near - 2; chunk <= near + 2; ++chunk)
+                    if (chunk >= 0 && chunk < (int64_t)1 << 31 && dfp4::page_of(by, (int)chunk) != (int)(chunk / n)) {
+                        std::printf("%lld / %u: %d\n", (long long)chunk, n, dfp4::page_of(by, (int)chunk));
+                        return 1;
+                    }
+    }
+    return 0;
+}
+""")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", csrc, str(tmp_path / "t.cpp"), "-o", str(tmp_path / "t")], check=True)
+    done = subprocess.run([str(tmp_path / "t")], capture_output=True, text=True)
+    assert done.returncode == 0, done.stdout
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [32, 64, 96])
+def test_positions_beyond_two_to_the_29(page):
+    """The last 102 tokens of a sequence whose earlier pages are not there."""
+    s = Sequences([102], 64, 2, page, seed=page)
+    first = -(-(1 << 29) // page) + 3                    # pages before them
+    table = torch.full((1, first + s.width), -1, dtype=torch.int32)
+    table[:, first:] = s.table
+    s.table = table
+    at = first * page + 102
+    dfp4.paged_write(s.k[0].cuda(), s.v[0].cuda(), s.cache, s.batch([102], [at]))
+    k, v = dfp4.paged_read(s.cache, s.batch([102], [at]))
+    torch.cuda.synchronize()
+    assert np.array_equal(k.double().cpu().numpy(), _keys(s.k[0])) and np.array_equal(v.double().cpu().numpy(), _values(s.v[0], 102))
+    q = torch.randn(3, 4, 64, generator=s.g).bfloat16()
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch([3], [at], max_new=3), window=90, return_lse=True)
+    _check_attention(got, lse, _attention(s, q, [3], 64 ** -0.5, window=90))
