@@ -289,7 +289,7 @@ def prepare(case, seed):
         s["cache"] = cache
         if case["kind"] == "cache":
             s["batch"] = kvcache.PagedBatch(s["cu_new"], s["length"], s["table"], s["slots"], s["most_new"])
-            s["back"] = kvcache.PagedBatch(s["cu_touched"], s["length"], s["table"], s["slots"], s["most_touched"])
+            s["back"] = kvcache.PagedBatch(s["cu_touched"], s["length"], s["table"], s["slots"], s["most_touched"], tokens=int(s["cu_touched"][-1]))
             n_past = s["touched"] - s["new"]
             cu_past = torch.cat([n_past.new_zeros(1), n_past.cumsum(0)]).int()
             dfp4.paged_write(s["k_before"][s["is_past"]], s["v_before"][s["is_past"]], cache,
