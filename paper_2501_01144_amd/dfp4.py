@@ -600,8 +600,10 @@ def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=N
     need = int(load().dfp4_paged_attention_workspace_bytes(cache.c, b, heads, window))
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
     _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, cache.c, b, scale, softcap, window, _ptr(slopes), _ptr(out), out.stride(0),
-                                       out.stride(1), _ptr(lse), _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream()),
+                                       out.stride(1), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                       _stream()),
            "dfp4_paged_attention")
     return (out, lse) if return_lse else out
 

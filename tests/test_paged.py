@@ -631,3 +631,18 @@ def test_positions_beyond_two_to_the_29(page):
     q = torch.randn(3, 4, 64, generator=s.g).bfloat16()
     got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch([3], [at], max_new=3), window=90, return_lse=True)
     _check_attention(got, lse, _attention(s, q, [3], 64 ** -0.5, window=90))
+
+
+# ---- arguments of the Python calls -----------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_workspaces_are_memory_of_the_device():
+    s = Sequences([2049], 64, 1, 64, seed=31).fill()
+    need = dfp4.load().dfp4_paged_attention_workspace_bytes(s.cache.c, s.batch([1], max_new=1).c(1), 4, 0)
+    q = torch.randn(1, 4, 64, generator=s.g).bfloat16().cuda()
+    for bad in (torch.empty(need, dtype=torch.uint8), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(AssertionError):
+            dfp4.paged_attention(q, s.cache, s.batch([1], max_new=1), workspace=bad)
+    # of any type: its bytes count
+    ws = torch.empty(-(-need // 4), dtype=torch.float32, device="cuda")
+    assert torch.equal(dfp4.paged_attention(q, s.cache, s.batch([1], max_new=1), workspace=ws), dfp4.paged_attention(q, s.cache, s.batch([1], max_new=1)))
