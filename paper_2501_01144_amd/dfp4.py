@@ -611,21 +611,21 @@ def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=N
 def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
     """dfp4_norm_rope: norms of queries and keys per head (where a weight, f32 [head_dim], is given) and their rotation by
     position, in one pass.  q bf16 [tokens, heads, head_dim], k the same with its heads (or None); positions int32 [tokens];
-    inv_freq f32 [rotary / 2].  Returns q and k (out=(q, k): into these, which may be the inputs where those are contiguous)."""
+    inv_freq f32 [rotary / 2] (None: no rotation, and positions may be None).  Returns q and k (out=(q, k): into these, which may be the inputs where those are contiguous)."""
     if out is None:
         return _calls().norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, bool(interleaved))
     tokens, heads, head_dim = q.shape
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_cuda and w.is_contiguous() and w.numel() == head_dim)
-    assert positions.dtype == torch.int32 and positions.is_cuda and positions.is_contiguous() and positions.numel() == tokens
-    assert inv_freq.dtype == torch.float32 and inv_freq.is_cuda and inv_freq.is_contiguous()
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_cuda and positions.is_contiguous() and positions.numel() == tokens)
+    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.is_cuda and inv_freq.is_contiguous())
     q_out, k_out = out
     for x, y in ((q, q_out), (k, k_out)):
         assert (x is None and y is None) or (x.dtype == y.dtype == torch.bfloat16 and x.is_cuda and y.is_cuda and x.stride(2) == 1 and y.is_contiguous() and
                                              y.shape == x.shape and (x.shape[0], x.shape[2]) == (tokens, head_dim))
     _check(load().dfp4_norm_rope(_ptr(q), q.stride(0), q.stride(1), heads, _ptr(k), k.stride(0) if k is not None else 0,
                                  k.stride(1) if k is not None else 0, k.shape[1] if k is not None else 0, tokens, head_dim, _ptr(q_weight),
-                                 _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel(), 1 if interleaved else 0,
+                                 _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel() if inv_freq is not None else 0, 1 if interleaved else 0,
                                  _ptr(q_out), _ptr(k_out), _stream()), "dfp4_norm_rope")
     return q_out, k_out
 

@@ -646,3 +646,16 @@ def test_workspaces_are_memory_of_the_device():
     # of any type: its bytes count
     ws = torch.empty(-(-need // 4), dtype=torch.float32, device="cuda")
     assert torch.equal(dfp4.paged_attention(q, s.cache, s.batch([1], max_new=1), workspace=ws), dfp4.paged_attention(q, s.cache, s.batch([1], max_new=1)))
+
+
+@pytest.mark.gpu
+def test_norm_rope_without_a_rotation():
+    x, w = torch.randn(5, 4, 64).bfloat16().cuda(), torch.rand(64, device="cuda")
+    q, k = dfp4.norm_rope(x, None, None, None, w)
+    want, size = _rope(x.cpu(), w.cpu(), torch.zeros(5), torch.zeros(0), False, 1e-6)
+    assert k is None and (np.abs(q.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size).all()
+    into = torch.empty_like(x)
+    q2, k2 = dfp4.norm_rope(x, None, None, None, w, out=(into, None))
+    assert q2 is into and k2 is None and torch.equal(q2, q)
+    with pytest.raises(dfp4.Dfp4Error):                  # a rotation by what?
+        dfp4.norm_rope(x, None, None, torch.ones(32, device="cuda"), w, out=(into, None))
