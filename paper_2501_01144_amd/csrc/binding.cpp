@@ -255,6 +255,8 @@ const at::Tensor& rows3(PyObject* o) {
         fail(PyExc_AssertionError, "bf16 [tokens, heads, head_dim] on the device, contiguous along head_dim, is expected");
     return x;
 }
+// stride of a dimension (a single token's, or a single head's, is nobody's concern: torch leaves anything there)
+int64_t step(const at::Tensor& x, int64_t d) { return x.size(d) > 1 ? x.stride(d) : 0; }
 // a contiguous tensor of `n` numbers on the device, or None
 template <class T>
 const T* numbers(PyObject* o, at::ScalarType type, int64_t n, const char* what) {
@@ -273,7 +275,7 @@ PyObject* paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
         batch.tokens = k.size(0);
         if (k.sizes() != v.sizes() || k.size(1) != cache.kv_heads || k.size(2) != cache.head_dim)
             fail(PyExc_AssertionError, "k and v: [tokens, kv_heads, head_dim] of the cache");
-        enqueue("dfp4_paged_write", p_dfp4_paged_write, data(k), k.stride(0), k.stride(1), data(v), v.stride(0), v.stride(1), cache, batch, stream());
+        enqueue("dfp4_paged_write", p_dfp4_paged_write, data(k), step(k, 0), step(k, 1), data(v), step(v, 0), step(v, 1), cache, batch, stream());
         Py_RETURN_NONE;
     });
 }
@@ -308,8 +310,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (with_lse) lse = result({batch.tokens, heads}, false, dev);
         const size_t need = p_dfp4_paged_attention_workspace_bytes(cache, batch, heads, window);
         if (need > 0) ws = bytes((int64_t)need, dev);
-        enqueue("dfp4_paged_attention", p_dfp4_paged_attention, data(q), q.stride(0), q.stride(1), heads, cache, batch, (float)real(a[3]), (float)real(a[4]),
-                window, slopes, data(out), out.stride(0), out.stride(1), with_lse ? reinterpret_cast<float*>(data(lse)) : nullptr,
+        enqueue("dfp4_paged_attention", p_dfp4_paged_attention, data(q), step(q, 0), step(q, 1), heads, cache, batch, (float)real(a[3]), (float)real(a[4]),
+                window, slopes, data(out), step(out, 0), step(out, 1), with_lse ? reinterpret_cast<float*>(data(lse)) : nullptr,
                 need > 0 ? data(ws) : nullptr, need, stream());
         if (!with_lse) return THPVariable_Wrap(std::move(out));
         return Py_BuildValue("NN", THPVariable_Wrap(std::move(out)), THPVariable_Wrap(std::move(lse)));
@@ -330,7 +332,7 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
                     *kw = numbers<float>(a[5], at::kFloat, dim, "k_weight: contiguous f32 [head_dim] on the device");
         at::Tensor q_out = result(q.sizes(), true, q.device()), k_out;
         if (both) k_out = result(k.sizes(), true, q.device());
-        enqueue("dfp4_norm_rope", p_dfp4_norm_rope, data(q), q.stride(0), q.stride(1), q.size(1), both ? data(k) : nullptr, k.stride(0), k.stride(1),
+        enqueue("dfp4_norm_rope", p_dfp4_norm_rope, data(q), step(q, 0), step(q, 1), q.size(1), both ? data(k) : nullptr, step(k, 0), step(k, 1),
                 both ? k.size(1) : 0, tokens, dim, qw, kw, (float)real(a[6]), positions, freq, a[3] == Py_None ? 0 : 2 * tensor(a[3]).numel(),
                 a[7] == Py_True ? 1 : 0, data(q_out), both ? data(k_out) : nullptr, stream());
         PyObject* second = both ? THPVariable_Wrap(std::move(k_out)) : Py_NewRef(Py_None);

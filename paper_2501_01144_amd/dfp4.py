@@ -195,6 +195,11 @@ def _ptr(t):
         else ctypes.c_void_p(0)
 
 
+def _steps(x):
+    # strides of tokens and heads (a single one's is nobody's concern: torch leaves anything there)
+    return tuple(x.stride(d) if x.shape[d] > 1 else 0 for d in (0, 1)) if x is not None else (0, 0)
+
+
 @dataclass
 class QTensor:
     """A quantized [rows, K] tensor on the device (layouts in include/dfp4.h)."""
@@ -601,8 +606,8 @@ def paged_attention(q, cache, batch, scale=None, softcap=0.0, window=0, slopes=N
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
-    _check(load().dfp4_paged_attention(_ptr(q), q.stride(0), q.stride(1), heads, cache.c, b, scale, softcap, window, _ptr(slopes), _ptr(out), out.stride(0),
-                                       out.stride(1), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+    _check(load().dfp4_paged_attention(_ptr(q), *_steps(q), heads, cache.c, b, scale, softcap, window, _ptr(slopes), _ptr(out), *_steps(out),
+                                       _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
                                        _stream()),
            "dfp4_paged_attention")
     return (out, lse) if return_lse else out
@@ -623,8 +628,7 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6,
     for x, y in ((q, q_out), (k, k_out)):
         assert (x is None and y is None) or (x.dtype == y.dtype == torch.bfloat16 and x.is_cuda and y.is_cuda and x.stride(2) == 1 and y.is_contiguous() and
                                              y.shape == x.shape and (x.shape[0], x.shape[2]) == (tokens, head_dim))
-    _check(load().dfp4_norm_rope(_ptr(q), q.stride(0), q.stride(1), heads, _ptr(k), k.stride(0) if k is not None else 0,
-                                 k.stride(1) if k is not None else 0, k.shape[1] if k is not None else 0, tokens, head_dim, _ptr(q_weight),
+    _check(load().dfp4_norm_rope(_ptr(q), *_steps(q), heads, _ptr(k), *_steps(k), k.shape[1] if k is not None else 0, tokens, head_dim, _ptr(q_weight),
                                  _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel() if inv_freq is not None else 0, 1 if interleaved else 0,
                                  _ptr(q_out), _ptr(k_out), _stream()), "dfp4_norm_rope")
     return q_out, k_out

@@ -659,3 +659,20 @@ def test_norm_rope_without_a_rotation():
     assert q2 is into and k2 is None and torch.equal(q2, q)
     with pytest.raises(dfp4.Dfp4Error):                  # a rotation by what?
         dfp4.norm_rope(x, None, None, torch.ones(32, device="cuda"), w, out=(into, None))
+
+
+@pytest.mark.gpu
+def test_the_stride_of_a_single_token_or_head_does_not_matter():
+    s = Sequences([40], 64, 1, 32, seed=33)
+    s.write([39], [39])
+    one = lambda x: torch.as_strided(x.cuda(), (1, 1, 64), (3, 5, 1))  # noqa: E731
+    dfp4.paged_write(one(s.k[0][39]), one(s.v[0][39]), s.cache, s.batch([1], [40]))
+    _check_read(s, [40], [40], torch.bfloat16)
+    q = torch.randn(1, 1, 64, generator=s.g).bfloat16()
+    freq, pos = torch.ones(32, device="cuda"), torch.tensor([7], dtype=torch.int32, device="cuda")
+    assert torch.equal(dfp4.norm_rope(one(q), one(q), pos, freq)[1], dfp4.norm_rope(q.cuda(), None, pos, freq)[0])
+    into = torch.empty(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(dfp4.norm_rope(one(q), None, pos, freq, out=(into, None))[0], dfp4.norm_rope(q.cuda(), None, pos, freq)[0])
+    want = dfp4.paged_attention(q.cuda(), s.cache, s.batch([1]))
+    assert torch.equal(dfp4.paged_attention(one(q), s.cache, s.batch([1])), want)
+    assert torch.equal(dfp4.paged_attention(one(q), s.cache, s.batch([1]), out=one(into)), want)
