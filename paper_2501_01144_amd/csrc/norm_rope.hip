@@ -150,12 +150,19 @@ int launch_norm_rope(const NormRopeArgs& a, hipStream_t stream) {
     tokens = tokens < 1 ? 1 : tokens < fit ? tokens : fit;
     const int64_t groups = ((int64_t)a.tokens + tokens - 1) / tokens;
     const int passes = groups >= 4 * cus ? rounds : 1;
-    const Launch p{a, tokens, passes};
-    const dim3 grid((uint32_t)groups, (uint32_t)((rounds + passes - 1) / passes)), block(kThreads);
-    if (lanes == 4) hipLaunchKernelGGL((norm_rope_kernel<4>), grid, block, 0, stream, p);
-    else if (lanes == 8) hipLaunchKernelGGL((norm_rope_kernel<8>), grid, block, 0, stream, p);
-    else if (lanes == 16) hipLaunchKernelGGL((norm_rope_kernel<16>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((norm_rope_kernel<32>), grid, block, 0, stream, p);
+    const int64_t most = ((int64_t)1 << 32) / kThreads - 1;          // workgroups of a launch: fewer than 2^32 threads
+    for (int64_t at = 0; at < groups; at += most) {
+        const int64_t t = at * tokens, left = groups - at < most ? groups - at : most;
+        Launch p{a, tokens, passes};
+        p.a.tokens = (int)(a.tokens - t < left * tokens ? a.tokens - t : left * tokens);
+        p.a.q += t * a.q_stride, p.a.k += t * a.k_stride, p.a.positions += t;
+        p.a.q_out += t * a.heads * a.head_dim, p.a.k_out += t * a.kv_heads * a.head_dim;
+        const dim3 grid((uint32_t)left, (uint32_t)((rounds + passes - 1) / passes)), block(kThreads);
+        if (lanes == 4) hipLaunchKernelGGL((norm_rope_kernel<4>), grid, block, 0, stream, p);
+        else if (lanes == 8) hipLaunchKernelGGL((norm_rope_kernel<8>), grid, block, 0, stream, p);
+        else if (lanes == 16) hipLaunchKernelGGL((norm_rope_kernel<16>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((norm_rope_kernel<32>), grid, block, 0, stream, p);
+    }
     return check_launch();
 }
 

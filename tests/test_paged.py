@@ -676,3 +676,23 @@ def test_the_stride_of_a_single_token_or_head_does_not_matter():
     want = dfp4.paged_attention(q.cuda(), s.cache, s.batch([1]))
     assert torch.equal(dfp4.paged_attention(one(q), s.cache, s.batch([1])), want)
     assert torch.equal(dfp4.paged_attention(one(q), s.cache, s.batch([1]), out=one(into)), want)
+
+
+# ---- sizes that one launch does not hold -----------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_norm_rope_of_more_tokens_than_a_launch_holds():
+    """Without a rotation a workgroup of 256 threads takes four tokens, and a launch has fewer than 2^32 threads."""
+    n = (1 << 26) + 5
+    x = torch.ones(n, 1, 32, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(3)
+    places = [0, 4 * ((1 << 24) - 1) - 3, n - 8]
+    for at in places:
+        x[at:at + 8] = torch.randn(8, 1, 32, generator=g).bfloat16().cuda()
+    w = torch.rand(32, generator=g) + 0.5
+    q, _ = dfp4.norm_rope(x, None, None, None, w.cuda())
+    for at in places:
+        want, _ = _rope(x[at:at + 8].cpu(), w, torch.zeros(8), torch.zeros(0), False, 1e-6)
+        assert (np.abs(q[at:at + 8].double().cpu().numpy() - want) <= (HALF + 20 * 2.0 ** -24) * np.abs(want)).all()
+    q[places[1]:places[1] + 8], q[-8:], q[:8] = q[1000], q[1000], q[1000]
+    assert bool((q == q[1000]).all())
