@@ -383,6 +383,8 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
  * Numbers in these arrays are used only as far as they lie in range: lengths are cut to the table's width, token ranges to
  * `tokens`; tokens in pages outside the pool, and values in slots outside `residual`, count as absent (not written, read as zeros,
  * not attended to).  Two sequences of one call must not share pages that are written, or slots.
+ * Refused as too large: batch * kv_heads from 2^23 on, table_width * page_tokens, tokens or tokens * heads (attention) above 2^30, a pool
+ * of more than 2^31 cells.
  */
 typedef struct dfp4_cache {
     uint8_t* pages;
@@ -427,7 +429,7 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  *   q, out   device, bf16 [tokens, heads, head_dim], token and head strides in elements (multiples of 8), 16-byte aligned
  *   slopes   device, f32 [heads], or NULL;  lse  device, f32 [tokens, heads], or NULL
  *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads, window) bytes, 16-byte aligned (0 where no context
- *            is split)
+ *            is split, and for sizes that the call refuses)
  * Scores, softmax and sums are in fp32.  The matrix instructions take keys and values as they are, q as the sum of two FP8 numbers (its
  * 8 bits) and a probability as the sum of two bf16 numbers, or where there are many rows as one.
  */

@@ -481,15 +481,22 @@ size_t dfp4_gemm_requant_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 
 // ---- serving operators over the paged cache -------------------------------------------------------------------------------
 
-static int check_paged(const dfp4_cache& c, const dfp4_batch& b) {
+static int check_paged_sizes(const dfp4_cache& c, const dfp4_batch& b) {
     if (cell_bytes(c.head_dim) == 0 || c.page_tokens < 32 || c.page_tokens % 32 != 0 || c.n_pages < 0 || c.n_slots < 0 || c.kv_heads < 1)
         return DFP4_ERR_SHAPE;
     if (b.batch < 0 || b.table_width < 0 || b.tokens < 0 || b.max_new < 0 || b.max_length < 0) return DFP4_ERR_SHAPE;
-    const int64_t most = (int64_t)1 << 30;
-    if (c.page_tokens > (1 << 20) || c.n_pages > most || c.n_slots > most || c.kv_heads > (1 << 16) || b.batch > most || b.tokens > most ||
-        b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most ||
+    // (a workgroup of up to 512 threads for each sequence and KV head, and a launch has fewer than 2^32 threads)
+    const int64_t most = (int64_t)1 << 30, most_groups = ((int64_t)1 << 23) - 1;
+    if (c.page_tokens > (1 << 20) || c.n_pages > most || c.n_slots > most || c.kv_heads > (1 << 16) || b.batch > most_groups || b.tokens > most ||
+        b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most_groups ||
         c.n_pages * c.kv_heads > ((int64_t)1 << 31) / (c.page_tokens / 32))
         return DFP4_ERR_SHAPE;
+    return DFP4_OK;
+}
+
+static int check_paged(const dfp4_cache& c, const dfp4_batch& b) {
+    const int rc = check_paged_sizes(c, b);
+    if (rc != DFP4_OK) return rc;
     if (b.batch == 0 || b.tokens == 0) return DFP4_OK;
     if ((c.n_pages > 0 && !c.pages) || (c.n_slots > 0 && !c.residual) || !b.cu_tokens || !b.lengths || !b.slots || (b.table_width > 0 && !b.table))
         return DFP4_ERR_NULL;
@@ -523,12 +530,16 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
     return launch_paged_read(cache, batch, k, v, dtype, static_cast<hipStream_t>(stream));
 }
 
-static bool grouped(const dfp4_cache& cache, int64_t heads) { return heads > 0 && heads <= (1 << 16) && heads % cache.kv_heads == 0; }
+static int check_attention_sizes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
+    const int rc = check_paged_sizes(cache, batch);
+    if (rc != DFP4_OK) return rc;
+    const bool good = heads > 0 && heads <= (1 << 16) && heads % cache.kv_heads == 0 && batch.tokens * heads <= (int64_t)1 << 30 && window >= 0 &&
+                      window <= (int64_t)1 << 30;
+    return good ? DFP4_OK : DFP4_ERR_SHAPE;
+}
 
 size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window) {
-    if (cell_bytes(cache.head_dim) == 0 || cache.kv_heads < 1 || cache.page_tokens < 32 || batch.batch < 1 || batch.tokens < 1 || batch.table_width < 0 || window < 0 ||
-        !grouped(cache, heads))
-        return 0;
+    if (check_attention_sizes(cache, batch, heads, window) != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return 0;
     return paged_attention_workspace_bytes(cache, batch, heads, window);
 }
 
@@ -536,8 +547,8 @@ int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride,
                          float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     int rc = check_paged(cache, batch);
-    if (rc == DFP4_OK && (!grouped(cache, heads) || batch.tokens * heads > (int64_t)1 << 30 || window < 0 || window > (int64_t)1 << 30 || !(softcap >= 0.0f && softcap <= 1e30f)))
-        rc = DFP4_ERR_SHAPE;
+    if (rc == DFP4_OK) rc = check_attention_sizes(cache, batch, heads, window);
+    if (rc == DFP4_OK && !(softcap >= 0.0f && softcap <= 1e30f)) rc = DFP4_ERR_SHAPE;
     if (rc != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return rc;
     if ((rc = check_rows(q, q_stride, q_head_stride)) != DFP4_OK || (rc = check_rows(out, out_stride, out_head_stride)) != DFP4_OK) return rc;
     if (!aligned(slopes, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return DFP4_ERR_ALIGN;

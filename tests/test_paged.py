@@ -696,3 +696,22 @@ def test_norm_rope_of_more_tokens_than_a_launch_holds():
         assert (np.abs(q[at:at + 8].double().cpu().numpy() - want) <= (HALF + 20 * 2.0 ** -24) * np.abs(want)).all()
     q[places[1]:places[1] + 8], q[-8:], q[:8] = q[1000], q[1000], q[1000]
     assert bool((q == q[1000]).all())
+
+
+BIG = 1 << 62
+
+
+@pytest.mark.parametrize("cache,batch,heads,window", [
+    (dict(kv_heads=8), dict(batch=1 << 20), 8, 0), ({}, dict(batch=1 << 23), 2, 0), (dict(page_tokens=BIG), {}, 2, 0), ({}, dict(table_width=BIG), 2, 0),
+    ({}, dict(tokens=BIG), 2, 0), (dict(kv_heads=BIG), {}, BIG, 0), ({}, dict(batch=BIG), 2, 0), ({}, {}, 2, BIG), ({}, {}, BIG, 0),
+    ({}, dict(tokens=1 << 30), 4, 0), (dict(n_pages=BIG), {}, 2, 0), ({}, dict(max_new=-1), 2, 0), (dict(page_tokens=40), {}, 2, 0)])
+def test_sizes_that_no_launch_holds_are_refused_before_one(cache, batch, heads, window):
+    """The call and the question for its workspace refuse the same sizes."""
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    batch = dict(dict(table_width=1 << 12), **batch)
+    c, b = _cache(**cache), _batch(**batch)
+    assert lib.dfp4_paged_attention_workspace_bytes(c, b, heads, window) == 0
+    assert lib.dfp4_paged_attention(vp(16), 256, 64, heads, c, b, 1.0, 0.0, window, vp(0), vp(16), 256, 64, vp(0), vp(16), BIG, vp(0)) == -2
+    if heads != BIG and window != BIG and batch.get("tokens") != 1 << 30:
+        assert lib.dfp4_paged_write(vp(16), 128, 64, vp(16), 128, 64, c, b, vp(0)) == -2
+        assert lib.dfp4_paged_read(c, b, vp(16), vp(16), 1, vp(0)) == -2
