@@ -108,7 +108,20 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Launch p) {
             const bool is_q = h < a.heads;
             if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
                 // (lanes of a head that are beyond head_dim hold zeros)
-                const float r = __builtin_amdgcn_rsqf(head_sum<LANES>(sum) * per + a.eps);
+                float mean = head_sum<LANES>(sum) * per + a.eps;
+                if (__any(mean < 0x1p-100f || mean == __builtin_inff())) {
+                    // squares beyond the range of fp32 (from |x| of about 2^60 on, or below 2^-50 with as small an eps): of numbers
+                    // scaled by a power of two
+                    const float by = mean == __builtin_inff() ? 0x1p-70f : mean < 0x1p-100f ? 0x1p100f : 1.0f;
+                    sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] *= by;
+                        sum += x[j] * x[j];
+                    }
+                    mean = head_sum<LANES>(sum) * per + a.eps * by * by;
+                }
+                const float r = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= r * (is_q ? wq[j] : wk[j]);
             }

@@ -715,3 +715,30 @@ def test_sizes_that_no_launch_holds_are_refused_before_one(cache, batch, heads, 
     if heads != BIG and window != BIG and batch.get("tokens") != 1 << 30:
         assert lib.dfp4_paged_write(vp(16), 128, 64, vp(16), 128, 64, c, b, vp(0)) == -2
         assert lib.dfp4_paged_read(c, b, vp(16), vp(16), 1, vp(0)) == -2
+
+
+# ---- norms of numbers whose squares leave fp32 ----------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 192, 256])
+@pytest.mark.parametrize("eps", [0.0, 1e-38, 1e-30, 1e-5])
+def test_norms_at_the_ends_of_bf16(dim, eps):
+    """Heads of every size beside each other, some of few large numbers among tiny ones."""
+    g = torch.Generator().manual_seed(dim)
+    sizes = [2.0 ** e for e in (-132, -126, -100, -64, -62, -50, -45, 0, 40, 60, 62, 64, 100, 124)]
+    x = torch.randn(3, 2 * len(sizes), dim, generator=g).double()
+    for h, size in enumerate(sizes):
+        x[:, [h, len(sizes) + h]] *= size
+    x[1, :, 1:] *= 2.0 ** -40
+    x = x.bfloat16()
+    x[..., 0] = torch.where(x[..., 0] == 0, torch.tensor(2.0 ** -133).bfloat16(), x[..., 0])      # (no head of zeros: 0 / 0 where eps is 0)
+    assert torch.isfinite(x).all()
+    pos, freq = torch.tensor([0, 5, 90000], dtype=torch.int32), (1.0 / 10000.0 ** (torch.arange(0, 32, 2).double() / 32)).float()
+    w = 1 + 0.3 * torch.randn(dim, generator=g)
+    for wq, wk in ((w, w), (w, None)):
+        d = x.cuda()
+        q, k = dfp4.norm_rope(d[:, :len(sizes)], d[:, len(sizes):], pos.cuda(), freq.cuda(), wq.cuda(), None if wk is None else wk.cuda(), eps=eps)
+        for got, part, weight in ((q, x[:, :len(sizes)], wq), (k, x[:, len(sizes):], wk)):
+            want, size = _rope(part, weight, pos, freq, False, float(np.float32(eps)))
+            # the same bound as for ordinary numbers, and half a step of the smallest ones
+            assert (np.abs(got.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size + 2.0 ** -134).all()
