@@ -367,8 +367,12 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
  * The cache: a pool of pages of `page_tokens` tokens (a multiple of 32, at most 2^20), each with all KV heads.  Per page, KV head and 32
  * tokens it holds one cell of dfp4_paged_cell_bytes(head_dim) bytes (4.375 bits an element, some padding), whose layout is
  * private to the library.  Values of a sequence's last length % 32 tokens are bf16 in the sequence's slot of `residual`.
+ * With two chunks a slot it also keeps those of the chunk before, which are in the cache in 4 bits: then the length may be taken back (drafted
+ * tokens that are not accepted) by up to 32 tokens from the largest that it has had, and written again from there.  With one a length
+ * is taken back within its incomplete chunk only.  (To a multiple of 32: always.)
  *   pages     device, [n_pages, kv_heads, page_tokens / 32, cell], 256-byte aligned
- *   residual  device, bf16 [n_slots, kv_heads, head_dim, 32], 16-byte aligned
+ *   residual  device, bf16 [n_slots, kv_heads, slot_chunks, head_dim, 32], 16-byte aligned; chunk c of a sequence is at c % slot_chunks
+ *   slot_chunks  2, or 1 (0 counts as 1)
  *   head_dim  64, 96, 128, 192 or 256
  * Neither need be cleared before use.
  *
@@ -389,7 +393,7 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
 typedef struct dfp4_cache {
     uint8_t* pages;
     uint16_t* residual;
-    int64_t n_pages, page_tokens, n_slots, kv_heads, head_dim;
+    int64_t n_pages, page_tokens, n_slots, kv_heads, head_dim, slot_chunks;
 } dfp4_cache;
 
 typedef struct dfp4_batch {
@@ -408,8 +412,7 @@ size_t dfp4_paged_cell_bytes(int64_t head_dim);
  *   k, v     device, bf16 [tokens, kv_heads, head_dim]: token strides k_stride, v_stride and head strides k_head_stride,
  *            v_head_stride in elements (multiples of 8), 16-byte aligned
  * The values of a chunk that these tokens make whole are quantized together with those that the slot holds; values of a chunk that
- * stays incomplete go to the slot.  So a sequence's tokens are written in order, and a length is taken back only within its
- * incomplete chunk.
+ * stays incomplete go to the slot.  So a sequence's tokens are written in order, from a length on that the slot allows (above).
  */
 int dfp4_paged_write(const void* k, int64_t k_stride, int64_t k_head_stride, const void* v, int64_t v_stride, int64_t v_head_stride,
                      dfp4_cache cache, dfp4_batch batch, void* stream);

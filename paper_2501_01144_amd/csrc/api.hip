@@ -482,7 +482,7 @@ size_t dfp4_gemm_requant_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 // ---- serving operators over the paged cache -------------------------------------------------------------------------------
 
 static int check_paged_sizes(const dfp4_cache& c, const dfp4_batch& b) {
-    if (cell_bytes(c.head_dim) == 0 || c.page_tokens < 32 || c.page_tokens % 32 != 0 || c.n_pages < 0 || c.n_slots < 0 || c.kv_heads < 1)
+    if (cell_bytes(c.head_dim) == 0 || c.page_tokens < 32 || c.page_tokens % 32 != 0 || c.n_pages < 0 || c.n_slots < 0 || c.slot_chunks < 0 || c.slot_chunks > 2 || c.kv_heads < 1)
         return DFP4_ERR_SHAPE;
     if (b.batch < 0 || b.table_width < 0 || b.tokens < 0 || b.max_new < 0 || b.max_length < 0) return DFP4_ERR_SHAPE;
     // (a workgroup of up to 512 threads for each sequence and KV head, and a launch has fewer than 2^32 threads)

@@ -519,7 +519,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                     l += x[i];
                 }
                 split8(x, p_hi, p_lo);
-                const uint16_t* v = residual<D>(p, s.slot, kv_head);
+                const uint16_t* v = residual<D>(p, s.slot, kv_head, r.whole);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const uint4 w = *reinterpret_cast<const uint4*>(v + (16u * j + c) * 32u + 8u * g);
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
                 const bool here = (there >> (piece / DT)) & 1u;
                 expand_bf16<2>(&v_code[n].x, table[(v_id[n] >> (4u * (d & 1u))) & 15u], here ? v_scale[n] : 127u, v);
                 if (here && chunk >= r.whole) {
-                    const uint16_t* from = residual<D>(p, s.slot, kv_head) + d * 32u + h * 16u;
+                    const uint16_t* from = residual<D>(p, s.slot, kv_head, chunk) + d * 32u + h * 16u;
                     const int left = s.length - 32 * chunk - 16 * (int)h;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {

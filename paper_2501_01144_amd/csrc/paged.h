@@ -54,12 +54,12 @@ struct PagedArgs {
     uint8_t* pages;
     uint16_t* residual;
     const int32_t *cu, *lengths, *table, *slots;
-    int n_pages, n_slots, page_chunks, kv_heads, batch, width, tokens;
+    int n_pages, n_slots, slot_chunks, page_chunks, kv_heads, batch, width, tokens;
     PageDivision pages_of;           // by page_chunks
 };
 
 inline PagedArgs paged_args(const dfp4_cache& c, const dfp4_batch& b) {
-    return PagedArgs{c.pages, c.residual, b.cu_tokens, b.lengths, b.table, b.slots, (int)c.n_pages, (int)c.n_slots,
+    return PagedArgs{c.pages, c.residual, b.cu_tokens, b.lengths, b.table, b.slots, (int)c.n_pages, (int)c.n_slots, c.slot_chunks == 2 ? 2 : 1,
                      (int)(c.page_tokens / 32), (int)c.kv_heads, (int)b.batch, (int)b.table_width, (int)b.tokens,
                      page_division((uint32_t)(c.page_tokens / 32))};
 }
@@ -128,10 +128,10 @@ __device__ __forceinline__ Four four_cells(const PagedArgs& p, int head, int chu
     return Four{one(0, pages.n0), one(1, pages.n1), one(2, pages.n2), one(3, pages.n3)};
 }
 
-// bf16 [head_dim, 32] of a slot
+// a chunk's bf16 [head_dim, 32] in a slot: chunks take its places in turn
 template <int D>
-__device__ __forceinline__ uint16_t* residual(const PagedArgs& p, int slot, int head) {
-    return p.residual + ((int64_t)slot * p.kv_heads + head) * (D * 32);
+__device__ __forceinline__ uint16_t* residual(const PagedArgs& p, int slot, int head, int chunk) {
+    return p.residual + (((int64_t)slot * p.kv_heads + head) * p.slot_chunks + (chunk & (p.slot_chunks - 1))) * (D * 32);
 }
 
 int launch_paged_write(const void* k, int64_t ks, int64_t khs, const void* v, int64_t vs, int64_t vhs, const dfp4_cache& cache,

@@ -34,9 +34,9 @@ __device__ __forceinline__ uint32_t key_meta(uint32_t token, uint32_t per_key, u
 __device__ __forceinline__ uint32_t next_quad(uint32_t v) { return (uint32_t)__shfl_xor((int)v, 4); }
 __device__ __forceinline__ uint32_t quad_after(uint32_t v, uint32_t lanes) { return (uint32_t)__shfl_down((int)v, lanes); }
 
-// One workgroup: one KV head's share of one chunk of 32 positions of one sequence.  The workgroup of a sequence's first touched
-// chunk also puts the values of the incomplete last chunk into the slot, after it has read what the slot held (both may be in
-// one call, and in the same place).
+// One workgroup: one KV head's share of one chunk of 32 positions of one sequence.  The values of the last chunks also go to the slot (two:
+// so many that the length may be taken back by 32 tokens; one: the incomplete chunk's), by their own workgroup, except where the
+// first touched chunk's older values still lie in the same place: that chunk's workgroup does it then, after it has read them.
 // A key's block is a quad of lanes; lanes of a token are a power of two, so that blocks p and p + 2, whose dialects share a byte,
 // are in one wave.  A chunk of values is turned through LDS.
 template <int D>
@@ -58,11 +58,13 @@ __global__ __launch_bounds__(kThreads) void paged_write_kernel(WriteArgs a) {
     const uint16_t* kh = a.k + head * a.k_head_stride;
     const uint16_t* vh = a.v + head * a.v_head_stride;
     auto row = [&](int position) { return (int64_t)(s.first + position - start); };          // of the dense arrays
+    const int places = a.paged.slot_chunks, first_kept = s.slot < 0 ? last + 1 : places > 1 ? max(s.length - 32, 0) / 32 : s.length / 32;
+    auto first_stores = [&](int chunk) { return chunk >= first_kept && chunk > first && (from & 31) != 0 && (chunk - first) % places == 0; };
 
     for (int chunk = first + (int)blockIdx.y; chunk <= last; chunk += (int)gridDim.y) {
         uint8_t* const at = cell<D>(a.paged, b, head, chunk);
         const int lo = max(from, chunk * 32), hi = min(s.length, chunk * 32 + 32);
-        const bool whole = hi == chunk * 32 + 32;
+        const bool whole = hi == chunk * 32 + 32, in_slot = chunk >= first_kept && !first_stores(chunk);
         __syncthreads();                                             // tables; s_v of the chunk before
         if (whole) {
             const int old = lo - chunk * 32;                         // values that the slot holds (the first chunk's)
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void paged_write_kernel(WriteArgs a) {
                 dst[0] = x.x; dst[1] = x.y; dst[2] = x.z; dst[3] = x.w;
             }
             if (old > 0) {
-                const uint16_t* r = s.slot >= 0 ? residual<D>(a.paged, s.slot, head) : nullptr;
+                const uint16_t* r = s.slot >= 0 ? residual<D>(a.paged, s.slot, head, chunk) : nullptr;
                 for (uint32_t i = tid; i < D * 4u; i += kThreads) {  // eight tokens of a d
                     const uint32_t d = i >> 2, t = (i & 3u) * 8u;
                     if ((int)t >= old) continue;
@@ -115,6 +117,7 @@ __global__ __launch_bounds__(kThreads) void paged_write_kernel(WriteArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     w[j] = (uint32_t)s_v[(sub * 8u + 2 * j) * kPitch + d] | ((uint32_t)s_v[(sub * 8u + 2 * j + 1) * kPitch + d] << 16);
+                if (in_slot) *reinterpret_cast<uint4*>(residual<D>(a.paged, s.slot, head, chunk) + i * 8u) = make_uint4(w[0], w[1], w[2], w[3]);
                 uint32_t code, ebyte, dial;
                 dfp4_pass_small(make_uint4(w[0], w[1], w[2], w[3]), lds_v, lds_i, code, ebyte, dial);
                 const uint32_t beside = next_quad(dial);             // d ^ 1's
@@ -127,10 +130,12 @@ __global__ __launch_bounds__(kThreads) void paged_write_kernel(WriteArgs a) {
                 }
             }
         }
-        if (chunk == first && (s.length & 31) != 0 && s.slot >= 0) {
-            uint16_t* r = residual<D>(a.paged, s.slot, head);
-            const int t0 = max(from, last * 32);
-            for (uint32_t i = tid; i < (uint32_t)(s.length - t0) * D; i += kThreads) {
+        // (16 bytes of a whole chunk's values went to the slot from the registers above)
+        for (int c = max(chunk, first_kept); c <= last; ++c) {
+            if (!(c == chunk ? in_slot && !whole : chunk == first && first_stores(c))) continue;
+            uint16_t* r = residual<D>(a.paged, s.slot, head, c);
+            const int t0 = max(from, c * 32), n = min(s.length, c * 32 + 32) - t0;
+            for (uint32_t i = tid; i < (uint32_t)n * D; i += kThreads) {
                 const uint32_t t = i / D, d = i % D;
                 r[d * 32u + ((uint32_t)(t0 & 31) + t)] = vh[row(t0 + (int)t) * a.v_stride + d];
             }
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void paged_read_kernel(ReadArgs a) {
                 for (int j = 0; j < 8; ++j) x[j] = (uint16_t)(as_u(v[j]) >> 16);
             } else {
                 const bool there = at && s.slot >= 0;
-                const uint4 w = there ? *reinterpret_cast<const uint4*>(residual<D>(a.paged, s.slot, head) + d * 32u + sub * 8u) : make_uint4(0, 0, 0, 0);
+                const uint4 w = there ? *reinterpret_cast<const uint4*>(residual<D>(a.paged, s.slot, head, chunk) + d * 32u + sub * 8u) : make_uint4(0, 0, 0, 0);
                 const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));

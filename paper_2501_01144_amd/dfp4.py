@@ -29,7 +29,7 @@ class _CTensor(ctypes.Structure):
 
 class _CCache(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64),
-                ("n_slots", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+                ("n_slots", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("slot_chunks", ctypes.c_int64)]
 
 
 class _CBatch(ctypes.Structure):

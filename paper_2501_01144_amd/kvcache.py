@@ -71,7 +71,11 @@ class ValueCache:
 
 class PagedCache:
     """Pages of `page_tokens` tokens (a multiple of 32) in 4 bits, and slots for the values of incomplete chunks of 32 tokens, which
-    are bf16 until the chunk is whole: one slot for a sequence as long as it lives."""
+    are bf16 until the chunk is whole: one slot for a sequence as long as it lives.  A slot also keeps the chunk before, so that a length may
+    be taken back (drafted tokens that are not accepted) by up to SLOT_CHUNKS * 32 - 32 tokens from the largest that it has had: give the
+    next batch the smaller length, the tokens after it are written again."""
+
+    SLOT_CHUNKS = 2
 
     def __init__(self, n_pages, page_tokens, kv_heads, head_dim, n_slots, device):
         cell = dfp4.paged_cell_bytes(head_dim)
@@ -79,9 +83,9 @@ class PagedCache:
         assert page_tokens > 0 and page_tokens % BLOCK == 0 and kv_heads > 0 and n_pages >= 0 and n_slots >= 0
         self.n_pages, self.page_tokens, self.kv_heads, self.head_dim, self.n_slots = n_pages, page_tokens, kv_heads, head_dim, n_slots
         self.pages = torch.zeros((n_pages, kv_heads, page_tokens // BLOCK, cell), dtype=torch.uint8, device=device)
-        self.residual = torch.zeros((n_slots, kv_heads, head_dim, BLOCK), dtype=torch.bfloat16, device=device)
+        self.residual = torch.zeros((n_slots, kv_heads, self.SLOT_CHUNKS, head_dim, BLOCK), dtype=torch.bfloat16, device=device)
         self.c = dfp4._CCache(self.pages.data_ptr() if n_pages else 0, self.residual.data_ptr() if n_slots else 0, n_pages, page_tokens,
-                              n_slots, kv_heads, head_dim)
+                              n_slots, kv_heads, head_dim, self.SLOT_CHUNKS)
         self.at = ctypes.addressof(self.c)       # for the native module
 
 

@@ -742,3 +742,56 @@ def test_norms_at_the_ends_of_bf16(dim, eps):
             want, size = _rope(part, weight, pos, freq, False, float(np.float32(eps)))
             # the same bound as for ordinary numbers, and half a step of the smallest ones
             assert (np.abs(got.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size + 2.0 ** -134).all()
+
+
+# ---- lengths that are taken back ------------------------------------------------------------------------------------------------
+
+def test_slots_hold_one_or_two_chunks():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    for chunks, rc in ((0, 0), (1, 0), (2, 0), (3, -2), (-1, -2)):
+        c, b = _cache(), _batch(tokens=0)
+        c.slot_chunks = chunks
+        assert lib.dfp4_paged_write(vp(16), 128, 64, vp(16), 128, 64, c, b, vp(0)) == lib.dfp4_paged_read(c, b, vp(16), vp(16), 1, vp(0)) == rc
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("chunks", [1, 2])
+@pytest.mark.parametrize("most", [4, 32, 75])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_drafted_tokens_are_taken_back(dim, most, chunks):
+    """Every step writes up to `most` tokens a sequence of which the last ones are wrong, and the next goes on after the last right one."""
+    s = Sequences([400, 330], dim, 2, 64, seed=most + chunks)
+    s.cache.c.slot_chunks = chunks                       # (with one: the same memory, half of it used)
+    lengths, s.lengths, at, largest = s.lengths, [0, 0], [0, 0], [0, 0]
+    k, v, s.k, s.v = s.k, s.v, None, None
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=s.g))  # noqa: E731
+    crossed = 0
+    for step in range(30 if most > 4 else 90):
+        new = [min(draw(0, most), lengths[b] - at[b]) for b in range(2)]
+        after = [at[b] + new[b] for b in range(2)]
+        largest = [max(largest[b], after[b]) for b in range(2)]
+        lowest = [largest[b] - 32 if chunks == 2 else largest[b] // 32 * 32 for b in range(2)]
+        right = [draw(max(at[b], lowest[b]), after[b]) if after[b] >= lowest[b] else after[b] for b in range(2)]
+        rows = []
+        for x in (k, v):
+            parts = [x[b][at[b]:after[b]].clone() for b in range(2)]
+            for b in range(2):
+                parts[b][right[b] - at[b]:] = 100.0
+            rows.append(torch.cat(parts).cuda())
+        if sum(new):
+            dfp4.paged_write(*rows, s.cache, s.batch(new, after))
+        crossed += sum(right[b] // 32 < after[b] // 32 and right[b] % 32 != 0 for b in range(2))
+        at = s.lengths = right
+        s.k, s.v = [x[:n] for x, n in zip(k, at)], [x[:n] for x, n in zip(v, at)]
+        _check_read(s, at, at, torch.bfloat16)
+        _attend(s, [min(n, 3) for n in at], 4)
+    assert (crossed > 0) == (chunks == 2)
+    # many rows, over an incomplete chunk that was whole before
+    s = Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40)
+    longer = [n + 32 for n in s.lengths]
+    true_k, true_v = s.k, s.v
+    s.k, s.v = ([torch.cat([x, torch.full((32, 2, dim), 50.0).bfloat16()]) for x in y] for y in (true_k, true_v))
+    s.write(longer, longer)
+    s.k, s.v = true_k, true_v
+    _check_read(s, s.lengths, s.lengths, torch.bfloat16)
+    _attend(s, [90, 33, 3, 0, 64], 8, max_new=90)
