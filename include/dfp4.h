@@ -437,6 +437,8 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  * 8 bits) and a probability as the sum of two bf16 numbers, or where there are many rows as one.
  */
 size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
+/* The query rows (new tokens times heads of a group) that a workgroup of that call takes: 16, or 256 where there are many; 0: no call. */
+int dfp4_paged_attention_rows(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
 int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
                          float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);

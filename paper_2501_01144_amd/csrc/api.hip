@@ -543,6 +543,11 @@ size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, 
     return paged_attention_workspace_bytes(cache, batch, heads, window);
 }
 
+int dfp4_paged_attention_rows(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window) {
+    if (check_attention_sizes(cache, batch, heads, window) != DFP4_OK || batch.batch == 0 || batch.tokens == 0) return 0;
+    return paged_attention_rows(cache, batch, heads, window);
+}
+
 int dfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t heads, dfp4_cache cache, dfp4_batch batch,
                          float scale, float softcap, int64_t window, const float* slopes, void* out, int64_t out_stride,
                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {

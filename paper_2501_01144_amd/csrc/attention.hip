@@ -1020,6 +1020,13 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
     }
 }
 
+// New tokens of the sequence with most, or, where the caller does not know, of one with as many as the others: 48 sequences with one token
+// each, 32 heads of 128 on 8, 8192 keys: 100 us, taken for one sequence's 48 tokens 250 (256 rows a workgroup).
+int64_t likely_new(const dfp4_batch& b) {
+    if (b.max_new == 0) return (b.tokens + b.batch - 1) / b.batch;
+    return b.max_new < b.tokens ? b.max_new : b.tokens;
+}
+
 struct Split {
     int rows, blocks;            // query rows of a workgroup, workgroups along them
     int splits, steps;           // workgroups along the keys, steps of 128 keys of each
@@ -1028,7 +1035,7 @@ struct Split {
 // first; `at_once` of them run at a time.  Of the numbers of parts that fill the chip once, twice, three or four times the one whose
 // (times) x (rounds + that) is least.
 Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
-    const int64_t new_tokens = batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens;
+    const int64_t new_tokens = likely_new(batch);
     int64_t most = batch.table_width * cache.page_tokens;
     if (batch.max_length > 0 && batch.max_length < most) most = batch.max_length;
     const int64_t new_rows = new_tokens * (heads / cache.kv_heads);
@@ -1041,6 +1048,12 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
                       batch.batch * cache.kv_heads * ((new_rows + 15) / 16) * ((keys + 511) / 512) > 5 * (int64_t)device_cu_count();
     const int64_t rows = wide ? 256 : 16;
     int64_t blocks = (new_rows + rows - 1) / rows;
+    if (batch.max_new == 0) {
+        // one sequence may have most of the rows: workgroups for as many as it could have, of which those without rows cost 0.6 ns each
+        const int64_t could = (batch.tokens * (heads / cache.kv_heads) + rows - 1) / rows, cheap = (wide ? 16384 : 4096) / (batch.batch * cache.kv_heads);
+        const int64_t more = could < cheap ? could : cheap;
+        if (more > blocks) blocks = more;
+    }
     if (blocks > 65535) blocks = 65535;
     const int64_t seen = (rows + heads / cache.kv_heads - 1) / (heads / cache.kv_heads) + window + 31;      // by a block of rows, with a window
     if (window > 0 && seen < most) most = seen;
@@ -1063,6 +1076,10 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
 }
 
 }  // namespace
+
+int paged_attention_rows(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
+    return choose_split(cache, batch, heads, window).rows;
+}
 
 size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window) {
     const Split sp = choose_split(cache, batch, heads, window);
@@ -1089,7 +1106,7 @@ int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_
             else hipLaunchKernelGGL((paged_attention_kernel<kD, false>), grid, dim3(kThreads), 0, stream, a);
         }
         if (sp.splits > 1) {
-            const int64_t rows = (batch.max_new > 0 && batch.max_new < batch.tokens ? batch.max_new : batch.tokens) * a.heads;
+            const int64_t rows = likely_new(batch) * a.heads;
             const int64_t blocks = sp.splits <= kFewParts ? (rows + 1024 / kD - 1) / (1024 / kD) : rows;
             const dim3 join((uint32_t)batch.batch, (uint32_t)(blocks < 65535 ? blocks : 65535));
             if (sp.splits <= kFewParts) hipLaunchKernelGGL((paged_attention_join_few_kernel<kD>), join, dim3(kThreads), 0, stream, a);

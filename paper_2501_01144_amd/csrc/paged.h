@@ -151,6 +151,7 @@ struct AttentionArgs {
     int rows;                        // query rows of a workgroup
 };
 size_t paged_attention_workspace_bytes(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window);
+int paged_attention_rows(const dfp4_cache& cache, const dfp4_batch& batch, int64_t heads, int64_t window);
 int launch_paged_attention(AttentionArgs a, const dfp4_cache& cache, const dfp4_batch& batch, hipStream_t stream);
 
 struct NormRopeArgs {

@@ -48,7 +48,7 @@ SYMBOLS = [
     "dfp4_gemm_native_packed", "mxfp4_gemm_native_packed", "dfp4_gemm_native_splitk_bytes",
     "dfp4_gemm_requant", "mxfp4_gemm_requant", "dfp4_gemm_requant_workspace_bytes", "dfp4_gemm_requant_batched",
     "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_gemm", "dfp4_formatbook", "dfp4_strerror",
-    "dfp4_paged_cell_bytes", "dfp4_paged_write", "dfp4_paged_read", "dfp4_paged_attention_workspace_bytes", "dfp4_paged_attention",
+    "dfp4_paged_cell_bytes", "dfp4_paged_write", "dfp4_paged_read", "dfp4_paged_attention_workspace_bytes", "dfp4_paged_attention_rows", "dfp4_paged_attention",
     "dfp4_norm_rope",
 ]
 
@@ -142,6 +142,8 @@ def load():
     lib.dfp4_paged_read.restype = ci
     lib.dfp4_paged_attention_workspace_bytes.argtypes = [_CCache, _CBatch, i64, i64]
     lib.dfp4_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.dfp4_paged_attention_rows.argtypes = [_CCache, _CBatch, i64, i64]
+    lib.dfp4_paged_attention_rows.restype = ci
     lib.dfp4_paged_attention.argtypes = [vp, i64, i64, i64, _CCache, _CBatch, cf, cf, i64, vp, vp, i64, i64, vp, vp, ctypes.c_size_t, vp]
     lib.dfp4_paged_attention.restype = ci
     lib.dfp4_norm_rope.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, i64, i64, vp, vp, cf, vp, vp, i64, ci, vp, vp, vp]
@@ -632,6 +634,11 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6,
                                  _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), 2 * inv_freq.numel() if inv_freq is not None else 0, 1 if interleaved else 0,
                                  _ptr(q_out), _ptr(k_out), _stream()), "dfp4_norm_rope")
     return q_out, k_out
+
+
+def paged_attention_rows(cache, batch, tokens, heads, window=0):
+    """dfp4_paged_attention_rows: the query rows a workgroup takes of a call with `tokens` new tokens, 16 or 256."""
+    return int(load().dfp4_paged_attention_rows(cache.c, batch.c(tokens), heads, window))
 
 
 def paged_cell_bytes(head_dim):

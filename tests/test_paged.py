@@ -795,3 +795,29 @@ def test_drafted_tokens_are_taken_back(dim, most, chunks):
     s.k, s.v = true_k, true_v
     _check_read(s, s.lengths, s.lengths, torch.bfloat16)
     _attend(s, [90, 33, 3, 0, 64], 8, max_new=90)
+
+
+# ---- what a call takes for its sizes ---------------------------------------------------------------------------------------------
+
+def test_rows_of_a_workgroup():
+    lib = dfp4.load()
+
+    def rows(batch, tokens, max_new=0, heads=32, kv_heads=8, dim=128, context=8192, window=0):
+        return lib.dfp4_paged_attention_rows(_cache(head_dim=dim, kv_heads=kv_heads, page_tokens=64),
+                                             _batch(batch=batch, tokens=tokens, table_width=context // 64, max_new=max_new), heads, window)
+    # one token of many sequences, whether the caller says so or not
+    for batch in (1, 2, 48, 256, 1000):
+        assert rows(batch, batch) == rows(batch, batch, max_new=1) == rows(batch, 3 * batch) == 16
+    # prompts: the same
+    for batch, new in ((1, 2048), (3, 512), (8, 700)):
+        assert rows(batch, batch * new) == rows(batch, batch * new, max_new=new) == 256
+    assert rows(1, 2048, dim=256) == rows(1, 2048, dim=192, max_new=2048) == 16
+    assert rows(0, 5) == rows(5, 0) == rows(4, 4, heads=12) == rows(4, 4, window=-1) == rows(4, 4, dim=80) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[1] * 7, [70, 1, 1, 1, 1, 1, 1], [1, 0, 0, 0, 0, 0, 90]])
+def test_attention_of_batches_that_say_nothing_of_themselves(new):
+    """The kernel is chosen for sequences that are alike; one of them may still have most of the tokens."""
+    s = Sequences([90, 31, 32, 400, 128, 3000, 99], 64, 2, 64, seed=sum(new)).fill()
+    _attend(s, new, 16)
