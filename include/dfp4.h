@@ -433,8 +433,8 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  *   slopes   device, f32 [heads], or NULL;  lse  device, f32 [tokens, heads], or NULL
  *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads, window) bytes, 16-byte aligned (0 where no context
  *            is split, and for sizes that the call refuses)
- * Scores, softmax and sums are in fp32.  The matrix instructions take keys and values as they are, q as the sum of two FP8 numbers (its
- * 8 bits) and a probability as the sum of two bf16 numbers, or where there are many rows as one.
+ * Scores, softmax and sums are in fp32.  The matrix instructions take queries, keys and values as they are.  A probability goes in as the
+ * sum of two bf16 numbers, or where there are many rows as one.
  */
 size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
 /* The query rows (new tokens times heads of a group) that a workgroup of that call takes: 16, or 256 where there are many; 0: no call. */

@@ -170,9 +170,6 @@ def build_library(verbose=True):
     f8_s = os.path.join(objdir, "gemm_f8.s")
     cmd = [hipcc, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, "gemm_f8.hip"), "-o", f8_s]
     procs.append(("gemm_f8.hip (assembly)", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    att_s = os.path.join(objdir, "attention.s")
-    cmd = [hipcc, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, "attention.hip"), "-o", att_s]
-    procs.append(("attention.hip (assembly)", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     # native module of the Python binding: host code only
     import torch
     troot = os.path.dirname(torch.__file__)
@@ -210,7 +207,7 @@ def build_library(verbose=True):
     problems = check_products_free_of_scratch(open(f8_s).read())
     if problems:
         raise RuntimeError("gemm_f8_kernel uses scratch memory among its products:\n" + "\n".join(problems))
-    problems = check_results_apart(open(gemm_s).read() + open(f8_s).read() + open(att_s).read())
+    problems = check_results_apart(open(gemm_s).read() + open(f8_s).read())
     if problems:
         raise RuntimeError("block-scaled products whose result overlaps an operand:\n" + "\n".join(problems))
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]

@@ -1,13 +1,14 @@
 // Attention of new tokens over the paged 4-bit cache (formulas and layouts: include/dfp4.h, paged.h).
 //
 // Rows of a (sequence, KV head) are its new tokens times the query heads of the group, so that they share keys and values.
-// With tokens as rows and query rows as columns, softmax statistics of a query are one number a lane:
-//   S^T = K Q^T, on the block-scaled instruction 16 x 16 x 128 in FP8.  Every DialectFP4 magnitude 0.5 u is an E4M3 number and a
-//     block's exponent byte is the instruction's scale, so a dword of codes costs eight vector instructions and no multiplication.
-//     A query goes in as the sum of two FP8 numbers (rounded to 4 bits, and what that left: the 8 bits of a bf16).
-//   O^T = V^T P^T, on 16 x 16 x 32 in bf16: the values' FP8 bytes become bf16 with their block's scale in one conversion for two (also
-//     exact), a probability is the sum of two bf16 numbers (one where there are many rows).  (As two FP8 numbers a probability has 8 bits
-//     down to 2^-19 of the largest and fewer below, which shows where the values at the largest are zero.)
+// With tokens as rows and query rows as columns, softmax statistics of a query are one number a lane: S^T = K Q^T and O^T = V^T P^T, both on
+// 16 x 16 x 32 in bf16.  Every DialectFP4 magnitude 0.5 u is an E4M3 number: eight vector instructions make a dword of codes FP8 bytes, and
+// these become bf16 with their block's scale in one conversion for two (exact).  A query goes in as it is, a probability as the sum of two bf16
+// numbers (one where there are many rows; as two FP8 numbers it has 8 bits down to 2^-19 of the largest and fewer below, which shows where the
+// values at the largest are zero).
+// (Keys on the block-scaled instruction in FP8, against a query as the sum of two FP8 numbers, take as many matrix clocks and no conversions: 117
+// instead of 118 us for 48 sequences of 8192, 511 instead of 540 for 2048 tokens over 16384.  But that instruction leaves a score off by up to 2.8e-4 of
+// its largest product, and a query's elements lose bits from 2^-14 of their block's largest on; in bf16 it is off by 2^-21 of sum |q||k|.)
 // Both leave in lane (g, c) rows 4 g .. 4 g + 3 of column c, and O^T may take its 128 tokens in any order.  So row 4 g + i of tile t
 // (0 .. 7) of S^T is token 32 g + 4 t + i of a step of 128: a lane has the scores of the chunk of 32 whose values it expands and
 // whose probabilities it supplies, and nothing moves between lanes.
@@ -24,11 +25,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-typedef short v2s __attribute__((ext_vector_type(2)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
@@ -53,42 +51,9 @@ __device__ __forceinline__ void each(F&& f, std::integer_sequence<int, I...>) { 
 template <int N, class F>
 __device__ __forceinline__ void each(F&& f) { each(f, std::make_integer_sequence<int, N>{}); }
 
-// 16 codes (two dwords in the cell's order) to 16 FP8 bytes
-template <int AT>                                                    // into registers AT .. AT + 3
-__device__ __forceinline__ void expand16(uint2 c, uint2 row, v8i& a) {
-    a[AT] = (int)(__builtin_amdgcn_perm(row.y, row.x, c.x & 0x07070707u) | ((c.x << 4) & 0x80808080u));
-    a[AT + 1] = (int)(__builtin_amdgcn_perm(row.y, row.x, (c.x >> 4) & 0x07070707u) | (c.x & 0x80808080u));
-    a[AT + 2] = (int)(__builtin_amdgcn_perm(row.y, row.x, c.y & 0x07070707u) | ((c.y << 4) & 0x80808080u));
-    a[AT + 3] = (int)(__builtin_amdgcn_perm(row.y, row.x, (c.y >> 4) & 0x07070707u) | (c.y & 0x80808080u));
-}
-
-// four numbers (|x| <= 448) as FP8, and 2^5 times what that leaves as FP8: what rounding to 4 bits leaves is at most 2^-5 of the
-// largest, and so much further down reach the subnormal numbers
-constexpr int kLoShift = 5;
-__device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, int& hi, int& lo) {
-    int h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
-    h = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, h, true);
-    const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-    constexpr float kBy = 1.0f / (1 << kLoShift);                   // the conversion divides by it
-    v2s l = {0, 0};
-    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x0 - a[0], x1 - a[1], kBy, false);
-    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x2 - b[0], x3 - b[1], kBy, true);
-    lo = __builtin_bit_cast(int, l);
-    hi = h;
-}
-
-// c += a (hi + 2^-5 lo), hi times 2^(sb - 127).  The compiler lets a result overlap an operand that it sees no further use of, which the
-// instruction overwrites before it has read it for the last time: operands are in use until the end here (the build checks).
-template <int OPSEL>
-__device__ __forceinline__ void product(const v8i& a, const v8i& hi, const v8i& lo, v4f& c, int sa, int sb, int sb_lo) {
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, c, 0, 0, OPSEL, sa, 0, sb);
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, c, 0, 0, OPSEL, sa, 0, sb_lo);
-    asm("" : "+v"(c) : "v"(a), "v"(hi), "v"(lo));
-}
-
-// N dwords of codes of a scale and a dialect to bf16: fragments of N instructions, tokens 8 q .. 8 q + 7 in the q-th
+// N dwords of codes of a scale and a dialect to bf16: fragments of N instructions, elements 8 q .. 8 q + 7 in the q-th
 template <int N>
-__device__ __forceinline__ void expand_bf16(const uint32_t* w, uint2 row, uint32_t ebyte, v8b (&v)[N]) {
+__device__ __forceinline__ void expand_bf16(const uint32_t* w, uint2 row, uint32_t ebyte, v8b* v) {
     const float scale = as_f(ebyte << 23);                          // the conversion goes by the exponent bits (0: 2^-127)
 #pragma unroll
     for (int q = 0; q < N; ++q) {
@@ -158,46 +123,14 @@ __device__ __forceinline__ Range key_range(const AttentionArgs& a, const Sequenc
     return r;
 }
 
-// A query row's 128 elements from kt * 128 on as this lane's share of an operand (`negative`: their negatives): both FP8 parts, and
-// the scale of block g
-template <int D, int kt>
-__device__ __forceinline__ int load_query(const uint16_t* row, bool ok, bool negative, uint32_t c, uint32_t g, v8i& hi, v8i& lo) {
-    const uint16_t* src = row + kt * 128;
-    uint32_t top = 0;
-    if (ok && (int)g < Cell<D>::blocks(kt)) {
-        const uint4* x = reinterpret_cast<const uint4*>(src + g * 32u);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint4 v = x[j];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) top = max(top, max((w[k] >> 7) & 0xffu, (w[k] >> 23) & 0xffu));
-        }
+// eight elements of a query row (`flip`: with what signs)
+__device__ __forceinline__ v8b query8(const uint16_t* at, bool ok, uint32_t flip) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (ok) {
+        v = *reinterpret_cast<const uint4*>(at);
+        v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
     }
-    const int scale = max((int)top - 7, kLoShift);                  // the largest magnitude becomes less than 2^8
-    each<2>([&](auto h_c) {
-        constexpr int h = decltype(h_c)::value;
-        const uint32_t block = 2u * h + (g >> 1);                   // half g % 2 of it; its scale is another lane's
-        const int by = __shfl(scale, (int)(block * 16u + c));
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (ok && (int)block < Cell<D>::blocks(kt)) v = *reinterpret_cast<const uint4*>(src + block * 32u + (g & 1u) * 16u + k * 8);
-            const uint32_t flip = negative ? 0x80008000u : 0u;
-            const uint32_t w[4] = {v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - by);
-            int a, b;
-            split4(x[0], x[1], x[2], x[3], a, b);
-            hi[4 * h + 2 * k] = a;
-            lo[4 * h + 2 * k] = b;
-            split4(x[4], x[5], x[6], x[7], a, b);
-            hi[4 * h + 2 * k + 1] = a;
-            lo[4 * h + 2 * k + 1] = b;
-        }
-    });
-    return scale;
+    return __builtin_bit_cast(v8b, v);
 }
 
 // What turns scores into exponents to base 2.  Where there is neither cap nor bias (nor a scale of zero) a score stays as it is,
@@ -317,11 +250,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
         const int pos = s.length - s.n + (row_ok ? row / group : 0);
         if (EXTRA && a.slopes) rule.slope = a.slopes[head] * kLog2e;
 
-        v8i q_hi[KT], q_lo[KT];
-        int q_scale[KT];
+        // a lane's elements of the 128 of kt: as its codes lie (paged.h)
+        v8b q[KT][4];
         each<KT>([&](auto kt_c) {
-            constexpr int kt = decltype(kt_c)::value;
-            q_scale[kt] = load_query<D, kt>(a.q + token * a.q_stride + (int64_t)head * a.q_head_stride, row_ok, a.scale < 0.0f, c, g, q_hi[kt], q_lo[kt]);
+            constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
+            const uint16_t* src = a.q + token * a.q_stride + (int64_t)head * a.q_head_stride + kt * 128;
+#pragma unroll
+            for (int n = 0; n < nb; ++n)
+                q[kt][n] = query8(src + (n < 2 ? 16u * g + 8u * n : nb == 3 ? 64u + 8u * g : 64u + 16u * g + 8u * (n - 2)), row_ok, a.scale < 0.0f ? 0x80008000u : 0u);
         });
 
         v4f o[NJ];
@@ -344,29 +280,35 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             return base;
         };
 
-        // scores of a tile: the lane's token is at kc's place `token`
-        auto scores = [&](const uint8_t* kc, uint32_t token, auto t_c, const int (&scale)[KT], const uint32_t (&id)[KT]) {
-            constexpr int t = decltype(t_c)::value;                 // byte of `scale`
+        // scores of a tile: the lane's token is at kc's place `token`; scales and dialects of its blocks g / 2 and 2 + g / 2 (of three: 2)
+        auto scores = [&](const uint8_t* kc, uint32_t token, const uint32_t (&scale)[KT][2], const uint32_t (&id)[KT][2]) {
             v4f acc = v4f{0, 0, 0, 0};
             each<KT>([&](auto kt_c) {
                 constexpr int kt = decltype(kt_c)::value, nb = C::blocks(kt);
                 const uint8_t* row = kc + token * (D / 2) + kt * 64;
-                v8i k8;
+                uint32_t w[4];
                 if constexpr (nb == 4) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(row + g * 16u);
-                    expand16<0>(make_uint2(w.x, w.y), table[id[kt] & 15u], k8);
-                    expand16<4>(make_uint2(w.z, w.w), table[id[kt] >> 4], k8);
+                    const uint4 x = *reinterpret_cast<const uint4*>(row + g * 16u);
+                    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
                 } else {
-                    expand16<0>(*reinterpret_cast<const uint2*>(row + g * 8u), table[id[kt] & 15u], k8);
-                    k8[4] = k8[5] = k8[6] = k8[7] = 0;
-                    // the queries are zero in lanes without a second half; what they read is their own first half
-                    if constexpr (nb == 3) expand16<4>(*reinterpret_cast<const uint2*>(row + (g < 2 ? 32u + g * 8u : g * 8u)), table[id[kt] >> 4], k8);
+                    const uint2 x = *reinterpret_cast<const uint2*>(row + g * 8u);
+                    w[0] = x.x, w[1] = x.y;
+                    if constexpr (nb == 3) w[2] = *reinterpret_cast<const uint32_t*>(row + 32u + g * 4u);
                 }
-                product<t>(k8, q_hi[kt], q_lo[kt], acc, scale[kt], q_scale[kt], q_scale[kt] - kLoShift);
+                v8b k[4];
+                expand_bf16<2>(w, table[id[kt][0]], scale[kt][0], k);
+                if constexpr (nb > 2) expand_bf16<nb - 2>(w + 2, table[id[kt][1]], scale[kt][1], k + 2);
+#pragma unroll
+                for (int n = 0; n < nb; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n], q[kt][n], acc, 0, 0, 0);
             });
             return acc;
         };
-        auto block_of = [&](int kt) { return kt * 4 + min(g, (uint32_t)(C::blocks(kt) - 1)); };
+        // places of the scales and the dialects of a lane's blocks: `half` 0: g / 2, 1: 2 + g / 2 (of three: 2); dialects of blocks p and p + 2 share a byte
+        auto scale_at = [&](int kt, uint32_t half) {
+            const uint32_t block = half == 0 ? g >> 1 : C::blocks(kt) == 3 ? 2u : 2u + (g >> 1);
+            return C::kKExps + ((c & 3u) * C::NB + 4u * kt + block) * 8u;
+        };
+        auto id_at = [&](int kt, uint32_t half) { return C::kKIds + ((c & 3u) * C::NP + kt * 2 + (half == 1 && C::blocks(kt) == 3 ? 0u : g >> 1)) * 8u; };
 
         constexpr int kKeyLoads = 4 * loads_of(C::kKeys), kValueLoads = 4 * loads_of(C::kValues);
         uint8_t* const stage = s_stage + wave * kStage;
@@ -400,22 +342,25 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
             // ---- scores of 128 keys
             float x[8][4];
             {
-                uint2 scales[KT], ids[KT];
+                uint2 scales[KT][2], ids[KT][2];
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    scales[kt] = *reinterpret_cast<const uint2*>(kc + C::kKExps + ((c & 3u) * C::NB + block_of(kt)) * 8u);
-                    ids[kt] = *reinterpret_cast<const uint2*>(kc + C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u);
-                }
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int half = 0; half < (C::blocks(kt) > 2 ? 2 : 1); ++half) {
+                        scales[kt][half] = *reinterpret_cast<const uint2*>(kc + scale_at(kt, half));
+                        ids[kt][half] = half == 1 && C::blocks(kt) == 4 ? ids[kt][0] : *reinterpret_cast<const uint2*>(kc + id_at(kt, half));
+                    }
                 each<8>([&](auto t_c) {
                     constexpr int t = decltype(t_c)::value;
-                    int scale[KT];
-                    uint32_t id[KT];
+                    uint32_t scale[KT][2], id[KT][2];
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        scale[kt] = (int)(t < 4 ? scales[kt].x : scales[kt].y);
-                        id[kt] = ((t < 4 ? ids[kt].x : ids[kt].y) >> (8 * (t & 3))) & 0xffu;
-                    }
-                    const v4f acc = scores(kc, 4u * t + (c & 3u), std::integral_constant<int, t & 3>{}, scale, id);
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int half = 0; half < (C::blocks(kt) > 2 ? 2 : 1); ++half) {
+                            scale[kt][half] = ((t < 4 ? scales[kt][half].x : scales[kt][half].y) >> (8 * (t & 3))) & 0xffu;
+                            id[kt][half] = ((t < 4 ? ids[kt][half].x : ids[kt][half].y) >> (8 * (t & 3) + 4 * half)) & 15u;
+                        }
+                    const v4f acc = scores(kc, 4u * t + (c & 3u), scale, id);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[t][i] = acc[i];
                 });
@@ -492,14 +437,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
                 each<2>([&](auto t_c) {
                     constexpr int t = decltype(t_c)::value;
                     const uint32_t token_in = 8u * (c >> 2) + 4u * t + (c & 3u);
-                    int scale[KT];
-                    uint32_t id[KT];
+                    uint32_t scale[KT][2], id[KT][2];
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        scale[kt] = kc[C::kKExps + ((c & 3u) * C::NB + block_of(kt)) * 8u + (token_in >> 2)];
-                        id[kt] = kc[C::kKIds + ((c & 3u) * C::NP + kt * 2 + (g >> 1)) * 8u + (token_in >> 2)];
-                    }
-                    const v4f acc = scores(kc, token_in, std::integral_constant<int, 0>{}, scale, id);
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int half = 0; half < (C::blocks(kt) > 2 ? 2 : 1); ++half) {
+                            scale[kt][half] = kc[scale_at(kt, half) + (token_in >> 2)];
+                            id[kt][half] = (kc[id_at(kt, half) + (token_in >> 2)] >> (4 * half)) & 15u;
+                        }
+                    const v4f acc = scores(kc, token_in, scale, id);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[4 * t + i] = acc[i];
                 });
@@ -593,9 +539,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Many query rows (head_dim up to 128): a workgroup expands every step of 128 keys once into LDS, as the operands that all its waves read (keys in FP8,
-// values in bf16), and each wave does both products for 32 rows, on 32 x 32 x 64 and 32 x 32 x 16: a query is a column again,
-// now of two lanes (h, c).  They hold rows 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
+// Many query rows (head_dim up to 128): a workgroup expands every step of 128 keys once into LDS, as the operands that all its waves read,
+// and each wave does both products for 32 rows, on 32 x 32 x 16: a query is a column again, now of two lanes (h, c).  They hold rows 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
 // 16 h + 4 a + i of a chunk, so that a lane supplies the probabilities of the 16 tokens whose scores it has, eight to an instruction.
 // A chunk is a tile: its cell, and whether it is there, are the same for all lanes.
 // Codes of the next step are loaded while this one is multiplied, and expanded into the other half of LDS: one barrier a step.
@@ -610,16 +555,17 @@ template <int D>
 struct Wide {
     static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32 * kWaves;
     static constexpr int NC = 4;                                     // chunks of a step
-    static constexpr int KS = (D + 63) / 64, DT = D / 32;            // instructions that add over a key, tiles of V^T
+    static constexpr int KS = (D + 63) / 64, DT = D / 32;            // pieces of 64 elements of a key, tiles of V^T
     static constexpr int KP = (NC * KS + kWaves - 1) / kWaves, VP = (NC * DT + kWaves - 1) / kWaves;      // pieces that a wave expands
-    static constexpr uint32_t kK = NC * KS * 2048, kV = NC * DT * 2048, kScales = KS * 256, kStep = kK + kV + kScales;
+    static constexpr int KI = D / 16;                                // instructions that add over a key
+    static constexpr uint32_t kK = NC * KI * 1024, kV = NC * DT * 2048, kStep = kK + kV;
 };
 
 template <int D, bool EXTRA>
 __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_kernel(AttentionArgs a) {
     using C = Cell<D>;
     using W = Wide<D>;
-    constexpr int KS = W::KS, DT = W::DT, NC = W::NC, KP = W::KP, VP = W::VP;
+    constexpr int KS = W::KS, KI = W::KI, DT = W::DT, NC = W::NC, KP = W::KP, VP = W::VP;
     __shared__ __attribute__((aligned(16))) uint8_t s_x[2 * W::kStep];
     __shared__ __attribute__((aligned(16))) uint8_t s_rows[kDialects * 8];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 31u, h = lane >> 5;
@@ -645,45 +591,12 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
         Scores<EXTRA> rule(a);
         if (EXTRA && a.slopes) rule.slope = a.slopes[head] * kLog2e;
 
-        // ---- queries: halves h of blocks 2 ks and 2 ks + 1, the scale of block 2 ks + h
-        v8i q_hi[KS], q_lo[KS];
-        int q_scale[KS];
+        // ---- queries: halves h of all blocks
+        v8b q[KI];
         {
             const uint16_t* src = a.q + (int64_t)(s.first + held / group) * a.q_stride + (int64_t)head * a.q_head_stride;
-            const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
-            each<KS>([&](auto ks_c) {
-                constexpr int ks = decltype(ks_c)::value;
-                uint4 v[2][2];
-                uint32_t top[2] = {0, 0};
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        v[y][k] = make_uint4(0, 0, 0, 0);
-                        if (row < rows && 2 * ks + y < C::NB) v[y][k] = *reinterpret_cast<const uint4*>(src + (2 * ks + y) * 32 + h * 16u + k * 8);
-                        const uint32_t w[4] = {v[y][k].x, v[y][k].y, v[y][k].z, v[y][k].w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) top[y] = max(top[y], max((w[j] >> 7) & 0xffu, (w[j] >> 23) & 0xffu));
-                    }
-                    top[y] = max(top[y], (uint32_t)__shfl_xor((int)top[y], 32));
-                    top[y] = (uint32_t)max((int)top[y] - 7, kLoShift);          // the largest magnitude becomes less than 2^8
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint32_t w[4] = {v[y][k].x ^ flip, v[y][k].y ^ flip, v[y][k].z ^ flip, v[y][k].w ^ flip};
-                        float x[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = ldexpf(as_f((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16), 127 - (int)top[y]);
-                        int hi, lo;
-                        split4(x[0], x[1], x[2], x[3], hi, lo);
-                        q_hi[ks][4 * y + 2 * k] = hi;
-                        q_lo[ks][4 * y + 2 * k] = lo;
-                        split4(x[4], x[5], x[6], x[7], hi, lo);
-                        q_hi[ks][4 * y + 2 * k + 1] = hi;
-                        q_lo[ks][4 * y + 2 * k + 1] = lo;
-                    }
-                }
-                q_scale[ks] = (int)(h ? top[1] : top[0]);
-            });
+            for (int n = 0; n < KI; ++n) q[n] = query8(src + n / 2 * 32 + h * 16u + n % 2 * 8, row < rows, a.scale < 0.0f ? 0x80008000u : 0u);
         }
         v16f o[DT];
 #pragma unroll
@@ -694,7 +607,7 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
 
         // ---- what a wave expands of a step: pieces wave, wave + kWaves, .. of the keys (chunk, ks) and of the values (chunk, tile)
         uint2 k_code[KP][2], v_code[VP];
-        uint32_t k_id[KP], k_scale[KP], v_id[VP], v_scale[VP];
+        uint32_t k_id[KP], k_scale[KP][2], v_id[VP], v_scale[VP];
         uint32_t there = 0;                                          // of the step loaded: bit k: chunk k
         int pages = step0 < step1 ? four_pages(p, b, r.first + NC * step0, r.end) : 0;
         auto load = [&](int step) {
@@ -707,14 +620,16 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
             auto place = [&](int k) { return p.pages + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(number, k) * C::kBytes; };
 #pragma unroll
             for (int n = 0; n < KP; ++n) {
-                const int piece = min(wave + n * W::kWaves, NC * KS - 1), ks = piece % KS, block = min(2 * ks + (int)h, C::NB - 1);
+                const int piece = min(wave + n * W::kWaves, NC * KS - 1), ks = piece % KS;
                 const uint8_t* kc = place(piece / KS);
                 const uint8_t* at = kc + key * (D / 2);
-                // (of a last block alone: the other half's queries are zero, and what is read there is the first's)
-                const int u0 = 4 * ks + (int)h, u1 = 2 * ks + 1 < C::NB ? u0 + 2 : u0;
+                // (of a last block alone: the other half is not multiplied, and what is read there is the first's)
+                const int u0 = 4 * ks + (int)h, other = 2 * ks + 1 < C::NB, u1 = u0 + 2 * other;
                 k_code[n][0] = *reinterpret_cast<const uint2*>(at + C::k_unit(u0) * 8);
                 k_code[n][1] = *reinterpret_cast<const uint2*>(at + C::k_unit(u1) * 8);
-                k_scale[n] = kc[C::kKExps + ((key & 3u) * C::NB + block) * 8u + (key >> 2)];
+                const uint8_t* exps = kc + C::kKExps + ((key & 3u) * C::NB + 2 * ks) * 8u + (key >> 2);
+                k_scale[n][0] = exps[0];
+                k_scale[n][1] = exps[8 * other];
                 // dialects of blocks 2 ks and 2 ks + 1: the same half of two bytes (pairs are two blocks apart)
                 const uint8_t* ids = kc + C::kKIds + ((key & 3u) * C::NP + ks / 2 * 2) * 8u + (key >> 2);
                 k_id[n] = ((uint32_t)ids[0] | (uint32_t)ids[8] << 8) >> (ks & 1 ? 4 : 0);
@@ -736,13 +651,14 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
             for (int n = 0; n < KP; ++n) {
                 const int piece = wave + n * W::kWaves;
                 if (NC * KS % W::kWaves != 0 && piece >= NC * KS) break;
-                v8i k8;
-                expand16<0>(k_code[n][0], table[k_id[n] & 15u], k8);
-                expand16<4>(k_code[n][1], table[(k_id[n] >> 8) & 15u], k8);
-                uint8_t* at = to + piece * 2048 + lane * 16u;
-                *reinterpret_cast<int4*>(at) = make_int4(k8[0], k8[1], k8[2], k8[3]);
-                *reinterpret_cast<int4*>(at + 1024) = make_int4(k8[4], k8[5], k8[6], k8[7]);
-                to[W::kK + W::kV + (piece % KS) * 256 + lane * 4u + piece / KS] = (uint8_t)k_scale[n];
+                const int ks = piece % KS;
+                v8b k[4];
+                expand_bf16<2>(&k_code[n][0].x, table[k_id[n] & 15u], k_scale[n][0], k);
+                expand_bf16<2>(&k_code[n][1].x, table[(k_id[n] >> 8) & 15u], k_scale[n][1], k + 2);
+                uint8_t* at = to + (piece / KS * KI + ks * 4) * 1024 + lane * 16u;
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    if (4 * ks + m < KI) *reinterpret_cast<v8b*>(at + m * 1024) = k[m];
             }
 #pragma unroll
             for (int n = 0; n < VP; ++n) {
@@ -778,29 +694,19 @@ __global__ __launch_bounds__(Wide<D>::kThreads, 2) void paged_attention_wide_ker
             if (wave_row >= rows || 32 * chunk0 > p_max) return;     // no rows, or all of them earlier
             const bool inside = present == (1u << NC) - 1u && 32 * (chunk0 + NC) - 1 <= p_min && chunk0 + NC <= r.whole &&
                                 (a.window <= 0 || 32 * chunk0 > p_max - a.window);
-            // operands are read an instruction pair ahead
-            auto key_tile = [&](int n) {
-                const uint8_t* at = from + n * 2048 + lane * 16u;
-                const int4 lo = *reinterpret_cast<const int4*>(at), hi = *reinterpret_cast<const int4*>(at + 1024);
-                return v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            };
+            // operands are read three instructions ahead
+            auto key_tile = [&](int n) { return *reinterpret_cast<const v8b*>(from + n * 1024 + lane * 16u); };
             auto value_tile = [&](int n) { return *reinterpret_cast<const v8b*>(from + W::kK + n * 1024 + lane * 16u); };
-            int scale[KS];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) scale[ks] = *reinterpret_cast<const int*>(from + W::kK + W::kV + ks * 256 + lane * 4u);
             v16f x[NC];
-            v8i k8[2];
-            k8[0] = key_tile(0);
+            v8b k8[4] = {key_tile(0), key_tile(1), key_tile(2)};
             each<NC>([&](auto t_c) {
                 constexpr int t = decltype(t_c)::value;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
-                each<KS>([&](auto ks_c) {
-                    constexpr int ks = decltype(ks_c)::value, n = t * KS + ks;
-                    if constexpr (n + 1 < NC * KS) k8[(n + 1) & 1] = key_tile(n + 1);
-                    x[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8[n & 1], q_hi[ks], x[t], 0, 0, t, scale[ks], 0, q_scale[ks]);
-                    x[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8[n & 1], q_lo[ks], x[t], 0, 0, t, scale[ks], 0, q_scale[ks] - kLoShift);
-                    asm("" : "+v"(x[t]) : "v"(k8[n & 1]), "v"(q_hi[ks]), "v"(q_lo[ks]));
+                each<KI>([&](auto i_c) {
+                    constexpr int i = decltype(i_c)::value, n = t * KI + i;
+                    if constexpr (n + 3 < NC * KI) k8[(n + 3) & 3] = key_tile(n + 3);
+                    x[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k8[n & 3], q[i], x[t], 0, 0, 0);
                 });
             });
             v8b v[2][DT];

@@ -1,10 +1,8 @@
 // The paged 4-bit cache: where a cell keeps what, and what a kernel knows of a batch.
 //
 // A cell holds 32 tokens of one KV head.  Its parts lie as the attention kernel's lanes read them (lane = 16 g + c).
-//   K codes  [token][unit of 16 elements, 8 bytes].  The block-scaled matrix instruction 16 x 16 x 128 on FP8 wants in lane (g, c) bytes
-//            16 g .. 16 g + 15 of both halves of the 128 it adds over, and the scale of the g-th 32 (checked on the hardware, random
-//            operands and scales): half g % 2 of blocks g / 2 and 2 + g / 2.  Where 128 elements are whole, both halves of a lane
-//            lie together (k_unit), so that it loads 16 bytes
+//   K codes  [token][unit of 16 elements, 8 bytes].  Of 128 elements lane (g, c) takes half g % 2 of blocks g / 2 and 2 + g / 2 (a product adds
+//            over them in any order).  Where 128 are whole, both halves of a lane lie together (k_unit), so that it loads 16 bytes
 //   V codes  [d][dword of 8 tokens]: a lane takes the 32 tokens of a d
 //   K exps   [token % 4][block][token / 4]: a lane takes the 8 tokens 4 t + i of a block, t = 0 .. 7
 //   K ids    [token % 4][pair][token / 4]: dialects of blocks p and p + 2 of a 128 in one byte
@@ -21,14 +19,14 @@ namespace dfp4 {
 template <int D>
 struct Cell {
     static constexpr int NB = D / 32;                    // blocks of a key
-    static constexpr int KT = (NB + 3) / 4;              // instructions that add over a key
+    static constexpr int KT = (NB + 3) / 4;              // 128 elements of a key
     static constexpr int NJ = D / 16;                    // 16-row tiles of V^T
     static constexpr int VE = (NJ + 3) / 4 * 4;          // bytes of a row of V exps
     static constexpr int NP = 2 * KT;                    // dialect bytes of a key
     // all of a cell's keys, then all of its values: each is loaded to LDS as it lies
     static constexpr uint32_t kKExps = 16 * D, kKIds = kKExps + 32 * NB, kKeys = kKIds + 32 * NP, kVCodes = kKeys, kVExps = kVCodes + 16 * D,
                               kVIds = kVExps + 16 * VE, kValues = kVIds + 8 * VE - kVCodes, kBytes = (kKeys + kValues + 63) / 64 * 64;
-    // blocks of instruction kt
+    // blocks of the kt-th 128
     static constexpr int blocks(int kt) { return NB - 4 * kt < 4 ? NB - 4 * kt : 4; }
     // place (in units of 8 bytes) of elements 16 u .. 16 u + 15 of a key
     static __host__ __device__ constexpr int k_unit(int u) {

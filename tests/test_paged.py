@@ -537,7 +537,9 @@ def test_the_layer_of_the_example():
 def _few_or_many_rows(dim, many):
     """Sequences, new tokens, heads and hints of a call with few rows, or with enough for the kernel that takes 256 rows a workgroup."""
     if many:
-        return Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40).fill(), [90, 33, 3, 0, 64], 8, dict(max_new=90)
+        s, new, hints = Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40).fill(), [90, 33, 3, 0, 64], dict(max_new=190)
+        assert dfp4.paged_attention_rows(s.cache, s.batch(new, **hints), sum(new), 8) == 256
+        return s, new, 8, hints
     return Sequences([300, 45, 129], dim, 2, 64, seed=dim).fill(), [9, 45, 1], 6, dict(max_new=45)
 
 
@@ -794,7 +796,9 @@ def test_drafted_tokens_are_taken_back(dim, most, chunks):
     s.write(longer, longer)
     s.k, s.v = true_k, true_v
     _check_read(s, s.lengths, s.lengths, torch.bfloat16)
-    _attend(s, [90, 33, 3, 0, 64], 8, max_new=90)
+    new = [90, 33, 3, 0, 64]
+    assert dfp4.paged_attention_rows(s.cache, s.batch(new, max_new=190), sum(new), 8) == 256
+    _attend(s, new, 8, max_new=190)
 
 
 # ---- what a call takes for its sizes ---------------------------------------------------------------------------------------------
@@ -821,3 +825,52 @@ def test_attention_of_batches_that_say_nothing_of_themselves(new):
     """The kernel is chosen for sequences that are alike; one of them may still have most of the tokens."""
     s = Sequences([90, 31, 32, 400, 128, 3000, 99], 64, 2, 64, seed=sum(new)).fill()
     _attend(s, new, 16)
+
+
+# ---- as many bits as the header says --------------------------------------------------------------------------------------------
+
+def _check_rounding(got, lse, want, probability):
+    """A probability is off by `probability` of itself and a score by 2^-19 of sum |q||k| (an instruction adds its products, which are
+    exact, with 2^-22 of their sizes, and at most eight follow each other), sums and exponentials in fp32 by 2^-16, and the result is rounded to bf16.  These are bounds of single elements; of all of them together the error is that of the rounding,
+    with probabilities of 8 bits another one of its size (sqrt(2), as products of independent signs add up), and a tenth for the rest."""
+    out, wlse, size, dot = want
+    got, lse = got.double().cpu().numpy(), lse.double().cpu().numpy()
+    score = 2.0 ** -19 * dot
+    tol = HALF * np.abs(out) + (1 + HALF) * (probability + 2.0 ** -16 + 2 * score[..., None]) * size
+    assert (np.abs(got - out) <= tol).all(), float((np.abs(got - out) / tol).max())
+    assert (np.abs(lse - wlse) <= score + 2.0 ** -20 * (1 + np.abs(wlse))).all(), float((np.abs(lse - wlse) / score).max())
+    rounding = np.linalg.norm(torch.from_numpy(out).bfloat16().double().numpy() - out)
+    assert np.linalg.norm(got - out) <= (1.1 if probability < 2.0 ** -10 else 1.1 * 2 ** 0.5) * rounding, np.linalg.norm(got - out) / rounding
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,many", [(64, False), (96, False), (128, False), (192, False), (256, False), (64, True), (96, True), (128, True)])
+def test_scores_of_numbers_of_many_sizes(dim, many):
+    """Queries and keys whose elements differ by a factor of thousands: the small ones meet the other's large ones, and count."""
+    s, new, heads, hints = _few_or_many_rows(dim, many)
+    s.k = [(k.double() * torch.exp(3 * torch.randn(k.shape, generator=s.g).double())).bfloat16() for k in s.k]
+    s.fill()
+    q = (torch.randn(sum(new), heads, dim, generator=s.g).double() * torch.exp(3 * torch.randn(sum(new), heads, dim, generator=s.g).double())).bfloat16()
+    assert dfp4.paged_attention_rows(s.cache, s.batch(new, **hints), sum(new), heads) == (256 if many else 16)
+    scale = 16.0 / float(_attention(s, q, new, 1.0)[3].max())                # (scores up to 16)
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch(new, **hints), scale=scale, return_lse=True)
+    _check_rounding(got, lse, _attention(s, q, new, scale), HALF if many else 2.0 ** -16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", DIMS)
+def test_a_score_is_a_sum_in_fp32(dim):
+    """One key a sequence: the log-sum-exp is its score."""
+    n = 500
+    s = Sequences([1] * n, dim, 1, 32, seed=dim, factor=1.0)
+    for size in (1.0, 8.0, 1000.0):
+        for x in range(n):
+            s.k[x][..., :2] *= size
+        s.fill()
+        q = torch.randn(n, 4, dim, generator=s.g)
+        q[..., 1:3] *= size
+        q = q.bfloat16()
+        _, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch([1] * n, max_new=1), scale=1.0, return_lse=True)
+        k = synth.to_f64(q) * np.concatenate(s.stands_for()[0])
+        # (a log-sum-exp passes through base 2: two roundings)
+        assert (np.abs(lse.double().cpu().numpy() - k.sum(-1)) <= 2.0 ** -19 * np.abs(k).sum(-1) + 2.0 ** -22 * np.abs(k.sum(-1))).all(), size
