@@ -383,7 +383,8 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
  *   cu_tokens int32 [batch + 1], ascending from 0 to `tokens`; lengths int32 [batch]; table int32 [batch, table_width];
  *   slots int32 [batch], all device memory
  *   max_new, max_length   the largest number of new tokens and the largest length of a sequence, as far as the caller knows (0: not
- *             known).  They decide how work is split, not what is computed.
+ *             known).  They decide how work is split, and with that the order of sums and, in attention, the rounding of
+ *             probabilities (dfp4_paged_attention_rows); results are right for any.
  * Numbers in these arrays are used only as far as they lie in range: lengths are cut to the table's width, token ranges to
  * `tokens`; tokens in pages outside the pool, and values in slots outside `residual`, count as absent (not written, read as zeros,
  * not attended to).  Two sequences of one call must not share pages that are written, or slots.
@@ -434,7 +435,9 @@ int dfp4_paged_read(dfp4_cache cache, dfp4_batch batch, void* k, void* v, int dt
  *   workspace   at least dfp4_paged_attention_workspace_bytes(cache, batch, heads, window) bytes, 16-byte aligned (0 where no context
  *            is split, and for sizes that the call refuses)
  * Scores, softmax and sums are in fp32.  The matrix instructions take queries, keys and values as they are.  A probability goes in as the
- * sum of two bf16 numbers, or where there are many rows as one.
+ * sum of two bf16 numbers (off by 2^-16 of itself) where a workgroup takes 16 rows, and rounded to one (2^-8) where it takes 256
+ * (dfp4_paged_attention_rows): the results are then off by 1.4 times their own rounding to bf16 instead of by that alone.  max_new = 1
+ * gives the first, with up to 64 heads a group.
  */
 size_t dfp4_paged_attention_workspace_bytes(dfp4_cache cache, dfp4_batch batch, int64_t heads, int64_t window);
 /* The query rows (new tokens times heads of a group) that a workgroup of that call takes: 16, or 256 where there are many; 0: no call. */

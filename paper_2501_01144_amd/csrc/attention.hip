@@ -544,11 +544,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 // 16 h + 4 a + i of a chunk, so that a lane supplies the probabilities of the 16 tokens whose scores it has, eight to an instruction.
 // A chunk is a tile: its cell, and whether it is there, are the same for all lanes.
 // Codes of the next step are loaded while this one is multiplied, and expanded into the other half of LDS: one barrier a step.
-// The incomplete chunk is part of the last step: its values are stored to LDS as they are.  A probability is one bf16 number here.
-// 2048 tokens over 16384, 32 heads of 128 on 8: 490 us = 1.05 PFLOP/s (a large bf16 library product: 1.25); 16 rows a workgroup took 1630,
-// 16 x 16 instructions 521.  What bounds it: about 4100 clocks of matrix and 4600 of vector instructions a step and SIMD, which hardly
-// overlap, the two waves of a SIMD being in the same part of a step (9600 clocks).  Tried: one of the two waves half a step behind
-// (registers spilled: 750 us), steps of 64 keys (543), two workgroups of half the rows on a compute unit (587), the next step's scores
+// The incomplete chunk is part of the last step: its values are stored to LDS as they are.
+// A probability is rounded to one bf16 number here, which leaves a result off by 1.4 times its own rounding to bf16 (1.0 with two, as above).
+// Two numbers are half again as many matrix instructions, which nothing hides: 2048 tokens over 16384 702 us instead of 530, three chunks of about 310 over
+// 4000 with a bias, heads of 64, 106 instead of 93.
+// 2048 tokens over 16384, 32 heads of 128 on 8: 530 us = 0.97 PFLOP/s (a large bf16 library product: 1.25).  16 rows a workgroup took 1630.  What bounds
+// it: about 4100 clocks of matrix and 4600 of vector instructions a step and SIMD, which hardly overlap, the two waves of a SIMD being in the same part
+// of a step (9600 clocks), and 4100 of LDS reads.  Operands read one, three, five or seven instructions ahead make no difference.  Tried, with keys in FP8: one of the two waves half a step behind
+// (registers spilled: 750 us instead of 490), steps of 64 keys (543), two workgroups of half the rows on a compute unit (587), the next step's scores
 // between this one's exponentials (560 to 600).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>

@@ -844,6 +844,36 @@ def _check_rounding(got, lse, want, probability):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("options", [dict(), dict(softcap=20.0), dict(window=200)])
+def test_probabilities_of_16_bits_with_16_rows(dim, options):
+    s = Sequences([300, 45, 700], dim, 2, 64, seed=dim + 1).fill()
+    new, heads = [9, 45, 1], 6
+    assert dfp4.paged_attention_rows(s.cache, s.batch(new), sum(new), heads, options.get("window", 0)) == 16
+    q = torch.randn(sum(new), heads, dim, generator=s.g).bfloat16()
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, s.batch(new), return_lse=True, **options)
+    _check_rounding(got, lse, _attention(s, q, new, dim ** -0.5, **options), 2.0 ** -16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 96, 128])
+@pytest.mark.parametrize("options", [dict(), dict(softcap=20.0), dict(window=300)])
+def test_probabilities_of_8_bits_with_256_rows(dim, options):
+    s = Sequences([600, 33, 431, 20, 64], dim, 2, 64, seed=dim, width=40).fill()
+    new, heads = [200, 33, 300, 0, 64], 8
+    b = s.batch(new, max_new=300)
+    assert dfp4.paged_attention_rows(s.cache, b, sum(new), heads, options.get("window", 0)) == 256
+    q = torch.randn(sum(new), heads, dim, generator=s.g).bfloat16()
+    want = _attention(s, q, new, dim ** -0.5, **options)
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, b, return_lse=True, **options)
+    _check_rounding(got, lse, want, HALF)
+    # the same rows by the other kernel: its bits
+    few = s.batch(new, max_new=1)
+    assert dfp4.paged_attention_rows(s.cache, few, sum(new), heads, options.get("window", 0)) == 16
+    _check_rounding(*dfp4.paged_attention(q.cuda(), s.cache, few, return_lse=True, **options), want, 2.0 ** -16)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dim,many", [(64, False), (96, False), (128, False), (192, False), (256, False), (64, True), (96, True), (128, True)])
 def test_scores_of_numbers_of_many_sizes(dim, many):
     """Queries and keys whose elements differ by a factor of thousands: the small ones meet the other's large ones, and count."""
