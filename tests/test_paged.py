@@ -904,3 +904,85 @@ def test_a_score_is_a_sum_in_fp32(dim):
         k = synth.to_f64(q) * np.concatenate(s.stands_for()[0])
         # (a log-sum-exp passes through base 2: two roundings)
         assert (np.abs(lse.double().cpu().numpy() - k.sum(-1)) <= 2.0 ** -19 * np.abs(k).sum(-1) + 2.0 ** -22 * np.abs(k.sum(-1))).all(), size
+
+
+# ---- paths that small calls do not take -----------------------------------------------------------------------------------------
+
+def _parts(s, b, tokens, heads, window):
+    """In how many parts the keys of a call are split at most (its workspace holds a result and two numbers of each part and row)."""
+    need = dfp4.load().dfp4_paged_attention_workspace_bytes(s.cache.c, b.c(tokens), heads, window)
+    return max(1, need // (tokens * heads * (s.dim + 2) * 4))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 96, 128])
+@pytest.mark.parametrize("lengths,new,window,many,parts", [
+    # 256 rows a workgroup; blocks of rows whose windows begin in other chunks and are split in other numbers of parts
+    ([3500, 2900], [500, 431], 3000, True, (2, 8)), ([7000], [700], 6000, True, (9, 256)), ([1300, 700, 900, 64, 1200], [700, 650, 300, 64, 333], 333, True, (1, 1)),
+    # 16 rows
+    ([5000, 700], [9, 3], 2000, False, (2, 8)), ([9000, 33, 5000], [5, 2, 1], 7000, False, (9, 256)), ([3000, 1500], [3, 1], 100, False, (1, 1)),
+])
+def test_windows_of_both_kernels_whole_and_split(dim, lengths, new, window, many, parts):
+    s = Sequences(lengths, dim, 1, 32, seed=dim + window, width=-(-max(lengths) // 32) + 3).fill()
+    heads, b = 4, s.batch(new, max_new=max(new))
+    assert dfp4.paged_attention_rows(s.cache, b, sum(new), heads, window) == (256 if many else 16)
+    assert parts[0] <= _parts(s, b, sum(new), heads, window) <= parts[1]
+    q = torch.randn(sum(new), heads, dim, generator=s.g).bfloat16()
+    got, lse = dfp4.paged_attention(q.cuda(), s.cache, b, window=window, return_lse=True)
+    # (every row where there are few, else some of each block of rows, its first and its last among them)
+    want = _attention_rows(s, q, new, dim ** -0.5, window, None if sum(new) < 20 else 29)
+    rows = want[0]
+    _check_rounding(got[rows], lse[rows], want[1:], HALF if many else 2.0 ** -16)
+
+
+def _attention_rows(s, q, new, scale, window, every):
+    """_attention of every `every`-th new token and of the first and last of each sequence: their numbers, and what _attention gives."""
+    picked, row = [], 0
+    for n in new:
+        picked += [row + i for i in range(n) if every is None or i % every == 0 or i % 64 in (0, 63) or i == n - 1]
+        row += n
+    ks, vs = s.stands_for()
+    q = synth.to_f64(q)
+    heads, group = q.shape[1], q.shape[1] // s.kv_heads
+    out, size, lse, dot = np.zeros((len(picked),) + q.shape[1:]), np.zeros((len(picked),) + q.shape[1:]), np.zeros((len(picked), heads)), np.zeros((len(picked), heads))
+    starts = np.cumsum([0] + list(new))
+    for at, row in enumerate(picked):
+        b = int(np.searchsorted(starts, row, side="right")) - 1
+        p = s.lengths[b] - new[b] + row - starts[b]
+        lo = max(0, p - window + 1) if window else 0
+        for h in range(heads):
+            k, v = ks[b][lo:p + 1, h // group], vs[b][lo:p + 1, h // group]
+            z = scale * (k @ q[row, h])
+            w = np.exp(z - z.max())
+            lse[at, h] = z.max() + math.log(w.sum())
+            w /= w.sum()
+            out[at, h], size[at, h], dot[at, h] = w @ v, w @ np.abs(v), (np.abs(k) @ np.abs(q[row, h])).max() * abs(scale)
+    return picked, out, lse, size, dot
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [1500, 2049, 5003])
+@pytest.mark.parametrize("dim,rotary,heads,kv_heads,interleaved,norm", [
+    (128, 128, 32, 8, False, True), (64, 32, 7, 3, True, True), (96, 16, 5, 1, False, False), (256, 256, 9, 2, False, True), (32, 32, 70, 2, True, True),
+    (192, 96, 3, 0, False, True), (128, 0, 11, 5, False, True)])
+def test_norm_rope_of_many_tokens(tokens, dim, rotary, heads, kv_heads, interleaved, norm):
+    """Several heads and several tokens a workgroup, the last one of fewer: queries and keys as slices of a joint row, and in place."""
+    g = torch.Generator().manual_seed(tokens + dim)
+    x = (torch.randn(tokens, heads + kv_heads + 1, dim, generator=g) * torch.exp(2 * torch.randn(tokens, 1, 1, generator=g))).bfloat16()
+    pos = torch.randint(0, 1 << 20, (tokens,), generator=g).int()
+    freq = (1.0 / 500000.0 ** (torch.arange(0, rotary, 2).double() / max(rotary, 1))).float()
+    wq, wk = ((1 + 0.3 * torch.randn(dim, generator=g)) if norm else None for _ in range(2))
+    cuda = lambda t: None if t is None else t.cuda()  # noqa: E731
+    d = x.cuda()
+    dq, dk = d[:, 1:1 + heads], d[:, 1 + heads:] if kv_heads else None
+    args = (cuda(pos), cuda(freq), cuda(wq), cuda(wk))
+    q, k = dfp4.norm_rope(dq, dk, *args, eps=1e-5, interleaved=interleaved)
+    into = (dq.contiguous(), None if dk is None else dk.contiguous())
+    dfp4.norm_rope(*into, *args, eps=1e-5, interleaved=interleaved, out=into)
+    torch.cuda.synchronize()
+    for got, same, part, w in ((q, into[0], x[:, 1:1 + heads], wq), (k, into[1], x[:, 1 + heads:], wk)):
+        if got is None:
+            continue
+        want, size = _rope(part, w, pos, freq, interleaved, 1e-5)
+        assert (np.abs(got.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size).all()
+        assert torch.equal(got.view(torch.int16), same.view(torch.int16))
