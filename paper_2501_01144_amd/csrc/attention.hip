@@ -207,10 +207,10 @@ __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0
 // One workgroup: 16 query rows of a KV head and a contiguous part of their keys; its four waves take steps of 128 keys in turn and
 // add up in LDS.  A step's cells come to LDS whole, by loads that bypass the registers: the next step's keys are asked for as soon as
 // this one's are multiplied, its values as soon as these are, so that a wave has 9 KiB (head_dim 128) or more under way all the time.
-// 48 sequences of about 8192 tokens, 32 heads of 128 on 8 (439 MB), one token each: 115 us = 3.8 TB/s; one token over 131072 (147 MB)
-// 35 us and the join 5.  What bounds it: vector instructions, some 1250 a wave and step beside 80 matrix instructions (47 % of the time of
-// the vector unit, counters), and waits for LDS and memory on top with two waves to a SIMD; codes loaded to registers at the top of a
-// step took 170 us, three waves to a SIMD (168 registers, spilled) 136.
+// 48 sequences of about 8192 tokens, 32 heads of 128 on 8 (439 MB), one token each: 118 us = 3.7 TB/s; one token over 131072 (147 MB)
+// 35 us and the join 5.  What bounds it: some 1300 vector instructions a wave and step beside 96 matrix instructions, each behind the one
+// before with two waves to a SIMD: counters say that vector instructions issue 47 % of the time, matrix instructions are busy 13 %, and a
+// wave waits for 30 %.  Codes loaded to registers at the top of a step took 170 us, three waves to a SIMD (168 registers, spilled) 136.
 template <int D, bool EXTRA>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionArgs a) {
     using C = Cell<D>;
@@ -540,7 +540,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Many query rows (head_dim up to 128): a workgroup expands every step of 128 keys once into LDS, as the operands that all its waves read,
-// and each wave does both products for 32 rows, on 32 x 32 x 16: a query is a column again, now of two lanes (h, c).  They hold rows 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
+// and each wave does both products for 32 rows, on 32 x 32 x 16: a query is a column again, now of two lanes (h, c).  They hold rows
+// 8 a + 4 h + i of a 32 x 32 tile; row 8 a + 4 h + i of a tile of scores is token
 // 16 h + 4 a + i of a chunk, so that a lane supplies the probabilities of the 16 tokens whose scores it has, eight to an instruction.
 // A chunk is a tile: its cell, and whether it is there, are the same for all lanes.
 // Codes of the next step are loaded while this one is multiplied, and expanded into the other half of LDS: one barrier a step.
@@ -548,9 +549,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 // A probability is rounded to one bf16 number here, which leaves a result off by 1.4 times its own rounding to bf16 (1.0 with two, as above).
 // Two numbers are half again as many matrix instructions, which nothing hides: 2048 tokens over 16384 702 us instead of 530, three chunks of about 310 over
 // 4000 with a bias, heads of 64, 106 instead of 93.
-// 2048 tokens over 16384, 32 heads of 128 on 8: 530 us = 0.97 PFLOP/s (a large bf16 library product: 1.25).  16 rows a workgroup took 1630.  What bounds
-// it: about 4100 clocks of matrix and 4600 of vector instructions a step and SIMD, which hardly overlap, the two waves of a SIMD being in the same part
-// of a step (9600 clocks), and 4100 of LDS reads.  Operands read one, three, five or seven instructions ahead make no difference.  Tried, with keys in FP8: one of the two waves half a step behind
+// 2048 tokens over 16384, 32 heads of 128 on 8: 520 to 530 us = 0.98 PFLOP/s (a large bf16 library product: 1.25).  16 rows a workgroup took
+// 1630.  What bounds it: about 4100 clocks of matrix and 4900 of vector instructions a step and SIMD (40 and 48 %, counters), which hardly overlap, the two
+// waves of a SIMD being in the same part of a step (10200 clocks); LDS is read for 26 % of the time, without conflicts.  Operands read one, three, five or seven instructions ahead make no difference.  Tried, with keys in FP8: one of the two waves half a step behind
 // (registers spilled: 750 us instead of 490), steps of 64 keys (543), two workgroups of half the rows on a compute unit (587), the next step's scores
 // between this one's exponentials (560 to 600).
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -948,9 +949,11 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     int64_t most = batch.table_width * cache.page_tokens;
     if (batch.max_length > 0 && batch.max_length < most) most = batch.max_length;
     const int64_t new_rows = new_tokens * (heads / cache.kv_heads);
-    // In rounds of 512 keys of 16 rows.  The wide kernel expands keys once for 256 rows but wants a compute unit for itself: heads of
-    // 128 on 8 KV heads, us wide / 16 rows a workgroup: 64 rows of 16 sequences of 4000 tokens 56 / 53, 96 rows 60 / 93; 96 rows of
-    // 4 sequences (1536 rounds) 31 / 35; 512 rows of one sequence of 2000 (1024 rounds) 33 / 28, 2048 rows 43 / 56.  Heads above 128 leave
+    // In rounds of 512 keys of 16 rows.  The wide kernel expands keys once for 256 rows but wants a compute unit for itself: 8 KV heads,
+    // us wide / 16 rows a workgroup, heads of 64, 96 and 128: 64 rows of 16 sequences of 4000 tokens 43 / 39, 51 / 47, 55 / 56, 96 rows 45 / 57, 55 / 76,
+    // 58 / 93; 96 rows of 4 sequences (1536 rounds) 20 / 24, 25 / 29, 27 / 34; 512 rows of one sequence of 2000 (1024 rounds) 22 / 18, 28 / 22, 31 / 26,
+    // 1024 rows (2048) 25 / 21, 31 / 27, 36 / 32, 2048 rows (4096) 30 / 33, 38 / 45, 41 / 54.  One KV head of 128: 96 x 8 rows of 4 sequences (1536) 33 / 34,
+    // 192 rows of 16 (1536) 29 / 34, 160 rows of 48 of 1000 (960) 29 / 20.  Heads above 128 leave
     // it no registers (a version with half the waves took 729 us for 2048 rows of 4 sequences, heads of 256; 609 so).
     const int64_t keys = window > 0 && window + new_tokens < most ? window + new_tokens : most;
     const bool wide = cache.head_dim <= 128 && new_rows > 64 &&
