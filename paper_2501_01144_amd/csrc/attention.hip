@@ -930,13 +930,6 @@ __global__ __launch_bounds__(kThreads) void paged_attention_join_kernel(Attentio
     }
 }
 
-// New tokens of the sequence with most, or, where the caller does not know, of one with as many as the others: 48 sequences with one token
-// each, 32 heads of 128 on 8, 8192 keys: 100 us, taken for one sequence's 48 tokens 250 (256 rows a workgroup).
-int64_t likely_new(const dfp4_batch& b) {
-    if (b.max_new == 0) return (b.tokens + b.batch - 1) / b.batch;
-    return b.max_new < b.tokens ? b.max_new : b.tokens;
-}
-
 struct Split {
     int rows, blocks;            // query rows of a workgroup, workgroups along them
     int splits, steps;           // workgroups along the keys, steps of 128 keys of each

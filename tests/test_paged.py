@@ -986,3 +986,17 @@ def test_norm_rope_of_many_tokens(tokens, dim, rotary, heads, kv_heads, interlea
         want, size = _rope(part, w, pos, freq, interleaved, 1e-5)
         assert (np.abs(got.double().cpu().numpy() - want) <= HALF * np.abs(want) + 20 * 2.0 ** -24 * size).all()
         assert torch.equal(got.view(torch.int16), same.view(torch.int16))
+
+
+@pytest.mark.gpu
+def test_cache_of_a_batch_that_says_nothing_of_itself():
+    """300 sequences of which one has most of the tokens: more chunks than there are workgroups for them."""
+    lengths = [1 + i % 40 for i in range(299)] + [3000]
+    s = Sequences(lengths, 64, 8, 64, seed=41)
+    s.write(lengths, lengths)
+    _check_read(s, lengths, lengths, torch.bfloat16)
+    s = Sequences([40] * 300, 64, 8, 64, seed=42)
+    for n in (31, 1, 8):
+        at = [sum((31, 1, 8)[:(31, 1, 8).index(n) + 1])] * 300
+        s.write([n] * 300, at)
+        _check_read(s, [n] * 300, at, torch.bfloat16)
