@@ -388,7 +388,7 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
  * Numbers in these arrays are used only as far as they lie in range: lengths are cut to the table's width, token ranges to
  * `tokens`; tokens in pages outside the pool, and values in slots outside `residual`, count as absent (not written, read as zeros,
  * not attended to).  Two sequences of one call must not share pages that are written, or slots.
- * Refused as too large: batch * kv_heads from 2^23 on, table_width * page_tokens, tokens or tokens * heads (attention) above 2^30, a pool
+ * Refused as too large: batch * kv_heads from 2^24 on, table_width * page_tokens, tokens or tokens * heads (attention) above 2^30, a pool
  * of more than 2^31 cells.
  */
 typedef struct dfp4_cache {

@@ -485,8 +485,8 @@ static int check_paged_sizes(const dfp4_cache& c, const dfp4_batch& b) {
     if (cell_bytes(c.head_dim) == 0 || c.page_tokens < 32 || c.page_tokens % 32 != 0 || c.n_pages < 0 || c.n_slots < 0 || c.slot_chunks < 0 || c.slot_chunks > 2 || c.kv_heads < 1)
         return DFP4_ERR_SHAPE;
     if (b.batch < 0 || b.table_width < 0 || b.tokens < 0 || b.max_new < 0 || b.max_length < 0) return DFP4_ERR_SHAPE;
-    // (a workgroup of up to 512 threads for each sequence and KV head, and a launch has fewer than 2^32 threads)
-    const int64_t most = (int64_t)1 << 30, most_groups = ((int64_t)1 << 23) - 1;
+    // (a workgroup of 256 threads for each sequence and KV head, and a launch has fewer than 2^32 threads)
+    const int64_t most = (int64_t)1 << 30, most_groups = ((int64_t)1 << 24) - 1;
     if (c.page_tokens > (1 << 20) || c.n_pages > most || c.n_slots > most || c.kv_heads > (1 << 16) || b.batch > most_groups || b.tokens > most ||
         b.table_width > most / c.page_tokens || b.batch * c.kv_heads > most_groups ||
         c.n_pages * c.kv_heads > ((int64_t)1 << 31) / (c.page_tokens / 32))

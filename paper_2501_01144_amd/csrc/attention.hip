@@ -949,7 +949,8 @@ Split choose_split(const dfp4_cache& cache, const dfp4_batch& batch, int64_t hea
     // 192 rows of 16 (1536) 29 / 34, 160 rows of 48 of 1000 (960) 29 / 20.  Heads above 128 leave
     // it no registers (a version with half the waves took 729 us for 2048 rows of 4 sequences, heads of 256; 609 so).
     const int64_t keys = window > 0 && window + new_tokens < most ? window + new_tokens : most;
-    const bool wide = cache.head_dim <= 128 && new_rows > 64 &&
+    // (its workgroups of 512 threads: fewer than 2^32 threads a launch.)
+    const bool wide = cache.head_dim <= 128 && new_rows > 64 && batch.batch * cache.kv_heads < (int64_t)1 << 23 &&
                       batch.batch * cache.kv_heads * ((new_rows + 15) / 16) * ((keys + 511) / 512) > 5 * (int64_t)device_cu_count();
     const int64_t rows = wide ? 256 : 16;
     int64_t blocks = (new_rows + rows - 1) / rows;

@@ -704,7 +704,7 @@ BIG = 1 << 62
 
 
 @pytest.mark.parametrize("cache,batch,heads,window", [
-    (dict(kv_heads=8), dict(batch=1 << 20), 8, 0), ({}, dict(batch=1 << 23), 2, 0), (dict(page_tokens=BIG), {}, 2, 0), ({}, dict(table_width=BIG), 2, 0),
+    (dict(kv_heads=8), dict(batch=1 << 21), 8, 0), ({}, dict(batch=1 << 23), 2, 0), (dict(page_tokens=BIG), {}, 2, 0), ({}, dict(table_width=BIG), 2, 0),
     ({}, dict(tokens=BIG), 2, 0), (dict(kv_heads=BIG), {}, BIG, 0), ({}, dict(batch=BIG), 2, 0), ({}, {}, 2, BIG), ({}, {}, BIG, 0),
     ({}, dict(tokens=1 << 30), 4, 0), (dict(n_pages=BIG), {}, 2, 0), ({}, dict(max_new=-1), 2, 0), (dict(page_tokens=40), {}, 2, 0)])
 def test_sizes_that_no_launch_holds_are_refused_before_one(cache, batch, heads, window):
@@ -816,6 +816,9 @@ def test_rows_of_a_workgroup():
     for batch, new in ((1, 2048), (3, 512), (8, 700)):
         assert rows(batch, batch * new) == rows(batch, batch * new, max_new=new) == 256
     assert rows(1, 2048, dim=256) == rows(1, 2048, dim=192, max_new=2048) == 16
+    # as many workgroups as a launch holds: of 256 threads, those for many rows have 512
+    assert rows(1 << 19, 1 << 26, heads=8) == 256 and rows(1 << 20, 1 << 26, heads=8) == rows((1 << 21) - 1, 1 << 26, heads=8) == 16
+    assert rows(1 << 21, 1 << 26, heads=8) == 0
     assert rows(0, 5) == rows(5, 0) == rows(4, 4, heads=12) == rows(4, 4, window=-1) == rows(4, 4, dim=80) == 0
 
 
