@@ -368,8 +368,9 @@ int mxfp4_gemm(dfp4_tensor A, dfp4_tensor W, void* out, int out_dtype, int64_t l
  * tokens it holds one cell of dfp4_paged_cell_bytes(head_dim) bytes (4.375 bits an element, some padding), whose layout is
  * private to the library.  Values of a sequence's last length % 32 tokens are bf16 in the sequence's slot of `residual`.
  * With two chunks a slot it also keeps those of the chunk before, which are in the cache in 4 bits: then the length may be taken back (drafted
- * tokens that are not accepted) by up to 32 tokens from the largest that it has had, and written again from there.  With one a length
- * is taken back within its incomplete chunk only.  (To a multiple of 32: always.)
+ * tokens that are not accepted) by up to 32 tokens from the largest that it has had, and written again from there (not over tokens that were
+ * written with another slot, as of a shared prefix).  With one a length is taken back within its incomplete chunk
+ * only.  (To a multiple of 32: always.)
  *   pages     device, [n_pages, kv_heads, page_tokens / 32, cell], 256-byte aligned
  *   residual  device, bf16 [n_slots, kv_heads, slot_chunks, head_dim, 32], 16-byte aligned; chunk c of a sequence is at c % slot_chunks
  *   slot_chunks  2, or 1 (0 counts as 1)

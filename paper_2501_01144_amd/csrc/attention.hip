@@ -13,7 +13,7 @@
 // (0 .. 7) of S^T is token 32 g + 4 t + i of a step of 128: a lane has the scores of the chunk of 32 whose values it expands and
 // whose probabilities it supplies, and nothing moves between lanes.
 //
-// Values of the sequence's last, incomplete chunk of 32 are bf16 and take the second instruction as they are, at the end.
+// Values of the sequence's last, incomplete chunk of 32 are bf16 and are multiplied as they are, at the end.
 #include <type_traits>
 #include <utility>
 
@@ -551,7 +551,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttentionA
 // 4000 with a bias, heads of 64, 106 instead of 93.
 // 2048 tokens over 16384, 32 heads of 128 on 8: 520 to 530 us = 0.98 PFLOP/s (a large bf16 library product: 1.25).  16 rows a workgroup took
 // 1630.  What bounds it: about 4100 clocks of matrix and 4900 of vector instructions a step and SIMD (40 and 48 %, counters), which hardly overlap, the two
-// waves of a SIMD being in the same part of a step (10200 clocks); LDS is read for 26 % of the time, without conflicts.  Operands read one, three, five or seven instructions ahead make no difference.  Tried, with keys in FP8: one of the two waves half a step behind
+// waves of a SIMD being in the same part of a step (10200 clocks); LDS is read for 26 % of the time, without conflicts.  Operands read one,
+// three, five or seven instructions ahead make no difference.  Tried, with keys in FP8: one of the two waves half a step behind
 // (registers spilled: 750 us instead of 490), steps of 64 keys (543), two workgroups of half the rows on a compute unit (587), the next step's scores
 // between this one's exponentials (560 to 600).
 // ---------------------------------------------------------------------------------------------------------------------------------

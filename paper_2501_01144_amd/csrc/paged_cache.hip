@@ -1,8 +1,8 @@
 // The paged 4-bit cache written and read back (paper, Appendix C: keys quantized along the head dimension as they come, values
 // along the tokens, 32 at a time; values of the incomplete chunk stay bf16).  The per-block arithmetic is that of the other
 // quantizers (quant_pass.h), the layout of a cell is in paged.h.
-// Bound by memory where there is much of it: 4 x 4096 tokens, 8 heads of 128: write 23 us (86 MB, 3.7 TB/s), read 17 us (5.0 TB/s).  One
-// token of 64 sequences: write 6 us, read 5, most of it the dependent loads (batch, table, rows) and the launch.
+// Bound by memory where there is much of it: 4 x 4096 tokens, 8 heads of 128: write 23 us (86 MB, 3.7 TB/s), read 17 us (5.0 TB/s), in
+// f32 28 (5.5).  One token of 64 sequences: write 6 us, read 5, most of it the dependent loads (batch, table, rows) and the launch.
 #include <type_traits>
 
 #include "paged.h"
