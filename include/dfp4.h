@@ -464,6 +464,90 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
                    int interleaved, void* q_out, void* k_out, void* stream);
 
 /*
+ * A sparse layer: every token goes to k of `experts` feed-forward networks whose weights are quantized.
+ *
+ * Router.  Scores of a token's experts, s = softmax(logits) or 1 / (1 + exp(-logits)); the choice is by c = s + bias.  Where there are
+ * groups (expert e in group e / (experts / groups)), the `kept` groups with the largest sums of their `best` largest c stay, the others'
+ * experts are not chosen.  ids: the k experts with the largest c, in that order; of equal ones the lowest index first (of groups too).
+ *   weights = s[ids] / (renormalize ? sum over the k of s[ids] : 1) * scale
+ * Scores, sums and choices are in 64 bits.  Logits may be -infinity (score 0; a token with no other logit, or a renormalized sum of 0,
+ * has weights 0); NaN counts as that, +infinity as the largest number.
+ *   logits   device, DFP4_F32 or DFP4_BF16 [tokens, experts], rows `ld` elements apart
+ *   bias     device, f32 [experts], or NULL
+ *   ids      device, int32 [tokens, k];  weights  device, f32 [tokens, k]
+ *   experts up to 1024, k up to 32; groups (up to 64) divides experts; kept * (experts / groups) >= k; best at most a group's experts, and 1 or 2
+ */
+enum { DFP4_SOFTMAX = 0, DFP4_SIGMOID = 1 };
+int dfp4_route(const void* logits, int dtype, int64_t ld, int64_t tokens, int64_t experts, int64_t k, int score, const float* bias,
+               int64_t groups, int64_t kept, int64_t best, int renormalize, float scale, int32_t* ids, float* weights, void* stream);
+
+/*
+ * Plan of the experts' products: pair p = token * k + j stands for token and its j-th expert; pairs in the order of their experts, those of
+ * an expert in their own.  An id that is no expert (another GPU's, say -1) makes its pair absent: it has no row and adds nothing.
+ *   data   device, int32, dfp4_expert_plan_bytes(tokens, k, experts) bytes, 16-byte aligned, written by dfp4_expert_plan:
+ *          offsets [experts + 1]      rows of expert e: offsets[e] .. offsets[e + 1] - 1
+ *          order [tokens * k]         pair of a row, -1 from row offsets[experts] on
+ *          place [tokens * k]         row of a pair, -1: absent
+ *          and what the products read besides.
+ *   tokens * k up to 2^27
+ */
+typedef struct dfp4_plan {
+    int32_t* data;
+    int64_t tokens, k, experts;
+} dfp4_plan;
+size_t dfp4_expert_plan_bytes(int64_t tokens, int64_t k, int64_t experts);
+int dfp4_expert_plan(const int32_t* ids, dfp4_plan plan, void* stream);
+
+/*
+ * Experts' weights, laid out once: expert e's matrix is rows e * rows .. of a quantized tensor [experts * rows, K]; two of them (gate and up)
+ * for the product with the activation.
+ *   packed   device, 256-byte aligned, dfp4_expert_weights_bytes(experts, rows, K, gated) bytes; the layout is private to the library
+ *            (0.79 bytes an element)
+ *   up       of dfp4_expert_weights: the second tensor (gated), or one with codes NULL
+ */
+typedef struct dfp4_experts {
+    void* packed;
+    int64_t experts, rows, K;
+    int gated;
+} dfp4_experts;
+size_t dfp4_expert_weights_bytes(int64_t experts, int64_t rows, int64_t K, int gated);
+int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* stream);
+
+/*
+ * Experts' products.  Rows are quantized as dfp4_quantize does and multiplied with the experts' weights in fp32.
+ *   up    (gated weights) h[row] = silu(G x^) * (U x^), x^ the quantized x of the row's token; rows in the plan's order
+ *   down  (others)        y[token] = sum over its pairs j, in their order, of weights[token, j] * (W h^[row of the pair]); 0 without any
+ *   (rows of the weights: a multiple of 8, up to 2^20, fewer than 2^28 of all experts; K up to 2^20)
+ *   x     device, bf16 [tokens, K], rows x_ld elements apart (a multiple of 8), 16-byte aligned
+ *   h     device, bf16 [tokens * k, rows of G]; dfp4_experts_down: [tokens * k, K], rows h_ld elements apart (a multiple of 8); 16-byte aligned.
+ *         Rows from offsets[experts] on are neither written nor read.
+ *   weights   device, f32 [tokens, k];  y  device, DFP4_F32 or DFP4_BF16 [tokens, rows of W], contiguous, 16-byte aligned
+ *   plan  as dfp4_expert_plan left it, of as many experts as the weights have
+ *   workspace   at least dfp4_experts_workspace_bytes(plan, w) bytes, 256-byte aligned
+ */
+size_t dfp4_experts_workspace_bytes(dfp4_plan plan, dfp4_experts w);
+int dfp4_experts_up(const void* x, int64_t x_ld, dfp4_plan plan, dfp4_experts w, void* h, void* workspace, size_t workspace_bytes, void* stream);
+int dfp4_experts_down(const void* h, int64_t h_ld, dfp4_plan plan, dfp4_experts w, const float* weights, void* y, int y_dtype, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * Norms before and after a block, with its gate and the residual:
+ *   z = post_weight ? y / sqrt(mean(y^2) + eps) * post_weight : y
+ *   r = residual + scale * gate * z         (gate NULL: 1)
+ *   normed = r / sqrt(mean(r^2) + eps) * weight
+ * all in fp32, r and normed rounded once each (normed is of r before its rounding).
+ *   y        device, bf16 [tokens, dim];  gate  device, bf16 [tokens, dim] (gate_ld 0: one row for all), or NULL
+ *   residual, residual_out   device, [tokens, dim] of residual_dtype (DFP4_F32 or DFP4_BF16); out contiguous (may be
+ *            the residual where that is contiguous)
+ *   post_weight, weight      device, f32 [dim]; post_weight may be NULL
+ *   normed   device, bf16 [tokens, dim], contiguous (may be y where that is contiguous)
+ *   dim a multiple of 8 up to 16384; row strides (ld) multiples of 8, matrices 16-byte aligned
+ */
+int dfp4_add_norm(const void* y, int64_t y_ld, const void* residual, int64_t residual_ld, int residual_dtype, const void* gate, int64_t gate_ld,
+                  int64_t tokens, int64_t dim, const float* post_weight, const float* weight, float scale, float eps, void* residual_out,
+                  void* normed, void* stream);
+
+/*
  * The formatbook in use (Section 3.1): out[d * 8 + i] = half-unit magnitude
  * (value = 0.5 * out[...]) of index i in dialect d, ascending.  `out` is a HOST
  * pointer to 128 bytes.

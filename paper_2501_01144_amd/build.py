@@ -19,7 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdfp4.so")
 BINDING = os.path.join(HERE, "_binding.so")
 HELPERS = os.path.join(ROOT, "bench_helpers")
-SOURCES = ["api.hip", "quantize.hip", "dequantize.hip", "gemm.hip", "gemm_f8.hip", "gemm_native.hip", "paged_cache.hip", "attention.hip", "norm_rope.hip"]
+SOURCES = ["api.hip", "quantize.hip", "dequantize.hip", "gemm.hip", "gemm_f8.hip", "gemm_native.hip", "paged_cache.hip", "attention.hip", "norm_rope.hip",
+           "route.hip", "experts.hip", "add_norm.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-fconstexpr-steps=200000000",
@@ -170,6 +171,9 @@ def build_library(verbose=True):
     f8_s = os.path.join(objdir, "gemm_f8.s")
     cmd = [hipcc, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, "gemm_f8.hip"), "-o", f8_s]
     procs.append(("gemm_f8.hip (assembly)", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    experts_s = os.path.join(objdir, "experts.s")
+    cmd = [hipcc, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, "experts.hip"), "-o", experts_s]
+    procs.append(("experts.hip (assembly)", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     # native module of the Python binding: host code only
     import torch
     troot = os.path.dirname(torch.__file__)
@@ -207,7 +211,7 @@ def build_library(verbose=True):
     problems = check_products_free_of_scratch(open(f8_s).read())
     if problems:
         raise RuntimeError("gemm_f8_kernel uses scratch memory among its products:\n" + "\n".join(problems))
-    problems = check_results_apart(open(gemm_s).read() + open(f8_s).read())
+    problems = check_results_apart(open(gemm_s).read() + open(f8_s).read() + open(experts_s).read())
     if problems:
         raise RuntimeError("block-scaled products whose result overlaps an operand:\n" + "\n".join(problems))
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]

@@ -3,6 +3,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "experts.h"
 #include "formatbook.h"
 #include "paged.h"
 
@@ -582,6 +583,112 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
                          q_weight, k_weight, inv_freq, positions, q_stride, q_head_stride, k_stride, k_head_stride, (int)heads, (int)kv_heads,
                          (int)tokens, (int)head_dim, (int)rotary, interleaved, eps};
     return launch_norm_rope(a, static_cast<hipStream_t>(stream));
+}
+
+int dfp4_route(const void* logits, int dtype, int64_t ld, int64_t tokens, int64_t experts, int64_t k, int score, const float* bias,
+               int64_t groups, int64_t kept, int64_t best, int renormalize, float scale, int32_t* ids, float* weights, void* stream) {
+    if (dtype != DFP4_F32 && dtype != DFP4_BF16) return DFP4_ERR_DTYPE;
+    if (tokens < 0 || tokens > (int64_t)1 << 27 || experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChoice || k > experts || ld < experts ||
+        ld > (int64_t)1 << 30 || (score != DFP4_SOFTMAX && score != DFP4_SIGMOID) || groups < 1 || groups > 64 || experts % groups != 0 || kept < 1 || kept > groups ||
+        kept * (experts / groups) < k || best < 1 || best > 2 || best > experts / groups)
+        return DFP4_ERR_SHAPE;
+    if (tokens == 0) return DFP4_OK;
+    if (!logits || !ids || !weights) return DFP4_ERR_NULL;
+    if (!aligned(logits, dtype == DFP4_F32 ? 4 : 2) || !aligned(bias, 4) || !aligned(ids, 4) || !aligned(weights, 4)) return DFP4_ERR_ALIGN;
+    const RouteArgs a{logits, bias, ids, weights, ld, scale, (int)tokens, (int)experts, (int)k, (int)groups, (int)kept, (int)best, dtype == DFP4_BF16,
+                      score == DFP4_SIGMOID, renormalize != 0};
+    return launch_route(a, static_cast<hipStream_t>(stream));
+}
+
+static int check_plan(const dfp4_plan& p) {
+    if (p.tokens < 0 || p.k < 1 || p.k > kMaxChoice || p.tokens > kMaxPairs / p.k || p.experts < 1 || p.experts > kMaxExperts) return DFP4_ERR_SHAPE;
+    return DFP4_OK;
+}
+
+size_t dfp4_expert_plan_bytes(int64_t tokens, int64_t k, int64_t experts) {
+    if (check_plan(dfp4_plan{nullptr, tokens, k, experts}) != DFP4_OK) return 0;
+    const int64_t pairs = tokens * k;
+    return (size_t)(2 * (experts + 1) + 3 * pairs + plan_groups(pairs, experts)) * 4;
+}
+
+int dfp4_expert_plan(const int32_t* ids, dfp4_plan plan, void* stream) {
+    const int rc = check_plan(plan);
+    if (rc != DFP4_OK) return rc;
+    if (!plan.data || (!ids && plan.tokens > 0)) return DFP4_ERR_NULL;
+    if (!aligned(ids, 4) || !aligned(plan.data, 16)) return DFP4_ERR_ALIGN;
+    return launch_expert_plan(ids, plan, static_cast<hipStream_t>(stream));
+}
+
+static int check_experts(const dfp4_experts& w) {
+    if (w.experts < 1 || w.experts > kMaxExperts || w.rows < 8 || w.rows % 8 != 0 || w.rows > (1 << 20) || w.K < kBlock || w.K % kBlock != 0 || w.K > (1 << 20) ||
+        w.experts * w.rows >= 1 << 28)
+        return DFP4_ERR_SHAPE;
+    return DFP4_OK;
+}
+
+size_t dfp4_expert_weights_bytes(int64_t experts, int64_t rows, int64_t K, int gated) {
+    return check_experts(dfp4_experts{nullptr, experts, rows, K, gated}) == DFP4_OK ? expert_weights_bytes(experts, rows, K, gated != 0) : 0;
+}
+
+int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* stream) {
+    int rc = check_experts(w);
+    if (rc != DFP4_OK) return rc;
+    for (int i = 0; i < (w.gated ? 2 : 1); ++i) {
+        const dfp4_tensor& t = i ? up : gate;
+        if (t.rows != w.experts * w.rows || t.K != w.K) return DFP4_ERR_SHAPE;
+        if (!t.codes || !t.dialect || !t.exponent) return DFP4_ERR_NULL;
+        if (!aligned(t.codes, 4)) return DFP4_ERR_ALIGN;
+    }
+    if (!w.packed) return DFP4_ERR_NULL;
+    if (!aligned(w.packed, 256)) return DFP4_ERR_ALIGN;
+    return launch_expert_weights(gate, up, w, static_cast<hipStream_t>(stream));
+}
+
+size_t dfp4_experts_workspace_bytes(dfp4_plan plan, dfp4_experts w) {
+    if (check_plan(plan) != DFP4_OK || check_experts(w) != DFP4_OK || plan.experts != w.experts || plan.tokens == 0) return 0;
+    return experts_workspace_bytes(plan, w);
+}
+
+static int experts_product(const ExpertsArgs& a, int64_t x_cols, size_t workspace_bytes, void* stream) {
+    int rc = check_plan(a.plan);
+    if (rc == DFP4_OK) rc = check_experts(a.w);
+    if (rc != DFP4_OK) return rc;
+    if (a.plan.experts != a.w.experts || a.ld < x_cols || a.ld > (int64_t)1 << 30) return DFP4_ERR_SHAPE;
+    if (a.plan.tokens == 0) return DFP4_OK;
+    if (!a.x || !a.out || !a.plan.data || !a.w.packed || (!a.w.gated && !a.weights)) return DFP4_ERR_NULL;
+    if (a.ld % 8 != 0 || !aligned(a.x, 16) || !aligned(a.out, 16) || !aligned(a.plan.data, 16) || !aligned(a.w.packed, 256) || !aligned(a.weights, 4) ||
+        !aligned(a.workspace, 256))
+        return DFP4_ERR_ALIGN;
+    if (!a.workspace || workspace_bytes < experts_workspace_bytes(a.plan, a.w)) return DFP4_ERR_WORKSPACE;
+    return launch_experts(a, static_cast<hipStream_t>(stream));
+}
+
+int dfp4_experts_up(const void* x, int64_t x_ld, dfp4_plan plan, dfp4_experts w, void* h, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!w.gated) return DFP4_ERR_SHAPE;
+    return experts_product(ExpertsArgs{static_cast<const uint16_t*>(x), x_ld, plan, w, h, DFP4_BF16, nullptr, static_cast<uint8_t*>(workspace)}, w.K, workspace_bytes, stream);
+}
+
+int dfp4_experts_down(const void* h, int64_t h_ld, dfp4_plan plan, dfp4_experts w, const float* weights, void* y, int y_dtype, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    if (y_dtype != DFP4_F32 && y_dtype != DFP4_BF16) return DFP4_ERR_DTYPE;
+    if (w.gated) return DFP4_ERR_SHAPE;
+    return experts_product(ExpertsArgs{static_cast<const uint16_t*>(h), h_ld, plan, w, y, y_dtype, weights, static_cast<uint8_t*>(workspace)}, w.K, workspace_bytes, stream);
+}
+
+int dfp4_add_norm(const void* y, int64_t y_ld, const void* residual, int64_t residual_ld, int residual_dtype, const void* gate, int64_t gate_ld,
+                  int64_t tokens, int64_t dim, const float* post_weight, const float* weight, float scale, float eps, void* residual_out,
+                  void* normed, void* stream) {
+    if (residual_dtype != DFP4_F32 && residual_dtype != DFP4_BF16) return DFP4_ERR_DTYPE;
+    if (tokens < 0 || tokens > (int64_t)1 << 40 || dim < 8 || dim % 8 != 0 || dim > 16384 || (tokens > 1 && (y_ld < dim || residual_ld < dim || (gate && gate_ld != 0 && gate_ld < dim))))
+        return DFP4_ERR_SHAPE;
+    if (tokens == 0) return DFP4_OK;
+    if (!y || !residual || !weight || !residual_out || !normed) return DFP4_ERR_NULL;
+    if (!aligned(y, 16) || !aligned(residual, 16) || !aligned(gate, 16) || !aligned(residual_out, 16) || !aligned(normed, 16) || !aligned(post_weight, 4) || !aligned(weight, 4) ||
+        (tokens > 1 && (y_ld % 8 != 0 || residual_ld % 8 != 0 || (gate && gate_ld % 8 != 0))))
+        return DFP4_ERR_ALIGN;
+    const AddNormArgs a{static_cast<const uint16_t*>(y), residual, residual_out, static_cast<const uint16_t*>(gate), post_weight, weight, static_cast<uint16_t*>(normed),
+                        y_ld, residual_ld, gate_ld, scale, eps, tokens, (int)dim, residual_dtype == DFP4_F32};
+    return launch_add_norm(a, static_cast<hipStream_t>(stream));
 }
 
 int dfp4_formatbook(uint8_t* out) {

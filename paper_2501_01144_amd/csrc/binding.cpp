@@ -22,7 +22,8 @@ PyObject* g_error = nullptr;          // Dfp4Error
     F(dfp4_gemm_prepare) F(mxfp4_gemm_prepare) F(dfp4_gemm_prepared_workspace_bytes) F(dfp4_gemm_prepared)                  \
     F(mxfp4_gemm_prepared) F(dfp4_native_packed_bytes) F(dfp4_native_pack) F(mxfp4_native_pack)                             \
     F(dfp4_gemm_native_packed) F(mxfp4_gemm_native_packed) F(dfp4_gemm_native_splitk_bytes) F(dfp4_strerror)         \
-    F(dfp4_paged_write) F(dfp4_paged_read) F(dfp4_paged_attention_workspace_bytes) F(dfp4_paged_attention) F(dfp4_norm_rope)
+    F(dfp4_paged_write) F(dfp4_paged_read) F(dfp4_paged_attention_workspace_bytes) F(dfp4_paged_attention) F(dfp4_norm_rope)  \
+    F(dfp4_route) F(dfp4_expert_plan_bytes) F(dfp4_expert_plan) F(dfp4_experts_workspace_bytes) F(dfp4_experts_up) F(dfp4_experts_down) F(dfp4_add_norm)
 #define DFP4_DECLARE(NAME) decltype(&::NAME) p_##NAME = nullptr;
 DFP4_FUNCTIONS(DFP4_DECLARE)
 #undef DFP4_DECLARE
@@ -340,6 +341,106 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- operators of a sparse layer
+
+// route(logits, k, sigmoid, bias or None, groups, kept, best, renormalize, scale) -> ids, weights
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 9, [&]() -> PyObject* {
+        const at::Tensor& x = tensor(a[0]);
+        const bool bf16 = x.scalar_type() == at::kBFloat16;
+        if ((!bf16 && x.scalar_type() != at::kFloat) || x.dim() != 2 || !x.is_cuda() || (x.stride(1) != 1 && x.size(1) != 1))
+            fail(PyExc_AssertionError, "logits: f32 or bf16 [tokens, experts] on the device, contiguous along the experts");
+        const int64_t tokens = x.size(0), experts = x.size(1), k = number(a[1]);
+        const float* bias = numbers<float>(a[3], at::kFloat, experts, "bias: contiguous f32 [experts] on the device");
+        if (k < 0) fail(PyExc_AssertionError, "k: a positive number");
+        at::Tensor ids = empty({tokens, k}, at::kInt, x.device()), weights = result({tokens, k}, false, x.device());
+        enqueue("dfp4_route", p_dfp4_route, data(x), dtype(bf16), tokens > 1 ? x.stride(0) : experts, tokens, experts, k, a[2] == Py_True ? DFP4_SIGMOID : DFP4_SOFTMAX, bias,
+                number(a[4]), number(a[5]), number(a[6]), a[7] == Py_True ? 1 : 0, (float)real(a[8]), reinterpret_cast<int32_t*>(data(ids)),
+                reinterpret_cast<float*>(data(weights)), stream());
+        return Py_BuildValue("NN", THPVariable_Wrap(std::move(ids)), THPVariable_Wrap(std::move(weights)));
+    });
+}
+
+// data, tokens, k, experts
+dfp4_plan plan_of(PyObject* const* a) { return dfp4_plan{reinterpret_cast<int32_t*>(data(a[0])), number(a[1]), number(a[2]), number(a[3])}; }
+// packed, experts, rows, K, gated
+dfp4_experts experts_of(PyObject* const* a) { return dfp4_experts{data(a[0]), number(a[1]), number(a[2]), number(a[3]), a[4] == Py_True ? 1 : 0}; }
+
+// expert_plan(ids, experts) -> data
+PyObject* expert_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 2, [&]() -> PyObject* {
+        const at::Tensor& ids = tensor(a[0]);
+        if (ids.scalar_type() != at::kInt || ids.dim() != 2 || !ids.is_cuda() || !ids.is_contiguous()) fail(PyExc_AssertionError, "ids: contiguous int32 [tokens, k] on the device");
+        dfp4_plan p{nullptr, ids.size(0), ids.size(1), number(a[1])};
+        at::Tensor buf = empty({(int64_t)(p_dfp4_expert_plan_bytes(p.tokens, p.k, p.experts) / 4)}, at::kInt, ids.device());
+        p.data = reinterpret_cast<int32_t*>(data(buf));
+        enqueue("dfp4_expert_plan", p_dfp4_expert_plan, reinterpret_cast<const int32_t*>(data(ids)), p, stream());
+        return THPVariable_Wrap(std::move(buf));
+    });
+}
+
+// experts_up(x, the plan's four, the weights' five) -> h
+PyObject* experts_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 10, [&]() -> PyObject* {
+        const at::Tensor& x = dense(a[0]);
+        const dfp4_plan plan = plan_of(a + 1);
+        const dfp4_experts w = experts_of(a + 5);
+        if (x.size(0) != plan.tokens || x.size(1) != w.K) fail(PyExc_AssertionError, "x: [tokens of the plan, K of the weights]");
+        at::Tensor h = result({plan.tokens * plan.k, w.rows}, true, x.device()), ws;
+        const size_t need = p_dfp4_experts_workspace_bytes(plan, w);
+        if (need > 0) ws = bytes((int64_t)need, x.device());
+        enqueue("dfp4_experts_up", p_dfp4_experts_up, data(x), plan.tokens > 1 ? x.stride(0) : w.K, plan, w, data(h), need > 0 ? data(ws) : nullptr, need, stream());
+        return THPVariable_Wrap(std::move(h));
+    });
+}
+
+// experts_down(h, the plan's four, the weights' five, the router's weights, bf16) -> y
+PyObject* experts_down(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 12, [&]() -> PyObject* {
+        const at::Tensor& h = dense(a[0]);
+        const dfp4_plan plan = plan_of(a + 1);
+        const dfp4_experts w = experts_of(a + 5);
+        if (h.size(0) != plan.tokens * plan.k || h.size(1) != w.K) fail(PyExc_AssertionError, "h: [tokens * k of the plan, K of the weights]");
+        if (a[10] == Py_None) fail(PyExc_AssertionError, "weights: contiguous f32 [tokens, k] on the device");
+        const float* weights = numbers<float>(a[10], at::kFloat, plan.tokens * plan.k, "weights: contiguous f32 [tokens, k] on the device");
+        const bool bf16 = a[11] == Py_True;
+        at::Tensor y = result({plan.tokens, w.rows}, bf16, h.device()), ws;
+        const size_t need = p_dfp4_experts_workspace_bytes(plan, w);
+        if (need > 0) ws = bytes((int64_t)need, h.device());
+        enqueue("dfp4_experts_down", p_dfp4_experts_down, data(h), h.size(0) > 1 ? h.stride(0) : w.K, plan, w, weights, data(y), dtype(bf16), need > 0 ? data(ws) : nullptr, need,
+                stream());
+        return THPVariable_Wrap(std::move(y));
+    });
+}
+
+// add_norm(y, residual, weight, post_weight or None, gate or None, scale, eps) -> residual, normed
+PyObject* add_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 7, [&]() -> PyObject* {
+        const at::Tensor &y = dense(a[0]), &r = tensor(a[1]);
+        const int64_t tokens = y.size(0), dim = y.size(1);
+        const bool bf16 = r.scalar_type() == at::kBFloat16;
+        if ((!bf16 && r.scalar_type() != at::kFloat) || r.sizes() != y.sizes() || !r.is_cuda() || r.stride(1) != 1)
+            fail(PyExc_AssertionError, "residual: f32 or bf16 [tokens, dim] on the device, contiguous along its rows");
+        if (a[2] == Py_None) fail(PyExc_AssertionError, "weight: contiguous f32 [dim] on the device");
+        const float *weight = numbers<float>(a[2], at::kFloat, dim, "weight: contiguous f32 [dim] on the device"),
+                    *post = numbers<float>(a[3], at::kFloat, dim, "post_weight: contiguous f32 [dim] on the device");
+        const uint8_t* gate = nullptr;
+        int64_t gate_ld = 0;
+        if (a[4] != Py_None) {
+            const at::Tensor& g = tensor(a[4]);
+            const bool one = g.dim() == 1;
+            if (g.scalar_type() != at::kBFloat16 || !g.is_cuda() || (one ? g.size(0) != dim : g.sizes() != y.sizes()) || g.stride(-1) != 1)
+                fail(PyExc_AssertionError, "gate: bf16 [dim] or [tokens, dim] on the device, contiguous along its rows");
+            gate = data(g);
+            gate_ld = one ? 0 : step(g, 0);
+        }
+        at::Tensor out = result(y.sizes(), bf16, y.device()), normed = result(y.sizes(), true, y.device());
+        enqueue("dfp4_add_norm", p_dfp4_add_norm, data(y), step(y, 0), data(r), step(r, 0), dtype(bf16), gate, gate_ld, tokens, dim, post, weight, (float)real(a[5]), (float)real(a[6]),
+                data(out), data(normed), stream());
+        return Py_BuildValue("NN", THPVariable_Wrap(std::move(out)), THPVariable_Wrap(std::move(normed)));
+    });
+}
+
 // bind(path of libdfp4.so, exception class)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 2, [&]() -> PyObject* {
@@ -361,7 +462,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {DFP4_METHOD(bind), DFP4_METHOD(quantize), DFP4_METHOD(dequantize), DFP4_METHOD(gemm), DFP4_METHOD(gemm_batched),
                          DFP4_METHOD(gemm_prepare), DFP4_METHOD(gemm_prepared), DFP4_METHOD(quantize_native), DFP4_METHOD(native_pack),
                          DFP4_METHOD(gemm_native_packed), DFP4_METHOD(paged_write), DFP4_METHOD(paged_read), DFP4_METHOD(paged_attention),
-                         DFP4_METHOD(norm_rope), {nullptr, nullptr, 0, nullptr}};
+                         DFP4_METHOD(norm_rope), DFP4_METHOD(route), DFP4_METHOD(expert_plan), DFP4_METHOD(experts_up), DFP4_METHOD(experts_down),
+                         DFP4_METHOD(add_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

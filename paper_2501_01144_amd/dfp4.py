@@ -38,6 +38,14 @@ class _CBatch(ctypes.Structure):
                 ("max_length", ctypes.c_int64)]
 
 
+class _CPlan(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("k", ctypes.c_int64), ("experts", ctypes.c_int64)]
+
+
+class _CExperts(ctypes.Structure):
+    _fields_ = [("packed", ctypes.c_void_p), ("experts", ctypes.c_int64), ("rows", ctypes.c_int64), ("K", ctypes.c_int64), ("gated", ctypes.c_int)]
+
+
 SYMBOLS = [
     "dfp4_quantize", "dfp4_quantize_b64", "dfp4_quantize_mse", "dfp4_quantize_t", "mxfp4_quantize_t", "dfp4_quantize_t_at", "dfp4_dequantize", "dfp4_gemm", "dfp4_gemm_batched", "dfp4_gemm_workspace_bytes", "dfp4_gemm_noalloc",
     "dfp4_quantize_block", "dfp4_dequantize_block", "dfp4_gemm_blocks",
@@ -50,6 +58,8 @@ SYMBOLS = [
     "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_gemm", "dfp4_formatbook", "dfp4_strerror",
     "dfp4_paged_cell_bytes", "dfp4_paged_write", "dfp4_paged_read", "dfp4_paged_attention_workspace_bytes", "dfp4_paged_attention_rows", "dfp4_paged_attention",
     "dfp4_norm_rope",
+    "dfp4_route", "dfp4_expert_plan_bytes", "dfp4_expert_plan", "dfp4_expert_weights_bytes", "dfp4_expert_weights", "dfp4_experts_workspace_bytes",
+    "dfp4_experts_up", "dfp4_experts_down", "dfp4_add_norm",
 ]
 
 
@@ -148,6 +158,24 @@ def load():
     lib.dfp4_paged_attention.restype = ci
     lib.dfp4_norm_rope.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, i64, i64, vp, vp, cf, vp, vp, i64, ci, vp, vp, vp]
     lib.dfp4_norm_rope.restype = ci
+    lib.dfp4_route.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, i64, i64, i64, ci, cf, vp, vp, vp]
+    lib.dfp4_route.restype = ci
+    lib.dfp4_expert_plan_bytes.argtypes = [i64, i64, i64]
+    lib.dfp4_expert_plan_bytes.restype = ctypes.c_size_t
+    lib.dfp4_expert_plan.argtypes = [vp, _CPlan, vp]
+    lib.dfp4_expert_plan.restype = ci
+    lib.dfp4_expert_weights_bytes.argtypes = [i64, i64, i64, ci]
+    lib.dfp4_expert_weights_bytes.restype = ctypes.c_size_t
+    lib.dfp4_expert_weights.argtypes = [_CTensor, _CTensor, _CExperts, vp]
+    lib.dfp4_expert_weights.restype = ci
+    lib.dfp4_experts_workspace_bytes.argtypes = [_CPlan, _CExperts]
+    lib.dfp4_experts_workspace_bytes.restype = ctypes.c_size_t
+    lib.dfp4_experts_up.argtypes = [vp, i64, _CPlan, _CExperts, vp, vp, ctypes.c_size_t, vp]
+    lib.dfp4_experts_up.restype = ci
+    lib.dfp4_experts_down.argtypes = [vp, i64, _CPlan, _CExperts, vp, vp, ci, vp, ctypes.c_size_t, vp]
+    lib.dfp4_experts_down.restype = ci
+    lib.dfp4_add_norm.argtypes = [vp, i64, vp, i64, ci, vp, i64, i64, i64, vp, vp, cf, cf, vp, vp, vp]
+    lib.dfp4_add_norm.restype = ci
     lib.dfp4_formatbook.argtypes = [vp]
     lib.dfp4_strerror.argtypes = [ci]
     lib.dfp4_strerror.restype = ctypes.c_char_p
@@ -643,6 +671,131 @@ def paged_attention_rows(cache, batch, tokens, heads, window=0):
 
 def paged_cell_bytes(head_dim):
     return int(load().dfp4_paged_cell_bytes(head_dim))
+
+
+def route(logits, k, score="softmax", bias=None, groups=1, kept=1, best=1, renormalize=True, scale=1.0):
+    """dfp4_route: the k experts of every token and their weights, from logits f32 or bf16 [tokens, experts] (row stride allowed).
+    score: "softmax" or "sigmoid"; bias: f32 [experts], added for the choice only; groups, kept, best: of `groups` groups of experts the
+    `kept` with the largest sums of their `best` largest scores stay.  Returns ids int32 [tokens, k] and weights f32 [tokens, k]."""
+    assert score in ("softmax", "sigmoid")
+    return _calls().route(logits, k, score == "sigmoid", bias, groups, kept, best, bool(renormalize), scale)
+
+
+class ExpertPlan:
+    """The order of the experts' products (include/dfp4.h): offsets int32 [experts + 1], order and place int32 [tokens * k]."""
+    __slots__ = ("data", "tokens", "k", "experts")
+
+    def __init__(self, data, tokens, k, experts):
+        self.data, self.tokens, self.k, self.experts = data, tokens, k, experts
+
+    @property
+    def offsets(self):
+        return self.data[:self.experts + 1]
+
+    @property
+    def order(self):
+        return self.data[self.experts + 1:self.experts + 1 + self.tokens * self.k]
+
+    @property
+    def place(self):
+        n = self.tokens * self.k
+        return self.data[self.experts + 1 + n:self.experts + 1 + 2 * n]
+
+    def c(self):
+        return _CPlan(_ptr(self.data).value, self.tokens, self.k, self.experts)
+
+
+def expert_plan(ids, experts):
+    """dfp4_expert_plan: the pairs of tokens and experts, ids int32 [tokens, k], in the order of their experts.  Ids that are no
+    expert (another GPU's) are absent."""
+    return ExpertPlan(_calls().expert_plan(ids, experts), *ids.shape, experts)
+
+
+@dataclass
+class ExpertWeights:
+    """The quantized matrices [rows, K] of `experts` experts in the matrix instruction's order (dfp4_expert_weights)."""
+    buf: torch.Tensor
+    experts: int
+    rows: int
+    K: int
+    gated: bool
+
+    def c(self):
+        return _CExperts(_ptr(self.buf).value, self.experts, self.rows, self.K, 1 if self.gated else 0)
+
+
+def expert_weights(w, experts, up=None, buf=None):
+    """dfp4_expert_weights: lay out the weights of `experts` experts, w a QTensor [experts * rows, K], once; up: a second one of the
+    same shape, w is then the gate (for experts_up)."""
+    assert experts > 0 and w.rows % experts == 0 and (up is None or (up.rows, up.K) == (w.rows, w.K))
+    rows = w.rows // experts
+    need = int(load().dfp4_expert_weights_bytes(experts, rows, w.K, 0 if up is None else 1))
+    if buf is None:
+        buf = torch.empty(max(need, 256), dtype=torch.uint8, device=w.codes.device)
+    assert buf.is_cuda and buf.is_contiguous()
+    if buf.numel() * buf.element_size() < need:
+        raise Dfp4Error(f"dfp4_expert_weights: {need} bytes are needed")
+    out = ExpertWeights(buf, experts, rows, w.K, up is not None)
+    _check(load().dfp4_expert_weights(w.c(), (w if up is None else up).c(), out.c(), _stream()), "dfp4_expert_weights")
+    return out
+
+
+def _product_workspace(plan, w, workspace, device):
+    need = int(load().dfp4_experts_workspace_bytes(plan.c(), w.c()))
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
+    return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def experts_up(x, plan, w, out=None, workspace=None):
+    """dfp4_experts_up: h = silu(gate x) * (up x), bf16 [tokens * k, rows], for every pair of a token of x, bf16 [tokens, K] (row
+    stride allowed), and one of its experts, in the plan's order.  Rows behind plan.offsets[-1] are not written."""
+    if out is None and workspace is None:
+        return _calls().experts_up(x, plan.data, plan.tokens, plan.k, plan.experts, w.buf, w.experts, w.rows, w.K, w.gated)
+    if out is None:
+        out = torch.empty((plan.tokens * plan.k, w.rows), dtype=torch.bfloat16, device=x.device)
+    assert x.dtype == out.dtype == torch.bfloat16 and x.is_cuda and out.is_cuda and x.shape == (plan.tokens, w.K) and x.stride(1) == 1
+    assert out.is_contiguous() and out.shape == (plan.tokens * plan.k, w.rows)
+    workspace, n = _product_workspace(plan, w, workspace, x.device)
+    _check(load().dfp4_experts_up(_ptr(x), x.stride(0) if plan.tokens > 1 else w.K, plan.c(), w.c(), _ptr(out), _ptr(workspace), n, _stream()), "dfp4_experts_up")
+    return out
+
+
+def experts_down(h, plan, w, weights, dtype=torch.bfloat16, out=None, workspace=None):
+    """dfp4_experts_down: y [tokens, rows], the sum over a token's experts of the router's weights (f32 [tokens, k]) times W h, from
+    h bf16 [tokens * k, K] in the plan's order (row stride allowed)."""
+    if out is None and workspace is None:
+        return _calls().experts_down(h, plan.data, plan.tokens, plan.k, plan.experts, w.buf, w.experts, w.rows, w.K, w.gated, weights, _is_bf16(dtype))
+    if out is None:
+        out = torch.empty((plan.tokens, w.rows), dtype=dtype, device=h.device)
+    assert h.dtype == torch.bfloat16 and h.is_cuda and out.is_cuda and h.shape == (plan.tokens * plan.k, w.K) and h.stride(1) == 1
+    assert out.is_contiguous() and out.shape == (plan.tokens, w.rows)
+    assert weights.dtype == torch.float32 and weights.is_cuda and weights.is_contiguous() and weights.numel() == plan.tokens * plan.k
+    workspace, n = _product_workspace(plan, w, workspace, h.device)
+    _check(load().dfp4_experts_down(_ptr(h), h.stride(0) if h.shape[0] > 1 else w.K, plan.c(), w.c(), _ptr(weights), _ptr(out), BF16 if _is_bf16(out.dtype) else F32,
+                                    _ptr(workspace), n, _stream()), "dfp4_experts_down")
+    return out
+
+
+def add_norm(y, residual, weight, post_weight=None, gate=None, scale=1.0, eps=1e-6, out=None):
+    """dfp4_add_norm: r = residual + scale * gate * norm(y) and norm(r), in one pass.  y bf16 [tokens, dim], residual f32 or bf16 (row
+    strides allowed); weight, post_weight f32 [dim] (post_weight None: y is not normalized); gate bf16 [dim] or [tokens, dim].
+    Returns r, of the residual's type, and its norm, bf16 (out=(r, normed): into these, which may be residual and y where those are
+    contiguous)."""
+    if out is None:
+        return _calls().add_norm(y, residual, weight, post_weight, gate, scale, eps)
+    r_out, normed = out
+    tokens, dim = y.shape
+    assert y.dtype == normed.dtype == torch.bfloat16 and residual.dtype == r_out.dtype and residual.shape == r_out.shape == normed.shape == y.shape
+    assert all(t.is_cuda and t.stride(1) == 1 for t in (y, residual)) and all(t.is_cuda and t.is_contiguous() for t in out)
+    assert all(t is None or (t.dtype == torch.float32 and t.is_cuda and t.is_contiguous() and t.numel() == dim) for t in (weight, post_weight)) and weight is not None
+    assert gate is None or (gate.dtype == torch.bfloat16 and gate.is_cuda and gate.stride(-1) == 1 and tuple(gate.shape) in ((dim,), (tokens, dim)))
+    ld = lambda t: t.stride(0) if tokens > 1 else 0  # noqa: E731
+    _check(load().dfp4_add_norm(_ptr(y), ld(y), _ptr(residual), ld(residual), BF16 if _is_bf16(residual.dtype) else F32, _ptr(gate),
+                                0 if gate is None or gate.dim() == 1 else ld(gate), tokens, dim, _ptr(post_weight), _ptr(weight), scale, eps, _ptr(r_out), _ptr(normed),
+                                _stream()), "dfp4_add_norm")
+    return r_out, normed
 
 
 def formatbook():

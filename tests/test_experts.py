@@ -1,0 +1,422 @@
+"""Operators of a sparse layer: the router, the plan of the experts' products, the products, the norms around a block, each against a
+plain implementation in float64 (the quantizer: the oracle)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import dfp4_oracle as O
+from paper_2501_01144_amd import dfp4, synth
+
+HALF = torch.finfo(torch.bfloat16).eps / 2          # a rounding to bf16, relative to the value
+gpu = pytest.mark.gpu
+
+
+# ---- refusals: no device is touched ----------------------------------------------------------------------------------------
+
+def test_route_refuses():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+
+    def route(logits=16, dtype=0, ld=64, tokens=4, experts=64, k=8, score=0, bias=0, groups=1, kept=1, best=1, ids=16, weights=16):
+        return lib.dfp4_route(vp(logits), dtype, ld, tokens, experts, k, score, vp(bias), groups, kept, best, 1, 1.0, vp(ids), vp(weights), vp(0))
+    assert (route(dtype=2), route(dtype=-1)) == (-4, -4)
+    for bad in (dict(tokens=-1), dict(experts=0), dict(experts=1025, ld=1025), dict(k=0), dict(k=33), dict(experts=4, k=5), dict(ld=63), dict(score=2), dict(groups=0),
+                dict(groups=3), dict(groups=4, kept=5), dict(groups=8, kept=0), dict(groups=16, kept=1, k=5), dict(best=0), dict(best=3), dict(groups=64, kept=64, best=2),
+                dict(experts=1024, ld=1024, groups=128, kept=128), dict(tokens=1 << 28)):
+        assert route(**bad) == -2, bad
+    assert (route(logits=0), route(ids=0), route(weights=0)) == (-1,) * 3
+    assert (route(logits=18), route(logits=17, dtype=1), route(bias=2), route(ids=6), route(weights=10)) == (-3,) * 5
+    assert route(tokens=0, logits=0, ids=0, weights=0) == 0
+
+
+def test_plan_refuses():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    plan = lambda ids=16, data=16, tokens=4, k=2, experts=8: lib.dfp4_expert_plan(vp(ids), dfp4._CPlan(data, tokens, k, experts), vp(0))  # noqa: E731
+    for bad in (dict(tokens=-1), dict(k=0), dict(k=33), dict(experts=0), dict(experts=1025), dict(tokens=1 << 27)):
+        assert plan(**bad) == -2, bad
+        assert lib.dfp4_expert_plan_bytes(*(dict(dict(tokens=4, k=2, experts=8), **bad)[n] for n in ("tokens", "k", "experts"))) == 0
+    assert (plan(ids=0), plan(data=0), plan(ids=2), plan(data=8)) == (-1, -1, -3, -3)
+    assert lib.dfp4_expert_plan_bytes(0, 2, 8) >= 4 * 9 and lib.dfp4_expert_plan_bytes(100, 2, 8) >= 4 * (9 + 400)
+
+
+def _weights_c(packed=256, experts=8, rows=64, K=64, gated=1):
+    return dfp4._CExperts(packed, experts, rows, K, gated)
+
+
+def test_expert_weights_refuse():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    t = lambda codes=256, dialect=256, exponent=256, rows=512, K=64: dfp4._CTensor(codes, dialect, exponent, rows, K)  # noqa: E731
+    call = lambda gate, up, w: lib.dfp4_expert_weights(gate, up, w, vp(0))  # noqa: E731
+    for bad in (dict(experts=0), dict(experts=2000), dict(rows=0), dict(rows=12), dict(rows=(1 << 20) + 8), dict(K=0), dict(K=48), dict(experts=1024, rows=1 << 19)):
+        assert call(t(), t(), _weights_c(**bad)) == -2, bad
+        w = _weights_c(**bad)
+        assert lib.dfp4_expert_weights_bytes(w.experts, w.rows, w.K, w.gated) == 0
+    assert (call(t(rows=256), t(), _weights_c()), call(t(), t(K=32), _weights_c()), call(t(K=32), t(), _weights_c())) == (-2,) * 3
+    assert (call(t(codes=0), t(), _weights_c()), call(t(), t(dialect=0), _weights_c()), call(t(), t(exponent=0), _weights_c()), call(t(), t(), _weights_c(packed=0))) == (-1,) * 4
+    assert (call(t(), t(), _weights_c(packed=128)), call(t(codes=2), t(), _weights_c())) == (-3, -3)
+    assert lib.dfp4_expert_weights_bytes(8, 64, 64, 0) > 8 * 64 * 64 * 0.78
+
+
+def test_products_refuse():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+    P = lambda data=16, tokens=4, k=2, experts=8: dfp4._CPlan(data, tokens, k, experts)  # noqa: E731
+
+    def up(x=16, ld=64, plan=P(), w=_weights_c(), h=16, ws=256, n=1 << 30):
+        return lib.dfp4_experts_up(vp(x), ld, plan, w, vp(h), vp(ws), n, vp(0))
+
+    def down(h=16, ld=64, plan=P(), w=_weights_c(gated=0), weights=16, y=16, dtype=1, ws=256, n=1 << 30):
+        return lib.dfp4_experts_down(vp(h), ld, plan, w, vp(weights), vp(y), dtype, vp(ws), n, vp(0))
+    for f, gated in ((up, 1), (down, 0)):
+        assert f(w=_weights_c(gated=1 - gated)) == -2
+        for bad in (dict(ld=56), dict(plan=P(experts=9)), dict(plan=P(tokens=-1)), dict(plan=P(k=0)), dict(w=_weights_c(gated=gated, K=40)), dict(w=_weights_c(gated=gated, rows=4))):
+            assert f(**bad) == -2, bad
+        assert (f(plan=P(data=0)), f(w=_weights_c(gated=gated, packed=0))) == (-1, -1)
+        assert (f(ld=68), f(plan=P(data=8)), f(w=_weights_c(gated=gated, packed=64)), f(ws=128)) == (-3,) * 4
+        need = lib.dfp4_experts_workspace_bytes(P(), _weights_c(gated=gated))
+        assert need > 0 and f(n=need - 1) == -5 and f(ws=0, n=0) == -5
+        assert f(plan=P(tokens=0)) == 0 and lib.dfp4_experts_workspace_bytes(P(tokens=0), _weights_c(gated=gated)) == 0
+    assert lib.dfp4_experts_workspace_bytes(P(experts=9), _weights_c()) == 0
+    assert (up(x=0), up(h=0), up(x=8), up(h=8)) == (-1, -1, -3, -3)
+    assert (down(h=0), down(y=0), down(weights=0), down(h=8), down(y=24), down(weights=2), down(dtype=3)) == (-1, -1, -1, -3, -3, -3, -4)
+
+
+def test_add_norm_refuses():
+    lib, vp = dfp4.load(), ctypes.c_void_p
+
+    def call(y=16, yl=64, r=16, rl=64, dtype=1, gate=0, gl=0, tokens=2, dim=64, post=0, weight=16, ro=16, normed=16):
+        return lib.dfp4_add_norm(vp(y), yl, vp(r), rl, dtype, vp(gate), gl, tokens, dim, vp(post), vp(weight), 1.0, 1e-6, vp(ro), vp(normed), vp(0))
+    for bad in (dict(tokens=-1), dict(dim=0), dict(dim=60), dict(dim=16392, yl=16392, rl=16392), dict(yl=56), dict(rl=32), dict(gate=16, gl=8)):
+        assert call(**bad) == -2, bad
+    assert call(dtype=2) == -4
+    assert (call(y=0), call(r=0), call(weight=0), call(ro=0), call(normed=0)) == (-1,) * 5
+    assert (call(y=8), call(r=8), call(gate=8), call(ro=8), call(normed=8), call(weight=18), call(post=2), call(yl=68), call(rl=68), call(gate=16, gl=68)) == (-3,) * 10
+    assert call(tokens=0, y=0, r=0) == 0
+
+
+# ---- plain implementations -------------------------------------------------------------------------------------------------
+
+def plain_route(logits, k, score="softmax", bias=None, groups=1, kept=1, best=1, renormalize=True, scale=1.0):
+    """float64 scores; ids by (largest choice, lowest index)."""
+    x = np.asarray(logits, np.float64)
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, np.finfo(np.float32).max))
+    ids, weights = [], []
+    for row in x:
+        if score == "softmax":
+            s = np.zeros_like(row) if np.all(row == -np.inf) else np.exp(row - row.max())
+            s = s / s.sum() if s.sum() > 0 else s
+        else:
+            s = 1 / (1 + np.exp(-row))
+        c = s + (0 if bias is None else np.asarray(bias, np.float64))
+        if groups > 1:
+            g = np.sort(c.reshape(groups, -1), 1)[:, ::-1][:, :best].sum(1)
+            stay = sorted(range(groups), key=lambda i: (-g[i], i))[:kept]
+            c = np.where(np.isin(np.arange(len(row)) // (len(row) // groups), stay), c, -np.inf)
+        i = sorted(range(len(row)), key=lambda e: (-c[e], e))[:k]
+        w = s[i]
+        if renormalize:
+            w = w / w.sum() if w.sum() > 0 else np.zeros_like(w)
+        ids.append(i)
+        weights.append(w * scale)
+    return np.array(ids), np.array(weights)
+
+
+def plain_plan(ids, experts):
+    flat = [int(i) for i in np.asarray(ids).reshape(-1)]
+    rows = sorted((i for i in range(len(flat)) if 0 <= flat[i] < experts), key=lambda i: (flat[i], i))
+    place = [-1] * len(flat)
+    for r, i in enumerate(rows):
+        place[i] = r
+    offsets = [sum(1 for i in rows if flat[i] < e) for e in range(experts + 1)]
+    return offsets, rows + [-1] * (len(flat) - len(rows)), place
+
+
+def quantized(x):
+    return O.dfp4_dequantize(*O.dfp4_quantize(synth.to_f64(x)))
+
+
+class Layer:
+    """Random experts: the library's handle and the values."""
+
+    def __init__(self, experts, rows, K, gated, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        w = [(torch.randn(experts * rows, K, generator=g) * 0.05).bfloat16() for _ in range(2 if gated else 1)]
+        q = [dfp4.quantize(x.cuda()) for x in w]
+        self.handle = dfp4.expert_weights(q[0], experts, up=q[1] if gated else None)
+        self.values = [quantized(x).reshape(experts, rows, K) for x in w]
+
+
+def ids_of(tokens, k, experts, seed=0, absent=0.0, twice=False, only=None):
+    g = torch.Generator().manual_seed(seed)
+    ids = torch.stack([torch.randperm(experts, generator=g)[:k] for _ in range(tokens)]).int() if tokens else torch.zeros(0, k, dtype=torch.int32)
+    if only is not None:
+        ids = torch.randint(0, only, (tokens, k), generator=g).int()
+    if twice and k > 1:
+        ids[:, 1] = ids[:, 0]
+    gone = torch.rand(tokens, k, generator=g) < absent
+    return torch.where(gone, torch.where(torch.rand(tokens, k, generator=g) < 0.5, -1, experts).int(), ids)
+
+
+def check_up(x, ids, layer, experts, h):
+    """h against float64, within the products' 1e-5 sum |x||w|, fp32 arithmetic of the activation and one rounding."""
+    xq = quantized(x)
+    offsets, order, _ = plain_plan(ids, experts)
+    k = ids.shape[1]
+    h = h.float().cpu().double().numpy()
+    for e in range(experts):
+        rows = np.array(order[offsets[e]:offsets[e + 1]], dtype=int) // k
+        if not len(rows):
+            continue
+        a = xq[rows]
+        g, u = (a @ w[e].T for w in layer.values)
+        dg, du = (1e-5 * np.abs(a) @ np.abs(w[e]).T for w in layer.values)
+        s = g / (1 + np.exp(-g))
+        # |silu'| <= 1.1; silu and the product in fp32: exp to 2^-20 (its argument's rounding, |g| up to 16, among it), three operations
+        want, tol = s * u, 1.1 * dg * (np.abs(u) + du) + np.abs(s) * du
+        tol = (tol + 2.0 ** -19 * np.abs(want)) * (1 + HALF) + HALF * np.abs(want) + 1e-38
+        got = h[offsets[e]:offsets[e + 1]]
+        assert (np.abs(got - want) <= tol).all(), (e, float((np.abs(got - want) / tol).max()))
+
+
+def check_down(h, ids, layer, experts, weights, y):
+    hq = quantized(h)
+    offsets, order, _ = plain_plan(ids, experts)
+    tokens, k = ids.shape
+    w = synth.to_f64(weights)
+    dim = layer.values[0].shape[1]
+    want, size, tol = np.zeros((tokens, dim)), np.zeros((tokens, dim)), np.zeros((tokens, dim))
+    for e in range(experts):
+        for r in range(offsets[e], offsets[e + 1]):
+            t, j = order[r] // k, order[r] % k
+            v = hq[r] @ layer.values[0][e].T
+            want[t] += w[t, j] * v
+            size[t] += np.abs(w[t, j] * v)
+            tol[t] += np.abs(w[t, j]) * (1e-5 * np.abs(hq[r]) @ np.abs(layer.values[0][e]).T)
+    # rows' products are held in no fewer bits than bf16 (half a step each), the sum in fp32
+    half = HALF if y.dtype == torch.bfloat16 else 2.0 ** -24
+    tol = (tol + (2.0 ** -23 * (k + 1) + (HALF if y.dtype == torch.bfloat16 else 0.0)) * size) * (1 + half) + half * np.abs(want) + 1e-38
+    got = y.float().cpu().double().numpy()
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
+# ---- router and plan ---------------------------------------------------------------------------------------------------------
+
+ROUTES = [
+    (1, 128, 8, {}), (5, 8, 2, dict(renormalize=False)), (3, 1, 1, {}), (67, 160, 6, dict(score="sigmoid", bias=True, groups=8, kept=3, best=2, scale=2.5)),
+    (33, 64, 32, dict(bias=True)), (130, 256, 8, dict(score="sigmoid")), (9, 300, 7, dict(groups=4, kept=1, best=1)), (4, 1024, 32, dict(score="sigmoid", bias=True, groups=64, kept=5, best=2)),
+    (12, 66, 3, dict(groups=33, kept=2, best=2, bias=True)), (2, 512, 1, dict(groups=64, kept=1)), (6, 64, 5, dict(groups=64, kept=5)),
+]
+
+
+@gpu
+@pytest.mark.parametrize("tokens,experts,k,more", ROUTES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_route(tokens, experts, k, more, dtype):
+    g = torch.Generator().manual_seed(tokens + experts)
+    wide = (torch.randn(tokens, experts + 3, generator=g) * 2).to(dtype)             # (bf16: many equal logits)
+    logits, more = wide[:, 1:experts + 1], dict(more)
+    if more.pop("bias", False):
+        more["bias"] = torch.randn(experts, generator=g) * 0.1
+    ids, weights = dfp4.route(wide.cuda()[:, 1:experts + 1], k, **{n: v.cuda() if n == "bias" else v for n, v in more.items()})
+    want, w = plain_route(logits.float().numpy(), k, **more)
+    assert ids.dtype == torch.int32 and np.array_equal(ids.cpu().numpy(), want)
+    got = weights.cpu().double().numpy()
+    # 64-bit arithmetic (far below 2^-40) and one rounding to fp32
+    assert (np.abs(got - w) <= (2.0 ** -24 + 2.0 ** -40) * np.abs(w)).all()
+
+
+@gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_of_masked_infinite_and_equal_logits(score):
+    inf, nan = float("inf"), float("nan")
+    rows = [[0.0] * 8, [-inf] * 8, [nan] * 8, [1.0, -inf, 3.0, -inf, -inf, -inf, -inf, -inf], [inf, 0.0, inf, 1.0, -inf, nan, 2.0, 2.0], [-inf, nan, 5.0, 5.0, 5.0, 5.0, 5.0, 5.0],
+            [-3.4e38] * 7 + [-inf], [3.4e38, 3.4e38] + [0.0] * 6, [torch.finfo(torch.float32).min] * 4 + [-1e30] * 4]
+    for more in ({}, dict(groups=4, kept=2, best=2), dict(bias=torch.tensor([0.0, 0, 0, 0.5, 0, 0, 0, 0.25]))):
+        ids, weights = dfp4.route(torch.tensor(rows).cuda(), 4, score=score, **{n: v.cuda() if n == "bias" else v for n, v in more.items()})
+        with np.errstate(all="ignore"):
+            want, w = plain_route(np.array(rows), 4, score=score, **more)
+        assert np.array_equal(ids.cpu().numpy(), want)
+        got = weights.cpu().double().numpy()
+        assert np.isfinite(got).all() and (np.abs(got - w) <= (2.0 ** -24 + 2.0 ** -40) * np.abs(w) + 2.0 ** -149).all()
+
+
+PLANS = [(1, 8, 128, {}), (1, 1, 1, {}), (0, 2, 4, {}), (37, 3, 5, {}), (300, 4, 9, dict(absent=0.3)), (50, 2, 4, dict(absent=1.0)), (1025, 8, 64, {}), (64, 6, 8, dict(twice=True)),
+         (700, 1, 1024, {}), (200, 32, 40, {}), (5000, 8, 16, dict(only=2)), (129, 2, 300, dict(absent=0.1, twice=True)), (3000, 7, 33, {})]
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,more", PLANS)
+def test_plan(tokens, k, experts, more):
+    ids = ids_of(tokens, k, experts, seed=tokens, **more)
+    for _ in range(2):
+        plan = dfp4.expert_plan(ids.cuda(), experts)
+        offsets, order, place = plain_plan(ids, experts)
+        assert plan.offsets.tolist() == offsets and plan.order.tolist() == order and plan.place.tolist() == place
+
+
+# ---- products ----------------------------------------------------------------------------------------------------------------
+
+PRODUCTS = [                                  # tokens, k, experts, K, rows
+    (1, 1, 1, 32, 8, {}), (1, 8, 16, 256, 96, {}), (3, 2, 4, 96, 40, {}), (33, 1, 2, 64, 72, {}), (65, 4, 9, 160, 128, dict(absent=0.3)), (40, 2, 4, 1056, 264, dict(twice=True)),
+    (7, 3, 40, 2080, 56, {}), (130, 2, 3, 544, 300 // 8 * 8, {}), (20, 2, 4, 64, 64, dict(absent=1.0)), (300, 2, 4, 128, 64, dict(only=1)), (257, 4, 8, 96, 520, {}),
+    (1100, 2, 2, 224, 136, {}), (600, 5, 20, 64, 256, dict(absent=0.5)),
+]
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,K,rows,more", PRODUCTS)
+def test_up(tokens, k, experts, K, rows, more):
+    layer = Layer(experts, rows, K, True, seed=tokens)
+    x = torch.randn(tokens, K, generator=torch.Generator().manual_seed(K))
+    x[:, 5] *= 20
+    x = x.bfloat16()
+    ids = ids_of(tokens, k, experts, seed=rows, **more)
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    h = dfp4.experts_up(x.cuda(), plan, layer.handle)
+    check_up(x, ids, layer, experts, h)
+    # into buffers of the caller's, from rows with a stride; what is behind the last row stays
+    wide = torch.zeros(tokens, K + 24, dtype=torch.bfloat16, device="cuda")
+    wide[:, 8:K + 8] = x.cuda()
+    out = torch.full_like(h, 7.0)
+    ws = torch.full((int(dfp4.load().dfp4_experts_workspace_bytes(plan.c(), layer.handle.c())),), 0xff, dtype=torch.uint8, device="cuda")
+    dfp4.experts_up(wide[:, 8:K + 8], plan, layer.handle, out=out, workspace=ws)
+    n = int(plan.offsets[-1])
+    assert torch.equal(out[:n], h[:n]) and (out[n:] == 7.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,K,rows,more", PRODUCTS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_down(tokens, k, experts, K, rows, more, dtype):
+    layer = Layer(experts, rows, K, False, seed=tokens)
+    g = torch.Generator().manual_seed(K)
+    h = (torch.randn(tokens * k, K, generator=g) * torch.rand(tokens * k, 1, generator=g)).bfloat16()
+    ids = ids_of(tokens, k, experts, seed=rows, **more)
+    weights = torch.rand(tokens, k, generator=g)
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    n = int(plan.offsets[-1])
+    mine = h.cuda()
+    mine[n:] = float("nan")                          # (rows behind the last are not read)
+    y = dfp4.experts_down(mine, plan, layer.handle, weights.cuda(), dtype=dtype)
+    check_down(h, ids, layer, experts, weights, y)
+    wide = torch.full((tokens * k, K + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, :K] = mine
+    out = torch.full_like(y, 7.0)
+    ws = torch.full((int(dfp4.load().dfp4_experts_workspace_bytes(plan.c(), layer.handle.c())),), 0xff, dtype=torch.uint8, device="cuda")
+    dfp4.experts_down(wide[:, :K], plan, layer.handle, weights.cuda(), out=out, workspace=ws)
+    assert torch.equal(out, y)
+
+
+@gpu
+def test_products_of_no_tokens():
+    up, down = Layer(4, 64, 64, True), Layer(4, 64, 64, False)
+    plan = dfp4.expert_plan(torch.zeros(0, 2, dtype=torch.int32, device="cuda"), 4)
+    assert plan.offsets.tolist() == [0] * 5
+    h = dfp4.experts_up(torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda"), plan, up.handle)
+    y = dfp4.experts_down(h, plan, down.handle, torch.zeros(0, 2, device="cuda"))
+    assert h.shape == (0, 64) and y.shape == (0, 64)
+
+
+# ---- norms -------------------------------------------------------------------------------------------------------------------
+
+def check_norm(y, residual, weight, post, gate, scale, eps, r_got, n_got):
+    y, r0, w = synth.to_f64(y), synth.to_f64(residual), synth.to_f64(weight)
+    z = y
+    if post is not None:
+        z = z / np.sqrt((z * z).mean(-1, keepdims=True) + eps) * synth.to_f64(post)
+    if gate is not None:
+        z = z * synth.to_f64(gate)
+    z = scale * z
+    r = r0 + z
+    rms = np.sqrt((r * r).mean(-1, keepdims=True) + eps)
+    n = r / rms * w
+    # sums of up to 16384 squares, at most 2^7 additions deep in fp32: 2^-17 of a sum, half of that of its root; a few operations more
+    f32 = 2.0 ** -17
+    e_r = f32 * np.abs(z) + 2.0 ** -23 * (np.abs(r) + np.abs(z))
+    half = HALF if r_got.dtype == torch.bfloat16 else 2.0 ** -24
+    got = r_got.float().cpu().double().numpy()
+    tol = e_r * (1 + half) + half * np.abs(r) + 1e-38
+    assert (np.abs(got - r) <= tol).all(), float((np.abs(got - r) / tol).max())
+    got = n_got.float().cpu().double().numpy()
+    tol = (e_r / rms * np.abs(w) + np.abs(n) * (f32 + np.sqrt((e_r * e_r).mean(-1, keepdims=True)) / rms)) * (1 + HALF) + HALF * np.abs(n) + 1e-38
+    assert (np.abs(got - n) <= tol).all(), float((np.abs(got - n) / tol).max())
+
+
+@gpu
+@pytest.mark.parametrize("tokens,dim", [(1, 8), (3, 512), (5, 520), (2, 2048), (7, 2056), (3, 4096), (2, 4104), (1, 8192), (2, 16384), (3, 16376), (1029, 64), (513, 1448)])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("post,gate", [(True, "token"), (False, None), (True, "all"), (False, "token")])
+def test_add_norm(tokens, dim, wide, post, gate):
+    g = torch.Generator().manual_seed(tokens + dim)
+    y, r = torch.randn(tokens, dim + 8, generator=g).bfloat16(), torch.randn(tokens, dim + 16, generator=g) * 3
+    y[:, 3] *= 50
+    r = r if wide else r.bfloat16()
+    w, p = 1 + 0.2 * torch.randn(dim, generator=g), 1 + 0.2 * torch.randn(dim, generator=g) if post else None
+    gt = None if gate is None else torch.randn(dim, generator=g).bfloat16() if gate == "all" else torch.randn(tokens, dim, generator=g).bfloat16()
+    dev = lambda t: None if t is None else t.cuda()  # noqa: E731
+    yc, rc = y.cuda()[:, :dim], r.cuda()[:, 8:dim + 8]
+    got = dfp4.add_norm(yc, rc, w.cuda(), post_weight=dev(p), gate=dev(gt), scale=0.7, eps=1e-5)
+    check_norm(y[:, :dim], r[:, 8:dim + 8], w, p, gt, 0.7, 1e-5, *got)
+    # in place
+    y2, r2 = yc.contiguous(), rc.contiguous()
+    same = dfp4.add_norm(y2, r2, w.cuda(), post_weight=dev(p), gate=dev(gt), scale=0.7, eps=1e-5, out=(r2, y2))
+    assert same[0] is r2 and torch.equal(r2, got[0]) and torch.equal(y2, got[1])
+
+
+@gpu
+@pytest.mark.parametrize("size", [2.0 ** -70, 2.0 ** 70, 2.0 ** 100])
+@pytest.mark.parametrize("dim", [64, 4096])
+def test_add_norm_of_numbers_whose_squares_leave_fp32(size, dim):
+    g = torch.Generator().manual_seed(1)
+    y, r = (torch.randn(3, dim, generator=g) * size).bfloat16(), torch.randn(3, dim, generator=g)
+    w = torch.ones(dim)
+    got = dfp4.add_norm(y.cuda(), r.cuda(), w.cuda(), post_weight=w.cuda(), eps=0.0)
+    check_norm(y, r, w, w, None, 1.0, 0.0, *got)
+    r = r * size
+    got = dfp4.add_norm(y.cuda(), r.cuda(), w.cuda(), eps=0.0)
+    check_norm(y, r, w, None, None, 1.0, 0.0, *got)
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("tokens", [1, 16, 700])
+def test_a_layer_eager_on_another_stream_and_in_a_graph(tokens):
+    """norm -> router -> plan -> experts -> norm, as a program runs them; every replay against eager calls."""
+    dim, inner, experts, k = 256, 160, 12, 3
+    up, down = Layer(experts, inner, dim, True, 1), Layer(experts, dim, inner, False, 2)
+    g = torch.Generator().manual_seed(3)
+    wr, w = torch.randn(experts, dim, generator=g).cuda() * 0.1, (1 + 0.1 * torch.randn(dim, generator=g)).cuda()
+    batches = [(torch.randn(tokens, dim, generator=g).bfloat16().cuda(), torch.randn(tokens, dim, generator=g).cuda()) for _ in range(3)]
+
+    def layer(y, r):
+        r, x = dfp4.add_norm(y, r, w, post_weight=w)
+        ids, weights = dfp4.route((x.float()[:, None, :] * wr).sum(-1), k)
+        plan = dfp4.expert_plan(ids, experts)
+        h = dfp4.experts_up(x, plan, up.handle)
+        return (x, ids, weights, h) + tuple(dfp4.add_norm(dfp4.experts_down(h, plan, down.handle, weights), r, w))
+
+    want = [layer(*b) for b in batches]
+    for (y, r), (x, ids, weights, h, *_) in zip(batches, want):
+        check_up(x.cpu(), ids.cpu(), up, experts, h)
+        plan = dfp4.expert_plan(ids, experts)
+        check_down(h.cpu(), ids.cpu(), down, experts, weights.cpu(), dfp4.experts_down(h, plan, down.handle, weights))
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = [layer(*b) for b in batches]
+    torch.cuda.current_stream().wait_stream(other)
+    for a, b in zip(want, got):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+    static = [t.clone() for t in batches[0]]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = layer(*static)
+    for turn in (0, 1, 2, 1, 0):
+        for t, b in zip(static, batches[turn]):
+            t.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want[turn])), turn
+        layer(*batches[(turn + 1) % 3])
