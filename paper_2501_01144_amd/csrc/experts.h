@@ -7,31 +7,35 @@ namespace dfp4 {
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxChoice = 32;                        // experts of a token
 constexpr int64_t kMaxPairs = (int64_t)1 << 27;
-// Rows of the products come in groups: an expert's rows begin with a group, so that a group has one expert.  128 rows share the scale
-// dwords of a packed operand.
-constexpr int kGroupRows = 128;
+// Rows of the products come in groups: an expert's rows begin with a group, so that a group has one expert.  256 rows are the largest
+// tile of the products.
+constexpr int kGroupRows = 256;
 
 // Groups that `pairs` rows of `experts` experts can take, at most
 __host__ __device__ inline int64_t plan_groups(int64_t pairs, int64_t experts) { return pairs / kGroupRows + (pairs < experts ? pairs : experts); }
 
-// int32 arrays of a plan, one after the other (the first three are public)
+struct PlanGroup {
+    int32_t expert, row0, rows, none;      // rows 0: behind the last group
+};
+// Arrays of a plan, one after the other (the first three are public)
 struct PlanView {
     int32_t* offsets;        // [experts + 1]
     int32_t* order;          // [pairs] pair of a row, -1 behind the last
     int32_t* place;          // [pairs] row of a pair, -1: none
-    int32_t* first_group;    // [experts + 1]
-    int32_t* group_expert;   // [groups] -1 behind the last
     int32_t* row_at;         // [pairs] group * kGroupRows + row in it, of a row
+    int32_t* used;           // [1] groups
+    PlanGroup* groups;       // 16-byte aligned
 };
+__host__ __device__ inline int64_t plan_groups_at(int64_t pairs, int64_t experts) { return (experts + 1 + 3 * pairs + 1 + 3) / 4 * 4; }
 inline PlanView plan_view(const dfp4_plan& p) {
     const int64_t pairs = p.tokens * p.k;
     PlanView v;
     v.offsets = p.data;
     v.order = v.offsets + p.experts + 1;
     v.place = v.order + pairs;
-    v.first_group = v.place + pairs;
-    v.group_expert = v.first_group + p.experts + 1;
-    v.row_at = v.group_expert + plan_groups(pairs, p.experts);
+    v.row_at = v.place + pairs;
+    v.used = v.row_at + pairs;
+    v.groups = reinterpret_cast<PlanGroup*>(p.data + plan_groups_at(pairs, p.experts));
     return v;
 }
 
@@ -71,6 +75,20 @@ struct ExpertsArgs {
     const float* weights;    // down: [tokens, k]
     uint8_t* workspace;
 };
+
+// the products of many rows (gemm_native.hip): tiles of 256 or 128 rows of a group and 256 of the weights
+struct ExpertTiles {
+    const void *a, *w;       // packed rows and weights, and the offsets of their scales
+    size_t a_scales, w_scales;
+    const int32_t* used;
+    const PlanGroup* groups;
+    int64_t max_groups;
+    int K, rows, tiles;      // packed rows of an expert, tiles of 256 of them
+    bool gated, half;        // half: tiles of 128 rows
+    void* out;               // gated: bf16 [row][rows / 2], else [row][rows] of out_dtype
+    int out_dtype;
+};
+int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream);
 
 int launch_route(const RouteArgs& a, hipStream_t stream);
 int launch_expert_plan(const int32_t* ids, const dfp4_plan& plan, hipStream_t stream);

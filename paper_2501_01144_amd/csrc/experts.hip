@@ -138,10 +138,11 @@ __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArg
 
 struct ProductArgs {
     Packed a, w;
-    const int32_t *offsets, *first_group, *group_expert;
+    const int32_t* used;
+    const PlanGroup* plan;
     void* out;                                   // up: bf16 [row][rows / 2], down: f32 [row][rows]
     int64_t groups;                              // at most
-    int experts, S, rows, tiles, row_tiles;      // of an expert: packed rows, tiles of 32 with padding, tiles that have rows
+    int S, rows, tiles, row_tiles;               // of an expert: packed rows, tiles of 32 with padding, tiles that have rows
 };
 
 __device__ __forceinline__ uint16_t bf16_of(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
@@ -153,14 +154,14 @@ __global__ __launch_bounds__(1024, 4) void experts_kernel(ProductArgs p) {
     __shared__ float s_red[8][16][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int S = p.S, per = (S + 15) / 16, s_lo = min(S, wave * per), s_hi = min(S, s_lo + per);
-    const int64_t used = min((int64_t)p.first_group[p.experts], p.groups), total = used * 4 * p.row_tiles;
+    const int64_t used = min((int64_t)*p.used, p.groups), total = used * 8 * p.row_tiles;
     for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
-        const int64_t quarter = id / p.row_tiles, group = quarter >> 2;
-        const int t = (int)(id - quarter * p.row_tiles), expert = p.group_expert[group];
-        const int64_t row0 = p.offsets[expert] + (group - p.first_group[expert]) * kGroupRows + (quarter & 3) * 32;
-        const int rows = (int)min((int64_t)32, p.offsets[expert + 1] - row0);
+        const int64_t eighth = id / p.row_tiles;
+        const PlanGroup group = p.plan[eighth >> 3];
+        const int t = (int)(id - eighth * p.row_tiles), skip = (int)(eighth & 7) * 32, rows = min(32, group.rows - skip);
         if (rows <= 0) continue;
-        const size_t a_tile = (size_t)quarter, w_tile = (size_t)expert * p.tiles + t;
+        const int64_t row0 = (int64_t)group.row0 + skip;
+        const size_t a_tile = (size_t)eighth, w_tile = (size_t)group.expert * p.tiles + t;
         v16f acc;
 #pragma unroll
         for (int x = 0; x < 16; ++x) acc[x] = 0.0f;
@@ -205,15 +206,16 @@ __global__ __launch_bounds__(1024, 4) void experts_kernel(ProductArgs p) {
 }
 
 struct JoinArgs {
-    const float *part, *weights;
+    const void* part;
+    const float* weights;
     const int32_t* place;
     void* y;
     int64_t tokens, pairs;
     int k, dim;
 };
 
-// y[token] = sum over j of weights[token, j] * part[place], four elements a thread
-template <bool BF16>
+// y[token] = sum over j of weights[token, j] * part[place], four elements a thread; PART16: part in bf16
+template <bool BF16, bool PART16>
 __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p) {
     const int64_t quads = p.dim / 4, total = p.tokens * quads;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -223,7 +225,13 @@ __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p) {
             const int32_t row = p.place[token * p.k + j];
             if (row < 0 || row >= p.pairs) continue;
             const float w = p.weights[token * p.k + j];
-            const float4 v = *reinterpret_cast<const float4*>(p.part + (int64_t)row * p.dim + d);
+            float4 v;
+            if constexpr (PART16) {
+                const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.part) + (int64_t)row * p.dim + d);
+                v = make_float4(as_f(u.x << 16), as_f(u.x & 0xffff0000u), as_f(u.y << 16), as_f(u.y & 0xffff0000u));
+            } else {
+                v = *reinterpret_cast<const float4*>(static_cast<const float*>(p.part) + (int64_t)row * p.dim + d);
+            }
             y.x += w * v.x, y.y += w * v.y, y.z += w * v.z, y.w += w * v.w;
         }
         if constexpr (BF16)
@@ -282,20 +290,34 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
     ProductArgs p{};
     p.a = q.to;
     p.w = packed_at(a.w.packed, a.w.experts * padded_rows(a.w), a.w.K);
-    p.offsets = plan.offsets, p.first_group = plan.first_group, p.group_expert = plan.group_expert;
+    p.used = plan.used, p.plan = plan.groups;
     p.out = a.w.gated ? a.out : a.workspace + ws.part;
     p.groups = plan_groups(pairs, a.plan.experts);
-    p.experts = (int)a.plan.experts, p.S = (int)S, p.rows = (int)expert_rows(a.w), p.tiles = (int)(padded_rows(a.w) / 32), p.row_tiles = (p.rows + 31) / 32;
-    const int64_t all = p.groups * 4 * p.row_tiles;
-    const dim3 grid((unsigned)(all < (1 << 20) ? all : 1 << 20));
-    if (a.w.gated) hipLaunchKernelGGL((experts_kernel<true>), grid, dim3(1024), 0, stream, p);
-    else hipLaunchKernelGGL((experts_kernel<false>), grid, dim3(1024), 0, stream, p);
+    p.S = (int)S, p.rows = (int)expert_rows(a.w), p.tiles = (int)(padded_rows(a.w) / 32), p.row_tiles = (p.rows + 31) / 32;
+    const bool many = pairs >= 64 * a.w.experts, part16 = many && a.out_dtype == DFP4_BF16;
+    if (many) {
+        ExpertTiles t{};
+        t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
+        t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);
+        t.used = plan.used, t.groups = plan.groups, t.max_groups = p.groups;
+        t.K = (int)a.w.K, t.rows = p.rows, t.tiles = p.tiles / 8;
+        t.gated = a.w.gated != 0, t.half = false;
+        t.out = p.out, t.out_dtype = a.out_dtype;
+        const int rc = launch_expert_tiles(t, stream);
+        if (rc != DFP4_OK) return rc;
+    } else {
+        const int64_t all = p.groups * 8 * p.row_tiles;
+        const dim3 grid((unsigned)(all < (1 << 20) ? all : 1 << 20));
+        if (a.w.gated) hipLaunchKernelGGL((experts_kernel<true>), grid, dim3(1024), 0, stream, p);
+        else hipLaunchKernelGGL((experts_kernel<false>), grid, dim3(1024), 0, stream, p);
+    }
     if (!a.w.gated) {
-        const JoinArgs j{static_cast<const float*>(p.out), a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
+        const JoinArgs j{p.out, a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
         const int64_t wgs = (a.plan.tokens * (a.w.rows / 4) + 255) / 256;
         const dim3 jg((unsigned)(wgs < (1 << 20) ? wgs : 1 << 20));
-        if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true>), jg, dim3(256), 0, stream, j);
-        else hipLaunchKernelGGL((experts_join_kernel<false>), jg, dim3(256), 0, stream, j);
+        if (part16) hipLaunchKernelGGL((experts_join_kernel<true, true>), jg, dim3(256), 0, stream, j);
+        else if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true, false>), jg, dim3(256), 0, stream, j);
+        else hipLaunchKernelGGL((experts_join_kernel<false, false>), jg, dim3(256), 0, stream, j);
     }
     return check_launch();
 }

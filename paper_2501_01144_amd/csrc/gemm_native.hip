@@ -48,6 +48,7 @@
 // x 50 and Gaussian weights the bound is 2^20.3 at K = 4096 and 2^22.1 at K = 14336.
 #include <type_traits>
 #include "common.h"
+#include "experts.h"
 #include "formatbook.h"
 #include "exact_norms.h"
 #include "fp6_pack.h"
@@ -453,11 +454,23 @@ __device__ __forceinline__ void quantize_flushed_piece(const GemmParams& p, int6
     __syncthreads();
 }
 
+// Products of experts (experts.hip): rows in groups of kGroupRows, a tile's weights are its group's expert's
+struct ExpertsParams : NativeParams {
+    const int32_t* used;              // groups there are
+    const PlanGroup* groups;
+    int max_groups, cols;             // tiles of 256 columns of an expert
+};
+__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
 // TA = 32-row tiles per wave: 4 (256 x 256 per workgroup) or 2 (128 x 256, for products with few tiles)
 // MODE: what is made of the sums.  kPlain: dfp4_gemm_native.  kExact: the exact products.  kRequant: those, quantized.
-constexpr int kPlain = 0, kExact = 1, kRequant = 2;
+// kExperts, kGated: rows of experts; columns are gate and up in turns, silu(gate) * up is kept.
+constexpr int kPlain = 0, kExact = 1, kRequant = 2, kExperts = 3, kGated = 4;
+template <int MODE>
+using ParamsOf = std::conditional_t<MODE == kPlain, NativeParams, std::conditional_t<(MODE >= kExperts), ExpertsParams, ExactParams>>;
 template <int FMT, bool BF16, int TA, int MODE>
-__global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<MODE == kPlain, NativeParams, ExactParams> p) {
+__global__ __launch_bounds__(256, 1) void gemm_native_kernel(ParamsOf<MODE> p) {
+    constexpr bool kIsExact = MODE == kExact || MODE == kRequant, kIsExperts = MODE >= kExperts;
     constexpr bool kFp6 = FMT == kFmtFp6;
     using PieceShape = DirectShape<2, 2, 2, 2, 1>;           // 128 x 128 by 256 threads
     constexpr int kTileLds = kFp6 ? 1536 : 1024, kStage = (2 * TA + 8) * kTileLds + 1024;
@@ -466,26 +479,40 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
     constexpr int kGStride = kFp6 ? kFp6PairBytes : 1024;    // global bytes per (pair of tiles, step) / (tile, step)
     __shared__ __attribute__((aligned(16))) uint8_t s_stage[kStages * kStage];
     constexpr int kPieceAt = MODE == kRequant ? offsetof(RequantLds, st) : 0;      // behind the quantizer's tables
-    static_assert(MODE == kPlain || (kPieceAt + sizeof(TileLds<PieceShape>) <= sizeof(s_stage) && kPieceAt % 16 == 0));
+    static_assert(!kIsExact || (kPieceAt + sizeof(TileLds<PieceShape>) <= sizeof(s_stage) && kPieceAt % 16 == 0));
     static_assert(MODE != kRequant || sizeof(RequantLds) <= sizeof(s_stage));
     __shared__ int s_ctl[5];                                 // exact: per wave, whether its sums are exact; arrivals (split K)
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (int)wave >> 1, wn = (int)wave & 1;
     // this workgroup's tile
     int bx = (int)blockIdx.x, by = (int)blockIdx.y;
-    if (p.rect_h) {
+    int expert = 0;
+    if constexpr (kIsExperts) {
+        // An XCD takes a stretch of row tiles, all columns of one after the other, so that its cache holds an expert's weights
+        constexpr int kUnits = kGroupRows / kRowsWg;
+        const int units = min(*p.used, p.max_groups) * kUnits, share = (units + 7) >> 3, in = bx >> 3, unit = in / p.cols, at = (bx & 7) * share + unit;
+        if (unit >= share || at >= units) return;
+        const PlanGroup g = p.groups[at / kUnits];
+        const int skip = at % kUnits * kRowsWg;
+        if (g.rows <= skip) return;
+        bx = in - unit * p.cols;
+        by = at;
+        expert = g.expert;
+        p.M = g.rows - skip;
+        p.out = static_cast<uint8_t*>(p.out) + (int64_t)(g.row0 + skip) * p.ldc * (BF16 ? 2 : 4);
+    } else if (p.rect_h) {
         const int id = by * (int)gridDim.x + bx, rect = id & 7, in = id >> 3;
         bx = ((rect & ((1 << p.rects_x) - 1)) << p.rect_w) + (in & ((1 << p.rect_w) - 1));
         by = (rect >> p.rects_x) * p.rect_h + (in >> p.rect_w);
     }
     // this workgroup's range of steps (split K: blockIdx.z, in exact products below the problem of a batch)
     const int per = (p.S + p.ksplit - 1) / p.ksplit;
-    const int sidx = MODE == kPlain ? (int)blockIdx.z : (int)(blockIdx.z % (unsigned)p.ksplit);
-    const int64_t bz = MODE == kPlain ? 0 : blockIdx.z / (unsigned)p.ksplit;
+    const int sidx = !kIsExact ? (int)blockIdx.z : (int)(blockIdx.z % (unsigned)p.ksplit);
+    const int64_t bz = !kIsExact ? 0 : blockIdx.z / (unsigned)p.ksplit;
     const int s_lo = sidx * per, S = min(p.S, s_lo + per) - s_lo;
     // norms of the wave's rows of A and of W: used after the main loop, on their way during it
     ExactStat stat_a[TA / 2], stat_w[2];
-    if constexpr (MODE != kPlain) {
+    if constexpr (kIsExact) {
         p.a.bits += bz * p.a_stride;
         p.w.bits += bz * p.w_stride;
         p.a.sc += bz * (p.a_stride / 4);
@@ -504,12 +531,14 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
         // this wave fetches A tiles 2w, 2w+1 (128-row form: tile w) and B tiles 2w, 2w+1 of the workgroup's 8 + 8,
         // and scale chunk w
         const uint64_t a_tile = (uint64_t)by * (2 * TA) + (TA == 4 ? 2 * wave : wave);
-        const uint64_t b_tile = (uint64_t)bx * 8 + 2 * wave;
+        uint64_t b_tile0 = (uint64_t)bx * 8;
+        if constexpr (kIsExperts) b_tile0 += (uint64_t)expert * (uint64_t)p.cols * 8;
+        const uint64_t b_tile = b_tile0 + 2 * wave;
         const uint64_t ab = reinterpret_cast<uint64_t>(p.a.bits) + (kFp6 ? fp6_lo(a_tile, 0, p.S) : a_tile * tstride);
         const uint64_t bb = reinterpret_cast<uint64_t>(p.w.bits) + (kFp6 ? fp6_lo(b_tile, 0, p.S) : b_tile * tstride);
         const uint64_t sb = wave < 2
             ? reinterpret_cast<uint64_t>(p.a.sc) + (TA == 4 ? (uint64_t)by * 2 + wave : (uint64_t)by) * (uint64_t)p.S * 256
-            : reinterpret_cast<uint64_t>(p.w.sc) + ((uint64_t)bx * 2 + (wave - 2)) * (uint64_t)p.S * 256;
+            : reinterpret_cast<uint64_t>(p.w.sc) + (b_tile0 / 4 + (wave - 2)) * (uint64_t)p.S * 256;
         uint32_t lane = threadIdx.x & 63u;
         asm volatile("" : "+v"(lane));                       // nothing of it is kept through the loop for what follows, registers are short
         const uint32_t l16 = lane * 16u, l4 = lane * 4u;
@@ -541,7 +570,7 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                            // (anew, see above)
     const int lane = tid & 63, q = lane >> 4, c = lane & 15;
-    const int m0 = by * kRowsWg + wm * kRowsWave, n0 = bx * 256 + wn * 128;
+    const int m0 = (kIsExperts ? 0 : by * kRowsWg) + wm * kRowsWave, n0 = bx * 256 + wn * 128;
 #define DFP4_NATIVE_READ(G, V)                                                                      \
     asm volatile(DFP4_NATIVE_ACC_READ_##G                                                           \
                  : "=v"(V[0]), "=v"(V[1]), "=v"(V[2]), "=v"(V[3]), "=v"(V[4]), "=v"(V[5]),          \
@@ -553,7 +582,7 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
     // exact products, split K: the tile's partial sums, [range][(16 tile + x) * 256 + thread]
     constexpr int kPartTile = TA * 4 * 16 * 256;
     const float* parts = nullptr;
-    if constexpr (MODE != kPlain) {
+    if constexpr (kIsExact) {
         // (nothing of this before the loop: the norms are still on their way there)
 #pragma unroll
         for (int i = 0; i < TA / 2; ++i) asm volatile("" : "+v"(stat_a[i].sq), "+v"(stat_a[i].sq_low), "+v"(stat_a[i].sum_high), "+v"(stat_a[i].top));
@@ -620,11 +649,11 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
             __syncthreads();
         }
     }
-    if constexpr (MODE == kPlain) __syncthreads();               // the operands in LDS are done with
+    if constexpr (!kIsExact) __syncthreads();               // the operands in LDS are done with
     if (m0 >= p.M || n0 >= p.N) return;
     // accumulator group G, with the other ranges' partial sums in exact products
     auto finish = [&](auto g_c, int (&v)[16]) {
-        if constexpr (MODE != kPlain) {
+        if constexpr (kIsExact) {
             if (p.ksplit > 1) {
                 for (int r = 0; r < p.ksplit; ++r) {
                     if (r == sidx) continue;
@@ -685,13 +714,43 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(std::conditional_t<
         }
         return;
     }
+    if constexpr (MODE == kGated) {
+        // Columns are gate and up in turns: a lane's neighbouring registers.  Two groups (16 rows x 128 columns) make 16 rows of 64 results,
+        // which pass through LDS and leave 16 bytes a lane (rows of results are multiples of 16 bytes)
+        constexpr int kPitch = 36;                                                                 // dwords of a row in LDS
+        uint32_t* st = reinterpret_cast<uint32_t*>(s_stage) + wave * (16 * kPitch);
+        const int lr = lane >> 3, lc = (lane & 7) * 8, left = (p.N - n0) / 2 - lc;                  // results from the lane's first on
+        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)(m0 + lr) * p.ldc + n0 / 2 + lc;
+#define DFP4_NATIVE_GATED(G)                                                                        \
+        {                                                                                           \
+            int v[16];                                                                              \
+            DFP4_NATIVE_READ(G, v);                                                                 \
+            float h[8];                                                                             \
+            _Pragma("unroll") for (int x = 0; x < 8; ++x)                                           \
+                h[x] = silu_times(__builtin_bit_cast(float, v[2 * x]), __builtin_bit_cast(float, v[2 * x + 1])); \
+            _Pragma("unroll") for (int j = 0; j < 4; ++j)                                           \
+                st[c * kPitch + (G & 1) * 16 + 4 * j + q] = bf16_pair(__builtin_bit_cast(int, h[2 * j]), __builtin_bit_cast(int, h[2 * j + 1])); \
+            if constexpr (G & 1) {                                                                  \
+                in_order();                                                                         \
+                _Pragma("unroll") for (int k = 0; k < 2; ++k) {                                     \
+                    const uint4 y = *reinterpret_cast<const uint4*>(st + (k * 8 + lr) * kPitch + lc / 2); \
+                    const int m = (G >> 1) * 16 + k * 8;                                            \
+                    if (left > 0 && m0 + m + lr < p.M) *reinterpret_cast<uint4*>(out + (int64_t)m * p.ldc) = y; \
+                }                                                                                   \
+                in_order();                                                                         \
+            }                                                                                       \
+        }
+        DFP4_NATIVE_TILES(DFP4_NATIVE_GATED)
+#undef DFP4_NATIVE_GATED
+        return;
+    }
     constexpr int kEsz = BF16 ? 2 : 4;
     // native products, split K: the fp32 partial tile of this range goes to part[blockIdx.z] (the kernel is then the fp32 one)
     const bool partial = MODE == kPlain && p.ksplit > 1;
     const int64_t ld = partial ? p.N : p.ldc;
     uint8_t* base = partial ? reinterpret_cast<uint8_t*>(p.part + (int64_t)blockIdx.z * p.M * p.N)
                             : static_cast<uint8_t*>(p.out);
-    if constexpr (MODE != kPlain) base += bz * p.g.strideC * kEsz;
+    if constexpr (kIsExact) base += bz * p.g.strideC * kEsz;
     uint8_t* wave_out = base + ((int64_t)m0 * ld + n0) * kEsz;                                 // uniform
     const int64_t row_bytes = ld * kEsz;                                                       // uniform
     const bool full = m0 + kRowsWave <= p.M && n0 + 128 <= p.N;                                // uniform
@@ -1063,6 +1122,39 @@ int launch_gemm_native_packed(bool fp6, const void* a_packed, const void* w_pack
         else
             hipLaunchKernelGGL((native_reduce_kernel<false>), dim3(gr), dim3(256), 0, stream, p.part, out, p.M, p.N, ldc, p.ksplit);
     }
+    return check_launch();
+}
+
+int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream) {
+    ExpertsParams p{};
+    auto packed = [](const void* at, size_t scales) {
+        uint8_t* b = static_cast<uint8_t*>(const_cast<void*>(at));
+        return PackedOperand{b, reinterpret_cast<uint32_t*>(b + scales)};
+    };
+    p.a = packed(t.a, t.a_scales);
+    p.w = packed(t.w, t.w_scales);
+    p.out = t.out;
+    p.N = t.rows;
+    p.S = (int)((t.K / kBlock + 1) / 2);
+    p.ldc = t.gated ? t.rows / 2 : t.rows;
+    p.ksplit = 1;
+    p.used = t.used;
+    p.groups = t.groups;
+    p.cols = t.tiles;
+    if (t.max_groups > 0x3fffffff) return DFP4_ERR_SHAPE;
+    p.max_groups = (int)t.max_groups;
+    const int64_t units = t.max_groups * (kGroupRows / (t.half ? 128 : 256)), wgs = (units + 7) / 8 * 8 * p.cols;
+    if (wgs >= (int64_t)1 << 24) return DFP4_ERR_SHAPE;                       // fewer than 2^32 threads
+    const dim3 grid((unsigned)wgs);
+    auto run = [&](auto bf16_c, auto mode_c) {
+        constexpr bool kBf16 = decltype(bf16_c)::value;
+        constexpr int kMode = decltype(mode_c)::value;
+        if (t.half) hipLaunchKernelGGL((gemm_native_kernel<kFmtFp6, kBf16, 2, kMode>), grid, dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((gemm_native_kernel<kFmtFp6, kBf16, 4, kMode>), grid, dim3(256), 0, stream, p);
+    };
+    if (t.gated) run(std::true_type{}, std::integral_constant<int, kGated>{});
+    else if (t.out_dtype == DFP4_BF16) run(std::true_type{}, std::integral_constant<int, kExperts>{});
+    else run(std::false_type{}, std::integral_constant<int, kExperts>{});
     return check_launch();
 }
 

@@ -199,17 +199,17 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
     const uint32_t count = s_count[mine], my_groups = (count + kGroupRows - 1) / kGroupRows;
     if (tid == 0) {
         v.offsets[mine] = (int32_t)row0;
-        v.first_group[mine] = (int32_t)group0;
     }
-    for (uint32_t g = tid; g < my_groups; g += kPlanThreads) v.group_expert[group0 + g] = mine;
+    for (uint32_t g = tid; g < my_groups; g += kPlanThreads)
+        v.groups[group0 + g] = PlanGroup{mine, (int32_t)(row0 + g * kGroupRows), (int32_t)min(count - g * kGroupRows, (uint32_t)kGroupRows), 0};
     for (uint32_t r = tid; r < count; r += kPlanThreads) v.row_at[row0 + r] = (int32_t)(group0 * kGroupRows + r);
     if (mine == experts - 1) {
         const uint32_t rows = row0 + count, used = group0 + my_groups;
         if (tid == 0) {
             v.offsets[experts] = (int32_t)rows;
-            v.first_group[experts] = (int32_t)used;
+            *v.used = (int32_t)used;
         }
-        for (int64_t g = used + tid; g < groups; g += kPlanThreads) v.group_expert[g] = -1;
+        for (int64_t g = used + tid; g < groups; g += kPlanThreads) v.groups[g] = PlanGroup{0, 0, 0, 0};
         for (int64_t r = (int64_t)rows + tid; r < pairs; r += kPlanThreads) v.order[r] = v.row_at[r] = -1;
     }
     uint32_t at = row0;
