@@ -502,7 +502,7 @@ int dfp4_expert_plan(const int32_t* ids, dfp4_plan plan, void* stream);
  * Experts' weights, laid out once: expert e's matrix is rows e * rows .. of a quantized tensor [experts * rows, K]; two of them (gate and up)
  * for the product with the activation.
  *   packed   device, 256-byte aligned, dfp4_expert_weights_bytes(experts, rows, K, gated) bytes; the layout is private to the library
- *            (0.79 bytes an element)
+ *            (1.35 bytes an element: one form for many rows an expert, one for few)
  *   up       of dfp4_expert_weights: the second tensor (gated), or one with codes NULL
  */
 typedef struct dfp4_experts {

@@ -17,8 +17,6 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-constexpr int kFmtFp6 = 2;                       // E2M3
-
 inline int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 inline int64_t steps_of(int64_t K) { return (K / kBlock + 1) / 2; }
 
@@ -38,13 +36,22 @@ __device__ __forceinline__ size_t scale_at(size_t tile, size_t step, size_t S) {
 
 // ---- weights
 
+// The 4-bit form for products of few rows: a quad of blocks (128 elements) of a tile of 32 packed rows is 64 lanes x 16 bytes of codes for each
+// of two steps, then 64 dwords: exponent bytes of the steps, dialects of the four blocks.  Lane (h, r) has half h of both of a step's blocks
+// of row r, and the exponents of block h (the order of the instruction's FP8 operands).
+constexpr int kQuadBytes = 2304;
+inline int64_t quads_of(int64_t K) { return (K / kBlock + 3) / 4; }
+inline int64_t row_tiles(const dfp4_experts& w) { return (expert_rows(w) + 31) / 32; }
+
 struct PackArgs {
     const uint8_t *codes[2], *dial[2], *expo[2];
     Packed to;
-    int rows, KB, S, gated;
+    uint8_t* quads;
+    int rows, KB, S, gated, tiles, Q;            // tiles of 32 packed rows of an expert in `quads`, quads of blocks
 };
 
-// One wave per (tile, step); lane (kh, c) takes row c of the tile, block 2 step + kh.  What is not there is zeros.
+// One wave per (tile, step); lane (kh, c) takes row c of the tile, block 2 step + kh.  What is not there is zeros.  The 4-bit form of the same:
+// half kh of both blocks of a step.
 __global__ __launch_bounds__(256) void experts_pack_kernel(PackArgs p) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kh = lane >> 5, c = lane & 31;
     const int s = blockIdx.x * 4 + wave;
@@ -64,6 +71,21 @@ __global__ __launch_bounds__(256) void experts_pack_kernel(PackArgs p) {
     *reinterpret_cast<uint4*>(p.to.bits + fp6_lo(tile, s, p.S) + lane * 16) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
     *reinterpret_cast<uint2*>(p.to.bits + fp6_hi(tile, s, p.S) + fp6_hi_lane(lane) * 8) = make_uint2(v.w[4], v.w[5]);
     p.to.scales[scale_at(tile, s, p.S) + lane * 4] = (uint8_t)eb;
+    if ((int)blockIdx.y >= p.tiles) return;
+    // the other half-wave's block: its half `kh` for half 0 of its own, its dialect
+    uint8_t* quad = p.quads + ((expert * p.tiles + blockIdx.y) * p.Q + (s >> 1)) * kQuadBytes;
+    const uint32_t keep0 = kh ? codes.z : codes.x, keep1 = kh ? codes.w : codes.y, give0 = kh ? codes.x : codes.z, give1 = kh ? codes.y : codes.w;
+    const uint32_t got0 = __shfl_xor(give0, 32), got1 = __shfl_xor(give1, 32), other = __shfl_xor(dl, 32);
+    *reinterpret_cast<uint4*>(quad + (s & 1) * 1024 + lane * 16) = kh ? make_uint4(got0, got1, keep0, keep1) : make_uint4(keep0, keep1, got0, got1);
+    const uint32_t first = kh ? other : dl, second = kh ? dl : other;
+    uint8_t* meta = quad + 2048 + lane * 4;
+    meta[s & 1] = (uint8_t)eb;
+    meta[2 + (s & 1)] = (uint8_t)(first | second << 4);
+    if (s == p.S - 1 && (p.S & 1)) {                             // no second step
+        *reinterpret_cast<uint4*>(quad + 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+        meta[1] = 0;
+        meta[3] = 0x77;
+    }
 }
 
 // ---- rows
@@ -134,74 +156,241 @@ __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArg
     }
 }
 
-// ---- products
+// ---- products of few rows an expert
 
-struct ProductArgs {
-    Packed a, w;
-    const int32_t* used;
+// FP8 E4M3 bit patterns of a dialect's 8 magnitudes (0.5 u, all exact)
+constexpr uint8_t e4m3_of_half_units(int u) {
+    int e = -1;                                                        // floor(log2(0.5 u))
+    for (int v = u; v > 1; v >>= 1) ++e;
+    return u == 0 ? 0 : (uint8_t)(((e + 7) << 3) | (((u << 3) >> (e + 1)) & 7));
+}
+struct F8Book { uint32_t w[kDialects][2]; };
+constexpr F8Book make_f8_book() {
+    F8Book b{};
+    for (int d = 0; d < kDialects; ++d)
+        for (int j = 0; j < 8; ++j) b.w[d][j / 4] |= (uint32_t)e4m3_of_half_units(kBook[d][j]) << (8 * (j % 4));
+    return b;
+}
+static __device__ const F8Book g_f8_book = make_f8_book();
+
+struct FewArgs {
+    const uint8_t *x_codes, *x_dial, *x_expo;    // quantized rows [.., K]
+    const uint8_t* quads;                        // the weights' 4-bit form
+    const int32_t *used, *order;
     const PlanGroup* plan;
     void* out;                                   // up: bf16 [row][rows / 2], down: f32 [row][rows]
     int64_t groups;                              // at most
-    int S, rows, tiles, row_tiles;               // of an expert: packed rows, tiles of 32 with padding, tiles that have rows
+    uint32_t k;                                  // rows of x are tokens', pair / k; 0: the plan's own
+    int KB, Q, rows, tiles;                      // blocks, quads of blocks; packed rows of an expert, tiles of 32 of them
 };
 
 __device__ __forceinline__ uint16_t bf16_of(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+// 8 codes -> FP8: elements 0, 2, 4, 6 and 1, 3, 5, 7 (rows and weights the same way, so that the order within a half of a block is free)
+__device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, uint32_t& odd) {
+    even = __builtin_amdgcn_perm(tab.y, tab.x, c & 0x07070707u) | ((c << 4) & 0x80808080u);
+    odd = __builtin_amdgcn_perm(tab.y, tab.x, (c >> 4) & 0x07070707u) | (c & 0x80808080u);
+}
 
-// 32 rows x 32 packed rows of weights a workgroup; its 16 waves share K and add their sums in a fixed order through LDS.
-template <bool GATED>
-__global__ __launch_bounds__(1024, 4) void experts_kernel(ProductArgs p) {
-    __shared__ float s_red[8][16][64];
+// A workgroup keeps 32 MT rows of a group in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
+// packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
+// Bound by the weights' stream (0.5625 bytes an element).
+template <bool GATED, int MT, int SPLIT>
+__global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
+    constexpr int kQuads = 32 / MT, kTiles = 16 / SPLIT, kAhead = 4;  // quads of rows in LDS (a chunk of K); tiles at a time
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[MT][kQuads * 2][2][64][16];      // [tile of rows][step][block][lane]
+    __shared__ __attribute__((aligned(16))) uint16_t s_xs[MT][kQuads][64];              // exponents of a quad's two steps
+    __shared__ float s_red[SPLIT > 1 ? 16 : 1][4][64];
+    __shared__ uint2 s_tab[kDialects];
+    __shared__ int32_t s_row[32 * MT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int S = p.S, per = (S + 15) / 16, s_lo = min(S, wave * per), s_hi = min(S, s_lo + per);
-    const int64_t used = min((int64_t)*p.used, p.groups), total = used * 8 * p.row_tiles;
-    for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
-        const int64_t eighth = id / p.row_tiles;
-        const PlanGroup group = p.plan[eighth >> 3];
-        const int t = (int)(id - eighth * p.row_tiles), skip = (int)(eighth & 7) * 32, rows = min(32, group.rows - skip);
-        if (rows <= 0) continue;
-        const int64_t row0 = (int64_t)group.row0 + skip;
-        const size_t a_tile = (size_t)eighth, w_tile = (size_t)group.expert * p.tiles + t;
-        v16f acc;
+    const int part = wave % SPLIT, sub = wave / SPLIT, h = lane >> 5, c = lane & 31;
+    if (tid < kDialects) s_tab[tid] = make_uint2(g_f8_book.w[tid][0], g_f8_book.w[tid][1]);
+    const int batches = (p.tiles + kTiles - 1) / kTiles, chunks = (p.Q + kQuads - 1) / kQuads;
+    const int64_t used = min((int64_t)*p.used, p.groups), items = used * batches;
+    const int64_t lo = items * blockIdx.x / gridDim.x, hi = items * (blockIdx.x + 1) / gridDim.x;
+    if (lo >= hi) return;
+
+    // where this wave is: item, block of rows, chunk
+    struct At {
+        int64_t item, group;
+        int batch, block, chunk;
+        PlanGroup g;
+    };
+    auto begin = [&](int64_t item) {
+        At a;
+        a.item = item;
+        a.group = item / batches;
+        a.batch = (int)(item - a.group * batches);
+        a.block = a.chunk = 0;
+        a.g = p.plan[a.group];
+        return a;
+    };
+    auto after = [&](const At& a) {
+        At n = a;
+        if (++n.chunk < chunks) return n;
+        n.chunk = 0;
+        if (++n.block * (32 * MT) < a.g.rows) return n;
+        return a.item + 1 < hi ? begin(a.item + 1) : a;              // (behind the last: loaded once more, not used)
+    };
+    // its quads there: the first one's address and their number
+    struct Segment {
+        const uint8_t* at;
+        int first, n;
+    };
+    auto segment = [&](const At& a) {
+        const int in = min(kQuads, p.Q - a.chunk * kQuads), per = (in + SPLIT - 1) / SPLIT, first = part * per, n = max(0, min(in, first + per) - first);
+        const int tile = min(a.batch * kTiles + sub, p.tiles - 1);
+        return Segment{p.quads + (((int64_t)a.g.expert * p.tiles + tile) * p.Q + a.chunk * kQuads + (n > 0 ? first : 0)) * kQuadBytes, first, n};
+    };
+    struct Quad {
+        uint4 c[2];
+        uint32_t meta;
+    } ring[kAhead];
+    auto load = [&](Quad& q, const Segment& s, int i) {
+        const uint8_t* at = s.at + (int64_t)max(0, min(i, s.n - 1)) * kQuadBytes;
+        q.c[0] = *reinterpret_cast<const uint4*>(at + lane * 16);
+        q.c[1] = *reinterpret_cast<const uint4*>(at + 1024 + lane * 16);
+        q.meta = *reinterpret_cast<const uint32_t*>(at + 2048 + lane * 4);
+    };
+    v16f acc[MT];
+    auto clear = [&] {
 #pragma unroll
-        for (int x = 0; x < 16; ++x) acc[x] = 0.0f;
-        for (int s = s_lo; s < s_hi; ++s) {
-            const uint4 alo = *reinterpret_cast<const uint4*>(p.a.bits + fp6_lo(a_tile, s, S) + lane * 16);
-            const uint2 ahi = *reinterpret_cast<const uint2*>(p.a.bits + fp6_hi(a_tile, s, S) + fp6_hi_lane(lane) * 8);
-            const uint4 wlo = *reinterpret_cast<const uint4*>(p.w.bits + fp6_lo(w_tile, s, S) + lane * 16);
-            const uint2 whi = *reinterpret_cast<const uint2*>(p.w.bits + fp6_hi(w_tile, s, S) + fp6_hi_lane(lane) * 8);
-            const int as = p.a.scales[scale_at(a_tile, s, S) + lane * 4], ws = p.w.scales[scale_at(w_tile, s, S) + lane * 4];
-            const v8i a = {(int)alo.x, (int)alo.y, (int)alo.z, (int)alo.w, (int)ahi.x, (int)ahi.y, 0, 0};
-            const v8i w = {(int)wlo.x, (int)wlo.y, (int)wlo.z, (int)wlo.w, (int)whi.x, (int)whi.y, 0, 0};
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, acc, kFmtFp6, kFmtFp6, 0, ws, 0, as);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
+    };
+    auto multiply = [&](const Quad& q, int at) {                     // quad `at` of the chunk
+        int xs[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xs[i] = s_xs[i][at][lane];
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            const uint32_t d = q.meta >> (16 + 8 * step);
+            const uint2 t0 = s_tab[d & 15u], t1 = s_tab[(d >> 4) & 15u];
+            uint32_t w[8];
+            expand8(q.c[step].x, t0, w[0], w[1]);
+            expand8(q.c[step].y, t0, w[2], w[3]);
+            expand8(q.c[step].z, t1, w[4], w[5]);
+            expand8(q.c[step].w, t1, w[6], w[7]);
+            const v8i wv = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], (int)w[6], (int)w[7]};
+            v8i xv[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int4 a = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][0][lane]), b = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][1][lane]);
+                xv[i] = v8i{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (step == 0) acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv[i], acc[i], 0, 0, 0, (int)q.meta, 0, xs[i]);
+                else acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv[i], acc[i], 0, 0, 1, (int)q.meta, 1, xs[i]);
+            }
+            // the operands are in use until here (a result must not overlap them, see gemm_f8.hip)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(acc[i]) : "v"(wv), "v"(xv[i]));
         }
-        __syncthreads();                                       // the sums of the round before are read
-        if (wave >= 8) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) s_red[wave - 8][x][lane] = acc[x];
+    };
+    // rows of the chunk into LDS; blocks behind the last of a quad as zeros
+    auto stage = [&](const At& a) {
+        const int rows = min(32 * MT, a.g.rows - a.block * 32 * MT), q0 = a.chunk * kQuads, blocks = min(kQuads, p.Q - q0) * 4;
+        __syncthreads();                                             // what was there is done with
+        for (int r = tid; r < rows; r += 1024) {
+            const int64_t row = (int64_t)a.g.row0 + a.block * 32 * MT + r;
+            s_row[r] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
         }
         __syncthreads();
-        if (wave < 8) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) s_red[wave][x][lane] += acc[x];
+        for (int i = tid; i < rows * blocks; i += 1024) {
+            const int r = i / blocks, b = i - r * blocks, kb = q0 * 4 + b;
+            const int64_t blk = (int64_t)s_row[r] * p.KB + kb;
+            uint4 codes = make_uint4(0, 0, 0, 0);
+            uint32_t e = 0, d = 7;
+            if (kb < p.KB) {
+                codes = *reinterpret_cast<const uint4*>(p.x_codes + blk * 16);
+                e = p.x_expo[blk];
+                d = p.x_dial[blk] & 15u;
+            }
+            const uint2 tab = s_tab[d];
+            uint4 lo4, hi4;
+            expand8(codes.x, tab, lo4.x, lo4.y);
+            expand8(codes.y, tab, lo4.z, lo4.w);
+            expand8(codes.z, tab, hi4.x, hi4.y);
+            expand8(codes.w, tab, hi4.z, hi4.w);
+            const int t = r >> 5, l = r & 31;
+            *reinterpret_cast<uint4*>(s_x[t][b >> 1][b & 1][l]) = lo4;
+            *reinterpret_cast<uint4*>(s_x[t][b >> 1][b & 1][32 + l]) = hi4;
+            reinterpret_cast<uint8_t*>(&s_xs[t][b >> 2][(b & 1) * 32 + l])[(b >> 1) & 1] = (uint8_t)e;
         }
         __syncthreads();
-        // register x of lane (h, c): packed row 8 (x / 4) + 4 h + x % 4, row c
-        const int c = lane & 31, h = lane >> 5;
-        auto sum = [&](int x) {
-            float v = 0.0f;
+    };
+    // registers x and x + 1 (x even) of lane (h, c): packed rows 8 (x / 4) + 4 h + x % 4 and the next, row c
+    auto emit = [&](const At& a, int i, int tile, int x, float v0, float v1) {
+        const int r = (a.block * MT + i) * 32 + c, n = tile * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
+        if (tile >= p.tiles || r >= a.g.rows || n >= p.rows) return;
+        const int64_t row = (int64_t)a.g.row0 + r;
+        if constexpr (GATED) static_cast<uint16_t*>(p.out)[row * (p.rows >> 1) + (n >> 1)] = bf16_of(silu_times(v0, v1));
+        else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + row * p.rows + n) = make_float2(v0, v1);
+    };
+
+    At now = begin(lo);
+    Segment seg = segment(now);
 #pragma unroll
-            for (int w8 = 0; w8 < 8; ++w8) v += s_red[w8][x][lane];
-            return v;
-        };
-        if constexpr (GATED) {
-            const int x = 2 * wave, n = t * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
-            if (wave < 8 && c < rows && n < p.rows)
-                static_cast<uint16_t*>(p.out)[(row0 + c) * (p.rows >> 1) + (n >> 1)] = bf16_of(silu_times(sum(x), sum(x + 1)));
-        } else {
-            const int x = wave, n = t * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
-            if (c < rows && n < p.rows) static_cast<float*>(p.out)[(row0 + c) * p.rows + n] = sum(x);
+    for (int d = 0; d < kAhead; ++d) load(ring[d], seg, d);
+    int64_t staged_group = -1;
+    int staged_block = 0, staged_chunk = 0;
+    clear();
+    for (;;) {
+        const bool last_chunk = now.chunk + 1 == chunks, last = last_chunk && (now.block + 1) * (32 * MT) >= now.g.rows && now.item + 1 >= hi;
+        if (staged_group != now.group || staged_block != now.block || staged_chunk != now.chunk) {
+            stage(now);
+            staged_group = now.group, staged_block = now.block, staged_chunk = now.chunk;
         }
+        const At then = after(now);
+        const Segment next = segment(then);
+        if (seg.n == 0) {
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) load(ring[d], next, d);
+        }
+        for (int q = 0; q < seg.n; q += kAhead) {
+            const bool more = q + kAhead < seg.n;
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) {
+                if (q + d < seg.n) multiply(ring[d], seg.first + q + d);
+                load(ring[d], more ? seg : next, more ? q + kAhead + d : d);
+            }
+        }
+        if (last_chunk) {
+            if constexpr (SPLIT == 1) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int x = 0; x < 16; x += 2) emit(now, i, now.batch * kTiles + sub, x, acc[i][x], acc[i][x + 1]);
+            } else {
+                // four registers at a time through LDS, the parts of K added in their order
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int x4 = 0; x4 < 16; x4 += 4) {
+                        __syncthreads();
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) s_red[wave][x][lane] = acc[i][x4 + x];
+                        __syncthreads();
+                        for (int job = wave; job < 2 * kTiles; job += 16) {
+                            const int tile = job >> 1, x = (job & 1) * 2;
+                            float v0 = 0.0f, v1 = 0.0f;
+#pragma unroll
+                            for (int w = 0; w < SPLIT; ++w) {
+                                v0 += s_red[tile * SPLIT + w][x][lane];
+                                v1 += s_red[tile * SPLIT + w][x + 1][lane];
+                            }
+                            emit(now, i, now.batch * kTiles + tile, x4 + x, v0, v1);
+                        }
+                    }
+            }
+            clear();
+        }
+        if (last) return;
+        now = then;
+        seg = next;
     }
 }
 
@@ -241,24 +430,36 @@ __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p) {
     }
 }
 
-// workspace: rows in operand order, and down their products
+// workspace: rows in operand order, or in their 4-bit form (few), and down their products
 struct Workspace {
-    int64_t rows, part, total;
+    bool many;
+    int64_t rows, dial, expo, part, total;
 };
 inline Workspace workspace_of(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t pairs = plan.tokens * plan.k;
     Workspace x{};
-    x.rows = plan_groups(pairs, plan.experts) * kGroupRows;
-    x.part = up256((int64_t)native_packed_bytes(x.rows, w.K, true));
+    x.many = pairs >= 64 * w.experts;
+    if (x.many) {
+        x.rows = plan_groups(pairs, plan.experts) * kGroupRows;
+        x.part = up256((int64_t)native_packed_bytes(x.rows, w.K, true));
+    } else {
+        x.rows = w.gated ? plan.tokens : pairs;
+        x.dial = up256(x.rows * (w.K / 2));
+        x.expo = x.dial + up256(x.rows * (w.K / kBlock));
+        x.part = x.expo + up256(x.rows * (w.K / kBlock));
+    }
     x.total = x.part + (w.gated ? 0 : up256(pairs * w.rows * 4));
     return x;
 }
 
 }  // namespace
 
+// where the 4-bit form lies in the packed weights
+static int64_t quads_offset(const dfp4_experts& w) { return up256((int64_t)native_packed_bytes(w.experts * padded_rows(w), w.K, true)); }
+
 size_t expert_weights_bytes(int64_t experts, int64_t rows, int64_t K, bool gated) {
     const dfp4_experts w{nullptr, experts, rows, K, gated ? 1 : 0};
-    return native_packed_bytes(experts * padded_rows(w), K, true);
+    return (size_t)(quads_offset(w) + up256(experts * row_tiles(w) * quads_of(K) * kQuadBytes));
 }
 
 int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& w, hipStream_t stream) {
@@ -267,6 +468,7 @@ int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& 
     p.codes[1] = up.codes, p.dial[1] = up.dialect, p.expo[1] = up.exponent;
     p.to = packed_at(w.packed, w.experts * padded_rows(w), w.K);
     p.rows = (int)w.rows, p.KB = (int)(w.K / kBlock), p.S = (int)steps_of(w.K), p.gated = w.gated ? 1 : 0;
+    p.quads = static_cast<uint8_t*>(w.packed) + quads_offset(w), p.tiles = (int)row_tiles(w), p.Q = (int)quads_of(w.K);
     const dim3 grid((unsigned)((p.S + 3) / 4), (unsigned)(padded_rows(w) / 32), (unsigned)w.experts);
     hipLaunchKernelGGL(experts_pack_kernel, grid, dim3(256), 0, stream, p);
     return check_launch();
@@ -274,45 +476,65 @@ int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& 
 
 size_t experts_workspace_bytes(const dfp4_plan& plan, const dfp4_experts& w) { return (size_t)workspace_of(plan, w).total; }
 
+template <bool GATED, int MT>
+static void launch_few(const FewArgs& p, int split, dim3 grid, hipStream_t stream) {
+    if (split == 1) hipLaunchKernelGGL((experts_few_kernel<GATED, MT, 1>), grid, dim3(1024), 0, stream, p);
+    else if (split == 2) hipLaunchKernelGGL((experts_few_kernel<GATED, MT, 2>), grid, dim3(1024), 0, stream, p);
+    else if (split == 4) hipLaunchKernelGGL((experts_few_kernel<GATED, MT, 4>), grid, dim3(1024), 0, stream, p);
+    else if (split == 8) hipLaunchKernelGGL((experts_few_kernel<GATED, MT, 8>), grid, dim3(1024), 0, stream, p);
+    else hipLaunchKernelGGL((experts_few_kernel<GATED, MT, 16>), grid, dim3(1024), 0, stream, p);
+}
+
 int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
-    const int64_t pairs = a.plan.tokens * a.plan.k, S = steps_of(a.w.K);
+    const int64_t pairs = a.plan.tokens * a.plan.k, S = steps_of(a.w.K), groups = plan_groups(pairs, a.plan.experts);
     const Workspace ws = workspace_of(a.plan, a.w);
     const PlanView plan = plan_view(a.plan);
     const int cus = device_cu_count();
-    QuantizeArgs q{};
-    q.x = a.x, q.ld = a.ld;
-    q.rows = plan.offsets + a.plan.experts, q.order = plan.order, q.row_at = plan.row_at;
-    q.to = packed_at(a.workspace, ws.rows, a.w.K);
-    q.k = a.w.gated ? (uint32_t)a.plan.k : 0, q.KB = (uint32_t)(a.w.K / kBlock), q.S = (uint32_t)S;
-    q.bound = pairs;
-    const int64_t units = (pairs + 7) / 8 * ((S + 3) / 4), want = (units + kQWaves - 1) / kQWaves;
-    hipLaunchKernelGGL(experts_quantize_kernel, dim3((unsigned)(want < 8 * cus ? want : 8 * cus)), dim3(kQThreads), 0, stream, q);
-    ProductArgs p{};
-    p.a = q.to;
-    p.w = packed_at(a.w.packed, a.w.experts * padded_rows(a.w), a.w.K);
-    p.used = plan.used, p.plan = plan.groups;
-    p.out = a.w.gated ? a.out : a.workspace + ws.part;
-    p.groups = plan_groups(pairs, a.plan.experts);
-    p.S = (int)S, p.rows = (int)expert_rows(a.w), p.tiles = (int)(padded_rows(a.w) / 32), p.row_tiles = (p.rows + 31) / 32;
-    const bool many = pairs >= 64 * a.w.experts, part16 = many && a.out_dtype == DFP4_BF16;
-    if (many) {
+    void* out = a.w.gated ? a.out : a.workspace + ws.part;
+    const bool part16 = ws.many && a.out_dtype == DFP4_BF16;
+    if (ws.many) {
+        QuantizeArgs q{};
+        q.x = a.x, q.ld = a.ld;
+        q.rows = plan.offsets + a.plan.experts, q.order = plan.order, q.row_at = plan.row_at;
+        q.to = packed_at(a.workspace, ws.rows, a.w.K);
+        q.k = a.w.gated ? (uint32_t)a.plan.k : 0, q.KB = (uint32_t)(a.w.K / kBlock), q.S = (uint32_t)S;
+        q.bound = pairs;
+        const int64_t units = (pairs + 7) / 8 * ((S + 3) / 4), want = (units + kQWaves - 1) / kQWaves;
+        hipLaunchKernelGGL(experts_quantize_kernel, dim3((unsigned)(want < 8 * cus ? want : 8 * cus)), dim3(kQThreads), 0, stream, q);
         ExpertTiles t{};
         t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
         t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);
-        t.used = plan.used, t.groups = plan.groups, t.max_groups = p.groups;
-        t.K = (int)a.w.K, t.rows = p.rows, t.tiles = p.tiles / 8;
+        t.used = plan.used, t.groups = plan.groups, t.max_groups = groups;
+        t.K = (int)a.w.K, t.rows = (int)expert_rows(a.w), t.tiles = (int)(padded_rows(a.w) / 256);
         t.gated = a.w.gated != 0, t.half = false;
-        t.out = p.out, t.out_dtype = a.out_dtype;
+        t.out = out, t.out_dtype = a.out_dtype;
         const int rc = launch_expert_tiles(t, stream);
         if (rc != DFP4_OK) return rc;
     } else {
-        const int64_t all = p.groups * 8 * p.row_tiles;
-        const dim3 grid((unsigned)(all < (1 << 20) ? all : 1 << 20));
-        if (a.w.gated) hipLaunchKernelGGL((experts_kernel<true>), grid, dim3(1024), 0, stream, p);
-        else hipLaunchKernelGGL((experts_kernel<false>), grid, dim3(1024), 0, stream, p);
+        const dfp4_tensor x{a.workspace, a.workspace + ws.dial, a.workspace + ws.expo, ws.rows, a.w.K};
+        const int rc = launch_quantize(false, a.x, ws.rows, a.w.K, a.ld, x, stream);
+        if (rc != DFP4_OK) return rc;
+        FewArgs p{};
+        p.x_codes = x.codes, p.x_dial = x.dialect, p.x_expo = x.exponent;
+        p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
+        p.used = plan.used, p.order = plan.order, p.plan = plan.groups;
+        p.out = out, p.groups = groups;
+        p.k = a.w.gated ? (uint32_t)a.plan.k : 0;
+        p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
+        // the experts that tokens go to, were all alike
+        const int64_t active = pairs < a.w.experts ? pairs : a.w.experts;
+        const int mt = pairs > 16 * active ? 2 : 1;
+        int split = 1;
+        while (split < 16 && split < p.Q && active * p.tiles * split < (int64_t)16 * 2 * cus) split *= 2;
+        const int64_t items = groups * ((p.tiles + 16 / split - 1) / (16 / split));
+        const dim3 grid((unsigned)(items < cus ? items : cus));
+        if (a.w.gated && mt == 1) launch_few<true, 1>(p, split, grid, stream);
+        else if (a.w.gated) launch_few<true, 2>(p, split, grid, stream);
+        else if (mt == 1) launch_few<false, 1>(p, split, grid, stream);
+        else launch_few<false, 2>(p, split, grid, stream);
     }
     if (!a.w.gated) {
-        const JoinArgs j{p.out, a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
+        const JoinArgs j{out, a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
         const int64_t wgs = (a.plan.tokens * (a.w.rows / 4) + 255) / 256;
         const dim3 jg((unsigned)(wgs < (1 << 20) ? wgs : 1 << 20));
         if (part16) hipLaunchKernelGGL((experts_join_kernel<true, true>), jg, dim3(256), 0, stream, j);
