@@ -607,8 +607,7 @@ static int check_plan(const dfp4_plan& p) {
 
 size_t dfp4_expert_plan_bytes(int64_t tokens, int64_t k, int64_t experts) {
     if (check_plan(dfp4_plan{nullptr, tokens, k, experts}) != DFP4_OK) return 0;
-    const int64_t pairs = tokens * k;
-    return (size_t)(plan_groups_at(pairs, experts) + 4 * plan_groups(pairs, experts)) * 4;
+    return (size_t)plan_sizes(tokens * k, experts).total * 4;
 }
 
 int dfp4_expert_plan(const int32_t* ids, dfp4_plan plan, void* stream) {

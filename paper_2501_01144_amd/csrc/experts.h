@@ -11,31 +11,53 @@ constexpr int64_t kMaxPairs = (int64_t)1 << 27;
 // tile of the products.
 constexpr int kGroupRows = 256;
 
-// Groups that `pairs` rows of `experts` experts can take, at most
-__host__ __device__ inline int64_t plan_groups(int64_t pairs, int64_t experts) { return pairs / kGroupRows + (pairs < experts ? pairs : experts); }
-
+// Rows of an expert, from the plan's row `row0` on; `at`: its first row among the padded ones
 struct PlanGroup {
-    int32_t expert, row0, rows, none;      // rows 0: behind the last group
+    int32_t expert, row0, rows, at;
 };
+// Three lists of them: groups, halves of 128 rows and, for products of few rows, blocks of 64; only what has rows
+constexpr int kListRows[3] = {kGroupRows, 128, 64};
+__host__ __device__ inline int64_t plan_list(int64_t pairs, int64_t experts, int list) { return pairs / kListRows[list] + (pairs < experts ? pairs : experts); }
+// The plan is made by up to 64 workgroups of shares of the pairs, each a multiple of 1024
+inline int64_t plan_share(int64_t pairs) {
+    const int64_t s = ((pairs + 63) / 64 + 1023) / 1024 * 1024;
+    return s < 4096 ? 4096 : s;
+}
+inline int64_t plan_shares(int64_t pairs) { return pairs <= plan_share(pairs) ? 1 : (pairs + plan_share(pairs) - 1) / plan_share(pairs); }
 // Arrays of a plan, one after the other (the first three are public)
 struct PlanView {
     int32_t* offsets;        // [experts + 1]
     int32_t* order;          // [pairs] pair of a row, -1 behind the last
     int32_t* place;          // [pairs] row of a pair, -1: none
     int32_t* row_at;         // [pairs] group * kGroupRows + row in it, of a row
-    int32_t* used;           // [1] groups
-    PlanGroup* groups;       // 16-byte aligned
+    int32_t* used;           // [3] of each list
+    PlanGroup* list[3];      // 16-byte aligned
+    int32_t* counts;         // [shares][experts], where there are several
 };
-__host__ __device__ inline int64_t plan_groups_at(int64_t pairs, int64_t experts) { return (experts + 1 + 3 * pairs + 1 + 3) / 4 * 4; }
+struct PlanSizes {
+    int64_t list_at[3], counts_at, total;      // int32
+};
+inline PlanSizes plan_sizes(int64_t pairs, int64_t experts) {
+    PlanSizes s;
+    s.counts_at = (experts + 1 + 3 * pairs + 3 + 3) / 4 * 4;
+    for (int q = 0; q < 3; ++q) {
+        s.list_at[q] = s.counts_at;
+        s.counts_at += 4 * plan_list(pairs, experts, q);
+    }
+    s.total = s.counts_at + (plan_shares(pairs) > 1 ? plan_shares(pairs) * experts : 0);
+    return s;
+}
 inline PlanView plan_view(const dfp4_plan& p) {
     const int64_t pairs = p.tokens * p.k;
+    const PlanSizes s = plan_sizes(pairs, p.experts);
     PlanView v;
     v.offsets = p.data;
     v.order = v.offsets + p.experts + 1;
     v.place = v.order + pairs;
     v.row_at = v.place + pairs;
     v.used = v.row_at + pairs;
-    v.groups = reinterpret_cast<PlanGroup*>(p.data + plan_groups_at(pairs, p.experts));
+    for (int q = 0; q < 3; ++q) v.list[q] = reinterpret_cast<PlanGroup*>(p.data + s.list_at[q]);
+    v.counts = p.data + s.counts_at;
     return v;
 }
 
@@ -80,9 +102,9 @@ struct ExpertsArgs {
 struct ExpertTiles {
     const void *a, *w;       // packed rows and weights, and the offsets of their scales
     size_t a_scales, w_scales;
-    const int32_t* used;
-    const PlanGroup* groups;
-    int64_t max_groups;
+    const int32_t* used;     // of the list that matches `half`
+    const PlanGroup* list;
+    int64_t most;
     int K, rows, tiles;      // packed rows of an expert, tiles of 256 of them
     bool gated, half;        // half: tiles of 128 rows
     void* out;               // gated: bf16 [row][rows / 2], else [row][rows] of out_dtype

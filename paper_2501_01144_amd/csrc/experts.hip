@@ -5,6 +5,7 @@
 // rows of its expert's weights; down, experts_join_kernel adds a token's rows in a fixed order.
 // Gate and up rows take turns in the packed weights, and weights are the instruction's first operand, rows its second: a lane then holds
 // both numbers that an element of h is made of.
+#include <math.h>
 #include <type_traits>
 #include "experts.h"
 #include "fp6_pack.h"
@@ -174,12 +175,14 @@ constexpr F8Book make_f8_book() {
 static __device__ const F8Book g_f8_book = make_f8_book();
 
 struct FewArgs {
+    const uint16_t* x;                           // rows in bf16, quantized on their way to LDS; or null:
+    int64_t ld;
     const uint8_t *x_codes, *x_dial, *x_expo;    // quantized rows [.., K]
     const uint8_t* quads;                        // the weights' 4-bit form
     const int32_t *used, *order;
     const PlanGroup* plan;
     void* out;                                   // up: bf16 [row][rows / 2], down: f32 [row][rows]
-    int64_t groups;                              // at most
+    int64_t blocks;                              // at most
     uint32_t k;                                  // rows of x are tokens', pair / k; 0: the plan's own
     int KB, Q, rows, tiles;                      // blocks, quads of blocks; packed rows of an expert, tiles of 32 of them
 };
@@ -192,7 +195,7 @@ __device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, u
     odd = __builtin_amdgcn_perm(tab.y, tab.x, (c >> 4) & 0x07070707u) | (c & 0x80808080u);
 }
 
-// A workgroup keeps 32 MT rows of a group in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
+// A workgroup keeps 32 MT rows of a block in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
 // packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
 // Bound by the weights' stream (0.5625 bytes an element).
 template <bool GATED, int MT, int SPLIT>
@@ -202,12 +205,15 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t s_xs[MT][kQuads][64];              // exponents of a quad's two steps
     __shared__ float s_red[SPLIT > 1 ? 16 : 1][4][64];
     __shared__ uint2 s_tab[kDialects];
+    __shared__ __attribute__((aligned(16))) uint8_t s_index[kDialects * 32], s_vote[kPairs * 32];
     __shared__ int32_t s_row[32 * MT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = wave % SPLIT, sub = wave / SPLIT, h = lane >> 5, c = lane & 31;
     if (tid < kDialects) s_tab[tid] = make_uint2(g_f8_book.w[tid][0], g_f8_book.w[tid][1]);
+    else if (p.x && tid >= 64 && tid < 96) reinterpret_cast<uint4*>(s_index)[tid - 64] = reinterpret_cast<const uint4*>(g_quant_tables.near_i)[tid - 64];
+    else if (p.x && tid >= 128 && tid < 144) reinterpret_cast<uint4*>(s_vote)[tid - 128] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[tid - 128];
     const int batches = (p.tiles + kTiles - 1) / kTiles, chunks = (p.Q + kQuads - 1) / kQuads;
-    const int64_t used = min((int64_t)*p.used, p.groups), items = used * batches;
+    const int64_t used = min((int64_t)*p.used, p.blocks), items = used * batches;
     const int64_t lo = items * blockIdx.x / gridDim.x, hi = items * (blockIdx.x + 1) / gridDim.x;
     if (lo >= hi) return;
 
@@ -260,7 +266,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
     };
-    auto multiply = [&](const Quad& q, int at) {                     // quad `at` of the chunk
+    auto multiply = [&](const Quad& q, int at, int tiles) {          // quad `at` of the chunk, tiles of rows there are
         int xs[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) xs[i] = s_xs[i][at][lane];
@@ -277,11 +283,13 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             v8i xv[MT];
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
+                if (i >= tiles) break;
                 const int4 a = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][0][lane]), b = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][1][lane]);
                 xv[i] = v8i{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
+                if (i >= tiles) break;
                 if (step == 0) acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv[i], acc[i], 0, 0, 0, (int)q.meta, 0, xs[i]);
                 else acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv[i], acc[i], 0, 0, 1, (int)q.meta, 1, xs[i]);
             }
@@ -299,7 +307,21 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             s_row[r] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
         }
         __syncthreads();
-        for (int i = tid; i < rows * blocks; i += 1024) {
+        // (four lanes a block: the quantizer's arithmetic)
+        if (p.x)
+            for (int i = tid; i < rows * blocks * 4; i += 1024) {
+                const int r = i / (blocks * 4), b = (i >> 2) - r * blocks, kb = q0 * 4 + b, quarter = i & 3;
+                const bool on = kb < p.KB;
+                const uint4 v = on ? *reinterpret_cast<const uint4*>(p.x + (int64_t)s_row[r] * p.ld + kb * kBlock + quarter * 8) : make_uint4(0, 0, 0, 0);
+                uint32_t code, e, d;
+                dfp4_pass_small(v, s_vote, s_index, code, e, d);
+                uint2 to;
+                expand8(code, s_tab[d], to.x, to.y);
+                const int t = r >> 5, l = (quarter >> 1) * 32 + (r & 31);
+                *reinterpret_cast<uint2*>(&s_x[t][b >> 1][b & 1][l][(quarter & 1) * 8]) = to;
+                if (quarter == 0) reinterpret_cast<uint8_t*>(&s_xs[t][b >> 2][(b & 1) * 32 + (r & 31)])[(b >> 1) & 1] = on ? (uint8_t)e : 0;
+            }
+        else for (int i = tid; i < rows * blocks; i += 1024) {
             const int r = i / blocks, b = i - r * blocks, kb = q0 * 4 + b;
             const int64_t blk = (int64_t)s_row[r] * p.KB + kb;
             uint4 codes = make_uint4(0, 0, 0, 0);
@@ -350,11 +372,12 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) load(ring[d], next, d);
         }
+        const int tiles = MT == 1 || now.g.rows - now.block * (32 * MT) > 32 ? MT : 1;
         for (int q = 0; q < seg.n; q += kAhead) {
             const bool more = q + kAhead < seg.n;
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) {
-                if (q + d < seg.n) multiply(ring[d], seg.first + q + d);
+                if (q + d < seg.n) multiply(ring[d], seg.first + q + d, tiles);
                 load(ring[d], more ? seg : next, more ? q + kAhead + d : d);
             }
         }
@@ -367,7 +390,8 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             } else {
                 // four registers at a time through LDS, the parts of K added in their order
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < MT; ++i) {
+                    if (i >= tiles) break;
 #pragma unroll
                     for (int x4 = 0; x4 < 16; x4 += 4) {
                         __syncthreads();
@@ -385,12 +409,145 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
                             emit(now, i, now.batch * kTiles + tile, x4 + x, v0, v1);
                         }
                     }
+                }
             }
             clear();
         }
         if (last) return;
         now = then;
         seg = next;
+    }
+}
+
+// ---- a few tokens, down: their results whole
+
+struct TokenArgs {
+    const uint16_t* h;
+    int64_t ld;
+    const uint8_t* quads;
+    const int32_t *place, *row_at;
+    const PlanGroup* groups;
+    const float* weights;
+    void* y;
+    int64_t pairs;
+    int k, KB, Q, rows, tiles;
+};
+constexpr int kTokenElements = 48 << 10;         // of a token's rows, in LDS
+
+// A workgroup a token and 32 results: its 16 waves share the quads of all the token's experts (a wave's are neighbours, of one or a few
+// experts), add them with the router's weights and join in the order of the waves.  Rows are quantized by every workgroup anew, on their way
+// to LDS, while the first weights come.  Bound by latency: loads of the plan, rows and weights in turn.
+template <bool BF16>
+__global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
+    constexpr int kAhead = 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_rows[];  // [j][step][block][half][16], then exponents [j][quad][half][2]
+    __shared__ float s_red[16][32];
+    __shared__ uint2 s_tab[kDialects];
+    __shared__ __attribute__((aligned(16))) uint8_t s_index[kDialects * 32], s_vote[kPairs * 32];
+    __shared__ int32_t s_row[kMaxChoice], s_expert[kMaxChoice];
+    __shared__ float s_weight[kMaxChoice];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int tile = blockIdx.x;
+    const int64_t token = blockIdx.y;
+    if (tid < kDialects) s_tab[tid] = make_uint2(g_f8_book.w[tid][0], g_f8_book.w[tid][1]);
+    else if (tid >= 64 && tid < 96) reinterpret_cast<uint4*>(s_index)[tid - 64] = reinterpret_cast<const uint4*>(g_quant_tables.near_i)[tid - 64];
+    else if (tid >= 128 && tid < 144) reinterpret_cast<uint4*>(s_vote)[tid - 128] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[tid - 128];
+    else if (tid >= 192 && tid < 192 + p.k) {
+        const int j = tid - 192;
+        const int32_t row = p.place[token * p.k + j];
+        const bool there = row >= 0 && row < p.pairs;
+        s_row[j] = there ? row : -1;
+        s_expert[j] = there ? p.groups[p.row_at[row] / kGroupRows].expert : 0;
+        s_weight[j] = there ? p.weights[token * p.k + j] : 0.0f;
+    }
+    __syncthreads();
+    const int units = p.k * p.Q, lo = units * wave / 16, hi = units * (wave + 1) / 16;
+    struct Quad {
+        uint4 c[2];
+        uint32_t meta;
+    } ring[kAhead];
+    auto load = [&](Quad& q, int u) {
+        u = min(max(u, 0), units - 1);
+        const int j = u / p.Q, expert = __builtin_amdgcn_readfirstlane(s_expert[j]);
+        const uint8_t* at = p.quads + (((int64_t)expert * p.tiles + tile) * p.Q + (u - j * p.Q)) * kQuadBytes;
+        q.c[0] = *reinterpret_cast<const uint4*>(at + lane * 16);
+        q.c[1] = *reinterpret_cast<const uint4*>(at + 1024 + lane * 16);
+        q.meta = *reinterpret_cast<const uint32_t*>(at + 2048 + lane * 4);
+    };
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) load(ring[d], min(lo + d, hi - 1));
+    const int blocks = p.Q * 4;
+    uint8_t* s_scale = s_rows + (size_t)p.k * p.Q * 128;
+    for (int i = tid; i < p.k * blocks * 4; i += 1024) {
+        const int j = i / (blocks * 4), b = (i >> 2) - j * blocks, quarter = i & 3;
+        const bool on = b < p.KB && s_row[j] >= 0;
+        const uint4 v = on ? *reinterpret_cast<const uint4*>(p.h + (int64_t)s_row[j] * p.ld + b * kBlock + quarter * 8) : make_uint4(0, 0, 0, 0);
+        uint32_t code, e, d;
+        dfp4_pass_small(v, s_vote, s_index, code, e, d);
+        uint2 to;
+        expand8(code, s_tab[d], to.x, to.y);
+        *reinterpret_cast<uint2*>(s_rows + (size_t)(j * blocks + b) * 32 + (quarter >> 1) * 16 + (quarter & 1) * 8) = to;
+        if (quarter == 0) s_scale[(j * p.Q + (b >> 2)) * 4 + (b & 1) * 2 + ((b >> 1) & 1)] = on ? (uint8_t)e : 0;
+    }
+    __syncthreads();
+    v16f acc, sum;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[x] = sum[x] = 0.0f;
+    int before = lo / p.Q;
+    for (int u0 = lo; u0 < hi; u0 += kAhead) {
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) {
+            const int u = u0 + d;
+            if (u < hi) {
+                const int j = u / p.Q;
+                if (j != before) {
+                    const float w = s_weight[before];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) sum[x] += w * acc[x], acc[x] = 0.0f;
+                    before = j;
+                }
+                const int xs = *reinterpret_cast<const uint16_t*>(s_scale + u * 4 + h * 2);
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+                    const uint32_t dl = ring[d].meta >> (16 + 8 * step);
+                    const uint2 t0 = s_tab[dl & 15u], t1 = s_tab[(dl >> 4) & 15u];
+                    uint32_t w[8];
+                    expand8(ring[d].c[step].x, t0, w[0], w[1]);
+                    expand8(ring[d].c[step].y, t0, w[2], w[3]);
+                    expand8(ring[d].c[step].z, t1, w[4], w[5]);
+                    expand8(ring[d].c[step].w, t1, w[6], w[7]);
+                    const v8i wv = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], (int)w[6], (int)w[7]};
+                    const uint8_t* from = s_rows + (size_t)u * 128 + step * 64 + h * 16;
+                    const int4 a = *reinterpret_cast<const int4*>(from), b = *reinterpret_cast<const int4*>(from + 32);
+                    const v8i xv = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    if (step == 0) acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv, acc, 0, 0, 0, (int)ring[d].meta, 0, xs);
+                    else acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv, acc, 0, 0, 1, (int)ring[d].meta, 1, xs);
+                    asm volatile("" : "+v"(acc) : "v"(wv), "v"(xv));       // (as above)
+                }
+            }
+            load(ring[d], min(u + kAhead, hi - 1));
+        }
+    }
+    if (hi > lo) {
+        const float w = s_weight[before];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sum[x] += w * acc[x];
+    }
+    // every column is the token's
+    if ((lane & 31) == 0) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s_red[wave][8 * (x >> 2) + 4 * h + (x & 3)] = sum[x];
+    }
+    __syncthreads();
+    if (tid < 32) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) v += s_red[w][tid];
+        const int n = tile * 32 + tid;
+        if (n < p.rows) {
+            if constexpr (BF16) static_cast<uint16_t*>(p.y)[token * p.rows + n] = bf16_of(v);
+            else static_cast<float*>(p.y)[token * p.rows + n] = v;
+        }
     }
 }
 
@@ -430,6 +587,27 @@ __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p) {
     }
 }
 
+// The experts that tokens go to, were all alike
+inline int64_t active_experts(const dfp4_plan& plan) {
+    const int64_t pairs = plan.tokens * plan.k;
+    if (pairs >= 8 * plan.experts) return plan.experts;
+    const double none = pow(1.0 - 1.0 / (double)plan.experts, (double)pairs);
+    const int64_t n = (int64_t)((double)plan.experts * (1.0 - none) + 0.5);
+    return n > 0 ? n : 1;
+}
+// Rows an expert up to which weights are streamed past them; both sides, us, few / many: 20 rows 28 / 35, 25 rows 11.8 / 13.9, 32 rows 56 / 57 and 49 / 42,
+// 42 rows 33 / 28, 64 rows 63 / 70 and 54 / 51, 128 rows 91 / 88 and 83 / 66
+constexpr int64_t kFewRows = 28;
+// ... and up to which the large kernel takes 128 rows at a time instead of 256: 42 rows 28 / 33, 128 rows 88 / 91 and 126 / 143, 250 rows 76 / 63, 117 / 107
+constexpr int64_t kHalfRows = 160;
+// Whether tokens are taken one by one (down): where there are few, and weights that several of them read, again for each, cost less than the two
+// launches that are spared (4 us): 4 tokens of 8 of 128 experts 11.9 us instead of 17.5, 8 tokens 21.7 and 22.5, 16 tokens 40 and 30
+inline bool token_by_token(const dfp4_plan& plan, const dfp4_experts& w) {
+    if (w.gated || plan.k * quads_of(w.K) * 128 > kTokenElements || plan.tokens * row_tiles(w) > 2 * device_cu_count()) return false;
+    const int64_t again = plan.tokens * plan.k - active_experts(plan);
+    return again * w.rows * w.K <= 28 << 20;
+}
+
 // workspace: rows in operand order, or in their 4-bit form (few), and down their products
 struct Workspace {
     bool many;
@@ -438,9 +616,9 @@ struct Workspace {
 inline Workspace workspace_of(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t pairs = plan.tokens * plan.k;
     Workspace x{};
-    x.many = pairs >= 64 * w.experts;
+    x.many = pairs > kFewRows * active_experts(plan);
     if (x.many) {
-        x.rows = plan_groups(pairs, plan.experts) * kGroupRows;
+        x.rows = plan_list(pairs, plan.experts, 0) * kGroupRows;
         x.part = up256((int64_t)native_packed_bytes(x.rows, w.K, true));
     } else {
         x.rows = w.gated ? plan.tokens : pairs;
@@ -486,10 +664,23 @@ static void launch_few(const FewArgs& p, int split, dim3 grid, hipStream_t strea
 }
 
 int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
-    const int64_t pairs = a.plan.tokens * a.plan.k, S = steps_of(a.w.K), groups = plan_groups(pairs, a.plan.experts);
+    const int64_t pairs = a.plan.tokens * a.plan.k, S = steps_of(a.w.K);
     const Workspace ws = workspace_of(a.plan, a.w);
     const PlanView plan = plan_view(a.plan);
     const int cus = device_cu_count();
+    if (token_by_token(a.plan, a.w)) {
+        TokenArgs p{};
+        p.h = a.x, p.ld = a.ld;
+        p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
+        p.place = plan.place, p.row_at = plan.row_at, p.groups = plan.list[0], p.weights = a.weights;
+        p.y = a.out, p.pairs = pairs;
+        p.k = (int)a.plan.k, p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)a.w.rows, p.tiles = (int)row_tiles(a.w);
+        const dim3 grid((unsigned)p.tiles, (unsigned)a.plan.tokens);
+        const size_t lds = (size_t)p.k * p.Q * 132;
+        if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_token_kernel<true>), grid, dim3(1024), lds, stream, p);
+        else hipLaunchKernelGGL((experts_token_kernel<false>), grid, dim3(1024), lds, stream, p);
+        return check_launch();
+    }
     void* out = a.w.gated ? a.out : a.workspace + ws.part;
     const bool part16 = ws.many && a.out_dtype == DFP4_BF16;
     if (ws.many) {
@@ -504,29 +695,46 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         ExpertTiles t{};
         t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
         t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);
-        t.used = plan.used, t.groups = plan.groups, t.max_groups = groups;
+        t.half = pairs <= kHalfRows * active_experts(a.plan);
+        t.used = plan.used + (t.half ? 1 : 0), t.list = plan.list[t.half ? 1 : 0], t.most = plan_list(pairs, a.plan.experts, t.half ? 1 : 0);
         t.K = (int)a.w.K, t.rows = (int)expert_rows(a.w), t.tiles = (int)(padded_rows(a.w) / 256);
-        t.gated = a.w.gated != 0, t.half = false;
+        t.gated = a.w.gated != 0;
         t.out = out, t.out_dtype = a.out_dtype;
         const int rc = launch_expert_tiles(t, stream);
         if (rc != DFP4_OK) return rc;
     } else {
         const dfp4_tensor x{a.workspace, a.workspace + ws.dial, a.workspace + ws.expo, ws.rows, a.w.K};
-        const int rc = launch_quantize(false, a.x, ws.rows, a.w.K, a.ld, x, stream);
-        if (rc != DFP4_OK) return rc;
+        const int64_t active = active_experts(a.plan);
         FewArgs p{};
+        // Quantized by the workgroups that take them where that is little work: a launch less (2.5 us), but 1.1 us a workgroup and 8192 elements
+        // (16 rows of 4096: 112 us instead of 107)
+        if (pairs * a.w.K <= active * 16384) {
+            p.x = a.x, p.ld = a.ld;
+        } else {
+            const int rc = launch_quantize(false, a.x, ws.rows, a.w.K, a.ld, x, stream);
+            if (rc != DFP4_OK) return rc;
+        }
         p.x_codes = x.codes, p.x_dial = x.dialect, p.x_expo = x.exponent;
         p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
-        p.used = plan.used, p.order = plan.order, p.plan = plan.groups;
-        p.out = out, p.groups = groups;
+        p.used = plan.used + 2, p.order = plan.order, p.plan = plan.list[2];
+        p.out = out, p.blocks = plan_list(pairs, a.plan.experts, 2);
         p.k = a.w.gated ? (uint32_t)a.plan.k : 0;
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
-        // the experts that tokens go to, were all alike
-        const int64_t active = pairs < a.w.experts ? pairs : a.w.experts;
-        const int mt = pairs > 16 * active ? 2 : 1;
+        // 64 rows at a time where there are that many, or, with many experts, the most popular ones will have more than 32 (those would read their
+        // weights twice): 200 tokens of 4 of 64 experts, 4096 x 512 up, 46 us instead of 56; 64 of 2 of 8, 4096 x 14336, 113 instead of 104.
+        const int mt = pairs > 20 * active || (pairs > 10 * active && active >= 32) ? 2 : 1;
+        // How many waves share K: rounds of items over the compute units, each with what it streams (20 bytes a ns) and what a sum over waves, or
+        // rows that come to LDS in several chunks, take; constants by measurement (us)
+        const int chunks = (p.Q + 32 / mt - 1) / (32 / mt);
         int split = 1;
-        while (split < 16 && split < p.Q && active * p.tiles * split < (int64_t)16 * 2 * cus) split *= 2;
-        const int64_t items = groups * ((p.tiles + 16 / split - 1) / (16 / split));
+        float least = 0.0f;
+        for (int s = 1; s <= 16; s *= 2) {
+            const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per);
+            const float r = (float)n / (float)cus, rounds = (float)((n + cus - 1) / cus), stream = 0.115f * (float)(per * p.Q);
+            const float us = rounds * (mt * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.5f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
+            if (s == 1 || us < least) least = us, split = s;
+        }
+        const int64_t items = p.blocks * ((p.tiles + 16 / split - 1) / (16 / split));
         const dim3 grid((unsigned)(items < cus ? items : cus));
         if (a.w.gated && mt == 1) launch_few<true, 1>(p, split, grid, stream);
         else if (a.w.gated) launch_few<true, 2>(p, split, grid, stream);

@@ -456,9 +456,9 @@ __device__ __forceinline__ void quantize_flushed_piece(const GemmParams& p, int6
 
 // Products of experts (experts.hip): rows in groups of kGroupRows, a tile's weights are its group's expert's
 struct ExpertsParams : NativeParams {
-    const int32_t* used;              // groups there are
-    const PlanGroup* groups;
-    int max_groups, cols;             // tiles of 256 columns of an expert
+    const int32_t* used;              // tiles of rows there are
+    const PlanGroup* list;
+    int most, cols;                   // at most; tiles of 256 columns of an expert
 };
 __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
@@ -489,17 +489,14 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(ParamsOf<MODE> p) {
     int expert = 0;
     if constexpr (kIsExperts) {
         // An XCD takes a stretch of row tiles, all columns of one after the other, so that its cache holds an expert's weights
-        constexpr int kUnits = kGroupRows / kRowsWg;
-        const int units = min(*p.used, p.max_groups) * kUnits, share = (units + 7) >> 3, in = bx >> 3, unit = in / p.cols, at = (bx & 7) * share + unit;
+        const int units = min(*p.used, p.most), share = (units + 7) >> 3, in = bx >> 3, unit = in / p.cols, at = (bx & 7) * share + unit;
         if (unit >= share || at >= units) return;
-        const PlanGroup g = p.groups[at / kUnits];
-        const int skip = at % kUnits * kRowsWg;
-        if (g.rows <= skip) return;
+        const PlanGroup g = p.list[at];
         bx = in - unit * p.cols;
-        by = at;
+        by = g.at / kRowsWg;
         expert = g.expert;
-        p.M = g.rows - skip;
-        p.out = static_cast<uint8_t*>(p.out) + (int64_t)(g.row0 + skip) * p.ldc * (BF16 ? 2 : 4);
+        p.M = g.rows;
+        p.out = static_cast<uint8_t*>(p.out) + (int64_t)g.row0 * p.ldc * (BF16 ? 2 : 4);
     } else if (p.rect_h) {
         const int id = by * (int)gridDim.x + bx, rect = id & 7, in = id >> 3;
         bx = ((rect & ((1 << p.rects_x) - 1)) << p.rect_w) + (in & ((1 << p.rect_w) - 1));
@@ -1139,11 +1136,10 @@ int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream) {
     p.ldc = t.gated ? t.rows / 2 : t.rows;
     p.ksplit = 1;
     p.used = t.used;
-    p.groups = t.groups;
+    p.list = t.list;
     p.cols = t.tiles;
-    if (t.max_groups > 0x3fffffff) return DFP4_ERR_SHAPE;
-    p.max_groups = (int)t.max_groups;
-    const int64_t units = t.max_groups * (kGroupRows / (t.half ? 128 : 256)), wgs = (units + 7) / 8 * 8 * p.cols;
+    p.most = (int)t.most;
+    const int64_t wgs = (t.most + 7) / 8 * 8 * p.cols;
     if (wgs >= (int64_t)1 << 24) return DFP4_ERR_SHAPE;                       // fewer than 2^32 threads
     const dim3 grid((unsigned)wgs);
     auto run = [&](auto bf16_c, auto mode_c) {

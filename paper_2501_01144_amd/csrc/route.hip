@@ -156,75 +156,115 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 
-// A workgroup an expert.  Each counts all ids (LDS), which gives it its first row and group; a wave then finds the expert's pairs in
-// its share of the ids, first how many, then where.
-__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int experts, int64_t groups) {
-    __shared__ uint32_t s_count[kMaxExperts], s_first[kPlanWaves];
-    __shared__ uint32_t s_sum[2][kPlanWaves];
+// A stable counting sort.  A workgroup takes a share of the pairs, 16 waves in turn; where there are several, a first kernel has counted each
+// share's experts.  Every workgroup knows all counts then, and with them each expert's first row and its entries of the lists; a wave ranks its pairs 64 at
+// a time by comparing bits of their experts.
+__global__ __launch_bounds__(kPlanThreads) void expert_count_kernel(const int32_t* __restrict__ ids, int32_t* counts, int64_t pairs, int64_t share, int experts) {
+    __shared__ int32_t s_count[kMaxExperts];
+    for (int e = threadIdx.x; e < experts; e += kPlanThreads) s_count[e] = 0;
+    __syncthreads();
+    const int64_t lo = blockIdx.x * share, hi = min(pairs, lo + share);
+    for (int64_t i = lo + threadIdx.x; i < hi; i += kPlanThreads) {
+        const uint32_t id = (uint32_t)ids[i];
+        if (id < (uint32_t)experts) atomicAdd(&s_count[id], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[(int64_t)blockIdx.x * experts + e] = s_count[e];
+}
+
+__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int64_t share, int experts, int bits) {
+    __shared__ uint32_t s_at[kPlanWaves][kMaxExperts];               // of a wave's pairs: how many, then the next row
+    __shared__ uint32_t s_row[kMaxExperts], s_group[kMaxExperts];
+    __shared__ uint32_t s_sum[4][kPlanWaves], s_rows;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int mine = (int)blockIdx.x;
-    for (int e = tid; e < experts; e += kPlanThreads) s_count[e] = 0;
+    const int64_t lo = blockIdx.x * share, hi = min(pairs, lo + share);
+    // (a wave's part of the share: whole rounds of 64)
+    const int64_t per = share / kPlanWaves, wlo = min(hi, lo + wave * per), whi = min(hi, wlo + per);
+    for (int i = tid; i < kPlanWaves * experts; i += kPlanThreads) s_at[i / experts][i % experts] = 0;
     __syncthreads();
-    // (whole waves' shares of 64 ids, in order)
-    const int64_t per = (pairs + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64, lo = wave * per, hi = lo + per < pairs ? lo + per : pairs;
-    uint32_t found = 0;
-    for (int64_t i0 = lo; i0 < hi; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const uint32_t id = i < hi ? (uint32_t)ids[i] : 0xffffffffu;
-        if (id < (uint32_t)experts) atomicAdd(&s_count[id], 1u);
-        else if (mine == 0 && i < hi) v.place[i] = -1;
-        found += __popcll(__ballot(id == (uint32_t)mine));
+    for (int64_t i = wlo + lane; i < whi; i += 64) {
+        const uint32_t id = (uint32_t)ids[i];
+        if (id < (uint32_t)experts) atomicAdd(&s_at[wave][id], 1u);
     }
-    if (lane == 0) s_first[wave] = found;
     __syncthreads();
-    // rows and groups before this expert's, and in all
-    auto sums = [&](int end, uint32_t& rows, uint32_t& groups_before) {
-        uint32_t r = 0, g = 0;
-        for (int e = tid; e < end; e += kPlanThreads) {
-            r += s_count[e];
-            g += (s_count[e] + kGroupRows - 1) / kGroupRows;
+    // a thread an expert: pairs in all, and in the shares before
+    const int e = tid;
+    uint32_t total = 0, before = 0;
+    if (e < experts) {
+        if (gridDim.x > 1) {
+            for (int b = 0; b < (int)gridDim.x; ++b) {
+                const uint32_t n = (uint32_t)v.counts[(int64_t)b * experts + e];
+                total += n;
+                before += b < (int)blockIdx.x ? n : 0;
+            }
+        } else {
+            for (int w = 0; w < kPlanWaves; ++w) total += s_at[w][e];
         }
+    }
+    uint32_t sum[4] = {total};                                       // of the experts up to this one: rows, entries of the lists
+    uint32_t entries[3];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) sum[q + 1] = entries[q] = (total + kListRows[q] - 1) / kListRows[q];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
         for (int x = 1; x < 64; x <<= 1) {
-            r += __shfl_xor(r, x);
-            g += __shfl_xor(g, x);
+            const uint32_t n = __shfl_up(sum[q], x);
+            if (lane >= x) sum[q] += n;
         }
-        __syncthreads();
-        if (lane == 0) s_sum[0][wave] = r, s_sum[1][wave] = g;
-        __syncthreads();
-        rows = groups_before = 0;
-        for (int w = 0; w < kPlanWaves; ++w) rows += s_sum[0][w], groups_before += s_sum[1][w];
-    };
-    uint32_t row0, group0;
-    sums(mine, row0, group0);
-    const uint32_t count = s_count[mine], my_groups = (count + kGroupRows - 1) / kGroupRows;
-    if (tid == 0) {
-        v.offsets[mine] = (int32_t)row0;
+        if (lane == 63) s_sum[q][wave] = sum[q];
     }
-    for (uint32_t g = tid; g < my_groups; g += kPlanThreads)
-        v.groups[group0 + g] = PlanGroup{mine, (int32_t)(row0 + g * kGroupRows), (int32_t)min(count - g * kGroupRows, (uint32_t)kGroupRows), 0};
-    for (uint32_t r = tid; r < count; r += kPlanThreads) v.row_at[row0 + r] = (int32_t)(group0 * kGroupRows + r);
-    if (mine == experts - 1) {
-        const uint32_t rows = row0 + count, used = group0 + my_groups;
-        if (tid == 0) {
-            v.offsets[experts] = (int32_t)rows;
-            *v.used = (int32_t)used;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        for (int w = 0; w < wave; ++w) sum[q] += s_sum[q][w];
+    if (e < experts) {
+        const uint32_t row0 = sum[0] - total, group0 = sum[1] - entries[0];
+        s_row[e] = row0;
+        s_group[e] = group0;
+        uint32_t at = row0 + before;
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const uint32_t n = s_at[w][e];
+            s_at[w][e] = at;
+            at += n;
         }
-        for (int64_t g = used + tid; g < groups; g += kPlanThreads) v.groups[g] = PlanGroup{0, 0, 0, 0};
-        for (int64_t r = (int64_t)rows + tid; r < pairs; r += kPlanThreads) v.order[r] = v.row_at[r] = -1;
+        if (e % (int)gridDim.x == (int)blockIdx.x) {                 // described by one of the workgroups
+            v.offsets[e] = (int32_t)row0;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                constexpr auto& kRows = kListRows;
+                PlanGroup* to = v.list[q] + (sum[q + 1] - entries[q]);
+                for (uint32_t g = 0; g < entries[q]; ++g)
+                    to[g] = PlanGroup{e, (int32_t)(row0 + g * kRows[q]), (int32_t)min(total - g * kRows[q], (uint32_t)kRows[q]), (int32_t)(group0 * kGroupRows + g * kRows[q])};
+                if (e == experts - 1) v.used[q] = (int32_t)sum[q + 1];
+            }
+            if (e == experts - 1) v.offsets[experts] = (int32_t)sum[0];
+        }
+        if (e == experts - 1) s_rows = sum[0];
     }
-    uint32_t at = row0;
-    for (int w = 0; w < wave; ++w) at += s_first[w];
-    for (int64_t i0 = lo; i0 < hi; i0 += 64) {
+    __syncthreads();
+    for (int64_t i0 = wlo; i0 < whi; i0 += 64) {
         const int64_t i = i0 + lane;
-        const bool is = i < hi && ids[i] == mine;
-        const uint64_t all = __ballot(is);
-        if (is) {
-            const uint32_t row = at + (uint32_t)__popcll(all & ((1ull << lane) - 1));
-            v.order[row] = (int32_t)i;
-            v.place[i] = (int32_t)row;
+        const uint32_t id = i < whi ? (uint32_t)ids[i] : 0xffffffffu;
+        const bool is = id < (uint32_t)experts;
+        uint64_t same = __ballot(is);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((id >> b) & 1);
+            same &= (id >> b) & 1 ? set : ~set;
         }
-        at += (uint32_t)__popcll(all);
+        if (is) {
+            const uint32_t row = s_at[wave][id] + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+            v.order[row] = (int32_t)i;
+            v.row_at[row] = (int32_t)(s_group[id] * kGroupRows + row - s_row[id]);
+            v.place[i] = (int32_t)row;
+        } else if (i < whi) {
+            v.place[i] = -1;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (is && (same >> lane) == 1) s_at[wave][id] += (uint32_t)__popcll(same);      // the last of them
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    // rows that no pair has
+    for (int64_t r = s_rows + (int64_t)blockIdx.x * kPlanThreads + tid; r < pairs; r += (int64_t)gridDim.x * kPlanThreads) v.order[r] = -1;
 }
 
 }  // namespace
@@ -240,8 +280,12 @@ int launch_route(const RouteArgs& a, hipStream_t stream) {
 }
 
 int launch_expert_plan(const int32_t* ids, const dfp4_plan& p, hipStream_t stream) {
-    const int64_t pairs = p.tokens * p.k;
-    hipLaunchKernelGGL(expert_plan_kernel, dim3((uint32_t)p.experts), dim3(kPlanThreads), 0, stream, ids, plan_view(p), pairs, (int)p.experts, plan_groups(pairs, p.experts));
+    const int64_t pairs = p.tokens * p.k, share = plan_share(pairs), shares = plan_shares(pairs);
+    const PlanView v = plan_view(p);
+    int bits = 0;
+    while ((1 << bits) < p.experts) ++bits;
+    if (shares > 1) hipLaunchKernelGGL(expert_count_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v.counts, pairs, share, (int)p.experts);
+    hipLaunchKernelGGL(expert_plan_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v, pairs, share, (int)p.experts, bits);
     return check_launch();
 }
 
