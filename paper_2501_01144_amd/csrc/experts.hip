@@ -195,49 +195,50 @@ __device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, u
     odd = __builtin_amdgcn_perm(tab.y, tab.x, (c >> 4) & 0x07070707u) | (c & 0x80808080u);
 }
 
-// A workgroup keeps 32 MT rows of a block in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
+// A workgroup keeps the rows of a block (MT 1: up to 32, 2: up to 64) in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
 // packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
 // Bound by the weights' stream (0.5625 bytes an element).
 template <bool GATED, int MT, int SPLIT>
 __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
-    constexpr int kQuads = 32 / MT, kTiles = 16 / SPLIT, kAhead = 4;  // quads of rows in LDS (a chunk of K); tiles at a time
-    __shared__ __attribute__((aligned(16))) uint8_t s_x[MT][kQuads * 2][2][64][16];      // [tile of rows][step][block][lane]
-    __shared__ __attribute__((aligned(16))) uint16_t s_xs[MT][kQuads][64];              // exponents of a quad's two steps
+    constexpr int kQuads = 32, kTiles = 16 / SPLIT, kAhead = 4;       // quads of 32 rows in LDS; tiles at a time
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[kQuads][2][2][64][16];           // [quad][step][block][lane], of the second tile of rows from quad 16 on
+    __shared__ __attribute__((aligned(16))) uint16_t s_xs[kQuads][64];                   // exponents of a quad's two steps
     __shared__ float s_red[SPLIT > 1 ? 16 : 1][4][64];
     __shared__ uint2 s_tab[kDialects];
     __shared__ __attribute__((aligned(16))) uint8_t s_index[kDialects * 32], s_vote[kPairs * 32];
-    __shared__ int32_t s_row[32 * MT];
+    __shared__ int32_t s_row[kListRows[2]];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = wave % SPLIT, sub = wave / SPLIT, h = lane >> 5, c = lane & 31;
     if (tid < kDialects) s_tab[tid] = make_uint2(g_f8_book.w[tid][0], g_f8_book.w[tid][1]);
     else if (p.x && tid >= 64 && tid < 96) reinterpret_cast<uint4*>(s_index)[tid - 64] = reinterpret_cast<const uint4*>(g_quant_tables.near_i)[tid - 64];
     else if (p.x && tid >= 128 && tid < 144) reinterpret_cast<uint4*>(s_vote)[tid - 128] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[tid - 128];
-    const int batches = (p.tiles + kTiles - 1) / kTiles, chunks = (p.Q + kQuads - 1) / kQuads;
+    const int batches = (p.tiles + kTiles - 1) / kTiles;
     const int64_t used = min((int64_t)*p.used, p.blocks), items = used * batches;
     const int64_t lo = items * blockIdx.x / gridDim.x, hi = items * (blockIdx.x + 1) / gridDim.x;
     if (lo >= hi) return;
 
-    // where this wave is: item, block of rows, chunk
+    // where this wave is: item (block of rows and batch of tiles), chunk of K (of all 32 quads, or of 16 for two tiles of rows)
     struct At {
-        int64_t item, group;
-        int batch, block, chunk;
+        int64_t item, block;
+        int batch, chunk, tiles;
         PlanGroup g;
     };
     auto begin = [&](int64_t item) {
         At a;
         a.item = item;
-        a.group = item / batches;
-        a.batch = (int)(item - a.group * batches);
-        a.block = a.chunk = 0;
-        a.g = p.plan[a.group];
+        a.block = item / batches;
+        a.batch = (int)(item - a.block * batches);
+        a.chunk = 0;
+        a.g = p.plan[a.block];
+        a.tiles = MT == 1 || a.g.rows <= 32 ? 1 : 2;
         return a;
     };
+    auto last_chunk_of = [&](const At& a) { return (a.chunk + 1) * (kQuads / a.tiles) >= p.Q; };
     auto after = [&](const At& a) {
         At n = a;
-        if (++n.chunk < chunks) return n;
-        n.chunk = 0;
-        if (++n.block * (32 * MT) < a.g.rows) return n;
-        return a.item + 1 < hi ? begin(a.item + 1) : a;              // (behind the last: loaded once more, not used)
+        if (!last_chunk_of(a)) ++n.chunk;
+        else if (a.item + 1 < hi) n = begin(a.item + 1);             // (behind the last: loaded once more, not used)
+        return n;
     };
     // its quads there: the first one's address and their number
     struct Segment {
@@ -245,9 +246,9 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
         int first, n;
     };
     auto segment = [&](const At& a) {
-        const int in = min(kQuads, p.Q - a.chunk * kQuads), per = (in + SPLIT - 1) / SPLIT, first = part * per, n = max(0, min(in, first + per) - first);
+        const int chunk = kQuads / a.tiles, in = min(chunk, p.Q - a.chunk * chunk), per = (in + SPLIT - 1) / SPLIT, first = part * per, n = max(0, min(in, first + per) - first);
         const int tile = min(a.batch * kTiles + sub, p.tiles - 1);
-        return Segment{p.quads + (((int64_t)a.g.expert * p.tiles + tile) * p.Q + a.chunk * kQuads + (n > 0 ? first : 0)) * kQuadBytes, first, n};
+        return Segment{p.quads + (((int64_t)a.g.expert * p.tiles + tile) * p.Q + a.chunk * chunk + (n > 0 ? first : 0)) * kQuadBytes, first, n};
     };
     struct Quad {
         uint4 c[2];
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     auto multiply = [&](const Quad& q, int at, int tiles) {          // quad `at` of the chunk, tiles of rows there are
         int xs[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xs[i] = s_xs[i][at][lane];
+        for (int i = 0; i < MT; ++i) xs[i] = s_xs[(at + 16 * i) % kQuads][lane];           // (the second: of no use where there is one)
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
             const uint32_t d = q.meta >> (16 + 8 * step);
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 if (i >= tiles) break;
-                const int4 a = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][0][lane]), b = *reinterpret_cast<const int4*>(s_x[i][2 * at + step][1][lane]);
+                const int4 a = *reinterpret_cast<const int4*>(s_x[at + 16 * i][step][0][lane]), b = *reinterpret_cast<const int4*>(s_x[at + 16 * i][step][1][lane]);
                 xv[i] = v8i{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             }
 #pragma unroll
@@ -300,10 +301,10 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     };
     // rows of the chunk into LDS; blocks behind the last of a quad as zeros
     auto stage = [&](const At& a) {
-        const int rows = min(32 * MT, a.g.rows - a.block * 32 * MT), q0 = a.chunk * kQuads, blocks = min(kQuads, p.Q - q0) * 4;
+        const int rows = min(32 * MT, a.g.rows), q0 = a.chunk * (kQuads / a.tiles), blocks = min(kQuads / a.tiles, p.Q - q0) * 4;
         __syncthreads();                                             // what was there is done with
         for (int r = tid; r < rows; r += 1024) {
-            const int64_t row = (int64_t)a.g.row0 + a.block * 32 * MT + r;
+            const int64_t row = (int64_t)a.g.row0 + r;
             s_row[r] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
         }
         __syncthreads();
@@ -317,9 +318,9 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
                 dfp4_pass_small(v, s_vote, s_index, code, e, d);
                 uint2 to;
                 expand8(code, s_tab[d], to.x, to.y);
-                const int t = r >> 5, l = (quarter >> 1) * 32 + (r & 31);
-                *reinterpret_cast<uint2*>(&s_x[t][b >> 1][b & 1][l][(quarter & 1) * 8]) = to;
-                if (quarter == 0) reinterpret_cast<uint8_t*>(&s_xs[t][b >> 2][(b & 1) * 32 + (r & 31)])[(b >> 1) & 1] = on ? (uint8_t)e : 0;
+                const int q = (r >> 5) * 16 + (b >> 2), l = (quarter >> 1) * 32 + (r & 31);
+                *reinterpret_cast<uint2*>(&s_x[q][(b >> 1) & 1][b & 1][l][(quarter & 1) * 8]) = to;
+                if (quarter == 0) reinterpret_cast<uint8_t*>(&s_xs[q][(b & 1) * 32 + (r & 31)])[(b >> 1) & 1] = on ? (uint8_t)e : 0;
             }
         else for (int i = tid; i < rows * blocks; i += 1024) {
             const int r = i / blocks, b = i - r * blocks, kb = q0 * 4 + b;
@@ -337,16 +338,16 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             expand8(codes.y, tab, lo4.z, lo4.w);
             expand8(codes.z, tab, hi4.x, hi4.y);
             expand8(codes.w, tab, hi4.z, hi4.w);
-            const int t = r >> 5, l = r & 31;
-            *reinterpret_cast<uint4*>(s_x[t][b >> 1][b & 1][l]) = lo4;
-            *reinterpret_cast<uint4*>(s_x[t][b >> 1][b & 1][32 + l]) = hi4;
-            reinterpret_cast<uint8_t*>(&s_xs[t][b >> 2][(b & 1) * 32 + l])[(b >> 1) & 1] = (uint8_t)e;
+            const int q = (r >> 5) * 16 + (b >> 2), l = r & 31;
+            *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][l]) = lo4;
+            *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][32 + l]) = hi4;
+            reinterpret_cast<uint8_t*>(&s_xs[q][(b & 1) * 32 + l])[(b >> 1) & 1] = (uint8_t)e;
         }
         __syncthreads();
     };
     // registers x and x + 1 (x even) of lane (h, c): packed rows 8 (x / 4) + 4 h + x % 4 and the next, row c
     auto emit = [&](const At& a, int i, int tile, int x, float v0, float v1) {
-        const int r = (a.block * MT + i) * 32 + c, n = tile * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
+        const int r = i * 32 + c, n = tile * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
         if (tile >= p.tiles || r >= a.g.rows || n >= p.rows) return;
         const int64_t row = (int64_t)a.g.row0 + r;
         if constexpr (GATED) static_cast<uint16_t*>(p.out)[row * (p.rows >> 1) + (n >> 1)] = bf16_of(silu_times(v0, v1));
@@ -357,14 +358,14 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     Segment seg = segment(now);
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) load(ring[d], seg, d);
-    int64_t staged_group = -1;
-    int staged_block = 0, staged_chunk = 0;
+    int64_t staged_block = -1;
+    int staged_chunk = 0;
     clear();
     for (;;) {
-        const bool last_chunk = now.chunk + 1 == chunks, last = last_chunk && (now.block + 1) * (32 * MT) >= now.g.rows && now.item + 1 >= hi;
-        if (staged_group != now.group || staged_block != now.block || staged_chunk != now.chunk) {
+        const bool last_chunk = last_chunk_of(now), last = last_chunk && now.item + 1 >= hi;
+        if (staged_block != now.block || staged_chunk != now.chunk) {
             stage(now);
-            staged_group = now.group, staged_block = now.block, staged_chunk = now.chunk;
+            staged_block = now.block, staged_chunk = now.chunk;
         }
         const At then = after(now);
         const Segment next = segment(then);
@@ -372,12 +373,11 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) load(ring[d], next, d);
         }
-        const int tiles = MT == 1 || now.g.rows - now.block * (32 * MT) > 32 ? MT : 1;
         for (int q = 0; q < seg.n; q += kAhead) {
             const bool more = q + kAhead < seg.n;
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) {
-                if (q + d < seg.n) multiply(ring[d], seg.first + q + d, tiles);
+                if (q + d < seg.n) multiply(ring[d], seg.first + q + d, now.tiles);
                 load(ring[d], more ? seg : next, more ? q + kAhead + d : d);
             }
         }
@@ -386,12 +386,13 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int x = 0; x < 16; x += 2) emit(now, i, now.batch * kTiles + sub, x, acc[i][x], acc[i][x + 1]);
+                    for (int x = 0; x < 16; x += 2)
+                        if (i < now.tiles) emit(now, i, now.batch * kTiles + sub, x, acc[i][x], acc[i][x + 1]);
             } else {
                 // four registers at a time through LDS, the parts of K added in their order
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    if (i >= tiles) break;
+                    if (i >= now.tiles) break;
 #pragma unroll
                     for (int x4 = 0; x4 < 16; x4 += 4) {
                         __syncthreads();
@@ -720,18 +721,16 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         p.out = out, p.blocks = plan_list(pairs, a.plan.experts, 2);
         p.k = a.w.gated ? (uint32_t)a.plan.k : 0;
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
-        // 64 rows at a time where there are that many, or, with many experts, the most popular ones will have more than 32 (those would read their
-        // weights twice): 200 tokens of 4 of 64 experts, 4096 x 512 up, 46 us instead of 56; 64 of 2 of 8, 4096 x 14336, 113 instead of 104.
-        const int mt = pairs > 20 * active || (pairs > 10 * active && active >= 32) ? 2 : 1;
+        const int mt = pairs > 32 ? 2 : 1;                           // rows of a block, at most
         // How many waves share K: rounds of items over the compute units, each with what it streams (20 bytes a ns) and what a sum over waves, or
         // rows that come to LDS in several chunks, take; constants by measurement (us)
-        const int chunks = (p.Q + 32 / mt - 1) / (32 / mt);
+        const int tiles = pairs > 20 * active ? 2 : 1, chunks = (p.Q * tiles + 31) / 32;
         int split = 1;
         float least = 0.0f;
         for (int s = 1; s <= 16; s *= 2) {
             const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per);
             const float r = (float)n / (float)cus, rounds = (float)((n + cus - 1) / cus), stream = 0.115f * (float)(per * p.Q);
-            const float us = rounds * (mt * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.5f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
+            const float us = rounds * (tiles * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.5f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
             if (s == 1 || us < least) least = us, split = s;
         }
         const int64_t items = p.blocks * ((p.tiles + 16 / split - 1) / (16 / split));

@@ -260,6 +260,8 @@ PRODUCTS = [                                  # tokens, k, experts, K, rows
     (1, 1, 1, 32, 8, {}), (1, 8, 16, 256, 96, {}), (3, 2, 4, 96, 40, {}), (33, 1, 2, 64, 72, {}), (65, 4, 9, 160, 128, dict(absent=0.3)), (40, 2, 4, 1056, 264, dict(twice=True)),
     (7, 3, 40, 2080, 56, {}), (130, 2, 3, 544, 300 // 8 * 8, {}), (20, 2, 4, 64, 64, dict(absent=1.0)), (300, 2, 4, 128, 64, dict(only=1)), (257, 4, 8, 96, 520, {}),
     (1100, 2, 2, 224, 136, {}), (600, 5, 20, 64, 256, dict(absent=0.5)),
+    (100, 1, 8, 2176, 40, dict(only=1)), (40, 2, 6, 4192, 48, {}), (70, 3, 12, 4128, 24, dict(only=3, absent=0.2)), (4, 3, 5, 4256, 104, dict(twice=True)),
+    (2, 32, 64, 96, 1000, dict(absent=0.4)), (260, 1, 10, 64, 1032, {}), (16, 1, 8, 8224, 16, {}), (3, 2, 4, 14336, 32, {}), (90, 2, 1024, 128, 8, {}),
 ]
 
 
