@@ -300,14 +300,16 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
         }
     };
     // rows of the chunk into LDS; blocks behind the last of a quad as zeros
-    auto stage = [&](const At& a) {
+    auto stage = [&](const At& a, bool other_rows) {
         const int rows = min(32 * MT, a.g.rows), q0 = a.chunk * (kQuads / a.tiles), blocks = min(kQuads / a.tiles, p.Q - q0) * 4;
         __syncthreads();                                             // what was there is done with
-        for (int r = tid; r < rows; r += 1024) {
-            const int64_t row = (int64_t)a.g.row0 + r;
-            s_row[r] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
+        if (other_rows) {
+            if (tid < rows) {
+                const int64_t row = (int64_t)a.g.row0 + tid;
+                s_row[tid] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
+            }
+            __syncthreads();
         }
-        __syncthreads();
         // (four lanes a block: the quantizer's arithmetic)
         if (p.x)
             for (int i = tid; i < rows * blocks * 4; i += 1024) {
@@ -322,26 +324,34 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
                 *reinterpret_cast<uint2*>(&s_x[q][(b >> 1) & 1][b & 1][l][(quarter & 1) * 8]) = to;
                 if (quarter == 0) reinterpret_cast<uint8_t*>(&s_xs[q][(b & 1) * 32 + (r & 31)])[(b >> 1) & 1] = on ? (uint8_t)e : 0;
             }
-        else for (int i = tid; i < rows * blocks; i += 1024) {
-            const int r = i / blocks, b = i - r * blocks, kb = q0 * 4 + b;
-            const int64_t blk = (int64_t)s_row[r] * p.KB + kb;
-            uint4 codes = make_uint4(0, 0, 0, 0);
-            uint32_t e = 0, d = 7;
-            if (kb < p.KB) {
-                codes = *reinterpret_cast<const uint4*>(p.x_codes + blk * 16);
-                e = p.x_expo[blk];
-                d = p.x_dial[blk] & 15u;
+        else for (int i0 = tid; i0 < rows * blocks; i0 += 2048) {
+            // two at a time, so that their loads are
+            uint4 codes[2];
+            uint32_t e[2], d[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = min(i0 + 1024 * u, rows * blocks - 1), r = i / blocks, b = i - r * blocks;
+                const int64_t blk = (int64_t)s_row[r] * p.KB + min(q0 * 4 + b, p.KB - 1);
+                codes[u] = *reinterpret_cast<const uint4*>(p.x_codes + blk * 16);
+                e[u] = p.x_expo[blk];
+                d[u] = p.x_dial[blk];
             }
-            const uint2 tab = s_tab[d];
-            uint4 lo4, hi4;
-            expand8(codes.x, tab, lo4.x, lo4.y);
-            expand8(codes.y, tab, lo4.z, lo4.w);
-            expand8(codes.z, tab, hi4.x, hi4.y);
-            expand8(codes.w, tab, hi4.z, hi4.w);
-            const int q = (r >> 5) * 16 + (b >> 2), l = r & 31;
-            *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][l]) = lo4;
-            *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][32 + l]) = hi4;
-            reinterpret_cast<uint8_t*>(&s_xs[q][(b & 1) * 32 + l])[(b >> 1) & 1] = (uint8_t)e;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = i0 + 1024 * u, r = i / blocks, b = i - r * blocks;
+                if (i >= rows * blocks) break;
+                const bool on = q0 * 4 + b < p.KB;
+                const uint2 tab = on ? s_tab[d[u] & 15u] : make_uint2(0, 0);
+                uint4 lo4, hi4;
+                expand8(codes[u].x, tab, lo4.x, lo4.y);
+                expand8(codes[u].y, tab, lo4.z, lo4.w);
+                expand8(codes[u].z, tab, hi4.x, hi4.y);
+                expand8(codes[u].w, tab, hi4.z, hi4.w);
+                const int q = (r >> 5) * 16 + (b >> 2), l = r & 31;
+                *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][l]) = lo4;
+                *reinterpret_cast<uint4*>(s_x[q][(b >> 1) & 1][b & 1][32 + l]) = hi4;
+                reinterpret_cast<uint8_t*>(&s_xs[q][(b & 1) * 32 + l])[(b >> 1) & 1] = on ? (uint8_t)e[u] : 0;
+            }
         }
         __syncthreads();
     };
@@ -364,7 +374,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     for (;;) {
         const bool last_chunk = last_chunk_of(now), last = last_chunk && now.item + 1 >= hi;
         if (staged_block != now.block || staged_chunk != now.chunk) {
-            stage(now);
+            stage(now, staged_block != now.block);
             staged_block = now.block, staged_chunk = now.chunk;
         }
         const At then = after(now);
