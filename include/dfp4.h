@@ -469,6 +469,7 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
  * Router.  Scores of a token's experts, s = softmax(logits) or 1 / (1 + exp(-logits)); the choice is by c = s + bias.  Where there are
  * groups (expert e in group e / (experts / groups)), the `kept` groups with the largest sums of their `best` largest c stay, the others'
  * experts are not chosen.  ids: the k experts with the largest c, in that order; of equal ones the lowest index first (of groups too).
+ * (Without a bias, and with best 1 or no groups, the choice is by the logits: the same order, but where scores are equal that logits are not.)
  *   weights = s[ids] / (renormalize ? sum over the k of s[ids] : 1) * scale
  * Scores, sums and choices are in 64 bits.  Logits may be -infinity (score 0; a token with no other logit, or a renormalized sum of 0,
  * has weights 0); NaN counts as that, +infinity as the largest number.

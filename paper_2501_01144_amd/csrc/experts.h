@@ -86,6 +86,9 @@ struct AddNormArgs {
     bool wide;               // the residual in f32
 };
 
+// silu(g) * u: a reciprocal to 1 ulp (a division in full costs the gated epilogue of a 256 x 256 tile 3 us more)
+__device__ __forceinline__ float silu_times(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
+
 // An experts' product: rows of `x` (up: a token's, down: a pair's) with the experts' matrices
 struct ExpertsArgs {
     const uint16_t* x;

@@ -102,6 +102,9 @@ struct QuantizeArgs {
 
 // Rows quantized in the plan's order (the arithmetic of the quantizer, quant_pass.h; as quantize_native_kernel, but for the rows' places).
 // A wave takes 8 rows x 8 blocks; what is behind the last row is left as it is: it is multiplied, and its results are not kept.
+// 32768 rows (of 4096 tokens) x 2048 28.6 us, bound by the quantizer's arithmetic; 32768 x 1024 26.7, by memory (3.5 TB/s).  Tried for tokens of several
+// experts: each quantized once and written to its places (57 us: 16 bytes here and there), or once to 4 bits (8.5) and from these to all places in whole lines
+// (23.5); and scale bytes through LDS, so that they leave as whole lines (31.8 instead of 26.7).
 constexpr int kQThreads = 256, kQWaves = kQThreads / 64, kPasses = 4;
 __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArgs p) {
     __shared__ __attribute__((aligned(16))) uint8_t lds_q[kDialects * 32];
@@ -188,7 +191,6 @@ struct FewArgs {
 };
 
 __device__ __forceinline__ uint16_t bf16_of(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 // 8 codes -> FP8: elements 0, 2, 4, 6 and 1, 3, 5, 7 (rows and weights the same way, so that the order within a half of a block is free)
 __device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, uint32_t& odd) {
     even = __builtin_amdgcn_perm(tab.y, tab.x, c & 0x07070707u) | ((c << 4) & 0x80808080u);
@@ -606,9 +608,9 @@ inline int64_t active_experts(const dfp4_plan& plan) {
     const int64_t n = (int64_t)((double)plan.experts * (1.0 - none) + 0.5);
     return n > 0 ? n : 1;
 }
-// Rows an expert up to which weights are streamed past them; both sides, us, few / many: 20 rows 28 / 35, 25 rows 11.8 / 13.9, 32 rows 56 / 57 and 49 / 42,
-// 42 rows 33 / 28, 64 rows 63 / 70 and 54 / 51, 128 rows 91 / 88 and 83 / 66
-constexpr int64_t kFewRows = 28;
+// Rows an expert up to which weights are streamed past them; both sides, us, few / many: 20 rows 28 / 35, 32 rows (up) 134 / 157, 83 / 92, 35 / 36,
+// 15.3 / 14.0, (down) 84 / 112, 54 / 53, 29 / 29, 42 rows 33 / 28, 48 rows 147 / 159 and 61 / 49, 50 rows 117 / 98 and 89 / 57
+constexpr int64_t kFewRows = 34;
 // ... and up to which the large kernel takes 128 rows at a time instead of 256: 42 rows 28 / 33, 128 rows 88 / 91 and 126 / 143, 250 rows 76 / 63, 117 / 107
 constexpr int64_t kHalfRows = 160;
 // Whether tokens are taken one by one (down): where there are few, and weights that several of them read, again for each, cost less than the two
@@ -733,8 +735,9 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
         const int mt = pairs > 32 ? 2 : 1;                           // rows of a block, at most
         // How many waves share K: rounds of items over the compute units, each with what it streams (20 bytes a ns) and what a sum over waves, or
-        // rows that come to LDS in several chunks, take; constants by measurement (us)
-        const int tiles = pairs > 20 * active ? 2 : 1, chunks = (p.Q * tiles + 31) / 32;
+        // rows that come to LDS in several chunks, take; constants by measurement (us).  From 10 rows an expert on some will have more than 32:
+        // 8 experts, 4096 x 14336 up, 2 waves / 4: 10 rows each 110 / 104, one of 35 among them 125 / 147.
+        const int tiles = pairs > 10 * active ? 2 : 1, chunks = (p.Q * tiles + 31) / 32;
         int split = 1;
         float least = 0.0f;
         for (int s = 1; s <= 16; s *= 2) {

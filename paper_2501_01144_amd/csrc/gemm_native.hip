@@ -460,7 +460,6 @@ struct ExpertsParams : NativeParams {
     const PlanGroup* list;
     int most, cols;                   // at most; tiles of 256 columns of an expert
 };
-__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
 // TA = 32-row tiles per wave: 4 (256 x 256 per workgroup) or 2 (128 x 256, for products with few tiles)
 // MODE: what is made of the sums.  kPlain: dfp4_gemm_native.  kExact: the exact products.  kRequant: those, quantized.
@@ -488,11 +487,12 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(ParamsOf<MODE> p) {
     int bx = (int)blockIdx.x, by = (int)blockIdx.y;
     int expert = 0;
     if constexpr (kIsExperts) {
-        // An XCD takes a stretch of row tiles, all columns of one after the other, so that its cache holds an expert's weights
-        const int units = min(*p.used, p.most), share = (units + 7) >> 3, in = bx >> 3, unit = in / p.cols, at = (bx & 7) * share + unit;
-        if (unit >= share || at >= units) return;
+        // An XCD takes a stretch of tiles, all columns of 256 (128) rows after the other, so that its cache holds an expert's weights
+        const int tiles = min(*p.used, p.most) * p.cols, share = (tiles + 7) >> 3, in = bx >> 3, tile = (bx & 7) * share + in;
+        if (in >= share || tile >= tiles) return;
+        const int at = tile / p.cols;
         const PlanGroup g = p.list[at];
-        bx = in - unit * p.cols;
+        bx = tile - at * p.cols;
         by = g.at / kRowsWg;
         expert = g.expert;
         p.M = g.rows;
@@ -1139,7 +1139,7 @@ int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream) {
     p.list = t.list;
     p.cols = t.tiles;
     p.most = (int)t.most;
-    const int64_t wgs = (t.most + 7) / 8 * 8 * p.cols;
+    const int64_t wgs = (t.most * p.cols + 7) / 8 * 8;
     if (wgs >= (int64_t)1 << 24) return DFP4_ERR_SHAPE;                       // fewer than 2^32 threads
     const dim3 grid((unsigned)wgs);
     auto run = [&](auto bf16_c, auto mode_c) {

@@ -1,8 +1,11 @@
 // The router of a sparse layer and the plan of its experts' products (formulas and arrays in include/dfp4.h).
 //
-// A wave takes a token: PER experts a lane (expert 64 j + lane).  Choices are by 64-bit keys that order as the scores do, the largest of a
-// wave by its upper halves first (DPP) and the lower ones only where several lanes share it, which is all but never.
-// Scores are in 64 bits because a choice is a whole number: next to a border fp32 would take another expert than the formula does.
+// A wave takes a token: PER experts a lane (expert 64 j + lane).  Choices are by 32-bit keys that order as the scores do; where several are the largest,
+// which for scores in 64 bits is all but never, by the scores themselves.  Scores are in 64 bits because a choice is a whole number: next to a
+// border fp32 would take another expert than the formula does.  Without a bias, and where groups go by one score, the order is the logits', and
+// only what the weights need is computed.
+// Bound by vector instructions (k rounds of a maximum over the wave): 16384 tokens of 8 of 256 XX us (with 64-bit keys, all scores computed, 25.5).
+#include <type_traits>
 #include "experts.h"
 
 namespace dfp4 {
@@ -30,20 +33,20 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// 64-bit integers that order as the numbers do; 0 is below all, NaN 1
+// Integers that order as the numbers do; 0 is below all, NaN 1
+__device__ __forceinline__ uint32_t key_of(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const uint32_t k = (b >> 31) ? ~b : b | 0x80000000u;
+    return v == v ? k : 1u;
+}
 __device__ __forceinline__ uint64_t key_of(double v) {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     const uint64_t k = (b >> 63) ? ~b : b | 0x8000000000000000ull;
     return v == v ? k : 1ull;
 }
-// The largest key of a wave, in all lanes
 __device__ __forceinline__ uint64_t wave_max(uint64_t k) {
     const uint32_t hi = wave_max((uint32_t)(k >> 32));
-    const uint64_t same = __ballot((uint32_t)(k >> 32) == hi);
-    uint32_t lo;
-    if (__popcll(same) == 1) lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, __ffsll((unsigned long long)same) - 1);
-    else lo = wave_max((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-    return (uint64_t)hi << 32 | lo;
+    return (uint64_t)hi << 32 | wave_max((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
 }
 
 template <int PER>
@@ -53,59 +56,66 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     const int64_t token = (int64_t)blockIdx.x * kWaves + wave;
     const bool on = token < a.tokens;
     const int E = a.experts;
-    double s[PER];
-    {
-        float x[PER], top = -__builtin_inff();
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int e = 64 * j + lane;
-            x[j] = -__builtin_inff();
-            if (on && e < E) {
-                const int64_t at = token * a.ld + e;
-                x[j] = a.bf16 ? as_f((uint32_t)static_cast<const uint16_t*>(a.logits)[at] << 16) : static_cast<const float*>(a.logits)[at];
-                x[j] = x[j] == x[j] ? fminf(x[j], 3.402823466e38f) : -__builtin_inff();
-            }
-            top = fmaxf(top, x[j]);
-        }
-        if (a.sigmoid) {
-#pragma unroll
-            for (int j = 0; j < PER; ++j) s[j] = 1.0 / (1.0 + exp(-(double)x[j]));
-        } else {
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-            double sum = 0.0;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                s[j] = top == -__builtin_inff() ? 0.0 : exp((double)x[j] - (double)top);
-                sum += s[j];
-            }
-            sum = wave_sum(sum);
-#pragma unroll
-            for (int j = 0; j < PER; ++j) s[j] = sum > 0.0 ? s[j] / sum : 0.0;
-        }
-    }
-    uint64_t key[PER];
+    const bool by_logit = !a.bias && (a.groups == 1 || a.best == 1);
+    float x[PER], top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const int e = 64 * j + lane;
-        const double c = a.bias && e < E ? s[j] + (double)a.bias[e] : s[j];
-        key[j] = e < E ? key_of(c) : 0;
-        if (a.groups > 1) s_score[wave][e] = c;
+        x[j] = -__builtin_inff();
+        if (on && e < E) {
+            const int64_t at = token * a.ld + e;
+            x[j] = a.bf16 ? as_f((uint32_t)static_cast<const uint16_t*>(a.logits)[at] << 16) : static_cast<const float*>(a.logits)[at];
+            x[j] = x[j] == x[j] ? fminf(x[j], 3.402823466e38f) : -__builtin_inff();
+        }
+        top = fmaxf(top, x[j]);
+    }
+    double sum = 1.0;                                     // of softmax
+    auto score = [&](float v) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : top == -__builtin_inff() ? 0.0 : exp((double)v - (double)top) / sum; };
+    if (!a.sigmoid) {
+        const uint32_t k = wave_max(key_of(top));
+        top = as_f((k >> 31) ? k & 0x7fffffffu : ~k);
+        if (!by_logit || !a.renormalize) {
+            double t = 0.0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) t += score(x[j]);
+            t = wave_sum(t);
+            sum = t > 0.0 ? t : 1.0;
+        }
+    }
+    // what is chosen by: the logit, or c in 64 bits (in LDS) and its rounding to 32
+    uint32_t key[PER];
+    if (by_logit) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = 64 * j + lane < E ? key_of(x[j]) : 0;
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int e = 64 * j + lane;
+            double c = score(x[j]);
+            if (a.bias && e < E) c += (double)a.bias[e];
+            s_score[wave][e] = c;
+            key[j] = e < E ? key_of((float)c) : 0;
+        }
     }
     if (a.groups > 1) {
-        __syncthreads();
         // a lane a group
         const int size = E / a.groups;
-        double first = -__builtin_inf(), second = -__builtin_inf();
+        uint64_t mine = 0;
+        if (by_logit) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) s_score[wave][64 * j + lane] = (double)x[j];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (lane < a.groups) {
+            double first = -__builtin_inf(), second = -__builtin_inf();
             for (int i = 0; i < size; ++i) {
                 double c = s_score[wave][lane * size + i];
                 c = c == c ? c : -__builtin_inf();
                 second = fmax(second, fmin(first, c));
                 first = fmax(first, c);
             }
+            mine = key_of(a.best == 2 ? first + second : first);
         }
-        const uint64_t mine = lane < a.groups ? key_of(a.best == 2 ? first + second : first) : 0;
         int better = 0;
         for (int g = 0; g < a.groups; ++g) {
             const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), g) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)mine, g);
@@ -117,34 +127,52 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
             const int e = 64 * j + lane;
             if (e < E && !((stays >> (e / size)) & 1)) key[j] = 0;
         }
-        __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < PER; ++j) s_score[wave][64 * j + lane] = s[j];
-    int chosen = 0;                                       // lane j: the j-th
+    int chosen = 0;                                       // lane j: the j-th, and its logit
+    float logit = 0.0f;
     for (int i = 0; i < a.k; ++i) {
-        uint64_t best = key[0];
+        uint32_t m = key[0];
 #pragma unroll
-        for (int j = 1; j < PER; ++j) best = best > key[j] ? best : key[j];
-        best = wave_max(best);
-        // the lowest index that has it
-        int e = 0;
+        for (int j = 1; j < PER; ++j) m = max(m, key[j]);
+        m = wave_max(m);
+        int e = 0, several = 0;
 #pragma unroll
         for (int j = PER - 1; j >= 0; --j) {
-            const uint64_t has = __ballot(key[j] == best);
-            if (has) e = 64 * j + __ffsll((unsigned long long)has) - 1;
+            const uint64_t has = __ballot(key[j] == m);
+            several += (int)__popcll(has);
+            if (has) e = 64 * j + __ffsll((unsigned long long)has) - 1;         // the lowest
         }
-        if (lane == i) chosen = e;
+        if (several > 1 && !by_logit) {
+            uint64_t best = 0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
+            for (int j = 0; j < PER; ++j) {
+                const uint64_t k = key[j] == m ? key_of(s_score[wave][64 * j + lane]) : 0;
+                best = best > k ? best : k;
+            }
+            best = wave_max(best);
+#pragma unroll
+            for (int j = PER - 1; j >= 0; --j) {
+                const uint64_t has = __ballot(key[j] == m && key_of(s_score[wave][64 * j + lane]) == best);
+                if (has) e = 64 * j + __ffsll((unsigned long long)has) - 1;
+            }
+        }
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (e >> 6 == j) v = x[j];
             if (64 * j + lane == e) key[j] = 0;
+        }
+        v = as_f((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), e & 63));
+        if (lane == i) chosen = e, logit = v;
     }
-    __syncthreads();
-    const double mine = lane < a.k ? s_score[wave][chosen] : 0.0;
+    const double mine = lane < a.k ? score(logit) : 0.0;
     double total = 1.0;
     if (a.renormalize) {
         total = 0.0;
-        for (int i = 0; i < a.k; ++i) total += __shfl(mine, i);
+        for (int i = 0; i < a.k; ++i) {
+            const uint64_t b = __builtin_bit_cast(uint64_t, mine);
+            total += __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, i));
+        }
     }
     if (on && lane < a.k) {
         a.ids[token * a.k + lane] = chosen;
@@ -155,6 +183,19 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 // ---- plan
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+// sums over the lanes up to each
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    auto add = [&](auto ctrl, auto rows) { v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    using std::integral_constant;
+    add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});      // from 1, 2, 4, 8 lanes before, within 16
+    add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});      // the last lane of 16 to the 16 after it, of 32 to the other 32
+    add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return v;
+}
 
 // A stable counting sort.  A workgroup takes a share of the pairs, 16 waves in turn; where there are several, a first kernel has counted each
 // share's experts.  Every workgroup knows all counts then, and with them each expert's first row and its entries of the lists; a wave ranks its pairs 64 at
@@ -175,12 +216,14 @@ __global__ __launch_bounds__(kPlanThreads) void expert_count_kernel(const int32_
 __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int64_t share, int experts, int bits) {
     __shared__ uint32_t s_at[kPlanWaves][kMaxExperts];               // of a wave's pairs: how many, then the next row
     __shared__ uint32_t s_row[kMaxExperts], s_group[kMaxExperts];
-    __shared__ uint32_t s_sum[4][kPlanWaves], s_rows;
+    __shared__ uint4 s_sum[kPlanWaves];
+    __shared__ uint32_t s_rows;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t lo = blockIdx.x * share, hi = min(pairs, lo + share);
     // (a wave's part of the share: whole rounds of 64)
     const int64_t per = share / kPlanWaves, wlo = min(hi, lo + wave * per), whi = min(hi, wlo + per);
-    for (int i = tid; i < kPlanWaves * experts; i += kPlanThreads) s_at[i / experts][i % experts] = 0;
+    for (int w = 0; w < kPlanWaves; ++w)
+        if (tid < experts) s_at[w][tid] = 0;
     __syncthreads();
     for (int64_t i = wlo + lane; i < whi; i += 64) {
         const uint32_t id = (uint32_t)ids[i];
@@ -192,6 +235,7 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
     uint32_t total = 0, before = 0;
     if (e < experts) {
         if (gridDim.x > 1) {
+#pragma unroll 16
             for (int b = 0; b < (int)gridDim.x; ++b) {
                 const uint32_t n = (uint32_t)v.counts[(int64_t)b * experts + e];
                 total += n;
@@ -206,17 +250,13 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
 #pragma unroll
     for (int q = 0; q < 3; ++q) sum[q + 1] = entries[q] = (total + kListRows[q] - 1) / kListRows[q];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        for (int x = 1; x < 64; x <<= 1) {
-            const uint32_t n = __shfl_up(sum[q], x);
-            if (lane >= x) sum[q] += n;
-        }
-        if (lane == 63) s_sum[q][wave] = sum[q];
-    }
+    for (int q = 0; q < 4; ++q) sum[q] = wave_scan(sum[q]);
+    if (lane == 63) s_sum[wave] = make_uint4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        for (int w = 0; w < wave; ++w) sum[q] += s_sum[q][w];
+    for (int w = 0; w < (experts + 63) / 64; ++w) {
+        const uint4 v = s_sum[w];
+        if (w < wave) sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;
+    }
     if (e < experts) {
         const uint32_t row0 = sum[0] - total, group0 = sum[1] - entries[0];
         s_row[e] = row0;

@@ -97,7 +97,8 @@ def test_add_norm_refuses():
 # ---- plain implementations -------------------------------------------------------------------------------------------------
 
 def plain_route(logits, k, score="softmax", bias=None, groups=1, kept=1, best=1, renormalize=True, scale=1.0):
-    """float64 scores; ids by (largest choice, lowest index)."""
+    """float64 scores; ids by (largest choice, lowest index).  Without a bias a choice is the score's, which orders strictly as the logit does
+    (-infinity: 0), where float64 rounds scores of different logits to one; only sums of two scores need the scores themselves."""
     x = np.asarray(logits, np.float64)
     x = np.where(np.isnan(x), -np.inf, np.minimum(x, np.finfo(np.float32).max))
     ids, weights = [], []
@@ -107,7 +108,7 @@ def plain_route(logits, k, score="softmax", bias=None, groups=1, kept=1, best=1,
             s = s / s.sum() if s.sum() > 0 else s
         else:
             s = 1 / (1 + np.exp(-row))
-        c = s + (0 if bias is None else np.asarray(bias, np.float64))
+        c = row if bias is None and (groups == 1 or best == 1) else s + (0 if bias is None else np.asarray(bias, np.float64))
         if groups > 1:
             g = np.sort(c.reshape(groups, -1), 1)[:, ::-1][:, :best].sum(1)
             stay = sorted(range(groups), key=lambda i: (-g[i], i))[:kept]
