@@ -518,7 +518,8 @@ int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* 
  * Experts' products.  Rows are quantized as dfp4_quantize does and multiplied with the experts' weights in fp32.
  *   up    (gated weights) h[row] = silu(G x^) * (U x^), x^ the quantized x of the row's token; rows in the plan's order
  *   down  (others)        y[token] = sum over its pairs j, in their order, of weights[token, j] * (W h^[row of the pair]); 0 without any
- *   (rows of the weights: a multiple of 8, up to 2^20, fewer than 2^28 of all experts; K up to 2^20)
+ *   (rows of the weights: a multiple of 8, up to 2^19, fewer than 2^28 of all experts; K up to 2^20.  Refused as too large: products of many rows of
+ *   more than about 2^24 tiles of 256 x 256.)
  *   x     device, bf16 [tokens, K], rows x_ld elements apart (a multiple of 8), 16-byte aligned
  *   h     device, bf16 [tokens * k, rows of G]; dfp4_experts_down: [tokens * k, K], rows h_ld elements apart (a multiple of 8); 16-byte aligned.
  *         Rows from offsets[experts] on are neither written nor read.

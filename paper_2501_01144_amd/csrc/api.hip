@@ -619,7 +619,7 @@ int dfp4_expert_plan(const int32_t* ids, dfp4_plan plan, void* stream) {
 }
 
 static int check_experts(const dfp4_experts& w) {
-    if (w.experts < 1 || w.experts > kMaxExperts || w.rows < 8 || w.rows % 8 != 0 || w.rows > (1 << 20) || w.K < kBlock || w.K % kBlock != 0 || w.K > (1 << 20) ||
+    if (w.experts < 1 || w.experts > kMaxExperts || w.rows < 8 || w.rows % 8 != 0 || w.rows > (1 << 19) || w.K < kBlock || w.K % kBlock != 0 || w.K > (1 << 20) ||
         w.experts * w.rows >= 1 << 28)
         return DFP4_ERR_SHAPE;
     return DFP4_OK;
@@ -644,7 +644,7 @@ int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* 
 }
 
 size_t dfp4_experts_workspace_bytes(dfp4_plan plan, dfp4_experts w) {
-    if (check_plan(plan) != DFP4_OK || check_experts(w) != DFP4_OK || plan.experts != w.experts || plan.tokens == 0) return 0;
+    if (check_plan(plan) != DFP4_OK || check_experts(w) != DFP4_OK || plan.experts != w.experts || plan.tokens == 0 || !experts_fit(plan, w)) return 0;
     return experts_workspace_bytes(plan, w);
 }
 
@@ -654,6 +654,7 @@ static int experts_product(const ExpertsArgs& a, int64_t x_cols, size_t workspac
     if (rc != DFP4_OK) return rc;
     if (a.plan.experts != a.w.experts || a.ld < x_cols || a.ld > (int64_t)1 << 30) return DFP4_ERR_SHAPE;
     if (a.plan.tokens == 0) return DFP4_OK;
+    if (!experts_fit(a.plan, a.w)) return DFP4_ERR_SHAPE;
     if (!a.x || !a.out || !a.plan.data || !a.w.packed || (!a.w.gated && !a.weights)) return DFP4_ERR_NULL;
     if (a.ld % 8 != 0 || !aligned(a.x, 16) || !aligned(a.out, 16) || !aligned(a.plan.data, 16) || !aligned(a.w.packed, 256) || !aligned(a.weights, 4) ||
         !aligned(a.workspace, 256))

@@ -379,6 +379,11 @@ PyObject* expert_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// piece(tensor of one dimension, first, count) -> view
+PyObject* piece(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 3, [&]() -> PyObject* { return THPVariable_Wrap(tensor(a[0]).narrow(0, number(a[1]), number(a[2]))); });
+}
+
 // experts_up(x, the plan's four, the weights' five) -> h
 PyObject* experts_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 10, [&]() -> PyObject* {
@@ -462,7 +467,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {DFP4_METHOD(bind), DFP4_METHOD(quantize), DFP4_METHOD(dequantize), DFP4_METHOD(gemm), DFP4_METHOD(gemm_batched),
                          DFP4_METHOD(gemm_prepare), DFP4_METHOD(gemm_prepared), DFP4_METHOD(quantize_native), DFP4_METHOD(native_pack),
                          DFP4_METHOD(gemm_native_packed), DFP4_METHOD(paged_write), DFP4_METHOD(paged_read), DFP4_METHOD(paged_attention),
-                         DFP4_METHOD(norm_rope), DFP4_METHOD(route), DFP4_METHOD(expert_plan), DFP4_METHOD(experts_up), DFP4_METHOD(experts_down),
+                         DFP4_METHOD(norm_rope), DFP4_METHOD(route), DFP4_METHOD(expert_plan), DFP4_METHOD(piece), DFP4_METHOD(experts_up), DFP4_METHOD(experts_down),
                          DFP4_METHOD(add_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -30,6 +30,7 @@ struct PlanView {
     int32_t* order;          // [pairs] pair of a row, -1 behind the last
     int32_t* place;          // [pairs] row of a pair, -1: none
     int32_t* row_at;         // [pairs] group * kGroupRows + row in it, of a row
+    int32_t* expert;         // [pairs] of a pair, -1: none
     int32_t* used;           // [3] of each list
     PlanGroup* list[3];      // 16-byte aligned
     int32_t* counts;         // [shares][experts], where there are several
@@ -39,7 +40,7 @@ struct PlanSizes {
 };
 inline PlanSizes plan_sizes(int64_t pairs, int64_t experts) {
     PlanSizes s;
-    s.counts_at = (experts + 1 + 3 * pairs + 3 + 3) / 4 * 4;
+    s.counts_at = (experts + 1 + 4 * pairs + 3 + 3) / 4 * 4;
     for (int q = 0; q < 3; ++q) {
         s.list_at[q] = s.counts_at;
         s.counts_at += 4 * plan_list(pairs, experts, q);
@@ -55,7 +56,8 @@ inline PlanView plan_view(const dfp4_plan& p) {
     v.order = v.offsets + p.experts + 1;
     v.place = v.order + pairs;
     v.row_at = v.place + pairs;
-    v.used = v.row_at + pairs;
+    v.expert = v.row_at + pairs;
+    v.used = v.expert + pairs;
     for (int q = 0; q < 3; ++q) v.list[q] = reinterpret_cast<PlanGroup*>(p.data + s.list_at[q]);
     v.counts = p.data + s.counts_at;
     return v;
@@ -120,6 +122,7 @@ int launch_expert_plan(const int32_t* ids, const dfp4_plan& plan, hipStream_t st
 int launch_add_norm(const AddNormArgs& a, hipStream_t stream);
 size_t expert_weights_bytes(int64_t experts, int64_t rows, int64_t K, bool gated);
 int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& w, hipStream_t stream);
+bool experts_fit(const dfp4_plan& plan, const dfp4_experts& w);
 size_t experts_workspace_bytes(const dfp4_plan& plan, const dfp4_experts& w);
 int launch_experts(const ExpertsArgs& a, hipStream_t stream);
 

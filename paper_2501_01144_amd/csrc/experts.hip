@@ -160,6 +160,37 @@ __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArg
     }
 }
 
+struct CodesArgs {
+    const uint16_t* x;
+    int64_t ld;
+    const int32_t* rows;                         // how many there are (device), or null: all
+    uint32_t* codes;
+    uint8_t *dial, *expo;
+    int64_t bound;
+    int KB;
+};
+
+// Rows in their 4-bit form, as dfp4_quantize leaves it, as many as there are (what is behind them may be anything, infinities too)
+__global__ __launch_bounds__(256) void experts_codes_kernel(CodesArgs p) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds_q[kDialects * 32];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_s[kPairs * 32];
+    if (threadIdx.x < 32) reinterpret_cast<uint4*>(lds_q)[threadIdx.x] = reinterpret_cast<const uint4*>(g_quant_tables.near_i)[threadIdx.x];
+    else if (threadIdx.x < 48) reinterpret_cast<uint4*>(lds_s)[threadIdx.x - 32] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[threadIdx.x - 32];
+    __syncthreads();
+    const int64_t rows = p.rows ? min((int64_t)*p.rows, p.bound) : p.bound, quarters = rows * p.KB * 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quarters; i += (int64_t)gridDim.x * 256) {
+        const int64_t blk = i >> 2, row = blk / p.KB;
+        const uint4 w = *reinterpret_cast<const uint4*>(p.x + row * p.ld + (blk - row * p.KB) * kBlock + (i & 3) * 8);
+        uint32_t code, eb, dl;
+        dfp4_pass_small(w, lds_s, lds_q, code, eb, dl);
+        p.codes[i] = code;
+        if ((i & 3) == 0) {
+            p.expo[blk] = (uint8_t)eb;
+            p.dial[blk] = (uint8_t)dl;
+        }
+    }
+}
+
 // ---- products of few rows an expert
 
 // FP8 E4M3 bit patterns of a dialect's 8 magnitudes (0.5 u, all exact)
@@ -187,6 +218,7 @@ struct FewArgs {
     void* out;                                   // up: bf16 [row][rows / 2], down: f32 [row][rows]
     int64_t blocks;                              // at most
     uint32_t k;                                  // rows of x are tokens', pair / k; 0: the plan's own
+    bool single;                                 // one token
     int KB, Q, rows, tiles;                      // blocks, quads of blocks; packed rows of an expert, tiles of 32 of them
 };
 
@@ -215,7 +247,8 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     else if (p.x && tid >= 64 && tid < 96) reinterpret_cast<uint4*>(s_index)[tid - 64] = reinterpret_cast<const uint4*>(g_quant_tables.near_i)[tid - 64];
     else if (p.x && tid >= 128 && tid < 144) reinterpret_cast<uint4*>(s_vote)[tid - 128] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[tid - 128];
     const int batches = (p.tiles + kTiles - 1) / kTiles;
-    const int64_t used = min((int64_t)*p.used, p.blocks), items = used * batches;
+    // (one token: as many blocks as there can be, some without rows, and its row is known: a load less, twice, before the first that counts)
+    const int64_t used = p.single ? p.blocks : min((int64_t)*p.used, p.blocks), items = used * batches;
     const int64_t lo = items * blockIdx.x / gridDim.x, hi = items * (blockIdx.x + 1) / gridDim.x;
     if (lo >= hi) return;
 
@@ -308,7 +341,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
         if (other_rows) {
             if (tid < rows) {
                 const int64_t row = (int64_t)a.g.row0 + tid;
-                s_row[tid] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
+                s_row[tid] = p.single && GATED ? 0 : p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
             }
             __syncthreads();
         }
@@ -438,12 +471,11 @@ struct TokenArgs {
     const uint16_t* h;
     int64_t ld;
     const uint8_t* quads;
-    const int32_t *place, *row_at;
-    const PlanGroup* groups;
+    const int32_t *place, *expert;
     const float* weights;
     void* y;
     int64_t pairs;
-    int k, KB, Q, rows, tiles;
+    int experts, k, KB, Q, rows, tiles;
 };
 constexpr int kTokenElements = 48 << 10;         // of a token's rows, in LDS
 
@@ -467,11 +499,12 @@ __global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
     else if (tid >= 128 && tid < 144) reinterpret_cast<uint4*>(s_vote)[tid - 128] = reinterpret_cast<const uint4*>(g_quant_tables.vote1)[tid - 128];
     else if (tid >= 192 && tid < 192 + p.k) {
         const int j = tid - 192;
-        const int32_t row = p.place[token * p.k + j];
-        const bool there = row >= 0 && row < p.pairs;
+        const int32_t row = p.place[token * p.k + j], expert = p.expert[token * p.k + j];
+        const float weight = p.weights[token * p.k + j];
+        const bool there = row >= 0 && row < p.pairs && (uint32_t)expert < (uint32_t)p.experts;
         s_row[j] = there ? row : -1;
-        s_expert[j] = there ? p.groups[p.row_at[row] / kGroupRows].expert : 0;
-        s_weight[j] = there ? p.weights[token * p.k + j] : 0.0f;
+        s_expert[j] = there ? expert : 0;
+        s_weight[j] = there ? weight : 0.0f;
     }
     __syncthreads();
     const int units = p.k * p.Q, lo = units * wave / 16, hi = units * (wave + 1) / 16;
@@ -665,6 +698,12 @@ int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& 
     return check_launch();
 }
 
+// Whether one launch holds the tiles of a product of many rows (fewer than 2^32 threads)
+bool experts_fit(const dfp4_plan& plan, const dfp4_experts& w) {
+    const int64_t pairs = plan.tokens * plan.k;
+    return !workspace_of(plan, w).many || plan_list(pairs, plan.experts, pairs <= kHalfRows * active_experts(plan) ? 1 : 0) * (padded_rows(w) / 256) < (1 << 24) - 8;
+}
+
 size_t experts_workspace_bytes(const dfp4_plan& plan, const dfp4_experts& w) { return (size_t)workspace_of(plan, w).total; }
 
 template <bool GATED, int MT>
@@ -685,8 +724,8 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         TokenArgs p{};
         p.h = a.x, p.ld = a.ld;
         p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
-        p.place = plan.place, p.row_at = plan.row_at, p.groups = plan.list[0], p.weights = a.weights;
-        p.y = a.out, p.pairs = pairs;
+        p.place = plan.place, p.expert = plan.expert, p.weights = a.weights;
+        p.y = a.out, p.pairs = pairs, p.experts = (int)a.plan.experts;
         p.k = (int)a.plan.k, p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)a.w.rows, p.tiles = (int)row_tiles(a.w);
         const dim3 grid((unsigned)p.tiles, (unsigned)a.plan.tokens);
         const size_t lds = (size_t)p.k * p.Q * 132;
@@ -724,14 +763,16 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         if (pairs * a.w.K <= active * 16384) {
             p.x = a.x, p.ld = a.ld;
         } else {
-            const int rc = launch_quantize(false, a.x, ws.rows, a.w.K, a.ld, x, stream);
-            if (rc != DFP4_OK) return rc;
+            const CodesArgs c{a.x, a.ld, a.w.gated ? nullptr : plan.offsets + a.plan.experts, reinterpret_cast<uint32_t*>(x.codes), x.dialect, x.exponent, ws.rows,
+                              (int)(a.w.K / kBlock)};
+            const int64_t wgs = (ws.rows * (a.w.K / 8) + 255) / 256;
+            hipLaunchKernelGGL(experts_codes_kernel, dim3((unsigned)(wgs < 16 * cus ? wgs : 16 * cus)), dim3(256), 0, stream, c);
         }
         p.x_codes = x.codes, p.x_dial = x.dialect, p.x_expo = x.exponent;
         p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
         p.used = plan.used + 2, p.order = plan.order, p.plan = plan.list[2];
         p.out = out, p.blocks = plan_list(pairs, a.plan.experts, 2);
-        p.k = a.w.gated ? (uint32_t)a.plan.k : 0;
+        p.k = a.w.gated ? (uint32_t)a.plan.k : 0, p.single = a.plan.tokens == 1;
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
         const int mt = pairs > 32 ? 2 : 1;                           // rows of a block, at most
         // How many waves share K: rounds of items over the compute units, each with what it streams (20 bytes a ns) and what a sum over waves, or

@@ -213,11 +213,11 @@ __global__ __launch_bounds__(kPlanThreads) void expert_count_kernel(const int32_
     for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[(int64_t)blockIdx.x * experts + e] = s_count[e];
 }
 
-__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int64_t share, int experts, int bits) {
+__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int64_t share, int experts, int bits, int64_t most_blocks) {
     __shared__ uint32_t s_at[kPlanWaves][kMaxExperts];               // of a wave's pairs: how many, then the next row
     __shared__ uint32_t s_row[kMaxExperts], s_group[kMaxExperts];
     __shared__ uint4 s_sum[kPlanWaves];
-    __shared__ uint32_t s_rows;
+    __shared__ uint32_t s_rows, s_blocks;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t lo = blockIdx.x * share, hi = min(pairs, lo + share);
     // (a wave's part of the share: whole rounds of 64)
@@ -279,30 +279,39 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
             }
             if (e == experts - 1) v.offsets[experts] = (int32_t)sum[0];
         }
-        if (e == experts - 1) s_rows = sum[0];
+        if (e == experts - 1) s_rows = sum[0], s_blocks = sum[3];
     }
     __syncthreads();
-    for (int64_t i0 = wlo; i0 < whi; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const uint32_t id = i < whi ? (uint32_t)ids[i] : 0xffffffffu;
-        const bool is = id < (uint32_t)experts;
-        uint64_t same = __ballot(is);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot((id >> b) & 1);
-            same &= (id >> b) & 1 ? set : ~set;
+    for (int64_t i4 = wlo; i4 < whi; i4 += 256) {
+        uint32_t next[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) next[q] = i4 + 64 * q + lane < whi ? (uint32_t)ids[i4 + 64 * q + lane] : 0xffffffffu;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t i = i4 + 64 * q + lane;
+            const uint32_t id = next[q];
+            const bool is = id < (uint32_t)experts;
+            uint64_t same = __ballot(is);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot((id >> b) & 1);
+                same &= (id >> b) & 1 ? set : ~set;
+            }
+            if (i < whi) v.expert[i] = is ? (int32_t)id : -1;
+            if (is) {
+                const uint32_t row = s_at[wave][id] + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+                v.order[row] = (int32_t)i;
+                v.row_at[row] = (int32_t)(s_group[id] * kGroupRows + row - s_row[id]);
+                v.place[i] = (int32_t)row;
+            } else if (i < whi) {
+                v.place[i] = -1;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (is && (same >> lane) == 1) s_at[wave][id] += (uint32_t)__popcll(same);  // the last of them
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        if (is) {
-            const uint32_t row = s_at[wave][id] + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-            v.order[row] = (int32_t)i;
-            v.row_at[row] = (int32_t)(s_group[id] * kGroupRows + row - s_row[id]);
-            v.place[i] = (int32_t)row;
-        } else if (i < whi) {
-            v.place[i] = -1;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (is && (same >> lane) == 1) s_at[wave][id] += (uint32_t)__popcll(same);      // the last of them
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    if (blockIdx.x == 0)                                             // (as many as there can be are looked at where there is one token)
+        for (int64_t g = s_blocks + tid; g < most_blocks; g += kPlanThreads) v.list[2][g] = PlanGroup{0, 0, 0, 0};
     // rows that no pair has
     for (int64_t r = s_rows + (int64_t)blockIdx.x * kPlanThreads + tid; r < pairs; r += (int64_t)gridDim.x * kPlanThreads) v.order[r] = -1;
 }
@@ -325,7 +334,8 @@ int launch_expert_plan(const int32_t* ids, const dfp4_plan& p, hipStream_t strea
     int bits = 0;
     while ((1 << bits) < p.experts) ++bits;
     if (shares > 1) hipLaunchKernelGGL(expert_count_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v.counts, pairs, share, (int)p.experts);
-    hipLaunchKernelGGL(expert_plan_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v, pairs, share, (int)p.experts, bits);
+    hipLaunchKernelGGL(expert_plan_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v, pairs, share, (int)p.experts, bits,
+                       p.tokens == 1 ? plan_list(pairs, p.experts, 2) : 0);
     return check_launch();
 }
 

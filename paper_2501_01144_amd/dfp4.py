@@ -690,16 +690,16 @@ class ExpertPlan:
 
     @property
     def offsets(self):
-        return self.data[:self.experts + 1]
+        return _calls().piece(self.data, 0, self.experts + 1)
 
     @property
     def order(self):
-        return self.data[self.experts + 1:self.experts + 1 + self.tokens * self.k]
+        return _calls().piece(self.data, self.experts + 1, self.tokens * self.k)
 
     @property
     def place(self):
         n = self.tokens * self.k
-        return self.data[self.experts + 1 + n:self.experts + 1 + 2 * n]
+        return _calls().piece(self.data, self.experts + 1 + n, n)
 
     def c(self):
         return _CPlan(_ptr(self.data).value, self.tokens, self.k, self.experts)

@@ -48,7 +48,7 @@ def test_expert_weights_refuse():
     lib, vp = dfp4.load(), ctypes.c_void_p
     t = lambda codes=256, dialect=256, exponent=256, rows=512, K=64: dfp4._CTensor(codes, dialect, exponent, rows, K)  # noqa: E731
     call = lambda gate, up, w: lib.dfp4_expert_weights(gate, up, w, vp(0))  # noqa: E731
-    for bad in (dict(experts=0), dict(experts=2000), dict(rows=0), dict(rows=12), dict(rows=(1 << 20) + 8), dict(K=0), dict(K=48), dict(experts=1024, rows=1 << 19)):
+    for bad in (dict(experts=0), dict(experts=2000), dict(rows=0), dict(rows=12), dict(rows=(1 << 19) + 8), dict(K=0), dict(K=48), dict(experts=1024, rows=1 << 18)):
         assert call(t(), t(), _weights_c(**bad)) == -2, bad
         w = _weights_c(**bad)
         assert lib.dfp4_expert_weights_bytes(w.experts, w.rows, w.K, w.gated) == 0
@@ -77,6 +77,9 @@ def test_products_refuse():
         assert need > 0 and f(n=need - 1) == -5 and f(ws=0, n=0) == -5
         assert f(plan=P(tokens=0)) == 0 and lib.dfp4_experts_workspace_bytes(P(tokens=0), _weights_c(gated=gated)) == 0
     assert lib.dfp4_experts_workspace_bytes(P(experts=9), _weights_c()) == 0
+    # more tiles than a launch holds
+    big = dict(plan=P(tokens=1 << 26, k=2, experts=8), w=_weights_c(rows=1 << 14))
+    assert up(**big) == -2 and lib.dfp4_experts_workspace_bytes(*big.values()) == 0
     assert (up(x=0), up(h=0), up(x=8), up(h=8)) == (-1, -1, -3, -3)
     assert (down(h=0), down(y=0), down(weights=0), down(h=8), down(y=24), down(weights=2), down(dtype=3)) == (-1, -1, -1, -3, -3, -3, -4)
 
@@ -300,6 +303,7 @@ def test_down(tokens, k, experts, K, rows, more, dtype):
     n = int(plan.offsets[-1])
     mine = h.cuda()
     mine[n:] = float("nan")                          # (rows behind the last are not read)
+    mine[n::2] = float("-inf")
     y = dfp4.experts_down(mine, plan, layer.handle, weights.cuda(), dtype=dtype)
     check_down(h, ids, layer, experts, weights, y)
     wide = torch.full((tokens * k, K + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
