@@ -35,12 +35,12 @@ __device__ __forceinline__ double wave_sum(double v) {
 
 // Integers that order as the numbers do; 0 is below all, NaN 1
 __device__ __forceinline__ uint32_t key_of(float v) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);       // (zeros are alike)
     const uint32_t k = (b >> 31) ? ~b : b | 0x80000000u;
     return v == v ? k : 1u;
 }
 __device__ __forceinline__ uint64_t key_of(double v) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);
     const uint64_t k = (b >> 63) ? ~b : b | 0x8000000000000000ull;
     return v == v ? k : 1ull;
 }
@@ -108,6 +108,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (lane < a.groups) {
             double first = -__builtin_inf(), second = -__builtin_inf();
+#pragma unroll 4
             for (int i = 0; i < size; ++i) {
                 double c = s_score[wave][lane * size + i];
                 c = c == c ? c : -__builtin_inf();
@@ -180,6 +181,112 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     }
 }
 
+// The same where the order is the logits', without groups, up to 256 experts and 16 of them: a token has 16 lanes, PER experts in a row each, so that a wave
+// takes four and no scalar instruction is in a round.  bf16: a key has the logit above the expert's number, so that no two are alike.
+template <int PER, bool BF16>
+__global__ __launch_bounds__(kThreads) void route_logits_kernel(RouteArgs a) {
+    const int lane = threadIdx.x & 63, l = lane & 15;
+    const int64_t token = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    const bool on = token < a.tokens;
+    const int E = a.experts, first = l * PER;
+    uint32_t raw[PER];                                    // bits, bf16 in the upper half
+    {
+        constexpr int kEach = BF16 ? 2 : 4, kVec = PER * kEach < 16 ? PER * kEach : 16;
+        const uint8_t* row = static_cast<const uint8_t*>(a.logits) + ((on ? token : 0) * a.ld + first) * kEach;
+        if (first + PER <= E) {
+            // (rows may begin anywhere)
+            uint8_t bytes[PER * kEach];
+#pragma unroll
+            for (int i = 0; i < PER * kEach; i += kVec) __builtin_memcpy(bytes + i, row + i, kVec);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                if constexpr (BF16) {
+                    uint16_t v;
+                    __builtin_memcpy(&v, bytes + 2 * j, 2);
+                    raw[j] = (uint32_t)v << 16;
+                } else {
+                    __builtin_memcpy(&raw[j], bytes + 4 * j, 4);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                raw[j] = 0;
+                if (first + j < E) {
+                    if constexpr (BF16) raw[j] = (uint32_t)reinterpret_cast<const uint16_t*>(row)[j] << 16;
+                    else raw[j] = reinterpret_cast<const uint32_t*>(row)[j];
+                }
+            }
+        }
+    }
+    // keys; NaN is -infinity, +infinity (f32) the largest number
+    uint32_t key[PER];
+    float x[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        x[j] = as_f(raw[j]);
+        x[j] = x[j] == x[j] ? x[j] : -__builtin_inff();
+        if constexpr (!BF16) x[j] = fminf(x[j], 3.402823466e38f);
+        const uint32_t k = key_of(x[j]);
+        key[j] = first + j >= E ? 0 : BF16 ? (k & 0xffff0000u) | (uint32_t)(0xffff - (first + j)) : k;
+    }
+    auto value_of = [](uint32_t k) { return fminf(as_f((k >> 31) ? k & 0x7fffffffu : ~k), 3.402823466e38f); };
+    int chosen = 0;                                       // lane i of the 16: the i-th, and its logit
+    float logit = -__builtin_inff(), top = 0.0f;
+    for (int i = 0; i < a.k; ++i) {
+        uint32_t m = key[0];
+#pragma unroll
+        for (int j = 1; j < PER; ++j) m = max(m, key[j]);
+        m = max(m, across<0xB1>(m));
+        m = max(m, across<0x4E>(m));
+        m = max(m, across<0x141>(m));
+        m = max(m, across<0x140>(m));
+        int e;
+        float v;
+        if constexpr (BF16) {
+            e = 0xffff - (int)(m & 0xffffu);
+            // (the lower half of a negative number's key is ones)
+            v = value_of((m >> 31) ? m & 0xffff0000u : m | 0xffffu);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) key[j] = key[j] == m ? 0 : key[j];
+        } else {
+            uint32_t at = 0xffff;                         // the lowest of those that have it
+#pragma unroll
+            for (int j = PER - 1; j >= 0; --j) at = key[j] == m ? (uint32_t)(first + j) : at;
+            uint32_t low = at;
+            low = min(low, across<0xB1>(low));
+            low = min(low, across<0x4E>(low));
+            low = min(low, across<0x141>(low));
+            low = min(low, across<0x140>(low));
+            e = (int)low;
+            v = value_of(m);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) key[j] = (uint32_t)(first + j) == low ? 0 : key[j];
+        }
+        if (i == 0) top = v;
+        if (l == i) chosen = e, logit = v;
+    }
+    auto sum16 = [](double t) {
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) t += __shfl_xor(t, d);
+        return t;
+    };
+    double sum = 1.0;                                     // of softmax
+    auto score = [&](float v) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : top == -__builtin_inff() ? 0.0 : exp((double)v - (double)top) / sum; };
+    if (!a.sigmoid && !a.renormalize) {
+        double t = 0.0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) t += first + j < E ? score(fminf(x[j], 3.402823466e38f)) : 0.0;
+        t = sum16(t);
+        sum = t > 0.0 ? t : 1.0;
+    }
+    const double mine = l < a.k ? score(logit) : 0.0, total = a.renormalize ? sum16(mine) : 1.0;
+    if (on && l < a.k) {
+        a.ids[token * a.k + l] = chosen;
+        a.weights[token * a.k + l] = (float)(total > 0.0 ? mine / total * (double)a.scale : 0.0);
+    }
+}
+
 // ---- plan
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
@@ -195,6 +302,14 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});      // the last lane of 16 to the 16 after it, of 32 to the other 32
     add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
     return v;
+}
+
+// entries of one of the plan's lists, every `by`-th
+constexpr uint32_t kListSerial = 512;                               // rows of an expert up to which one thread writes them
+__device__ __forceinline__ void list_entries(PlanGroup* to, int list, int expert, uint32_t row0, uint32_t total, uint32_t group0, uint32_t from, uint32_t by) {
+    const uint32_t rows = list == 0 ? kListRows[0] : list == 1 ? kListRows[1] : kListRows[2], n = (total + rows - 1) / rows;
+    for (uint32_t g = from; g < n; g += by)
+        to[g] = PlanGroup{expert, (int32_t)(row0 + g * rows), (int32_t)min(total - g * rows, rows), (int32_t)(group0 * kGroupRows + g * rows)};
 }
 
 // A stable counting sort.  A workgroup takes a share of the pairs, 16 waves in turn; where there are several, a first kernel has counted each
@@ -215,7 +330,7 @@ __global__ __launch_bounds__(kPlanThreads) void expert_count_kernel(const int32_
 
 __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t* __restrict__ ids, PlanView v, int64_t pairs, int64_t share, int experts, int bits, int64_t most_blocks) {
     __shared__ uint32_t s_at[kPlanWaves][kMaxExperts];               // of a wave's pairs: how many, then the next row
-    __shared__ uint32_t s_row[kMaxExperts], s_group[kMaxExperts];
+    __shared__ uint32_t s_row[kMaxExperts], s_group[kMaxExperts], s_total[kMaxExperts], s_list[3][kMaxExperts];
     __shared__ uint4 s_sum[kPlanWaves];
     __shared__ uint32_t s_rows, s_blocks;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -259,6 +374,9 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
     }
     if (e < experts) {
         const uint32_t row0 = sum[0] - total, group0 = sum[1] - entries[0];
+        s_total[e] = total;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) s_list[q][e] = sum[q + 1] - entries[q];
         s_row[e] = row0;
         s_group[e] = group0;
         uint32_t at = row0 + before;
@@ -271,10 +389,7 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
             v.offsets[e] = (int32_t)row0;
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
-                constexpr auto& kRows = kListRows;
-                PlanGroup* to = v.list[q] + (sum[q + 1] - entries[q]);
-                for (uint32_t g = 0; g < entries[q]; ++g)
-                    to[g] = PlanGroup{e, (int32_t)(row0 + g * kRows[q]), (int32_t)min(total - g * kRows[q], (uint32_t)kRows[q]), (int32_t)(group0 * kGroupRows + g * kRows[q])};
+                if (total <= kListSerial) list_entries(v.list[q] + (sum[q + 1] - entries[q]), q, e, row0, total, group0, 0, 1);
                 if (e == experts - 1) v.used[q] = (int32_t)sum[q + 1];
             }
             if (e == experts - 1) v.offsets[experts] = (int32_t)sum[0];
@@ -282,6 +397,10 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
         if (e == experts - 1) s_rows = sum[0], s_blocks = sum[3];
     }
     __syncthreads();
+    // (experts of many rows: a wave each)
+    for (int x = (int)blockIdx.x + (int)gridDim.x * wave; x < experts; x += (int)gridDim.x * kPlanWaves)
+        if (s_total[x] > kListSerial)
+            for (int q = 0; q < 3; ++q) list_entries(v.list[q] + s_list[q][x], q, x, s_row[x], s_total[x], s_group[x], lane, 64);
     for (int64_t i4 = wlo; i4 < whi; i4 += 256) {
         uint32_t next[4];
 #pragma unroll
@@ -319,6 +438,19 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
 }  // namespace
 
 int launch_route(const RouteArgs& a, hipStream_t stream) {
+    if (!a.bias && a.groups == 1 && a.experts <= 256 && a.k <= 16) {
+        const dim3 by16((uint32_t)((a.tokens + kThreads / 16 - 1) / (kThreads / 16)));
+        auto run = [&](auto per) {
+            if (a.bf16) hipLaunchKernelGGL((route_logits_kernel<decltype(per)::value, true>), by16, dim3(kThreads), 0, stream, a);
+            else hipLaunchKernelGGL((route_logits_kernel<decltype(per)::value, false>), by16, dim3(kThreads), 0, stream, a);
+        };
+        if (a.experts <= 16) run(std::integral_constant<int, 1>{});
+        else if (a.experts <= 32) run(std::integral_constant<int, 2>{});
+        else if (a.experts <= 64) run(std::integral_constant<int, 4>{});
+        else if (a.experts <= 128) run(std::integral_constant<int, 8>{});
+        else run(std::integral_constant<int, 16>{});
+        return check_launch();
+    }
     const dim3 grid((uint32_t)((a.tokens + kWaves - 1) / kWaves)), block(kThreads);
     if (a.experts <= 64) hipLaunchKernelGGL((route_kernel<1>), grid, block, 0, stream, a);
     else if (a.experts <= 128) hipLaunchKernelGGL((route_kernel<2>), grid, block, 0, stream, a);

@@ -244,8 +244,27 @@ def test_route_of_masked_infinite_and_equal_logits(score):
         assert np.isfinite(got).all() and (np.abs(got - w) <= (2.0 ** -24 + 2.0 ** -40) * np.abs(w) + 2.0 ** -149).all()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("experts,k", [(8, 8), (16, 3), (100, 16), (256, 9), (300, 17)])
+def test_route_of_few_values(dtype, experts, k):
+    # zeros of both signs, equal numbers, infinities and NaN, in every position
+    g = torch.Generator().manual_seed(experts)
+    values = torch.tensor([0.0, -0.0, 1.0, -1.0, float("inf"), float("-inf"), float("nan"), 3.3895e38, -3.3895e38, 1e-40])
+    logits = values[torch.randint(0, len(values), (50, experts), generator=g)].to(dtype)
+    logits[:25][logits[:25].isinf()] = 0.5
+    for more in ({}, dict(score="sigmoid"), dict(renormalize=False), dict(groups=4, kept=3) if experts % 4 == 0 and 3 * experts >= 4 * k else {}):
+        ids, weights = dfp4.route(logits.cuda(), k, **more)
+        with np.errstate(all="ignore"):
+            want, w = plain_route(logits.float().numpy(), k, **more)
+        assert np.array_equal(ids.cpu().numpy(), want)
+        got = weights.cpu().double().numpy()
+        assert (np.abs(got - w) <= (2.0 ** -24 + 2.0 ** -40) * np.abs(w) + 2.0 ** -149).all()
+
+
 PLANS = [(1, 8, 128, {}), (1, 1, 1, {}), (0, 2, 4, {}), (37, 3, 5, {}), (300, 4, 9, dict(absent=0.3)), (50, 2, 4, dict(absent=1.0)), (1025, 8, 64, {}), (64, 6, 8, dict(twice=True)),
-         (700, 1, 1024, {}), (200, 32, 40, {}), (5000, 8, 16, dict(only=2)), (129, 2, 300, dict(absent=0.1, twice=True)), (3000, 7, 33, {})]
+         (700, 1, 1024, {}), (200, 32, 40, {}), (5000, 8, 16, dict(only=2)), (129, 2, 300, dict(absent=0.1, twice=True)), (3000, 7, 33, {}),
+         (4096, 1, 7, {}), (4097, 1, 7, dict(only=1)), (9000, 8, 12, dict(only=3, absent=0.01))]
 
 
 @gpu
