@@ -784,7 +784,7 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         for (int s = 1; s <= 16; s *= 2) {
             const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per);
             const float r = (float)n / (float)cus, rounds = (float)((n + cus - 1) / cus), stream = 0.115f * (float)(per * p.Q);
-            const float us = rounds * (tiles * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.5f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
+            const float us = rounds * (tiles * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.0f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
             if (s == 1 || us < least) least = us, split = s;
         }
         const int64_t items = p.blocks * ((p.tiles + 16 / split - 1) / (16 / split));
