@@ -102,9 +102,7 @@ struct QuantizeArgs {
 
 // Rows quantized in the plan's order (the arithmetic of the quantizer, quant_pass.h; as quantize_native_kernel, but for the rows' places).
 // A wave takes 8 rows x 8 blocks; what is behind the last row is left as it is: it is multiplied, and its results are not kept.
-// 32768 rows (of 4096 tokens) x 2048 28.6 us, bound by the quantizer's arithmetic; 32768 x 1024 26.7, by memory (3.5 TB/s).  Tried for tokens of several
-// experts: each quantized once and written to its places (57 us: 16 bytes here and there), or once to 4 bits (8.5) and from these to all places in whole lines
-// (23.5); and scale bytes through LDS, so that they leave as whole lines (31.8 instead of 26.7).
+// 32768 rows x 1024 26.7 us, by memory (3.5 TB/s).  Tried: scale bytes through LDS, so that they leave as whole lines (31.8).
 constexpr int kQThreads = 256, kQWaves = kQThreads / 64, kPasses = 4;
 __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArgs p) {
     __shared__ __attribute__((aligned(16))) uint8_t lds_q[kDialects * 32];
@@ -156,6 +154,62 @@ __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArg
             if (store && sub == 2)
                 *reinterpret_cast<uint2*>(p.to.bits + fp6_hi(tile, step, p.S) + fp6_hi_lane(slot) * 8u) =
                     on[q] ? make_uint2(hi16 | (next_lo << 16), next_mid) : make_uint2(0, 0);
+        }
+    }
+}
+
+struct GatherArgs {
+    const uint8_t *codes, *dial, *expo;          // quantized tokens
+    const int32_t *used, *order;
+    const PlanGroup* halves;
+    Packed to;
+    int64_t most;                                // halves, at most
+    uint32_t k;
+    int KB, S;
+};
+
+// Quantized tokens rewritten in operand order for each of their experts, in whole lines.  A wave takes 128 rows and two steps; lane (kh, c) row c of
+// each of four tiles, block 2 step + kh.  With the quantizer before it (8.5 us) 4096 tokens of 2048, 8 experts each, take 33 us; quantizing every row
+// 45.7, bound by the quantizer's arithmetic; a token once, written to its places, 57 (16 bytes here and there).
+__global__ __launch_bounds__(256) void experts_gather_kernel(GatherArgs p) {
+    __shared__ uint2 s_fp6[kDialects];
+    if (threadIdx.x < kDialects) s_fp6[threadIdx.x] = make_uint2(g_fp6_book.w[threadIdx.x][0], g_fp6_book.w[threadIdx.x][1]);
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kh = lane >> 5, c = lane & 31;
+    const int steps8 = (p.S + 7) / 8;
+    const int64_t units = min((int64_t)*p.used, p.most) * steps8;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int64_t half = u / steps8;
+        const int s0 = (int)(u - half * steps8) * 8 + wave * 2;
+        const PlanGroup g = p.halves[half];
+        if (s0 >= p.S) continue;
+        uint4 codes[4][2];
+        uint32_t e[4], d[4];                     // of four blocks: both steps', both lanes'
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t row = (int64_t)((uint32_t)p.order[g.row0 + min(t * 32 + c, g.rows - 1)] / p.k) * p.KB;
+            __builtin_memcpy(&e[t], p.expo + row + 2 * s0, 4);               // (behind the last block: another row's, not used; the workspace has room)
+            __builtin_memcpy(&d[t], p.dial + row + 2 * s0, 4);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) codes[t][q] = *reinterpret_cast<const uint4*>(p.codes + (row + min(2 * (s0 + q) + kh, p.KB - 1)) * 16);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int s = s0 + q, at = 8 * (2 * q + kh);
+            if (s >= p.S) break;
+            const bool on = 2 * s + kh < p.KB;
+            uint32_t scale = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (t * 32 >= g.rows) break;
+                const size_t tile = (size_t)(g.at >> 5) + t;
+                const uint2 tab = s_fp6[(d[t] >> at) & 15u];
+                const Fp6Lane v = pack6_lane(on ? codes[t][q] : make_uint4(0, 0, 0, 0), tab.x, tab.y);
+                *reinterpret_cast<uint4*>(p.to.bits + fp6_lo(tile, s, p.S) + lane * 16) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+                *reinterpret_cast<uint2*>(p.to.bits + fp6_hi(tile, s, p.S) + fp6_hi_lane(lane) * 8) = make_uint2(v.w[4], v.w[5]);
+                scale |= (on ? (e[t] >> at) & 255u : 0) << (8 * t);
+            }
+            *reinterpret_cast<uint32_t*>(p.to.scales + ((size_t)(g.at >> 7) * p.S + s) * 256 + lane * 4) = scale;
         }
     }
 }
@@ -657,7 +711,7 @@ inline bool token_by_token(const dfp4_plan& plan, const dfp4_experts& w) {
 // workspace: rows in operand order, or in their 4-bit form (few), and down their products
 struct Workspace {
     bool many;
-    int64_t rows, dial, expo, part, total;
+    int64_t rows, codes, dial, expo, part, total;
 };
 inline Workspace workspace_of(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t pairs = plan.tokens * plan.k;
@@ -666,6 +720,14 @@ inline Workspace workspace_of(const dfp4_plan& plan, const dfp4_experts& w) {
     if (x.many) {
         x.rows = plan_list(pairs, plan.experts, 0) * kGroupRows;
         x.part = up256((int64_t)native_packed_bytes(x.rows, w.K, true));
+        // Quantized once a token where that spares more than the launch that it adds: 333 tokens of 5 experts, 1440 elements each, 28.0 us instead of 23.6
+        // (all of up), 4096 of 8, 2048 each, 158 instead of 167
+        if (w.gated && plan.k > 1 && pairs * w.K >= 1 << 25) {
+            x.codes = x.part;
+            x.dial = x.codes + up256(plan.tokens * (w.K / 2));
+            x.expo = x.dial + up256(plan.tokens * (w.K / kBlock) + 4);
+            x.part = x.expo + up256(plan.tokens * (w.K / kBlock) + 4);
+        }
     } else {
         x.rows = w.gated ? plan.tokens : pairs;
         x.dial = up256(x.rows * (w.K / 2));
@@ -742,8 +804,18 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         q.to = packed_at(a.workspace, ws.rows, a.w.K);
         q.k = a.w.gated ? (uint32_t)a.plan.k : 0, q.KB = (uint32_t)(a.w.K / kBlock), q.S = (uint32_t)S;
         q.bound = pairs;
-        const int64_t units = (pairs + 7) / 8 * ((S + 3) / 4), want = (units + kQWaves - 1) / kQWaves;
-        hipLaunchKernelGGL(experts_quantize_kernel, dim3((unsigned)(want < 8 * cus ? want : 8 * cus)), dim3(kQThreads), 0, stream, q);
+        if (ws.codes) {
+            const dfp4_tensor x{a.workspace + ws.codes, a.workspace + ws.dial, a.workspace + ws.expo, a.plan.tokens, a.w.K};
+            const int rc = launch_quantize(false, a.x, a.plan.tokens, a.w.K, a.ld, x, stream);
+            if (rc != DFP4_OK) return rc;
+            const GatherArgs g{x.codes, x.dialect, x.exponent, plan.used + 1, plan.order, plan.list[1], q.to, plan_list(pairs, a.plan.experts, 1),
+                               (uint32_t)a.plan.k, (int)q.KB, (int)S};
+            const int64_t wgs = g.most * ((S + 7) / 8);
+            hipLaunchKernelGGL(experts_gather_kernel, dim3((unsigned)(wgs < 16 * cus ? wgs : 16 * cus)), dim3(256), 0, stream, g);
+        } else {
+            const int64_t units = (pairs + 7) / 8 * ((S + 3) / 4), want = (units + kQWaves - 1) / kQWaves;
+            hipLaunchKernelGGL(experts_quantize_kernel, dim3((unsigned)(want < 8 * cus ? want : 8 * cus)), dim3(kQThreads), 0, stream, q);
+        }
         ExpertTiles t{};
         t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
         t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);

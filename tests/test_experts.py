@@ -334,6 +334,29 @@ def test_down(tokens, k, experts, K, rows, more, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("tokens,k,experts,K,absent", [(2100, 4, 5, 4000, 0.0), (1500, 3, 4, 8224, 0.3), (4200, 8, 7, 1056, 0.0)])
+def test_up_of_tokens_quantized_once(tokens, k, experts, K, absent):
+    """Long rows of several experts (tokens * k * K from 2^25 on): the rows of a token are alike, and those of its neighbours in a smaller call."""
+    layer = Layer(experts, 40, K, True, seed=K)
+    x = torch.randn(tokens, K, generator=torch.Generator().manual_seed(1)).bfloat16()
+    ids = ids_of(tokens, min(k, experts), experts, seed=2, absent=absent)
+    k = ids.shape[1]
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    wide = torch.zeros(tokens, K + 8, dtype=torch.bfloat16, device="cuda")
+    wide[:, :K] = x.cuda()
+    h = dfp4.experts_up(wide[:, :K], plan, layer.handle)
+    assert torch.equal(h[:int(plan.offsets[-1])], dfp4.experts_up(x.cuda(), plan, layer.handle)[:int(plan.offsets[-1])])
+    # a few tokens from everywhere against the plain form
+    some = torch.linspace(0, tokens - 1, 33).long()
+    few = dfp4.expert_plan(ids[some].contiguous().cuda(), experts)
+    rows = plan.place.cpu().view(tokens, k)[some].flatten()
+    mine = torch.zeros(33 * k, 40, dtype=torch.bfloat16)
+    there = rows >= 0
+    mine[few.place.cpu()[there].long()] = h.cpu()[rows[there].long()]
+    check_up(x[some], ids[some], layer, experts, mine)
+
+
+@gpu
 def test_products_of_no_tokens():
     up, down = Layer(4, 64, 64, True), Layer(4, 64, 64, False)
     plan = dfp4.expert_plan(torch.zeros(0, 2, dtype=torch.int32, device="cuda"), 4)
