@@ -464,7 +464,7 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
                    int interleaved, void* q_out, void* k_out, void* stream);
 
 /*
- * A sparse layer: every token goes to k of `experts` feed-forward networks whose weights are quantized.
+ * A sparse layer: every token goes to k of `experts` feed-forward networks whose weights are quantized (blocks along the contraction, Appendix C).
  *
  * Router.  Scores of a token's experts, s = softmax(logits) or 1 / (1 + exp(-logits)); the choice is by c = s + bias.  Where there are
  * groups (expert e in group e / (experts / groups)), the `kept` groups with the largest sums of their `best` largest c stay, the others'

@@ -1,7 +1,8 @@
 // Norms before and after a block with its gate and the residual, in one pass (formulas in include/dfp4.h).
 //
 // Bound by memory: 8 bytes an element (bf16 residual, no gate).  A row stays in registers between the two sums: eight elements a lane and
-// pass, a workgroup (or, up to 512 elements, a wave) a row.
+// pass, a workgroup (or, up to 512 elements, a wave) a row.  8192 x 4096 (268 MB) 51 us = 5.2 TB/s, what a large copy reaches; the kernel alone 40, its
+// outputs then in the last cache.
 #include "experts.h"
 
 namespace dfp4 {

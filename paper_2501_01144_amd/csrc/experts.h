@@ -85,8 +85,8 @@ struct AddNormArgs {
     bool wide;               // the residual in f32
 };
 
-// silu(g) * u by the hardware's exponential and reciprocal (1 ulp each; the exponent's rounding is 2^-24 |g| / ln 2): six instructions.  What
-// the compiler makes of __expf and a division costs the gated epilogue of a 256 x 256 tile XX us more.
+// silu(g) * u by the hardware's exponential and reciprocal (1 ulp each; the rounding of the exponent is 2^-23 |g| of the result for negative g,
+// far below a rounding to bf16): six instructions, where a division in full would take ten more, in an epilogue that nothing runs beside.
 __device__ __forceinline__ float silu_times(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)) * u;
 }

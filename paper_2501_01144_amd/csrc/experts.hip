@@ -1,10 +1,16 @@
 // Products of a sparse layer's experts on the block-scaled matrix instruction (include/dfp4.h; operand layout: fp6_pack.h, gemm_native.hip).
 //
-// Rows (pairs of a token and an expert) come in the plan's order, an expert's from a group of kGroupRows on, so that every tile of rows
-// has one expert.  experts_quantize_kernel quantizes rows straight into operand order, experts_kernel multiplies a tile of 32 rows with 32
-// rows of its expert's weights; down, experts_join_kernel adds a token's rows in a fixed order.
-// Gate and up rows take turns in the packed weights, and weights are the instruction's first operand, rows its second: a lane then holds
-// both numbers that an element of h is made of.
+// Rows (pairs of a token and an expert) come in the plan's order.  Three ways, by how many an expert has (rules at kFewRows, token_by_token):
+//   many   rows are quantized to FP6 in operand order, an expert's from a group of kGroupRows on, so that every tile has one expert
+//          (experts_quantize_kernel, experts_gather_kernel), and the large block-scaled kernel takes tiles of 256 or 128 of them with the
+//          weights' FP6 form (gemm_native.hip, kExperts, kGated).  Bound by the tiles' operands on their way to the compute units and by what
+//          stands before and after a tile's loop (the matrix instructions are busy 32 % of the time).
+//   few    experts_few_kernel streams the weights' 4-bit form past rows that lie in LDS.  Bound by that stream.
+//   a few tokens, down   experts_token_kernel, one launch.
+// The weights' two forms cost memory (0.79 + 0.56 bytes an element) and spare either way a pass over them.
+// Gate and up rows take turns in both: a lane then holds both numbers that an element of h is made of (few: weights are the instruction's
+// first operand, rows its second).  Down, rows leave weighted by nothing, in the type of y where there are many (bf16: 1.4 times the error of its rounding)
+// and in fp32 else, and experts_join_kernel adds a token's in their order: no sum depends on when a workgroup runs.
 #include <math.h>
 #include <type_traits>
 #include "experts.h"
@@ -285,7 +291,10 @@ __device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, u
 
 // A workgroup keeps the rows of a block (MT 1: up to 32, 2: up to 64) in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
 // packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
-// Bound by the weights' stream (0.5625 bytes an element).
+// Bound by the weights' stream (0.5625 bytes an element): 64 tokens of 2 of 8 experts, 4096 x 14336 up, 104 to 109 us = 5.0 TB/s, a large copy's rate; with
+// blocks of more than 32 rows among them, whose K takes two turns in LDS, 125.  Registers: 2 to 28 bytes of a thread's in scratch memory with two tiles of
+// rows.  Tried: FP6 weights (a third more bytes); loads that move nothing behind a wave's last quad (buffer descriptors: no faster for one token, and
+// the registers they take made two tiles of rows 5 to 20 % slower).
 template <bool GATED, int MT, int SPLIT>
 __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     constexpr int kQuads = 32, kTiles = 16 / SPLIT, kAhead = 4;       // quads of 32 rows in LDS; tiles at a time
@@ -535,7 +544,7 @@ constexpr int kTokenElements = 48 << 10;         // of a token's rows, in LDS
 
 // A workgroup a token and 32 results: its 16 waves share the quads of all the token's experts (a wave's are neighbours, of one or a few
 // experts), add them with the router's weights and join in the order of the waves.  Rows are quantized by every workgroup anew, on their way
-// to LDS, while the first weights come.  Bound by latency: loads of the plan, rows and weights in turn.
+// to LDS, while the first weights come.  Bound by latency: one token of 8 of 128 experts, 2048 x 1024, 8.5 us, of which 5.7 are what an empty call takes.
 template <bool BF16>
 __global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
     constexpr int kAhead = 4;

@@ -1,6 +1,8 @@
 """Operators of a sparse layer: the router, the plan of the experts' products, the products, the norms around a block, each against a
 plain implementation in float64 (the quantizer: the oracle)."""
 import ctypes
+import importlib.util
+import os
 
 import numpy as np
 import pytest
@@ -427,6 +429,38 @@ def test_add_norm_of_numbers_whose_squares_leave_fp32(size, dim):
 
 
 # ---- together ----------------------------------------------------------------------------------------------------------------
+
+@gpu
+def test_the_example_runs():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "sparse_layer.py")
+    spec = importlib.util.spec_from_file_location("sparse_layer", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    off, _ = module.run(tokens=40, hidden=256, inner=96, experts=8, k=2, steps=4)
+    # bf16 results: HALF of every element at most, twice where rows are rounded before they are added; fp32 sums besides
+    assert off <= 2 * HALF + 2.0 ** -12
+
+
+@gpu
+def test_calls_from_python_refuse():
+    layer = Layer(4, 64, 64, True)
+    x, ids = torch.zeros(6, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(6, 2, dtype=torch.int32, device="cuda")
+    plan = dfp4.expert_plan(ids, 4)
+    for bad in (lambda: dfp4.expert_plan(ids.long(), 4), lambda: dfp4.expert_plan(ids[:, ::2], 4), lambda: dfp4.experts_up(x[:5], plan, layer.handle),
+                lambda: dfp4.experts_up(x.float(), plan, layer.handle), lambda: dfp4.experts_up(x[:, :32], plan, layer.handle), lambda: dfp4.route(x[0].float(), 2),
+                lambda: dfp4.route(x.half(), 2), lambda: dfp4.route(x, 2, bias=x[0]), lambda: dfp4.route(x, 2, score="other"),
+                lambda: dfp4.add_norm(x, x[:, :32], torch.ones(64, device="cuda")), lambda: dfp4.add_norm(x, x, torch.ones(32, device="cuda")),
+                lambda: dfp4.add_norm(x, x, torch.ones(64, device="cuda"), gate=x[:3]), lambda: dfp4.expert_weights(dfp4.empty_qtensor(10, 64, x.device), 4),
+                lambda: dfp4.experts_down(x, plan, layer.handle, torch.zeros(6, 2, device="cuda"))):
+        with pytest.raises(AssertionError):
+            bad()
+    h = torch.zeros(12, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (lambda: dfp4.experts_down(h, plan, layer.handle, torch.zeros(6, 2, device="cuda")), lambda: dfp4.experts_up(x, dfp4.expert_plan(ids, 5), layer.handle),
+                lambda: dfp4.route(x.float(), 65), lambda: dfp4.route(x.float(), 0), lambda: dfp4.expert_plan(ids, 2000), lambda: dfp4.route(x.float(), 4, groups=5),
+                lambda: dfp4.add_norm(x[:, 4:], x[:, 4:], torch.ones(60, device="cuda")), lambda: dfp4.expert_weights(dfp4.empty_qtensor(16, 64, x.device, mx=True), 4)):
+        with pytest.raises(dfp4.Dfp4Error):
+            bad()
+
 
 @gpu
 @pytest.mark.parametrize("tokens", [1, 16, 700])
