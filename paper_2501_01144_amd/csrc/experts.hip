@@ -289,12 +289,27 @@ __device__ __forceinline__ void expand8(uint32_t c, uint2 tab, uint32_t& even, u
     odd = __builtin_amdgcn_perm(tab.y, tab.x, (c >> 4) & 0x07070707u) | (c & 0x80808080u);
 }
 
+// A quad of weights of a lane.  Loads go through a buffer's descriptor, made anew for each, that has no records for a quad behind the wave's last: such a
+// load moves nothing.  (A load behind a branch would be waited for together with all others.)
+struct Quad {
+    uint4 c[2];
+    uint32_t meta;
+};
+__device__ __forceinline__ void load_quad(Quad& q, const uint8_t* at, bool there, int lane) {
+    typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+    const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(at), 0, there ? kQuadBytes : 0, 0x00027000);
+#pragma unroll
+    for (int step = 0; step < 2; ++step)
+        q.c[step] = __builtin_bit_cast(uint4, (v4u)__builtin_amdgcn_raw_buffer_load_b128(from, lane * 16 + step * 1024, 0, 0));
+    q.meta = __builtin_amdgcn_raw_buffer_load_b32(from, lane * 4 + 2048, 0, 0);
+}
+
 // A workgroup keeps the rows of a block (MT 1: up to 32, 2: up to 64) in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
 // packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
 // Bound by the weights' stream (0.5625 bytes an element): 64 tokens of 2 of 8 experts, 4096 x 14336 up, 104 to 109 us = 5.0 TB/s, a large copy's rate; with
-// blocks of more than 32 rows among them, whose K takes two turns in LDS, 125.  Registers: 2 to 28 bytes of a thread's in scratch memory with two tiles of
-// rows.  Tried: FP6 weights (a third more bytes); loads that move nothing behind a wave's last quad (buffer descriptors: no faster for one token, and
-// the registers they take made two tiles of rows 5 to 20 % slower).
+// blocks of more than 32 rows among them, whose K takes two turns in LDS, 121 to 125.  Registers: 8 to 32 bytes of a thread's in scratch memory with two
+// tiles of rows.  Tried: FP6 weights (a third more bytes); the last quad loaded again where there is none (whole K in a wave 7 % slower over 300 drawn
+// products); offsets of quads in vector registers (two tiles of rows 5 to 20 % slower).
 template <bool GATED, int MT, int SPLIT>
 __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     constexpr int kQuads = 32, kTiles = 16 / SPLIT, kAhead = 4;       // quads of 32 rows in LDS; tiles at a time
@@ -335,7 +350,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     auto after = [&](const At& a) {
         At n = a;
         if (!last_chunk_of(a)) ++n.chunk;
-        else if (a.item + 1 < hi) n = begin(a.item + 1);             // (behind the last: loaded once more, not used)
+        else if (a.item + 1 < hi) n = begin(a.item + 1);
         return n;
     };
     // its quads there: the first one's address and their number
@@ -344,20 +359,12 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
         int first, n;
     };
     auto segment = [&](const At& a) {
-        const int chunk = kQuads / a.tiles, in = min(chunk, p.Q - a.chunk * chunk), per = (in + SPLIT - 1) / SPLIT, first = part * per, n = max(0, min(in, first + per) - first);
-        const int tile = min(a.batch * kTiles + sub, p.tiles - 1);
-        return Segment{p.quads + (((int64_t)a.g.expert * p.tiles + tile) * p.Q + a.chunk * chunk + (n > 0 ? first : 0)) * kQuadBytes, first, n};
+        const int chunk = kQuads / a.tiles, in = min(chunk, p.Q - a.chunk * chunk), per = (in + SPLIT - 1) / SPLIT, first = part * per;
+        const int tile = a.batch * kTiles + sub, n = tile < p.tiles ? max(0, min(in, first + per) - first) : 0;
+        return Segment{p.quads + (((int64_t)a.g.expert * p.tiles + tile) * p.Q + a.chunk * chunk + first) * kQuadBytes, first, n};
     };
-    struct Quad {
-        uint4 c[2];
-        uint32_t meta;
-    } ring[kAhead];
-    auto load = [&](Quad& q, const Segment& s, int i) {
-        const uint8_t* at = s.at + (int64_t)max(0, min(i, s.n - 1)) * kQuadBytes;
-        q.c[0] = *reinterpret_cast<const uint4*>(at + lane * 16);
-        q.c[1] = *reinterpret_cast<const uint4*>(at + 1024 + lane * 16);
-        q.meta = *reinterpret_cast<const uint32_t*>(at + 2048 + lane * 4);
-    };
+    Quad ring[kAhead];
+    auto load = [&](Quad& q, const Segment& s, int i) { load_quad(q, s.at + (int64_t)i * kQuadBytes, i < s.n, lane); };
     v16f acc[MT];
     auto clear = [&] {
 #pragma unroll
@@ -476,7 +483,8 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             staged_block = now.block, staged_chunk = now.chunk;
         }
         const At then = after(now);
-        const Segment next = segment(then);
+        Segment next = segment(then);
+        if (last) next.n = 0;
         if (seg.n == 0) {
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) load(ring[d], next, d);
@@ -571,20 +579,13 @@ __global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
     }
     __syncthreads();
     const int units = p.k * p.Q, lo = units * wave / 16, hi = units * (wave + 1) / 16;
-    struct Quad {
-        uint4 c[2];
-        uint32_t meta;
-    } ring[kAhead];
+    Quad ring[kAhead];
     auto load = [&](Quad& q, int u) {
-        u = min(max(u, 0), units - 1);
-        const int j = u / p.Q, expert = __builtin_amdgcn_readfirstlane(s_expert[j]);
-        const uint8_t* at = p.quads + (((int64_t)expert * p.tiles + tile) * p.Q + (u - j * p.Q)) * kQuadBytes;
-        q.c[0] = *reinterpret_cast<const uint4*>(at + lane * 16);
-        q.c[1] = *reinterpret_cast<const uint4*>(at + 1024 + lane * 16);
-        q.meta = *reinterpret_cast<const uint32_t*>(at + 2048 + lane * 4);
+        const int j = min(u, units - 1) / p.Q, expert = __builtin_amdgcn_readfirstlane(s_expert[j]);
+        load_quad(q, p.quads + (((int64_t)expert * p.tiles + tile) * p.Q + (u - j * p.Q)) * kQuadBytes, u < hi, lane);
     };
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) load(ring[d], min(lo + d, hi - 1));
+    for (int d = 0; d < kAhead; ++d) load(ring[d], lo + d);
     const int blocks = p.Q * 4;
     uint8_t* s_scale = s_rows + (size_t)p.k * p.Q * 128;
     for (int i = tid; i < p.k * blocks * 4; i += 1024) {
@@ -634,7 +635,7 @@ __global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
                     asm volatile("" : "+v"(acc) : "v"(wv), "v"(xv));       // (as above)
                 }
             }
-            load(ring[d], min(u + kAhead, hi - 1));
+            load(ring[d], u + kAhead);
         }
     }
     if (hi > lo) {
@@ -707,8 +708,13 @@ inline int64_t active_experts(const dfp4_plan& plan) {
 // Rows an expert up to which weights are streamed past them; both sides, us, few / many: 20 rows 28 / 35, 32 rows (up) 134 / 157, 83 / 92, 35 / 36,
 // 15.3 / 14.0, (down) 84 / 112, 54 / 53, 29 / 29, 42 rows 33 / 28, 48 rows 147 / 159 and 61 / 49, 50 rows 117 / 98 and 89 / 57
 constexpr int64_t kFewRows = 34;
-// ... and up to which the large kernel takes 128 rows at a time instead of 256: 42 rows 28 / 33, 128 rows 88 / 91 and 126 / 143, 250 rows 76 / 63, 117 / 107
-constexpr int64_t kHalfRows = 160;
+// Whether the large kernel takes 128 rows at a time instead of 256: where an expert has no more than 160 (half / whole: 42 rows 28 / 33 us, 128 rows 88 / 91 and
+// 126 / 143, 250 rows 76 / 63, 117 / 107), or tiles of 256 would leave half of the compute units idle (325 rows, 4 columns of tiles, 27.6 / 33.7).  Of 81
+// drawn products the better one is missed by 0.7 % in the mean.
+inline bool half_tiles(const dfp4_plan& plan, const dfp4_experts& w) {
+    const int64_t active = active_experts(plan), rows = plan.tokens * plan.k / active;
+    return rows <= 160 || active * ((rows + 255) / 256) * (padded_rows(w) / 256) * 2 <= device_cu_count();
+}
 // Whether tokens are taken one by one (down): where there are few, and weights that several of them read, again for each, cost less than the two
 // launches that are spared (4 us): 4 tokens of 8 of 128 experts 11.9 us instead of 17.5, 8 tokens 21.7 and 22.5, 16 tokens 40 and 30
 inline bool token_by_token(const dfp4_plan& plan, const dfp4_experts& w) {
@@ -772,7 +778,7 @@ int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& 
 // Whether one launch holds the tiles of a product of many rows (fewer than 2^32 threads)
 bool experts_fit(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t pairs = plan.tokens * plan.k;
-    return !workspace_of(plan, w).many || plan_list(pairs, plan.experts, pairs <= kHalfRows * active_experts(plan) ? 1 : 0) * (padded_rows(w) / 256) < (1 << 24) - 8;
+    return !workspace_of(plan, w).many || plan_list(pairs, plan.experts, half_tiles(plan, w) ? 1 : 0) * (padded_rows(w) / 256) < (1 << 24) - 8;
 }
 
 size_t experts_workspace_bytes(const dfp4_plan& plan, const dfp4_experts& w) { return (size_t)workspace_of(plan, w).total; }
@@ -828,7 +834,7 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         ExpertTiles t{};
         t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
         t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);
-        t.half = pairs <= kHalfRows * active_experts(a.plan);
+        t.half = half_tiles(a.plan, a.w);
         t.used = plan.used + (t.half ? 1 : 0), t.list = plan.list[t.half ? 1 : 0], t.most = plan_list(pairs, a.plan.experts, t.half ? 1 : 0);
         t.K = (int)a.w.K, t.rows = (int)expert_rows(a.w), t.tiles = (int)(padded_rows(a.w) / 256);
         t.gated = a.w.gated != 0;
@@ -841,7 +847,7 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         FewArgs p{};
         // Quantized by the workgroups that take them where that is little work: a launch less (2.5 us), but 1.1 us a workgroup and 8192 elements
         // (16 rows of 4096: 112 us instead of 107)
-        if (pairs * a.w.K <= active * 16384) {
+        if (pairs * a.w.K <= active * 12288) {
             p.x = a.x, p.ld = a.ld;
         } else {
             const CodesArgs c{a.x, a.ld, a.w.gated ? nullptr : plan.offsets + a.plan.experts, reinterpret_cast<uint32_t*>(x.codes), x.dialect, x.exponent, ws.rows,
@@ -856,16 +862,17 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         p.k = a.w.gated ? (uint32_t)a.plan.k : 0, p.single = a.plan.tokens == 1;
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
         const int mt = pairs > 32 ? 2 : 1;                           // rows of a block, at most
-        // How many waves share K: rounds of items over the compute units, each with what it streams (20 bytes a ns) and what a sum over waves, or
-        // rows that come to LDS in several chunks, take; constants by measurement (us).  From 10 rows an expert on some will have more than 32:
-        // 8 experts, 4096 x 14336 up, 2 waves / 4: 10 rows each 110 / 104, one of 35 among them 125 / 147.
-        const int tiles = pairs > 10 * active ? 2 : 1, chunks = (p.Q * tiles + 31) / 32;
+        // How many waves share K, by rounds of items over the compute units: a wave takes 1.08 us for a quad (the chip's memory among its waves), an item 2 us
+        // more, a sum over waves 1.5 to 2.9 for 32 rows, K in turns 2.5 a turn.  Of 234 drawn products the best of the five is missed by 2.2 % in the mean
+        // (always two: 12 %).  From 10 rows an expert on, some have more than 32.
+        const int two = pairs > 10 * active ? 2 : 1, turns = (p.Q * two + 31) / 32;
         int split = 1;
         float least = 0.0f;
         for (int s = 1; s <= 16; s *= 2) {
-            const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per);
-            const float r = (float)n / (float)cus, rounds = (float)((n + cus - 1) / cus), stream = 0.115f * (float)(per * p.Q);
-            const float us = rounds * (tiles * (s == 1 ? 0.1f : s == 16 ? 1.4f : s == 8 ? 0.65f : 0.45f) + (chunks > 1 ? 2.0f * chunks : 0.0f)) + (0.5f * (r + rounds) + 0.4f) * stream;
+            const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per), rounds = (n + cus - 1) / cus;
+            const int chunk = p.Q < 32 / two ? p.Q : 32 / two, quads = turns * ((chunk + s - 1) / s);
+            const float sum = s == 1 ? 0.0f : s == 16 ? 2.85f : s == 8 ? 2.0f : 1.47f;
+            const float us = (float)rounds * (1.08f * (float)quads + 2.0f + (float)two * (sum + (turns > 1 ? 2.46f * (float)turns : 0.0f)));
             if (s == 1 || us < least) least = us, split = s;
         }
         const int64_t items = p.blocks * ((p.tiles + 16 / split - 1) / (16 / split));
