@@ -352,8 +352,8 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
             fail(PyExc_AssertionError, "logits: f32 or bf16 [tokens, experts] on the device, contiguous along the experts");
         const int64_t tokens = x.size(0), experts = x.size(1), k = number(a[1]);
         const float* bias = numbers<float>(a[3], at::kFloat, experts, "bias: contiguous f32 [experts] on the device");
-        if (k < 0) fail(PyExc_AssertionError, "k: a positive number");
-        at::Tensor ids = empty({tokens, k}, at::kInt, x.device()), weights = result({tokens, k}, false, x.device());
+        const int64_t cols = k >= 1 && k <= experts ? k : 0;              // (others are refused)
+        at::Tensor ids = empty({tokens, cols}, at::kInt, x.device()), weights = result({tokens, cols}, false, x.device());
         enqueue("dfp4_route", p_dfp4_route, data(x), dtype(bf16), tokens > 1 ? x.stride(0) : experts, tokens, experts, k, a[2] == Py_True ? DFP4_SIGMOID : DFP4_SOFTMAX, bias,
                 number(a[4]), number(a[5]), number(a[6]), a[7] == Py_True ? 1 : 0, (float)real(a[8]), reinterpret_cast<int32_t*>(data(ids)),
                 reinterpret_cast<float*>(data(weights)), stream());

@@ -18,8 +18,8 @@ struct PlanGroup {
 // Three lists of them: groups, halves of 128 rows and, for products of few rows, blocks of 64; only what has rows
 constexpr int kListRows[3] = {kGroupRows, 128, 64};
 __host__ __device__ inline int64_t plan_list(int64_t pairs, int64_t experts, int list) { return pairs / kListRows[list] + (pairs < experts ? pairs : experts); }
-// The plan is made by up to 64 workgroups of shares of the pairs, each a multiple of 1024: one up to 4096 pairs
-inline int64_t plan_share(int64_t pairs) { return pairs <= 4096 ? 4096 : ((pairs + 63) / 64 + 1023) / 1024 * 1024; }
+// The plan is made by up to 64 workgroups of shares of the pairs, each a multiple of 1024: one up to 2048 pairs
+inline int64_t plan_share(int64_t pairs) { return pairs <= 2048 ? 2048 : ((pairs + 63) / 64 + 1023) / 1024 * 1024; }
 inline int64_t plan_shares(int64_t pairs) { return pairs <= 0 ? 1 : (pairs + plan_share(pairs) - 1) / plan_share(pairs); }
 // Arrays of a plan, one after the other (the first three are public)
 struct PlanView {

@@ -305,6 +305,8 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     return v;
 }
 
+constexpr int64_t kRecount = 16384;                                 // pairs up to which every workgroup counts all, which spares a launch
+
 // entries of one of the plan's lists, every `by`-th
 constexpr uint32_t kListSerial = 512;                               // rows of an expert up to which one thread writes them
 __device__ __forceinline__ void list_entries(PlanGroup* to, int list, int expert, uint32_t row0, uint32_t total, uint32_t group0, uint32_t from, uint32_t by) {
@@ -314,8 +316,8 @@ __device__ __forceinline__ void list_entries(PlanGroup* to, int list, int expert
 }
 
 // A stable counting sort, bound by latency: 131072 pairs of 256 experts 2.9 + 10.2 us (a workgroup an expert, each looking at all ids: 76); a few pairs
-// 3 to 5.  A workgroup takes a share of the pairs, 16 waves in turn; where there are several, a first kernel has counted each
-// share's experts.  Every workgroup knows all counts then, and with them each expert's first row and its entries of the lists; a wave ranks its pairs 64 at
+// 3 to 5.  A workgroup takes a share of the pairs, 16 waves in turn; where there are several, each counts all pairs, or a first
+// kernel has counted each share's experts.  Every workgroup knows all counts then, and with them each expert's first row and its entries of the lists; a wave ranks its pairs 64 at
 // a time by comparing bits of their experts.
 __global__ __launch_bounds__(kPlanThreads) void expert_count_kernel(const int32_t* __restrict__ ids, int32_t* counts, int64_t pairs, int64_t share, int experts) {
     __shared__ int32_t s_count[kMaxExperts];
@@ -341,7 +343,18 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
     const int64_t per = share / kPlanWaves, wlo = min(hi, lo + wave * per), whi = min(hi, wlo + per);
     for (int w = 0; w < kPlanWaves; ++w)
         if (tid < experts) s_at[w][tid] = 0;
+    if (tid < experts) s_total[tid] = s_list[0][tid] = 0;
     __syncthreads();
+    if (gridDim.x > 1 && pairs <= kRecount) {
+#pragma unroll 4
+        for (int i = tid; i < (int)pairs; i += kPlanThreads) {
+            const uint32_t id = (uint32_t)ids[i];
+            if (id < (uint32_t)experts) {
+                atomicAdd(&s_total[id], 1u);
+                if (i < lo) atomicAdd(&s_list[0][id], 1u);
+            }
+        }
+    }
     for (int64_t i = wlo + lane; i < whi; i += 64) {
         const uint32_t id = (uint32_t)ids[i];
         if (id < (uint32_t)experts) atomicAdd(&s_at[wave][id], 1u);
@@ -351,7 +364,10 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
     const int e = tid;
     uint32_t total = 0, before = 0;
     if (e < experts) {
-        if (gridDim.x > 1) {
+        if (gridDim.x > 1 && pairs <= kRecount) {
+            total = s_total[e];
+            before = s_list[0][e];
+        } else if (gridDim.x > 1) {
 #pragma unroll 16
             for (int b = 0; b < (int)gridDim.x; ++b) {
                 const uint32_t n = (uint32_t)v.counts[(int64_t)b * experts + e];
@@ -409,6 +425,7 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const int32_t
         for (int q = 0; q < 4; ++q) next[q] = i4 + 64 * q + lane < whi ? (uint32_t)ids[i4 + 64 * q + lane] : 0xffffffffu;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+            if (i4 + 64 * q >= whi) break;
             const int64_t i = i4 + 64 * q + lane;
             const uint32_t id = next[q];
             const bool is = id < (uint32_t)experts;
@@ -467,7 +484,7 @@ int launch_expert_plan(const int32_t* ids, const dfp4_plan& p, hipStream_t strea
     const PlanView v = plan_view(p);
     int bits = 0;
     while ((1 << bits) < p.experts) ++bits;
-    if (shares > 1) hipLaunchKernelGGL(expert_count_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v.counts, pairs, share, (int)p.experts);
+    if (shares > 1 && pairs > kRecount) hipLaunchKernelGGL(expert_count_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v.counts, pairs, share, (int)p.experts);
     hipLaunchKernelGGL(expert_plan_kernel, dim3((uint32_t)shares), dim3(kPlanThreads), 0, stream, ids, v, pairs, share, (int)p.experts, bits,
                        p.tokens == 1 ? plan_list(pairs, p.experts, 2) : 0);
     return check_launch();

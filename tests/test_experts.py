@@ -456,7 +456,7 @@ def test_calls_from_python_refuse():
             bad()
     h = torch.zeros(12, 64, dtype=torch.bfloat16, device="cuda")
     for bad in (lambda: dfp4.experts_down(h, plan, layer.handle, torch.zeros(6, 2, device="cuda")), lambda: dfp4.experts_up(x, dfp4.expert_plan(ids, 5), layer.handle),
-                lambda: dfp4.route(x.float(), 65), lambda: dfp4.route(x.float(), 0), lambda: dfp4.expert_plan(ids, 2000), lambda: dfp4.route(x.float(), 4, groups=5),
+                lambda: dfp4.route(x.float(), 65), lambda: dfp4.route(x.float(), 0), lambda: dfp4.route(x.float(), 1 << 40), lambda: dfp4.route(x.float(), -3), lambda: dfp4.expert_plan(ids, 2000), lambda: dfp4.route(x.float(), 4, groups=5),
                 lambda: dfp4.add_norm(x[:, 4:], x[:, 4:], torch.ones(60, device="cuda")), lambda: dfp4.expert_weights(dfp4.empty_qtensor(16, 64, x.device, mx=True), 4)):
         with pytest.raises(dfp4.Dfp4Error):
             bad()
