@@ -476,7 +476,7 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
  *   logits   device, DFP4_F32 or DFP4_BF16 [tokens, experts], rows `ld` elements apart
  *   bias     device, f32 [experts], or NULL
  *   ids      device, int32 [tokens, k];  weights  device, f32 [tokens, k]
- *   experts up to 1024, k up to 32; groups (up to 64) divides experts; kept * (experts / groups) >= k; best at most a group's experts, and 1 or 2
+ *   tokens up to 2^25, experts up to 1024, k up to 32; groups (up to 64) divides experts; kept * (experts / groups) >= k; best at most a group's experts, and 1 or 2
  */
 enum { DFP4_SOFTMAX = 0, DFP4_SIGMOID = 1 };
 int dfp4_route(const void* logits, int dtype, int64_t ld, int64_t tokens, int64_t experts, int64_t k, int score, const float* bias,

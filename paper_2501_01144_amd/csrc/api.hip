@@ -588,7 +588,7 @@ int dfp4_norm_rope(const void* q, int64_t q_stride, int64_t q_head_stride, int64
 int dfp4_route(const void* logits, int dtype, int64_t ld, int64_t tokens, int64_t experts, int64_t k, int score, const float* bias,
                int64_t groups, int64_t kept, int64_t best, int renormalize, float scale, int32_t* ids, float* weights, void* stream) {
     if (dtype != DFP4_F32 && dtype != DFP4_BF16) return DFP4_ERR_DTYPE;
-    if (tokens < 0 || tokens > (int64_t)1 << 27 || experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChoice || k > experts || ld < experts ||
+    if (tokens < 0 || tokens > (int64_t)1 << 25 || experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChoice || k > experts || ld < experts ||
         ld > (int64_t)1 << 30 || (score != DFP4_SOFTMAX && score != DFP4_SIGMOID) || groups < 1 || groups > 64 || experts % groups != 0 || kept < 1 || kept > groups ||
         kept * (experts / groups) < k || best < 1 || best > 2 || best > experts / groups)
         return DFP4_ERR_SHAPE;

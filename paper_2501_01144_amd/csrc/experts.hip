@@ -108,7 +108,8 @@ struct QuantizeArgs {
 
 // Rows quantized in the plan's order (the arithmetic of the quantizer, quant_pass.h; as quantize_native_kernel, but for the rows' places).
 // A wave takes 8 rows x 8 blocks; what is behind the last row is left as it is: it is multiplied, and its results are not kept.
-// 32768 rows x 1024 26.7 us, by memory (3.5 TB/s).  Tried: scale bytes through LDS, so that they leave as whole lines (31.8).
+// 32768 rows x 1024 26.7 us, by memory (3.5 TB/s).  Tried: scale bytes through LDS, so that they leave as whole lines (31.8);
+// the larger tables of half as many lookups (25.6).
 constexpr int kQThreads = 256, kQWaves = kQThreads / 64, kPasses = 4;
 __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArgs p) {
     __shared__ __attribute__((aligned(16))) uint8_t lds_q[kDialects * 32];
@@ -670,30 +671,56 @@ struct JoinArgs {
     int k, dim;
 };
 
-// y[token] = sum over j of weights[token, j] * part[place], four elements a thread; PART16: part in bf16
+// y[token] = sum over j of weights[token, j] * part[place]; a token has 2^lanes threads of eight elements.  PART16: part in bf16.  Four rows at a time, none
+// behind a branch: one that is absent reads row 0 and is left out.
 template <bool BF16, bool PART16>
-__global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p) {
-    const int64_t quads = p.dim / 4, total = p.tokens * quads;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t token = i / quads, d = (i - token * quads) * 4;
-        float4 y = make_float4(0, 0, 0, 0);
-        for (int j = 0; j < p.k; ++j) {
-            const int32_t row = p.place[token * p.k + j];
-            if (row < 0 || row >= p.pairs) continue;
-            const float w = p.weights[token * p.k + j];
-            float4 v;
-            if constexpr (PART16) {
-                const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.part) + (int64_t)row * p.dim + d);
-                v = make_float4(as_f(u.x << 16), as_f(u.x & 0xffff0000u), as_f(u.y << 16), as_f(u.y & 0xffff0000u));
-            } else {
-                v = *reinterpret_cast<const float4*>(static_cast<const float*>(p.part) + (int64_t)row * p.dim + d);
+__global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p, int lanes) {
+    for (int64_t token = (int64_t)blockIdx.x * (256 >> lanes) + (threadIdx.x >> lanes); token < p.tokens; token += (int64_t)gridDim.x * (256 >> lanes)) {
+        const int32_t* place = p.place + token * p.k;
+        const float* weights = p.weights + token * p.k;
+        for (int d = (int)(threadIdx.x & ((1u << lanes) - 1)) * 8; d < p.dim; d += 8 << lanes) {
+            float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            for (int j0 = 0; j0 < p.k; j0 += 4) {
+                constexpr int kWords = PART16 ? 1 : 2;
+                uint4 u[4][kWords];
+                bool there[4];
+                float w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int j = min(j0 + q, p.k - 1);
+                    const int32_t row = place[j];
+                    there[q] = j0 + q < p.k && row >= 0 && row < p.pairs;
+                    w[q] = weights[j];
+                    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.part) + ((int64_t)(there[q] ? row : 0) * p.dim + d) * (PART16 ? 2 : 4));
+#pragma unroll
+                    for (int x = 0; x < kWords; ++x) u[q][x] = from[x];
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (!there[q]) continue;
+                    if constexpr (PART16) {
+                        const uint32_t v[4] = {u[q][0].x, u[q][0].y, u[q][0].z, u[q][0].w};
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) y[x] += w[q] * as_f((x & 1) ? v[x / 2] & 0xffff0000u : v[x / 2] << 16);
+                    } else {
+                        const uint32_t v[8] = {u[q][0].x, u[q][0].y, u[q][0].z, u[q][0].w, u[q][1].x, u[q][1].y, u[q][1].z, u[q][1].w};
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) y[x] += w[q] * as_f(v[x]);
+                    }
+                }
             }
-            y.x += w * v.x, y.y += w * v.y, y.z += w * v.z, y.w += w * v.w;
+            if constexpr (BF16) {
+                typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+                v8b o;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) o[x] = (__bf16)y[x];
+                *reinterpret_cast<v8b*>(static_cast<uint16_t*>(p.y) + token * p.dim + d) = o;
+            } else {
+                float4* to = reinterpret_cast<float4*>(static_cast<float*>(p.y) + token * p.dim + d);
+                to[0] = make_float4(y[0], y[1], y[2], y[3]);
+                to[1] = make_float4(y[4], y[5], y[6], y[7]);
+            }
         }
-        if constexpr (BF16)
-            *reinterpret_cast<ushort4*>(static_cast<uint16_t*>(p.y) + token * p.dim + d) = make_ushort4(bf16_of(y.x), bf16_of(y.y), bf16_of(y.z), bf16_of(y.w));
-        else
-            *reinterpret_cast<float4*>(static_cast<float*>(p.y) + token * p.dim + d) = y;
     }
 }
 
@@ -884,11 +911,13 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
     }
     if (!a.w.gated) {
         const JoinArgs j{out, a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
-        const int64_t wgs = (a.plan.tokens * (a.w.rows / 4) + 255) / 256;
+        int lanes = 0;
+        while (lanes < 8 && (8 << lanes) < a.w.rows) ++lanes;
+        const int64_t wgs = (a.plan.tokens + (256 >> lanes) - 1) / (256 >> lanes);
         const dim3 jg((unsigned)(wgs < (1 << 20) ? wgs : 1 << 20));
-        if (part16) hipLaunchKernelGGL((experts_join_kernel<true, true>), jg, dim3(256), 0, stream, j);
-        else if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true, false>), jg, dim3(256), 0, stream, j);
-        else hipLaunchKernelGGL((experts_join_kernel<false, false>), jg, dim3(256), 0, stream, j);
+        if (part16) hipLaunchKernelGGL((experts_join_kernel<true, true>), jg, dim3(256), 0, stream, j, lanes);
+        else if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true, false>), jg, dim3(256), 0, stream, j, lanes);
+        else hipLaunchKernelGGL((experts_join_kernel<false, false>), jg, dim3(256), 0, stream, j, lanes);
     }
     return check_launch();
 }

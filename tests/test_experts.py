@@ -25,7 +25,7 @@ def test_route_refuses():
     assert (route(dtype=2), route(dtype=-1)) == (-4, -4)
     for bad in (dict(tokens=-1), dict(experts=0), dict(experts=1025, ld=1025), dict(k=0), dict(k=33), dict(experts=4, k=5), dict(ld=63), dict(score=2), dict(groups=0),
                 dict(groups=3), dict(groups=4, kept=5), dict(groups=8, kept=0), dict(groups=16, kept=1, k=5), dict(best=0), dict(best=3), dict(groups=64, kept=64, best=2),
-                dict(experts=1024, ld=1024, groups=128, kept=128), dict(tokens=1 << 28)):
+                dict(experts=1024, ld=1024, groups=128, kept=128), dict(tokens=(1 << 25) + 1)):
         assert route(**bad) == -2, bad
     assert (route(logits=0), route(ids=0), route(weights=0)) == (-1,) * 3
     assert (route(logits=18), route(logits=17, dtype=1), route(bias=2), route(ids=6), route(weights=10)) == (-3,) * 5
@@ -287,6 +287,7 @@ PRODUCTS = [                                  # tokens, k, experts, K, rows
     (1100, 2, 2, 224, 136, {}), (600, 5, 20, 64, 256, dict(absent=0.5)),
     (100, 1, 8, 2176, 40, dict(only=1)), (40, 2, 6, 4192, 48, {}), (70, 3, 12, 4128, 24, dict(only=3, absent=0.2)), (4, 3, 5, 4256, 104, dict(twice=True)),
     (2, 32, 64, 96, 1000, dict(absent=0.4)), (260, 1, 10, 64, 1032, {}), (16, 1, 8, 8224, 16, {}), (3, 2, 4, 14336, 32, {}), (90, 2, 1024, 128, 8, {}),
+    (40, 2, 3, 64, 2056, {}), (700, 1, 2, 32, 4104, dict(absent=0.1)),
 ]
 
 
@@ -356,6 +357,27 @@ def test_up_of_tokens_quantized_once(tokens, k, experts, K, absent):
     there = rows >= 0
     mine[few.place.cpu()[there].long()] = h.cpu()[rows[there].long()]
     check_up(x[some], ids[some], layer, experts, mine)
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [2, 40, 400])
+@pytest.mark.parametrize("span", [12, 30])
+def test_products_of_uneven_blocks(tokens, span):
+    """Blocks whose scales lie up to 2^60 apart in a product, by every way."""
+    K, rows, experts, k = 1312, 48, 4, 2
+    g = torch.Generator().manual_seed(span)
+    uneven = lambda n: (torch.randn(n, K // 32, 32, generator=g) * torch.exp2(torch.randint(-span, 1, (n, K // 32, 1), generator=g).float())).view(n, K).bfloat16()  # noqa: E731
+    up, down = Layer(experts, rows, K, True), Layer(experts, rows, K, False)
+    for layer in (up, down):
+        w = [uneven(experts * rows) for _ in layer.values]
+        q = [dfp4.quantize(x.cuda()) for x in w]
+        layer.handle = dfp4.expert_weights(q[0], experts, up=q[1] if len(q) > 1 else None)
+        layer.values = [quantized(x).reshape(experts, rows, K) for x in w]
+    ids, x, h = ids_of(tokens, k, experts, seed=1), uneven(tokens), uneven(tokens * k)
+    plan, weights = dfp4.expert_plan(ids.cuda(), experts), torch.rand(tokens, k, generator=g)
+    check_up(x, ids, up, experts, dfp4.experts_up(x.cuda(), plan, up.handle))
+    for dtype in (torch.bfloat16, torch.float32):
+        check_down(h, ids, down, experts, weights, dfp4.experts_down(h.cuda(), plan, down.handle, weights.cuda(), dtype=dtype))
 
 
 @gpu
