@@ -405,14 +405,15 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(acc[i]) : "v"(wv), "v"(xv[i]));
         }
     };
+    auto row_of = [&](int r) { return p.single && GATED ? (int64_t)0 : (int64_t)s_row[r]; };
     // rows of the chunk into LDS; blocks behind the last of a quad as zeros
     auto stage = [&](const At& a, bool other_rows) {
         const int rows = min(32 * MT, a.g.rows), q0 = a.chunk * (kQuads / a.tiles), blocks = min(kQuads / a.tiles, p.Q - q0) * 4;
         __syncthreads();                                             // what was there is done with
-        if (other_rows) {
+        if (other_rows && !(p.single && GATED)) {
             if (tid < rows) {
                 const int64_t row = (int64_t)a.g.row0 + tid;
-                s_row[tid] = p.single && GATED ? 0 : p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
+                s_row[tid] = p.k ? (int32_t)((uint32_t)p.order[row] / p.k) : (int32_t)row;
             }
             __syncthreads();
         }
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
             for (int i = tid; i < rows * blocks * 4; i += 1024) {
                 const int r = i / (blocks * 4), b = (i >> 2) - r * blocks, kb = q0 * 4 + b, quarter = i & 3;
                 const bool on = kb < p.KB;
-                const uint4 v = on ? *reinterpret_cast<const uint4*>(p.x + (int64_t)s_row[r] * p.ld + kb * kBlock + quarter * 8) : make_uint4(0, 0, 0, 0);
+                const uint4 v = on ? *reinterpret_cast<const uint4*>(p.x + row_of(r) * p.ld + kb * kBlock + quarter * 8) : make_uint4(0, 0, 0, 0);
                 uint32_t code, e, d;
                 dfp4_pass_small(v, s_vote, s_index, code, e, d);
                 uint2 to;
@@ -437,7 +438,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int i = min(i0 + 1024 * u, rows * blocks - 1), r = i / blocks, b = i - r * blocks;
-                const int64_t blk = (int64_t)s_row[r] * p.KB + min(q0 * 4 + b, p.KB - 1);
+                const int64_t blk = row_of(r) * p.KB + min(q0 * 4 + b, p.KB - 1);
                 codes[u] = *reinterpret_cast<const uint4*>(p.x_codes + blk * 16);
                 e[u] = p.x_expo[blk];
                 d[u] = p.x_dial[blk];
@@ -505,8 +506,26 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
 #pragma unroll
                     for (int x = 0; x < 16; x += 2)
                         if (i < now.tiles) emit(now, i, now.batch * kTiles + sub, x, acc[i][x], acc[i][x + 1]);
+            } else if (now.tiles == 1 && p.Q <= kQuads / 2) {
+                // the parts of K are added in their order, all registers at once through the half of LDS that the rows leave
+                float(*red)[16][64] = reinterpret_cast<float(*)[16][64]>(s_x[kQuads / 2]);
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < 16; ++x) red[wave][x][lane] = acc[0][x];
+                __syncthreads();
+#pragma unroll 1
+                for (int job = wave; job < 8 * kTiles; job += 16) {
+                    const int tile = job >> 3, x = (job & 7) * 2;
+                    float v0 = 0.0f, v1 = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < SPLIT; ++w) {
+                        v0 += red[tile * SPLIT + w][x][lane];
+                        v1 += red[tile * SPLIT + w][x + 1][lane];
+                    }
+                    emit(now, 0, now.batch * kTiles + tile, x, v0, v1);
+                }
             } else {
-                // four registers at a time through LDS, the parts of K added in their order
+                // four registers at a time
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if (i >= now.tiles) break;
