@@ -310,7 +310,8 @@ __device__ __forceinline__ void load_quad(Quad& q, const uint8_t* at, bool there
 // Bound by the weights' stream (0.5625 bytes an element): 64 tokens of 2 of 8 experts, 4096 x 14336 up, 104 to 109 us = 5.0 TB/s, a large copy's rate; with
 // blocks of more than 32 rows among them, whose K takes two turns in LDS, 121 to 125.  Registers: 8 to 32 bytes of a thread's in scratch memory with two
 // tiles of rows.  Tried: FP6 weights (a third more bytes); the last quad loaded again where there is none (whole K in a wave 7 % slower over 300 drawn
-// products); offsets of quads in vector registers (two tiles of rows 5 to 20 % slower).
+// products); offsets of quads in vector registers (two tiles of rows 5 to 20 % slower).  One token of 8 of 128 experts, 2048 x 1024 up, is bound
+// by loads in turn (plan, row, weights): 7.8 us, 8.3 with the sums over waves in four steps.
 template <bool GATED, int MT, int SPLIT>
 __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
     constexpr int kQuads = 32, kTiles = 16 / SPLIT, kAhead = 4;       // quads of 32 rows in LDS; tiles at a time
