@@ -517,7 +517,8 @@ int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* 
 /*
  * Experts' products.  Rows are quantized as dfp4_quantize does and multiplied with the experts' weights in fp32.
  *   up    (gated weights) h[row] = silu(G x^) * (U x^), x^ the quantized x of the row's token; rows in the plan's order
- *   down  (others)        y[token] = sum over its pairs j, in their order, of weights[token, j] * (W h^[row of the pair]); 0 without any
+ *   down  (others)        y[token] = sum over its pairs j, in their order, of weights[token, j] * (W h^[row of the pair]); 0 without any.
+ *         In fp32 throughout, and rounded once, to y's type
  *   (rows of the weights: a multiple of 8, up to 2^19, fewer than 2^28 of all experts; K up to 2^20.  Refused as too large: products of many rows of
  *   more than about 2^24 tiles of 256 x 256.)
  *   x     device, bf16 [tokens, K], rows x_ld elements apart (a multiple of 8), 16-byte aligned

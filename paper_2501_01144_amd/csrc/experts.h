@@ -112,8 +112,7 @@ struct ExpertTiles {
     int64_t most;
     int K, rows, tiles;      // packed rows of an expert, tiles of 256 of them
     bool gated, half;        // half: tiles of 128 rows
-    void* out;               // gated: bf16 [row][rows / 2], else [row][rows] of out_dtype
-    int out_dtype;
+    void* out;               // gated: bf16 [row][rows / 2], else f32 [row][rows]
 };
 int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream);
 

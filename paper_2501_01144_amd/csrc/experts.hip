@@ -9,8 +9,9 @@
 //   a few tokens, down   experts_token_kernel, one launch.
 // The weights' two forms cost memory (0.79 + 0.56 bytes an element) and spare either way a pass over them.
 // Gate and up rows take turns in both: a lane then holds both numbers that an element of h is made of (few: weights are the instruction's
-// first operand, rows its second).  Down, rows leave weighted by nothing, in the type of y where there are many (bf16: 1.4 times the error of its rounding)
-// and in fp32 else, and experts_join_kernel adds a token's in their order: no sum depends on when a workgroup runs.
+// first operand, rows its second).  Down, rows leave weighted by nothing, in fp32, and experts_join_kernel adds a token's in their order: no sum
+// depends on when a workgroup runs, and y is rounded once, whatever way its rows took.  (Rows in bf16 are half of what is moved there, but
+// where a token's experts cancel, their roundings are more than all of y: of 8 normal rows, weights of one sign, 1 % of y is off by 33 half steps.)
 #include <math.h>
 #include <type_traits>
 #include "experts.h"
@@ -683,7 +684,7 @@ __global__ __launch_bounds__(1024, 4) void experts_token_kernel(TokenArgs p) {
 }
 
 struct JoinArgs {
-    const void* part;
+    const float* part;
     const float* weights;
     const int32_t* place;
     void* y;
@@ -691,9 +692,9 @@ struct JoinArgs {
     int k, dim;
 };
 
-// y[token] = sum over j of weights[token, j] * part[place]; a token has 2^lanes threads of eight elements.  PART16: part in bf16.  Four rows at a time, none
+// y[token] = sum over j of weights[token, j] * part[place]; a token has 2^lanes threads of eight elements.  Four rows at a time, none
 // behind a branch: one that is absent reads row 0 and is left out.
-template <bool BF16, bool PART16>
+template <bool BF16>
 __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p, int lanes) {
     for (int64_t token = (int64_t)blockIdx.x * (256 >> lanes) + (threadIdx.x >> lanes); token < p.tokens; token += (int64_t)gridDim.x * (256 >> lanes)) {
         const int32_t* place = p.place + token * p.k;
@@ -701,8 +702,7 @@ __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p, int lanes
         for (int d = (int)(threadIdx.x & ((1u << lanes) - 1)) * 8; d < p.dim; d += 8 << lanes) {
             float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             for (int j0 = 0; j0 < p.k; j0 += 4) {
-                constexpr int kWords = PART16 ? 1 : 2;
-                uint4 u[4][kWords];
+                float4 u[4][2];
                 bool there[4];
                 float w[4];
 #pragma unroll
@@ -711,22 +711,15 @@ __global__ __launch_bounds__(256) void experts_join_kernel(JoinArgs p, int lanes
                     const int32_t row = place[j];
                     there[q] = j0 + q < p.k && row >= 0 && row < p.pairs;
                     w[q] = weights[j];
-                    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.part) + ((int64_t)(there[q] ? row : 0) * p.dim + d) * (PART16 ? 2 : 4));
-#pragma unroll
-                    for (int x = 0; x < kWords; ++x) u[q][x] = from[x];
+                    const float4* from = reinterpret_cast<const float4*>(p.part + (int64_t)(there[q] ? row : 0) * p.dim + d);
+                    u[q][0] = from[0], u[q][1] = from[1];
                 }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (!there[q]) continue;
-                    if constexpr (PART16) {
-                        const uint32_t v[4] = {u[q][0].x, u[q][0].y, u[q][0].z, u[q][0].w};
+                    const float v[8] = {u[q][0].x, u[q][0].y, u[q][0].z, u[q][0].w, u[q][1].x, u[q][1].y, u[q][1].z, u[q][1].w};
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) y[x] += w[q] * as_f((x & 1) ? v[x / 2] & 0xffff0000u : v[x / 2] << 16);
-                    } else {
-                        const uint32_t v[8] = {u[q][0].x, u[q][0].y, u[q][0].z, u[q][0].w, u[q][1].x, u[q][1].y, u[q][1].z, u[q][1].w};
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) y[x] += w[q] * as_f(v[x]);
-                    }
+                    for (int x = 0; x < 8; ++x) y[x] += w[q] * v[x];
                 }
             }
             if constexpr (BF16) {
@@ -858,7 +851,6 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         return check_launch();
     }
     void* out = a.w.gated ? a.out : a.workspace + ws.part;
-    const bool part16 = ws.many && a.out_dtype == DFP4_BF16;
     if (ws.many) {
         QuantizeArgs q{};
         q.x = a.x, q.ld = a.ld;
@@ -885,7 +877,7 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         t.used = plan.used + (t.half ? 1 : 0), t.list = plan.list[t.half ? 1 : 0], t.most = plan_list(pairs, a.plan.experts, t.half ? 1 : 0);
         t.K = (int)a.w.K, t.rows = (int)expert_rows(a.w), t.tiles = (int)(padded_rows(a.w) / 256);
         t.gated = a.w.gated != 0;
-        t.out = out, t.out_dtype = a.out_dtype;
+        t.out = out;
         const int rc = launch_expert_tiles(t, stream);
         if (rc != DFP4_OK) return rc;
     } else {
@@ -930,14 +922,13 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         else launch_few<false, 2>(p, split, grid, stream);
     }
     if (!a.w.gated) {
-        const JoinArgs j{out, a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
+        const JoinArgs j{static_cast<const float*>(out), a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};
         int lanes = 0;
         while (lanes < 8 && (8 << lanes) < a.w.rows) ++lanes;
         const int64_t wgs = (a.plan.tokens + (256 >> lanes) - 1) / (256 >> lanes);
         const dim3 jg((unsigned)(wgs < (1 << 20) ? wgs : 1 << 20));
-        if (part16) hipLaunchKernelGGL((experts_join_kernel<true, true>), jg, dim3(256), 0, stream, j, lanes);
-        else if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true, false>), jg, dim3(256), 0, stream, j, lanes);
-        else hipLaunchKernelGGL((experts_join_kernel<false, false>), jg, dim3(256), 0, stream, j, lanes);
+        if (a.out_dtype == DFP4_BF16) hipLaunchKernelGGL((experts_join_kernel<true>), jg, dim3(256), 0, stream, j, lanes);
+        else hipLaunchKernelGGL((experts_join_kernel<false>), jg, dim3(256), 0, stream, j, lanes);
     }
     return check_launch();
 }

@@ -1142,15 +1142,14 @@ int launch_expert_tiles(const ExpertTiles& t, hipStream_t stream) {
     const int64_t wgs = (t.most * p.cols + 7) / 8 * 8;
     if (wgs >= (int64_t)1 << 24) return DFP4_ERR_SHAPE;                       // fewer than 2^32 threads
     const dim3 grid((unsigned)wgs);
-    auto run = [&](auto bf16_c, auto mode_c) {
-        constexpr bool kBf16 = decltype(bf16_c)::value;
+    auto run = [&](auto mode_c) {
         constexpr int kMode = decltype(mode_c)::value;
+        constexpr bool kBf16 = kMode == kGated;                                // (rows of down are added in fp32)
         if (t.half) hipLaunchKernelGGL((gemm_native_kernel<kFmtFp6, kBf16, 2, kMode>), grid, dim3(256), 0, stream, p);
         else hipLaunchKernelGGL((gemm_native_kernel<kFmtFp6, kBf16, 4, kMode>), grid, dim3(256), 0, stream, p);
     };
-    if (t.gated) run(std::true_type{}, std::integral_constant<int, kGated>{});
-    else if (t.out_dtype == DFP4_BF16) run(std::true_type{}, std::integral_constant<int, kExperts>{});
-    else run(std::false_type{}, std::integral_constant<int, kExperts>{});
+    if (t.gated) run(std::integral_constant<int, kGated>{});
+    else run(std::integral_constant<int, kExperts>{});
     return check_launch();
 }
 

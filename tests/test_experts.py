@@ -525,3 +525,38 @@ def test_a_layer_eager_on_another_stream_and_in_a_graph(tokens):
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, want[turn])), turn
         layer(*batches[(turn + 1) % 3])
+
+
+def check_down_to_its_rounding(h, ids, layer, experts, weights, y):
+    """y against float64: rows' products within 1e-5 sum |h||w|, k products and additions in fp32 (2^-24 each), and one rounding, y's own."""
+    hq = quantized(h)
+    offsets, order, _ = plain_plan(ids, experts)
+    tokens, k = ids.shape
+    dim = layer.values[0].shape[1]
+    want, size, tol = np.zeros((tokens, dim)), np.zeros((tokens, dim)), np.zeros((tokens, dim))
+    for e in range(experts):
+        pairs, a = np.array(order[offsets[e]:offsets[e + 1]], dtype=int), hq[offsets[e]:offsets[e + 1]]
+        if not len(pairs):
+            continue
+        w = synth.to_f64(weights).reshape(-1)[pairs][:, None]
+        v = w * (a @ layer.values[0][e].T)
+        np.add.at(want, pairs // k, v)
+        np.add.at(size, pairs // k, np.abs(v))
+        np.add.at(tol, pairs // k, 1e-5 * np.abs(w) * (np.abs(a) @ np.abs(layer.values[0][e]).T))
+    half = HALF if y.dtype == torch.bfloat16 else 2.0 ** -24
+    tol = (tol + 2.0 ** -23 * (k + 1) * size) * (1 + half) + half * np.abs(want) + 1e-38
+    got = y.float().cpu().double().numpy()
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,K,rows", [(300, 2, 4, 128, 64), (333, 5, 12, 224, 264), (1030, 2, 2, 96, 1800), (64, 2, 8, 128, 2056), (5, 3, 8, 96, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_down_rounds_once(tokens, k, experts, K, rows, dtype):
+    """Weights of both signs, so that the experts' results cancel in part: what is rounded before their sum shows."""
+    layer = Layer(experts, rows, K, False, seed=tokens)
+    g = torch.Generator().manual_seed(K)
+    h, weights = torch.randn(tokens * k, K, generator=g).bfloat16(), torch.rand(tokens, k, generator=g) - 0.5
+    ids = ids_of(tokens, k, experts, seed=rows)
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    check_down_to_its_rounding(h, ids, layer, experts, weights, dfp4.experts_down(h.cuda(), plan, layer.handle, weights.cuda(), dtype=dtype))
