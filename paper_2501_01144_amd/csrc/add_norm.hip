@@ -60,8 +60,8 @@ __device__ __forceinline__ void normalize(float (&x)[PASSES][8], float per, floa
     };
     float mean = sum() * per + eps;
     if (mean < 0x1p-100f || mean == __builtin_inff()) {  // (the same for the whole row)
-        // squares beyond the range of fp32: of numbers scaled by a power of two
-        const float by = mean == __builtin_inff() ? 0x1p-70f : 0x1p100f;
+        // squares beyond the range of fp32: of numbers scaled by a power of two, below 2^48 then, so that 2^14 squares have a sum
+        const float by = mean == __builtin_inff() ? 0x1p-80f : 0x1p100f;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i)
 #pragma unroll

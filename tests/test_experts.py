@@ -450,6 +450,22 @@ def test_add_norm_of_numbers_whose_squares_leave_fp32(size, dim):
     check_norm(y, r, w, None, None, 1.0, 0.0, *got)
 
 
+@gpu
+@pytest.mark.parametrize("dim", [4104, 8192, 16384])
+@pytest.mark.parametrize("wide", [False, True])
+def test_add_norm_of_rows_near_the_largest_number(dim, wide):
+    """Up to dim numbers of 2^127 and more: their squares, scaled, still have a sum in fp32."""
+    g = torch.Generator().manual_seed(dim)
+    sign = lambda: torch.randint(0, 2, (3, dim), generator=g).float() * 2 - 1  # noqa: E731
+    big, w = sign() * torch.linspace(1.7e38, 3.3e38, dim), 1 + 0.2 * torch.randn(dim, generator=g)
+    y, r = big.bfloat16(), (big if wide else big.bfloat16())
+    small = torch.randn(3, dim, generator=g)
+    got = dfp4.add_norm(y.cuda(), (small if wide else small.bfloat16()).cuda(), w.cuda(), post_weight=w.cuda())         # the norm before
+    check_norm(y, small if wide else small.bfloat16(), w, w, None, 1.0, 1e-6, *got)
+    got = dfp4.add_norm(small.bfloat16().cuda(), r.cuda(), w.cuda())                                                    # the norm after
+    check_norm(small.bfloat16(), r, w, None, None, 1.0, 1e-6, *got)
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------------
 
 @gpu
