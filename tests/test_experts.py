@@ -381,6 +381,34 @@ def test_products_of_uneven_blocks(tokens, span):
 
 
 @gpu
+@pytest.mark.parametrize("tokens", [1, 40, 200])
+def test_up_of_far_gates(tokens):
+    """silu where exp(-g) leaves fp32 and its product with u does not: results down to the least normal number.  g and u are single products of
+    numbers of a few bits, so exact."""
+    experts, rows, K = 2, 256, 64
+    g, u = torch.linspace(-160.0, 100.0, experts * rows), 2.0 ** (torch.arange(experts * rows) % 101)
+    w = [torch.zeros(experts * rows, K) for _ in range(2)]
+    w[0][:, 0], w[1][:, 32] = g, u
+    w = [t.bfloat16() for t in w]
+    q = [dfp4.quantize(t.cuda()) for t in w]
+    handle, (gate, up) = dfp4.expert_weights(q[0], experts, up=q[1]), (quantized(t).reshape(experts, rows, K) for t in w)
+    x = torch.zeros(tokens, K)
+    x[:, 0], x[:, 32] = 1.0, 1.0
+    ids = (torch.arange(tokens) % experts).int()[:, None].contiguous()
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    h = dfp4.experts_up(x.bfloat16().cuda(), plan, handle).float().cpu().double().numpy()
+    offsets, _, _ = plain_plan(ids, experts)
+    for e in range(experts):
+        a, b = gate[e][:, 0], up[e][:, 32]
+        want = a / (1 + np.exp(-a)) * b
+        # exp's argument is off by 2^-23 of itself at most (its factor's rounding and its own), which is 2^-23 |g| of the result; a few operations in
+        # fp32; one rounding to bf16; numbers below the least normal one may be zero
+        tol = (2.0 ** -23 * np.abs(a) + 2.0 ** -20) * np.abs(want) * (1 + HALF) + HALF * np.abs(want) + 2.0 ** -126
+        got = h[offsets[e]:offsets[e + 1]]
+        assert (np.abs(got - want) <= tol).all(), (e, a[(np.abs(got - want) > tol).any(0)])
+
+
+@gpu
 def test_products_of_no_tokens():
     up, down = Layer(4, 64, 64, True), Layer(4, 64, 64, False)
     plan = dfp4.expert_plan(torch.zeros(0, 2, dtype=torch.int32, device="cuda"), 4)
