@@ -529,6 +529,14 @@ int dfp4_expert_weights(dfp4_tensor gate, dfp4_tensor up, dfp4_experts w, void* 
  *   workspace   at least dfp4_experts_workspace_bytes(plan, w) bytes, 256-byte aligned
  */
 size_t dfp4_experts_workspace_bytes(dfp4_plan plan, dfp4_experts w);
+/*
+ * The way that such a product takes, by its sizes alone (the plan's tokens, no data; results are right by any).  way: HOST, three numbers:
+ *   the rows a workgroup takes at a time: 1 (down, all experts of a token), 32 or 64 (weights in 4 bits streamed past them), 128 or 256 (tiles);
+ *   how many of its waves share K;
+ *   how rows are quantized: 0 within the product, 1 in a launch before it, 2 (up) once a token in a launch before it, then rewritten for each expert.
+ * Refuses sizes that the products refuse, and none.
+ */
+int dfp4_experts_way(dfp4_plan plan, dfp4_experts w, int32_t* way);
 int dfp4_experts_up(const void* x, int64_t x_ld, dfp4_plan plan, dfp4_experts w, void* h, void* workspace, size_t workspace_bytes, void* stream);
 int dfp4_experts_down(const void* h, int64_t h_ld, dfp4_plan plan, dfp4_experts w, const float* weights, void* y, int y_dtype, void* workspace,
                       size_t workspace_bytes, void* stream);

@@ -648,6 +648,17 @@ size_t dfp4_experts_workspace_bytes(dfp4_plan plan, dfp4_experts w) {
     return experts_workspace_bytes(plan, w);
 }
 
+int dfp4_experts_way(dfp4_plan plan, dfp4_experts w, int32_t* way) {
+    int rc = check_plan(plan);
+    if (rc == DFP4_OK) rc = check_experts(w);
+    if (rc != DFP4_OK) return rc;
+    if (plan.experts != w.experts || plan.tokens == 0 || !experts_fit(plan, w)) return DFP4_ERR_SHAPE;
+    if (!way) return DFP4_ERR_NULL;
+    const ExpertsWay x = experts_way(plan, w);
+    way[0] = x.rows, way[1] = x.waves, way[2] = x.quantized;
+    return DFP4_OK;
+}
+
 static int experts_product(const ExpertsArgs& a, int64_t x_cols, size_t workspace_bytes, void* stream) {
     int rc = check_plan(a.plan);
     if (rc == DFP4_OK) rc = check_experts(a.w);

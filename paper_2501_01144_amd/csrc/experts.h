@@ -94,6 +94,12 @@ __device__ __forceinline__ float silu_times(float g, float u) {
     return g * m * __builtin_amdgcn_rcpf(__builtin_fmaf(t, t, 1.0f)) * (u * m);
 }
 
+// The way that a product takes (dfp4_experts_way)
+enum { kWithin = 0, kBefore = 1, kOnceAToken = 2 };
+struct ExpertsWay {
+    int rows, waves, quantized;
+};
+
 // An experts' product: rows of `x` (up: a token's, down: a pair's) with the experts' matrices
 struct ExpertsArgs {
     const uint16_t* x;
@@ -124,6 +130,7 @@ int launch_expert_plan(const int32_t* ids, const dfp4_plan& plan, hipStream_t st
 int launch_add_norm(const AddNormArgs& a, hipStream_t stream);
 size_t expert_weights_bytes(int64_t experts, int64_t rows, int64_t K, bool gated);
 int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& w, hipStream_t stream);
+ExpertsWay experts_way(const dfp4_plan& plan, const dfp4_experts& w);
 bool experts_fit(const dfp4_plan& plan, const dfp4_experts& w);
 size_t experts_workspace_bytes(const dfp4_plan& plan, const dfp4_experts& w);
 int launch_experts(const ExpertsArgs& a, hipStream_t stream);

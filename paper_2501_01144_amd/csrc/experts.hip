@@ -763,6 +763,24 @@ inline bool token_by_token(const dfp4_plan& plan, const dfp4_experts& w) {
     return again * w.rows * w.K <= 28 << 20;
 }
 
+// How many waves share K in products of few rows, by rounds of items over the compute units: a wave takes 1.08 us for a quad (the chip's memory among its waves), an item 2 us
+// more, a sum over waves 1.5 to 2.9 for 32 rows, K in turns 2.5 a turn.  Of 234 drawn products the best of the five is missed by 2.2 % in the mean
+// (always two: 12 %).  From 10 rows an expert on, some have more than 32.
+inline int waves_of_K(const dfp4_plan& plan, const dfp4_experts& w) {
+    const int64_t active = active_experts(plan), tiles = row_tiles(w), cus = device_cu_count();
+    const int Q = (int)quads_of(w.K), two = plan.tokens * plan.k > 10 * active ? 2 : 1, turns = (Q * two + 31) / 32;
+    int split = 1;
+    float least = 0.0f;
+    for (int s = 1; s <= 16; s *= 2) {
+        const int64_t per = 16 / s, n = active * ((tiles + per - 1) / per), rounds = (n + cus - 1) / cus;
+        const int chunk = Q < 32 / two ? Q : 32 / two, quads = turns * ((chunk + s - 1) / s);
+        const float sum = s == 1 ? 0.0f : s == 16 ? 2.85f : s == 8 ? 2.0f : 1.47f;
+        const float us = (float)rounds * (1.08f * (float)quads + 2.0f + (float)two * (sum + (turns > 1 ? 2.46f * (float)turns : 0.0f)));
+        if (s == 1 || us < least) least = us, split = s;
+    }
+    return split;
+}
+
 // workspace: rows in operand order, or in their 4-bit form (few), and down their products
 struct Workspace {
     bool many;
@@ -815,6 +833,16 @@ int launch_expert_weights(dfp4_tensor gate, dfp4_tensor up, const dfp4_experts& 
     return check_launch();
 }
 
+ExpertsWay experts_way(const dfp4_plan& plan, const dfp4_experts& w) {
+    const int64_t pairs = plan.tokens * plan.k;
+    if (token_by_token(plan, w)) return ExpertsWay{1, 16, kWithin};
+    const Workspace ws = workspace_of(plan, w);
+    if (ws.many) return ExpertsWay{half_tiles(plan, w) ? 128 : 256, 1, ws.codes ? kOnceAToken : kBefore};
+    // Quantized by the workgroups that take them where that is little work: a launch less (2.5 us), but 1.1 us a workgroup and 8192 elements
+    // (16 rows of 4096: 112 us instead of 107)
+    return ExpertsWay{pairs > 32 ? 64 : 32, waves_of_K(plan, w), pairs * w.K <= active_experts(plan) * 12288 ? kWithin : kBefore};
+}
+
 // Whether one launch holds the tiles of a product of many rows (fewer than 2^32 threads)
 bool experts_fit(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t pairs = plan.tokens * plan.k;
@@ -835,9 +863,10 @@ static void launch_few(const FewArgs& p, int split, dim3 grid, hipStream_t strea
 int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
     const int64_t pairs = a.plan.tokens * a.plan.k, S = steps_of(a.w.K);
     const Workspace ws = workspace_of(a.plan, a.w);
+    const ExpertsWay way = experts_way(a.plan, a.w);
     const PlanView plan = plan_view(a.plan);
     const int cus = device_cu_count();
-    if (token_by_token(a.plan, a.w)) {
+    if (way.rows == 1) {
         TokenArgs p{};
         p.h = a.x, p.ld = a.ld;
         p.quads = static_cast<const uint8_t*>(a.w.packed) + quads_offset(a.w);
@@ -851,14 +880,14 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         return check_launch();
     }
     void* out = a.w.gated ? a.out : a.workspace + ws.part;
-    if (ws.many) {
+    if (way.rows >= 128) {
         QuantizeArgs q{};
         q.x = a.x, q.ld = a.ld;
         q.rows = plan.offsets + a.plan.experts, q.order = plan.order, q.row_at = plan.row_at;
         q.to = packed_at(a.workspace, ws.rows, a.w.K);
         q.k = a.w.gated ? (uint32_t)a.plan.k : 0, q.KB = (uint32_t)(a.w.K / kBlock), q.S = (uint32_t)S;
         q.bound = pairs;
-        if (ws.codes) {
+        if (way.quantized == kOnceAToken) {
             const dfp4_tensor x{a.workspace + ws.codes, a.workspace + ws.dial, a.workspace + ws.expo, a.plan.tokens, a.w.K};
             const int rc = launch_quantize(false, a.x, a.plan.tokens, a.w.K, a.ld, x, stream);
             if (rc != DFP4_OK) return rc;
@@ -873,7 +902,7 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         ExpertTiles t{};
         t.a = q.to.bits, t.a_scales = native_scale_offset(ws.rows, a.w.K, true);
         t.w = a.w.packed, t.w_scales = native_scale_offset(a.w.experts * padded_rows(a.w), a.w.K, true);
-        t.half = half_tiles(a.plan, a.w);
+        t.half = way.rows == 128;
         t.used = plan.used + (t.half ? 1 : 0), t.list = plan.list[t.half ? 1 : 0], t.most = plan_list(pairs, a.plan.experts, t.half ? 1 : 0);
         t.K = (int)a.w.K, t.rows = (int)expert_rows(a.w), t.tiles = (int)(padded_rows(a.w) / 256);
         t.gated = a.w.gated != 0;
@@ -882,11 +911,8 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         if (rc != DFP4_OK) return rc;
     } else {
         const dfp4_tensor x{a.workspace, a.workspace + ws.dial, a.workspace + ws.expo, ws.rows, a.w.K};
-        const int64_t active = active_experts(a.plan);
         FewArgs p{};
-        // Quantized by the workgroups that take them where that is little work: a launch less (2.5 us), but 1.1 us a workgroup and 8192 elements
-        // (16 rows of 4096: 112 us instead of 107)
-        if (pairs * a.w.K <= active * 12288) {
+        if (way.quantized == kWithin) {
             p.x = a.x, p.ld = a.ld;
         } else {
             const CodesArgs c{a.x, a.ld, a.w.gated ? nullptr : plan.offsets + a.plan.experts, reinterpret_cast<uint32_t*>(x.codes), x.dialect, x.exponent, ws.rows,
@@ -900,26 +926,12 @@ int launch_experts(const ExpertsArgs& a, hipStream_t stream) {
         p.out = out, p.blocks = plan_list(pairs, a.plan.experts, 2);
         p.k = a.w.gated ? (uint32_t)a.plan.k : 0, p.single = a.plan.tokens == 1;
         p.KB = (int)(a.w.K / kBlock), p.Q = (int)quads_of(a.w.K), p.rows = (int)expert_rows(a.w), p.tiles = (int)row_tiles(a.w);
-        const int mt = pairs > 32 ? 2 : 1;                           // rows of a block, at most
-        // How many waves share K, by rounds of items over the compute units: a wave takes 1.08 us for a quad (the chip's memory among its waves), an item 2 us
-        // more, a sum over waves 1.5 to 2.9 for 32 rows, K in turns 2.5 a turn.  Of 234 drawn products the best of the five is missed by 2.2 % in the mean
-        // (always two: 12 %).  From 10 rows an expert on, some have more than 32.
-        const int two = pairs > 10 * active ? 2 : 1, turns = (p.Q * two + 31) / 32;
-        int split = 1;
-        float least = 0.0f;
-        for (int s = 1; s <= 16; s *= 2) {
-            const int64_t per = 16 / s, n = active * ((p.tiles + per - 1) / per), rounds = (n + cus - 1) / cus;
-            const int chunk = p.Q < 32 / two ? p.Q : 32 / two, quads = turns * ((chunk + s - 1) / s);
-            const float sum = s == 1 ? 0.0f : s == 16 ? 2.85f : s == 8 ? 2.0f : 1.47f;
-            const float us = (float)rounds * (1.08f * (float)quads + 2.0f + (float)two * (sum + (turns > 1 ? 2.46f * (float)turns : 0.0f)));
-            if (s == 1 || us < least) least = us, split = s;
-        }
-        const int64_t items = p.blocks * ((p.tiles + 16 / split - 1) / (16 / split));
+        const int64_t items = p.blocks * ((p.tiles + 16 / way.waves - 1) / (16 / way.waves));
         const dim3 grid((unsigned)(items < cus ? items : cus));
-        if (a.w.gated && mt == 1) launch_few<true, 1>(p, split, grid, stream);
-        else if (a.w.gated) launch_few<true, 2>(p, split, grid, stream);
-        else if (mt == 1) launch_few<false, 1>(p, split, grid, stream);
-        else launch_few<false, 2>(p, split, grid, stream);
+        if (a.w.gated && way.rows == 32) launch_few<true, 1>(p, way.waves, grid, stream);
+        else if (a.w.gated) launch_few<true, 2>(p, way.waves, grid, stream);
+        else if (way.rows == 32) launch_few<false, 1>(p, way.waves, grid, stream);
+        else launch_few<false, 2>(p, way.waves, grid, stream);
     }
     if (!a.w.gated) {
         const JoinArgs j{static_cast<const float*>(out), a.weights, plan.place, a.out, a.plan.tokens, pairs, (int)a.plan.k, (int)a.w.rows};

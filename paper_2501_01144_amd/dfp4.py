@@ -58,7 +58,7 @@ SYMBOLS = [
     "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_gemm", "dfp4_formatbook", "dfp4_strerror",
     "dfp4_paged_cell_bytes", "dfp4_paged_write", "dfp4_paged_read", "dfp4_paged_attention_workspace_bytes", "dfp4_paged_attention_rows", "dfp4_paged_attention",
     "dfp4_norm_rope",
-    "dfp4_route", "dfp4_expert_plan_bytes", "dfp4_expert_plan", "dfp4_expert_weights_bytes", "dfp4_expert_weights", "dfp4_experts_workspace_bytes",
+    "dfp4_route", "dfp4_expert_plan_bytes", "dfp4_expert_plan", "dfp4_expert_weights_bytes", "dfp4_expert_weights", "dfp4_experts_workspace_bytes", "dfp4_experts_way",
     "dfp4_experts_up", "dfp4_experts_down", "dfp4_add_norm",
 ]
 
@@ -170,6 +170,8 @@ def load():
     lib.dfp4_expert_weights.restype = ci
     lib.dfp4_experts_workspace_bytes.argtypes = [_CPlan, _CExperts]
     lib.dfp4_experts_workspace_bytes.restype = ctypes.c_size_t
+    lib.dfp4_experts_way.argtypes = [_CPlan, _CExperts, vp]
+    lib.dfp4_experts_way.restype = ci
     lib.dfp4_experts_up.argtypes = [vp, i64, _CPlan, _CExperts, vp, vp, ctypes.c_size_t, vp]
     lib.dfp4_experts_up.restype = ci
     lib.dfp4_experts_down.argtypes = [vp, i64, _CPlan, _CExperts, vp, vp, ci, vp, ctypes.c_size_t, vp]
@@ -746,6 +748,14 @@ def _product_workspace(plan, w, workspace, device):
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
     return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def experts_way(plan, w):
+    """dfp4_experts_way: the rows that a workgroup of the product takes (1, 32, 64, 128 or 256), the waves that share K, and how rows are
+    quantized (0 within, 1 before, 2 once a token)."""
+    way = (ctypes.c_int32 * 3)()
+    _check(load().dfp4_experts_way(plan.c(), w.c(), way), "dfp4_experts_way")
+    return tuple(way)
 
 
 def experts_up(x, plan, w, out=None, workspace=None):

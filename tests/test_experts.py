@@ -418,6 +418,139 @@ def test_products_of_no_tokens():
     assert h.shape == (0, 64) and y.shape == (0, 64)
 
 
+# ---- every way of the products -----------------------------------------------------------------------------------------------
+
+# tokens, k, experts, K, rows, absent; the way: rows a workgroup takes, waves that share K, how rows are quantized (0 within, 1 before, 2 once a token).
+# Blocks of 32 rows have up to 32 quads of K (4096 elements) in LDS at a time, those of more rows 16
+UP_WAYS = [
+    (9, 2, 8, 96, 104, 0.2, (32, 1, 0)), (4, 2, 3, 416, 8240, 0.0, (32, 2, 0)), (16, 2, 2, 800, 8736, 0.1, (32, 2, 1)), (7, 1, 2, 288, 48, 0.0, (32, 4, 0)),
+    (30, 1, 1, 480, 72, 0.0, (32, 4, 1)), (27, 1, 2, 2112, 4472, 0.1, (32, 4, 1)), (5, 2, 3, 544, 40, 0.3, (32, 8, 0)), (23, 1, 1, 576, 56, 0.1, (32, 8, 1)),
+    (4, 1, 2, 4320, 4128, 0.0, (32, 4, 0)), (2, 1, 1, 4320, 4128, 0.0, (32, 8, 0)), (11, 1, 1, 2144, 4112, 0.0, (32, 8, 1)), (3, 2, 4, 1056, 136, 0.2, (32, 16, 0)), (1, 8, 9, 4128, 40, 0.4, (32, 16, 0)),
+    (19, 1, 2, 8224, 24, 0.1, (32, 16, 1)),
+    (70, 2, 20, 96, 104, 0.2, (64, 1, 0)), (100, 2, 6, 384, 72, 0.1, (64, 1, 1)), (242, 1, 33, 416, 464, 0.0, (64, 2, 0)), (327, 2, 33, 672, 480, 0.1, (64, 2, 1)),
+    (17, 4, 8, 416, 40, 0.2, (64, 4, 0)), (60, 1, 2, 448, 72, 0.0, (64, 4, 1)), (205, 2, 33, 2144, 232, 0.1, (64, 4, 1)), (33, 1, 2, 576, 24, 0.0, (64, 8, 0)),
+    (66, 1, 2, 992, 40, 0.1, (64, 8, 1)), (36, 2, 33, 4320, 144, 0.2, (64, 8, 0)), (17, 4, 5, 2080, 848, 0.1, (64, 8, 1)), (20, 4, 8, 1088, 56, 0.2, (64, 16, 0)),
+    (23, 2, 5, 1344, 40, 0.0, (64, 16, 1)), (19, 2, 16, 4832, 24, 0.2, (64, 16, 0)), (60, 2, 5, 4256, 72, 0.1, (64, 16, 1)),
+    (300, 2, 4, 288, 72, 0.1, (128, 1, 1)), (1500, 3, 4, 7488, 40, 0.1, (128, 1, 2)), (2100, 2, 2, 1056, 904, 0.1, (256, 1, 1)), (2100, 2, 2, 1024, 904, 0.0, (256, 1, 1)),
+    (4200, 7, 7, 2048, 136, 0.1, (256, 1, 2)), (4200, 7, 8, 1184, 136, 0.0, (256, 1, 2)),
+]
+DOWN_WAYS = [
+    (5, 3, 8, 1056, 72, 0.3, (1, 16, 0)), (1, 8, 16, 2080, 264, 0.5, (1, 16, 0)),
+    (31, 1, 1, 32, 648, 0.0, (32, 1, 0)), (4, 2, 3, 416, 11048, 0.1, (32, 2, 0)), (10, 3, 3, 1376, 11448, 0.0, (32, 2, 1)), (25, 1, 1, 416, 1016, 0.0, (32, 4, 0)),
+    (27, 1, 1, 480, 1392, 0.1, (32, 4, 1)), (26, 1, 2, 2240, 8208, 0.0, (32, 4, 1)), (15, 1, 1, 544, 1192, 0.0, (32, 8, 0)), (29, 1, 1, 576, 712, 0.2, (32, 8, 1)),
+    (6, 2, 5, 4160, 1776, 0.2, (32, 8, 0)), (11, 1, 1, 2144, 9128, 0.0, (32, 8, 1)), (28, 1, 3, 1056, 688, 0.1, (32, 16, 0)), (1, 8, 16, 8224, 72, 0.4, (32, 16, 0)),
+    (19, 1, 2, 1376, 952, 0.0, (32, 16, 1)), (31, 1, 1, 4320, 232, 0.1, (32, 16, 1)),
+    (258, 1, 8, 32, 40, 0.0, (64, 1, 0)), (266, 2, 16, 384, 40, 0.2, (64, 1, 1)), (58, 3, 33, 416, 920, 0.1, (64, 2, 0)), (139, 4, 33, 736, 920, 0.1, (64, 2, 1)),
+    (117, 1, 5, 448, 136, 0.0, (64, 4, 0)), (191, 2, 12, 448, 72, 0.1, (64, 4, 1)), (264, 1, 24, 2112, 672, 0.0, (64, 4, 1)), (317, 1, 16, 576, 56, 0.1, (64, 8, 0)),
+    (276, 1, 12, 608, 40, 0.0, (64, 8, 1)), (41, 2, 33, 4288, 272, 0.1, (64, 8, 0)), (255, 2, 33, 2144, 232, 0.1, (64, 8, 1)), (67, 1, 8, 1056, 288, 0.0, (64, 16, 0)),
+    (322, 1, 33, 1440, 40, 0.1, (64, 16, 1)), (82, 2, 5, 2592, 72, 0.2, (64, 16, 1)),
+    (300, 2, 4, 288, 64, 0.1, (128, 1, 1)), (700, 3, 5, 1056, 1032, 0.2, (128, 1, 1)), (2100, 2, 2, 1056, 1800, 0.1, (256, 1, 1)), (2100, 2, 2, 224, 1800, 0.0, (256, 1, 1)),
+]
+
+
+def way_of(tokens, k, experts, K, rows, gated):
+    way = (ctypes.c_int32 * 3)()
+    rc = dfp4.load().dfp4_experts_way(dfp4._CPlan(16, tokens, k, experts), dfp4._CExperts(256, experts, rows, K, gated), way)
+    return rc, tuple(way)
+
+
+def test_the_way_of_a_product():
+    """Without a device, as on one of 256 compute units."""
+    for gated, ways in ((1, UP_WAYS), (0, DOWN_WAYS)):
+        for *sizes, _, way in ways:
+            assert way_of(*sizes, gated) == (0, way), (gated, sizes)
+        seen = {w for *_, w in ways}
+        assert seen >= {(rows, waves, q) for rows in (32, 64) for waves in (2, 4, 8, 16) for q in (0, 1)} | {(64, 1, 0), (64, 1, 1), (32, 1, 0), (128, 1, 1), (256, 1, 1)}
+    assert {(128, 1, 2), (256, 1, 2)} <= {w for *_, w in UP_WAYS} and (1, 16, 0) in {w for *_, w in DOWN_WAYS}
+    assert [way_of(*s, 1)[0] for s in ((0, 2, 8, 64, 64), (4, 0, 8, 64, 64), (4, 2, 8, 48, 64), (4, 2, 8, 64, 4), (1 << 26, 2, 8, 64, 1 << 14))] == [-2] * 5
+    lib = dfp4.load()
+    assert lib.dfp4_experts_way(dfp4._CPlan(16, 4, 2, 8), dfp4._CExperts(256, 8, 64, 64, 1), None) == -1
+    assert lib.dfp4_experts_way(dfp4._CPlan(16, 4, 2, 9), dfp4._CExperts(256, 8, 64, 64, 1), None) == -2
+
+
+class UnevenLayer:
+    """Experts whose blocks' sizes lie up to 2^4 apart, and rows alike; values from the dequantizer (exact), in float64 on the device."""
+
+    def __init__(self, experts, rows, K, gated):
+        self.g = torch.Generator(device="cuda").manual_seed(K + rows)
+        self.values, q = [], []
+        for _ in range(2 if gated else 1):
+            q.append(dfp4.quantize(self.uneven(experts * rows, K)))
+            self.values.append(dfp4.dequantize(q[-1], dtype=torch.float32).double().view(experts, rows, K))
+        self.handle = dfp4.expert_weights(q[0], experts, up=q[1] if gated else None)
+
+    def uneven(self, n, K):
+        blocks = torch.randn(n, K // 32, 32, generator=self.g, device="cuda")
+        return (blocks * torch.exp2(torch.randint(-4, 1, (n, K // 32, 1), generator=self.g, device="cuda").float())).view(n, K).bfloat16()
+
+
+def quantized_on_device(x):
+    return dfp4.dequantize(dfp4.quantize(x), dtype=torch.float32).double()
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,K,rows,absent,way", UP_WAYS)
+def test_up_by_every_way(tokens, k, experts, K, rows, absent, way):
+    layer = UnevenLayer(experts, rows, K, True)
+    x, ids = layer.uneven(tokens, K), ids_of(tokens, k, experts, seed=rows, absent=absent)
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    assert dfp4.experts_way(plan, layer.handle) == way
+    out = torch.full((tokens * k, rows), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((int(dfp4.load().dfp4_experts_workspace_bytes(plan.c(), layer.handle.c())),), 0xff, dtype=torch.uint8, device="cuda")
+    h = dfp4.experts_up(x, plan, layer.handle, out=out, workspace=ws)
+    offsets, order, _ = plain_plan(ids, experts)
+    xq = quantized_on_device(x)
+    for e in range(experts):
+        lo, hi = offsets[e], offsets[e + 1]
+        if hi == lo:
+            continue
+        a = xq[torch.tensor(order[lo:hi], device="cuda") // k]
+        g, u = (a @ w[e].T for w in layer.values)
+        dg, du = (1e-5 * (a.abs() @ w[e].abs().T) for w in layer.values)
+        s = g / (1 + torch.exp(-g))
+        # as check_up: |silu'| <= 1.1, fp32 arithmetic of silu, one rounding
+        want, tol = s * u, 1.1 * dg * (u.abs() + du) + s.abs() * du
+        tol = (tol + (2.0 ** -19 + 2.0 ** -23 * g.abs()) * want.abs()) * (1 + HALF) + HALF * want.abs() + 1e-38
+        off = (h[lo:hi].double() - want).abs() / tol
+        assert (off <= 1).all(), (e, float(off.max()))
+    assert (h[offsets[-1]:] == 7.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("tokens,k,experts,K,rows,absent,way", DOWN_WAYS)
+def test_down_by_every_way(tokens, k, experts, K, rows, absent, way):
+    layer = UnevenLayer(experts, rows, K, False)
+    ids, weights = ids_of(tokens, k, experts, seed=rows, absent=absent), torch.rand(tokens, k, generator=layer.g, device="cuda") - 0.5
+    plan = dfp4.expert_plan(ids.cuda(), experts)
+    assert dfp4.experts_way(plan, layer.handle) == way
+    h = layer.uneven(tokens * k, K)
+    offsets, order, _ = plain_plan(ids, experts)
+    hq = quantized_on_device(h)
+    h[offsets[-1]:] = float("nan")                   # (rows behind the last are not read)
+    h[offsets[-1]::2] = float("inf")
+    shape = (tokens, rows)
+    want, size, tol = (torch.zeros(shape, dtype=torch.float64, device="cuda") for _ in range(3))
+    for e in range(experts):
+        lo, hi = offsets[e], offsets[e + 1]
+        if hi == lo:
+            continue
+        pairs, a = torch.tensor(order[lo:hi], device="cuda"), hq[lo:hi]
+        w = weights.double().flatten()[pairs, None]
+        v = w * (a @ layer.values[0][e].T)
+        want.index_add_(0, pairs // k, v)
+        size.index_add_(0, pairs // k, v.abs())
+        tol.index_add_(0, pairs // k, 1e-5 * w.abs() * (a.abs() @ layer.values[0][e].abs().T))
+    for dtype in (torch.bfloat16, torch.float32):
+        out = torch.full(shape, 7.0, dtype=dtype, device="cuda")
+        ws = torch.full((int(dfp4.load().dfp4_experts_workspace_bytes(plan.c(), layer.handle.c())),), 0xff, dtype=torch.uint8, device="cuda")
+        y = dfp4.experts_down(h, plan, layer.handle, weights, out=out, workspace=ws)
+        # k products and additions in fp32, one rounding, y's own
+        half = HALF if dtype == torch.bfloat16 else 2.0 ** -24
+        off = (y.double() - want).abs() / ((tol + 2.0 ** -23 * (k + 1) * size) * (1 + half) + half * want.abs() + 1e-38)
+        assert (off <= 1).all(), (dtype, float(off.max()))
+        assert torch.equal(y, dfp4.experts_down(h, plan, layer.handle, weights, dtype=dtype))
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------------------
 
 def check_norm(y, residual, weight, post, gate, scale, eps, r_got, n_got):
