@@ -469,7 +469,7 @@ __global__ __launch_bounds__(1024, 4) void experts_few_kernel(FewArgs p) {
         const int r = i * 32 + c, n = tile * 32 + 8 * (x >> 2) + 4 * h + (x & 3);
         if (tile >= p.tiles || r >= a.g.rows || n >= p.rows) return;
         const int64_t row = (int64_t)a.g.row0 + r;
-        if constexpr (GATED) static_cast<uint16_t*>(p.out)[row * (p.rows >> 1) + (n >> 1)] = bf16_of(silu_times(v0, v1));
+        if constexpr (GATED) static_cast<uint16_t*>(p.out)[row * (p.rows >> 1) + (n >> 1)] = bf16_of(v0 < kFarGate ? silu_far(v0, v1) : silu_times(v0, v1));
         else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + row * p.rows + n) = make_float2(v0, v1);
     };
 

@@ -723,8 +723,18 @@ __global__ __launch_bounds__(256, 1) void gemm_native_kernel(ParamsOf<MODE> p) {
             int v[16];                                                                              \
             DFP4_NATIVE_READ(G, v);                                                                 \
             float h[8];                                                                             \
-            _Pragma("unroll") for (int x = 0; x < 8; ++x)                                           \
-                h[x] = silu_times(__builtin_bit_cast(float, v[2 * x]), __builtin_bit_cast(float, v[2 * x + 1])); \
+            float least = 0.0f;                                                                     \
+            _Pragma("unroll") for (int x = 0; x < 8; ++x) {                                         \
+                const float g = __builtin_bit_cast(float, v[2 * x]);                                \
+                h[x] = silu_times(g, __builtin_bit_cast(float, v[2 * x + 1]));                      \
+                least = __builtin_fminf(least, g);                                                  \
+            }                                                                                       \
+            if (least < kFarGate) {                                                                 \
+                _Pragma("unroll") for (int x = 0; x < 8; ++x) {                                     \
+                    const float g = __builtin_bit_cast(float, v[2 * x]);                            \
+                    if (g < kFarGate) h[x] = silu_far(g, __builtin_bit_cast(float, v[2 * x + 1]));  \
+                }                                                                                   \
+            }                                                                                       \
             _Pragma("unroll") for (int j = 0; j < 4; ++j)                                           \
                 st[c * kPitch + (G & 1) * 16 + 4 * j + q] = bf16_pair(__builtin_bit_cast(int, h[2 * j]), __builtin_bit_cast(int, h[2 * j + 1])); \
             if constexpr (G & 1) {                                                                  \
