@@ -4,7 +4,8 @@
 //   many   rows are quantized to FP6 in operand order, an expert's from a group of kGroupRows on, so that every tile has one expert
 //          (experts_quantize_kernel, experts_gather_kernel), and the large block-scaled kernel takes tiles of 256 or 128 of them with the
 //          weights' FP6 form (gemm_native.hip, kExperts, kGated).  Bound by the tiles' operands on their way to the compute units and by what
-//          stands before and after a tile's loop (the matrix instructions are busy 32 % of the time).
+//          stands before and after a tile's loop (the matrix instructions are busy 32 % of the time up), down by what leaves and is added too
+//          (4096 tokens of 8 of 64 experts x 2048: 268 MB; the product 103 us, matrix instructions busy 16 %, the sums 50 us, 5.7 TB/s).
 //   few    experts_few_kernel streams the weights' 4-bit form past rows that lie in LDS.  Bound by that stream.
 //   a few tokens, down   experts_token_kernel, one launch.
 // The weights' two forms cost memory (0.79 + 0.56 bytes an element) and spare either way a pass over them.
@@ -109,7 +110,7 @@ struct QuantizeArgs {
 
 // Rows quantized in the plan's order (the arithmetic of the quantizer, quant_pass.h; as quantize_native_kernel, but for the rows' places).
 // A wave takes 8 rows x 8 blocks; what is behind the last row is left as it is: it is multiplied, and its results are not kept.
-// 32768 rows x 1024 26.7 us, by memory (3.5 TB/s).  Tried: scale bytes through LDS, so that they leave as whole lines (31.8);
+// 32768 rows x 1024 27 to 29 us: 3.3 TB/s, vector instructions busy 54 % of the time, so by neither alone.  Tried: scale bytes through LDS, so that they leave as whole lines (31.8);
 // the larger tables of half as many lookups (25.6).
 constexpr int kQThreads = 256, kQWaves = kQThreads / 64, kPasses = 4;
 __global__ __launch_bounds__(kQThreads) void experts_quantize_kernel(QuantizeArgs p) {
@@ -309,8 +310,8 @@ __device__ __forceinline__ void load_quad(Quad& q, const uint8_t* at, bool there
 // A workgroup keeps the rows of a block (MT 1: up to 32, 2: up to 64) in LDS as FP8 and streams its expert's weights past them: 16 waves, SPLIT of which share K of a tile of 32
 // packed rows of weights.  Weights go from memory to registers kAhead quads ahead, over the ends of tiles, and are expanded there.
 // Bound by the weights' stream (0.5625 bytes an element): 64 tokens of 2 of 8 experts, 4096 x 14336 up, 104 to 109 us = 5.0 TB/s, a large copy's rate; with
-// blocks of more than 32 rows among them, whose K takes two turns in LDS, 121 to 125.  Registers: 8 to 32 bytes of a thread's in scratch memory with two
-// tiles of rows.  Tried: FP6 weights (a third more bytes); the last quad loaded again where there is none (whole K in a wave 7 % slower over 300 drawn
+// blocks of more than 32 rows among them, whose K takes two turns in LDS, 121 to 125.  Registers: with two tiles of rows 8 to 24 bytes of a thread's are in
+// scratch memory (down, SPLIT 16: 60).  Tried: FP6 weights (a third more bytes); the last quad loaded again where there is none (whole K in a wave 7 % slower over 300 drawn
 // products); offsets of quads in vector registers (two tiles of rows 5 to 20 % slower).  One token of 8 of 128 experts, 2048 x 1024 up, is bound
 // by loads in turn (plan, row, weights): 7.8 us, 8.3 with the sums over waves in four steps.
 template <bool GATED, int MT, int SPLIT>
@@ -745,12 +746,13 @@ inline int64_t active_experts(const dfp4_plan& plan) {
     const int64_t n = (int64_t)((double)plan.experts * (1.0 - none) + 0.5);
     return n > 0 ? n : 1;
 }
-// Rows an expert up to which weights are streamed past them; both sides, us, few / many: 20 rows 28 / 35, 32 rows (up) 134 / 157, 83 / 92, 35 / 36,
-// 15.3 / 14.0, (down) 84 / 112, 54 / 53, 29 / 29, 42 rows 33 / 28, 48 rows 147 / 159 and 61 / 49, 50 rows 117 / 98 and 89 / 57
+// Rows an expert up to which weights are streamed past them; both sides, us, few / many, up: 16 rows 117 / 148, 32 rows 132 / 152, 71 / 73, 105 / 94, 47 / 35,
+// 40 rows 71 / 48, 48 rows 130 / 156, 50 rows 112 / 98, 64 rows 70 / 74; down: 16 rows 63 / 110, 32 rows 84 / 114, 42 / 52, 84 / 55, 37 / 29, 42 rows 32 / 23, 48 rows 163 / 117,
+// 64 rows 66 / 55.  Of 54 products up and 58 down of 4 to 100 rows the better one is missed by 5 % in the mean (lines at 24 and 40: 5 and 6 %)
 constexpr int64_t kFewRows = 34;
 // Whether the large kernel takes 128 rows at a time instead of 256: where an expert has no more than 160 (half / whole: 42 rows 28 / 33 us, 128 rows 88 / 91 and
-// 126 / 143, 250 rows 76 / 63, 117 / 107), or tiles of 256 would leave half of the compute units idle (325 rows, 4 columns of tiles, 27.6 / 33.7).  Of 81
-// drawn products the better one is missed by 0.7 % in the mean.
+// 126 / 143, 250 rows 76 / 63, 117 / 107; down 64 rows 57 / 55, 128 rows 73 / 76, 512 rows 207 / 181), or tiles of 256 would leave half of the compute units idle (325 rows,
+// 4 columns of tiles, 27.6 / 33.7).  Of 81 drawn products the better one is missed by 0.7 % in the mean, of 44 others, down, by 0.8 %.
 inline bool half_tiles(const dfp4_plan& plan, const dfp4_experts& w) {
     const int64_t active = active_experts(plan), rows = plan.tokens * plan.k / active;
     return rows <= 160 || active * ((rows + 255) / 256) * (padded_rows(w) / 256) * 2 <= device_cu_count();

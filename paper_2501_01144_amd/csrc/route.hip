@@ -4,8 +4,8 @@
 // which for scores in 64 bits is all but never, by the scores themselves.  Scores are in 64 bits because a choice is a whole number: next to a
 // border fp32 would take another expert than the formula does.  Without a bias, and where groups go by one score, the order is the logits', and
 // only what the weights need is computed.
-// Bound by vector instructions (k rounds of a maximum over the wave): 16384 tokens of 8 of 256 18.8 us (with 64-bit keys, all
-// scores computed, 25.5); route_logits_kernel 9.0.
+// Bound by latency (k rounds of a maximum over the wave, each waiting for the one before): 16384 tokens of 8 of 256 18.8 us (with 64-bit keys, all
+// scores computed, 25.5); route_logits_kernel 9.2, vector instructions busy 35 % of the time, waves waiting half of theirs.
 #include <type_traits>
 #include "experts.h"
 
